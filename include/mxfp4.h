@@ -377,6 +377,144 @@ int mxfp4_linear_static(int pass, const void* a, const void* b, void* out, int64
                         uint64_t seed, int out_dtype, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------
+ * 8-bit product with one fp32 scale per 128 elements along the reduction axis: the other common
+ * recipe for the passes the ladder leaves in 8 bits.  E4M3 codes; blocks of 1 x 128 (activations,
+ * gradients) or 128 x 128 (weights); the partial product of each block is formed on the tensor
+ * cores and added, scaled, to a sum kept in fp32 outside of them, so no chain of the tensor cores'
+ * truncating additions is longer than a block.
+ *
+ * mxfp4_quantize_block128: operand view and axis as in mxfp4_quantize.  Per block
+ *     a = max(largest magnitude, 2^-100),  scale = a / 448,  code = E4M3(x * (448 / a)),
+ *   each operation rounded to fp32 (nearest), the code to nearest, ties to even, saturating at 448.
+ *   block_shape  MXFP4_BLOCK_1X128: 128 consecutive elements of an operand row;
+ *                MXFP4_BLOCK_128X128: 128 operand rows x 128 elements (the transposed operand has the
+ *                transposed codes and scales).  Last blocks may be shorter both ways.
+ *   codes        out, [outer x K] bytes, 16-byte aligned; K a multiple of 16, outer any.
+ *   scales       out, fp32, mxfp4_block128_scales_bytes(outer, K, block_shape) bytes, 16-byte aligned:
+ *                the scale of (row o, block t) is at t * pitch + o, pitch = 128 * ceil(outer / 128), for
+ *                1 x 128 (entries of rows past `outer` are written as 0) and at
+ *                t * ceil(outer / 128) + o / 128 for 128 x 128.
+ *   ld_src a multiple of 8; src 16-byte aligned; inputs finite.
+ *
+ * mxfp4_gemm_block128: out[m][n] = sum_t sa(m, t) * sb(n, t) * sum_{k in block t} A[m][k] * B[n][k]
+ *   A always has 1 x 128 blocks, B the ones b_block_shape names.  out as in mxfp4_gemm.
+ *   workspace   mxfp4_gemm_block128_workspace_bytes(M, N, K) bytes (0 for most shapes: only products with
+ *               too few output tiles for the device are split along K and joined in a fixed order),
+ *               16-byte aligned; free again once the call's work has run.
+ *
+ * mxfp4_linear_pass_block128: one pass of a linear with both operands quantized in the call;
+ *   (a, b, out) as in mxfp4_linear_pass.  Activations and gradients get 1 x 128 blocks along the
+ *   reduction axis, W 128 x 128 blocks.  The reduction size is a multiple of 16, in and out of 8.
+ *   Workspace: mxfp4_linear_pass_block128_workspace_bytes (0 for a bad argument), 256-byte aligned.
+ */
+#define MXFP4_BLOCK_1X128 2
+#define MXFP4_BLOCK_128X128 3
+size_t mxfp4_block128_scales_bytes(int64_t outer, int64_t K, int block_shape);
+int mxfp4_quantize_block128(const void* src_bf16, int64_t rows, int64_t cols, int64_t ld_src, int axis,
+                            int block_shape, void* codes, void* scales, void* stream);
+size_t mxfp4_gemm_block128_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int mxfp4_gemm_block128(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales,
+                        int b_block_shape, int64_t M, int64_t N, int64_t K, void* out, int out_dtype, int64_t ld_out,
+                        void* workspace, size_t workspace_bytes, void* stream);
+size_t mxfp4_linear_pass_block128_workspace_bytes(int64_t T, int64_t in_features, int64_t out_features, int pass);
+int mxfp4_linear_pass_block128(int pass, const void* a, const void* b, void* out, int64_t T, int64_t in_features,
+                               int64_t out_features, int out_dtype, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * The end of one residual block and the start of the next, between two linears:
+ *     n = u * rsqrt(mean(u^2) + eps)        u = branch, the block's output (without w_post: n = u)
+ *     b = n * w_post                        norm after the block
+ *     g = act(gate)                         (without a gate: g = 1)
+ *     y = skip_scale * x + branch_scale * g * b     x = stream; rounded to the stream's type, stored
+ *     h = y * rsqrt(mean(y^2) + eps) * w_pre        norm before the next block, of the stored y
+ * Means run over the `width` elements of a token's row.  fp32 arithmetic throughout.
+ *   branch   bf16 [tokens x width], leading dimension ld_branch
+ *   stream   forward: x, or NULL (nothing is added); backward: y as the forward stored it, needed
+ *            when w_pre is given; bf16 or fp32 (stream_dtype, MXFP4_OUT_*)
+ *   gate     MXFP4_GATE_NONE: NULL; _CHANNEL: fp32 [width]; _ELEMENT: bf16 [tokens x width], ld_gate
+ *   gate_act MXFP4_GATE_LINEAR: g = gate; _SIGMOID; _SILU: gate * sigmoid(gate)
+ *   w_post, w_pre  fp32 [width] or NULL: that norm is left out
+ * width a multiple of 8, at most 16384; matrices 16-byte aligned with leading dimensions that are
+ * multiples of 8.  The struct is a HOST struct of DEVICE pointers, as mxfp4_quant_desc.
+ *
+ * Forward: y [tokens x width] of the stream's type (may be the x it reads), h bf16 (given exactly
+ *   when w_pre is).
+ * Backward: dh bf16 (given exactly when w_pre is) and dy (the stream's type; NULL: zero) in; any of
+ *   dx (the stream's type), dbranch (bf16), dgate (bf16 [tokens x width], or fp32 [width] for a
+ *   channel gate), dw_post, dw_pre (fp32 [width]) out, NULL where not wanted.  dx may be dy and dbranch
+ *   may be dh.  workspace: mxfp4_residual_norm_workspace_bytes bytes, 16-byte aligned, when a
+ *   [width] gradient is wanted; those sums run in a fixed order, so calls repeat bit for bit.
+ */
+#define MXFP4_GATE_NONE 0
+#define MXFP4_GATE_CHANNEL 1
+#define MXFP4_GATE_ELEMENT 2
+#define MXFP4_GATE_LINEAR 0
+#define MXFP4_GATE_SIGMOID 1
+#define MXFP4_GATE_SILU 2
+typedef struct mxfp4_norm_desc {
+    int64_t tokens, width;
+    const void* branch;
+    int64_t ld_branch;
+    const void* stream;
+    int64_t ld_stream;
+    const void* gate;
+    int64_t ld_gate;
+    const float* w_post;
+    const float* w_pre;
+    int32_t stream_dtype, gate_kind, gate_act;
+    float skip_scale, branch_scale, eps;
+} mxfp4_norm_desc;
+int mxfp4_residual_norm_forward(const mxfp4_norm_desc* norm, void* y, int64_t ld_y, void* h, int64_t ld_h,
+                                void* stream);
+size_t mxfp4_residual_norm_workspace_bytes(int64_t tokens, int64_t width);
+int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, int64_t ld_dh, const void* dy,
+                                 int64_t ld_dy, void* dx, int64_t ld_dx, void* dbranch, int64_t ld_dbranch,
+                                 void* dgate, int64_t ld_dgate, float* dw_post, float* dw_pre, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Log probabilities of given tokens from an output layer's logits, with the entropy and the top
+ * alternatives of each row (a row: the `vocab` logits of one position), and the gradient.
+ *     z = scale * logits,  lse = log sum exp z,  logp = z[target] - lse,
+ *     entropy = lse - sum_i p_i z_i  (p = exp(z - lse)),
+ *     top_logp / top_index: the top_k largest z - lse, descending, equal ones by lowest index.
+ *   logits   [tokens x vocab] bf16 or fp32 (dtype, MXFP4_OUT_*), leading dimension ld >= vocab; any
+ *            vocab, any ld, aligned to the element only
+ *   targets  int64 [tokens].  A negative target is a position without one: logp 0, and no gradient
+ *            through it.  A target >= vocab gives NaN in logp and in the row's gradient.
+ *   scale    finite, > 0 (1 / temperature)
+ *   logp, entropy, lse  fp32 [tokens]; logp (with targets) and entropy may be NULL
+ *   top_logp fp32, top_index int64, [tokens x top_k]; 0 <= top_k <= 32
+ *   workspace  mxfp4_logprobs_workspace_bytes(tokens, vocab, top_k) bytes, 16-byte aligned (0 when the
+ *            device is filled without splitting rows)
+ * Logits of -infinity are masked: probability 0, never an alternative.  Alternatives a row does not
+ * have are (-infinity, -1).  A row masked entirely has lse -infinity, logp -infinity, entropy 0 and
+ * a zero gradient.  A NaN or +infinity makes its row's results NaN (index -1).
+ *
+ * lse is an fp32 number: where it is beyond about 2^20 in magnitude (a row of the type's lowest value,
+ * say) it no longer resolves the row's probabilities, which the backward pass takes from it; logp,
+ * entropy and the alternatives' order do not depend on that.
+ *
+ * Backward: dlogits[t][i] = scale * (d_logp[t] * (delta(i, target) - p_i)
+ *                                    - d_entropy[t] * p_i * (z_i - lse + entropy[t]))
+ *   from the forward's lse and entropy; d_logp / d_entropy fp32 [tokens], either may be NULL (zero;
+ *   targets may then be NULL with d_logp, entropy with d_entropy).  dlogits has the logits' type and
+ *   may be the logits.  A row whose two gradients are 0 is set to 0 without being read.
+ */
+size_t mxfp4_logprobs_workspace_bytes(int64_t tokens, int64_t vocab, int top_k);
+int mxfp4_logprobs_forward(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                           const int64_t* targets, float scale, float* logp, float* entropy, float* lse, int top_k,
+                           float* top_logp, int64_t* top_index, void* workspace, size_t workspace_bytes,
+                           void* stream);
+int mxfp4_logprobs_backward(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                            const int64_t* targets, float scale, const float* lse, const float* entropy,
+                            const float* d_logp, const float* d_entropy, void* dlogits, int64_t ld_d, void* stream);
+
+/*
  * Synchronises `stream` and returns the sticky device-side status of the current device:
  * MXFP4_OK, MXFP4_ERR_TIMEOUT (a kernel gave up a bounded wait; its output is invalid) or
  * MXFP4_ERR_CUDA.  The status word is cleared by the call.

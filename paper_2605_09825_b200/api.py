@@ -16,12 +16,14 @@ from . import build as _build
 HADAMARD_NONE, HADAMARD_DET, HADAMARD_RAND, HADAMARD_DET16, HADAMARD_RAND16 = 0, 1, 2, 3, 4
 ROUND_RNE, ROUND_SR = 0, 1
 SCALES_CANONICAL, SCALES_TILED = 0, 1
-BLOCK_1X32, BLOCK_32X32 = 0, 1
+BLOCK_1X32, BLOCK_32X32, BLOCK_1X128, BLOCK_128X128 = 0, 1, 2, 3
 OUT_BF16, OUT_FP32 = 0, 1
 LAYER_SAVED, LAYER_FORWARD, LAYER_BACKWARD = 0, 1, 2
 PRECISION_MXFP4, PRECISION_MXFP8, PRECISION_MXFP4_32X32 = 0, 1, 2
 PASS_FPROP, PASS_DGRAD, PASS_WGRAD = 0, 1, 2
 AXIS_ROWS, AXIS_COLS = 0, 1
+GATE_NONE, GATE_CHANNEL, GATE_ELEMENT = 0, 1, 2      # kinds
+GATE_LINEAR, GATE_SIGMOID, GATE_SILU = 0, 1, 2       # activations
 
 EXPORTS = (
     "mxfp4_version", "mxfp4_status_string", "mxfp4_codes_bytes", "mxfp4_scales_bytes",
@@ -31,6 +33,10 @@ EXPORTS = (
     "mxfp4_linear_pass_workspace_bytes", "mxfp4_linear_pass", "mxfp4_linear_host", "mxfp4_linear_static",
     "mxfp4_check", "mxfp4_selftest_wait_timeout", "mxfp4_bounds_checked", "mxfp4_selftest_bounds",
     "mxfp4_probe_mma_rate",
+    "mxfp4_block128_scales_bytes", "mxfp4_quantize_block128", "mxfp4_gemm_block128_workspace_bytes",
+    "mxfp4_gemm_block128", "mxfp4_linear_pass_block128_workspace_bytes", "mxfp4_linear_pass_block128",
+    "mxfp4_residual_norm_forward", "mxfp4_residual_norm_workspace_bytes", "mxfp4_residual_norm_backward",
+    "mxfp4_logprobs_workspace_bytes", "mxfp4_logprobs_forward", "mxfp4_logprobs_backward",
 )
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 
@@ -40,6 +46,16 @@ class QuantDesc(ctypes.Structure):
     _fields_ = [("src_bf16", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("ld_src", ctypes.c_int64), ("axis", ctypes.c_int32), ("operand_tag", ctypes.c_uint32),
                 ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class NormDesc(ctypes.Structure):
+    """``mxfp4_norm_desc``: what both directions of ``mxfp4_residual_norm_*`` read."""
+    _fields_ = [("tokens", ctypes.c_int64), ("width", ctypes.c_int64), ("branch", ctypes.c_void_p),
+                ("ld_branch", ctypes.c_int64), ("stream", ctypes.c_void_p), ("ld_stream", ctypes.c_int64),
+                ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64), ("w_post", ctypes.c_void_p),
+                ("w_pre", ctypes.c_void_p), ("stream_dtype", ctypes.c_int32), ("gate_kind", ctypes.c_int32),
+                ("gate_act", ctypes.c_int32), ("skip_scale", ctypes.c_float), ("branch_scale", ctypes.c_float),
+                ("eps", ctypes.c_float)]
 
 
 class Mxfp4Error(RuntimeError):
@@ -111,6 +127,22 @@ def load_library() -> ctypes.CDLL:
     lib.mxfp4_linear_static.argtypes = [ci, vp, vp, vp, i64, i64, i64, ci, ci, u64, ci, vp]
     lib.mxfp4_linear_static.restype = ci
     lib.mxfp4_check.argtypes, lib.mxfp4_check.restype = [vp], ci
+    f32, norm = ctypes.c_float, ctypes.POINTER(NormDesc)
+    for name, args, res in (
+            ("mxfp4_block128_scales_bytes", [i64, i64, ci], sz),
+            ("mxfp4_quantize_block128", [vp, i64, i64, i64, ci, ci, vp, vp, vp], ci),
+            ("mxfp4_gemm_block128_workspace_bytes", [i64, i64, i64], sz),
+            ("mxfp4_gemm_block128", [vp, vp, vp, vp, ci, i64, i64, i64, vp, ci, i64, vp, sz, vp], ci),
+            ("mxfp4_linear_pass_block128_workspace_bytes", [i64, i64, i64, ci], sz),
+            ("mxfp4_linear_pass_block128", [ci, vp, vp, vp, i64, i64, i64, ci, vp, sz, vp], ci),
+            ("mxfp4_residual_norm_forward", [norm, vp, i64, vp, i64, vp], ci),
+            ("mxfp4_residual_norm_workspace_bytes", [i64, i64], sz),
+            ("mxfp4_residual_norm_backward", [norm] + [vp, i64] * 5 + [vp, vp, vp, sz, vp], ci),
+            ("mxfp4_logprobs_workspace_bytes", [i64, i64, ci], sz),
+            ("mxfp4_logprobs_forward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, ci, vp, vp, vp, sz, vp], ci),
+            ("mxfp4_logprobs_backward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp], ci)):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, res
     lib.mxfp4_selftest_wait_timeout.argtypes, lib.mxfp4_selftest_wait_timeout.restype = [vp], ci
     lib.mxfp4_selftest_bounds.argtypes, lib.mxfp4_selftest_bounds.restype = [vp], ci
     lib.mxfp4_bounds_checked.argtypes, lib.mxfp4_bounds_checked.restype = [], ci
@@ -479,6 +511,254 @@ def linear_static(pass_: int, a: torch.Tensor, b: torch.Tensor, T: int, in_f: in
                                             _stream())
     _raise(rc, "mxfp4_linear_static")
     return out
+
+
+# ---------------------------------------------------------------- 8-bit product, 128-blocks
+def _matrix(t: torch.Tensor, name: str, dtypes) -> tuple:
+    """Pointer and leading dimension of a 2-D CUDA tensor with contiguous rows."""
+    if t.dtype not in dtypes or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D tensor of {' or '.join(map(str, dtypes))} with contiguous rows")
+    rows, cols = t.shape
+    return _dev_ptr(t), t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _expect(t: torch.Tensor, name: str, dtype, numel: int) -> int:
+    """Pointer of a contiguous CUDA tensor with at least ``numel`` elements."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} elements")
+    return _dev_ptr(t)
+
+
+def block128_scales_bytes(outer: int, K: int, block_shape: int) -> int:
+    return int(load_library().mxfp4_block128_scales_bytes(outer, K, block_shape))
+
+
+def quantize_block128(src: torch.Tensor, axis: int = AXIS_COLS, block_shape: int = BLOCK_1X128,
+                      codes: torch.Tensor | None = None, scales: torch.Tensor | None = None):
+    """``mxfp4_quantize_block128``: E4M3 codes of a 2-D bf16 CUDA tensor with one fp32 scale per 128
+    elements along the reduction axis (``BLOCK_1X128``) or per 128 x 128 block (``BLOCK_128X128``).
+
+    Returns ``(codes uint8 [outer, K], scales float32 [ceil(K / 128), pitch])``, pitch = outer rounded up
+    to 128 for ``BLOCK_1X128`` and the number of row blocks for ``BLOCK_128X128``.
+    """
+    ptr, ld = _matrix(src, "src", (torch.bfloat16,))
+    rows, cols = src.shape
+    outer, K = (rows, cols) if axis == AXIS_COLS else (cols, rows)
+    need = block128_scales_bytes(outer, K, block_shape)
+    if need == 0:
+        _raise(-2 if block_shape in (BLOCK_1X128, BLOCK_128X128) else -4, "mxfp4_quantize_block128")
+    if codes is None:
+        codes = torch.empty((outer, K), dtype=torch.uint8, device=src.device)
+    if scales is None:
+        blocks = (K + 127) // 128
+        scales = torch.empty((blocks, need // (4 * blocks)), dtype=torch.float32, device=src.device)
+    rc = load_library().mxfp4_quantize_block128(ptr, rows, cols, ld, axis, block_shape,
+                                                _expect(codes, "codes", torch.uint8, outer * K),
+                                                _expect(scales, "scales", torch.float32, need // 4), _stream())
+    _raise(rc, "mxfp4_quantize_block128")
+    return codes, scales
+
+
+def gemm_block128(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor,
+                  b_block_shape: int = BLOCK_128X128, out_dtype: int = OUT_BF16, out: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None):
+    """``mxfp4_gemm_block128``: ``A B^T`` from E4M3 codes [M, K], [N, K] and their fp32 scales; A has
+    1 x 128 blocks, B those ``b_block_shape`` names."""
+    M, K = a_codes.shape
+    N, K2 = b_codes.shape
+    if K != K2:
+        raise ValueError("A and B disagree on K")
+    lib = load_library()
+    a_need = lib.mxfp4_block128_scales_bytes(M, K, BLOCK_1X128) // 4
+    b_need = lib.mxfp4_block128_scales_bytes(N, K, b_block_shape) // 4
+    if a_need == 0 or b_need == 0:
+        _raise(-2 if b_block_shape in (BLOCK_1X128, BLOCK_128X128) else -4, "mxfp4_gemm_block128")
+    out = _out_tensor((M, N), out_dtype, a_codes.device, out)
+    need = lib.mxfp4_gemm_block128_workspace_bytes(M, N, K)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=a_codes.device)
+    rc = lib.mxfp4_gemm_block128(_expect(a_codes, "a_codes", torch.uint8, M * K),
+                                 _expect(a_scales, "a_scales", torch.float32, a_need),
+                                 _expect(b_codes, "b_codes", torch.uint8, N * K),
+                                 _expect(b_scales, "b_scales", torch.float32, b_need), b_block_shape, M, N, K,
+                                 _dev_ptr(out), out_dtype, out.stride(0) if M > 1 else max(N, out.stride(0)),
+                                 _dev_ptr(workspace) if workspace is not None else None,
+                                 workspace.numel() if workspace is not None else 0, _stream())
+    _raise(rc, "mxfp4_gemm_block128")
+    return out
+
+
+def linear_pass_block128(pass_: int, a: torch.Tensor, b: torch.Tensor, out_dtype: int = OUT_BF16, workspace=None,
+                         out=None):
+    """``mxfp4_linear_pass_block128``: one pass in 8 bits with 128-blocks; (a, b) = (X, W) / (dY, W) / (dY, X)."""
+    for t in (a, b):
+        if t.dtype != torch.bfloat16 or not t.is_contiguous():
+            raise ValueError("inputs must be contiguous bf16 tensors")
+    if pass_ == PASS_FPROP:
+        T, in_f, out_f, shape = a.shape[0], a.shape[1], b.shape[0], (a.shape[0], b.shape[0])
+    elif pass_ == PASS_DGRAD:
+        T, out_f, in_f, shape = a.shape[0], a.shape[1], b.shape[1], (a.shape[0], b.shape[1])
+    else:
+        T, out_f, in_f, shape = a.shape[0], a.shape[1], b.shape[1], (a.shape[1], b.shape[1])
+    want = {PASS_FPROP: (out_f, in_f), PASS_DGRAD: (out_f, in_f), PASS_WGRAD: (T, in_f)}.get(pass_, tuple(b.shape))
+    if tuple(b.shape) != want:
+        raise ValueError("the operands disagree on the reduction size")
+    lib = load_library()
+    if workspace is None:
+        need = lib.mxfp4_linear_pass_block128_workspace_bytes(T, in_f, out_f, pass_)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=a.device)
+    out = _out_tensor(shape, out_dtype, a.device, out)
+    rc = lib.mxfp4_linear_pass_block128(pass_, _dev_ptr(a), _dev_ptr(b), _dev_ptr(out), T, in_f, out_f, out_dtype,
+                                        _dev_ptr(workspace), workspace.numel(), _stream())
+    _raise(rc, "mxfp4_linear_pass_block128")
+    return out
+
+
+# ---------------------------------------------------------------- residual norm
+_STREAM_TYPES = {torch.bfloat16: OUT_BF16, torch.float32: OUT_FP32}
+
+
+def _norm_desc(branch, stream, stream_dtype, w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps) -> NormDesc:
+    ptr, ld = _matrix(branch, "branch", (torch.bfloat16,))
+    tokens, width = branch.shape
+    d = NormDesc(tokens, width, ptr, ld, None, 0, None, 0, None, None, stream_dtype, GATE_NONE, gate_act, skip_scale,
+                 branch_scale, eps)
+    if stream is not None:
+        if stream.shape != branch.shape:
+            raise ValueError("stream and branch must have the same shape")
+        d.stream, d.ld_stream = _matrix(stream, "stream", tuple(_STREAM_TYPES))
+    if gate is not None:
+        if gate.dim() == 1:
+            d.gate_kind, d.gate = GATE_CHANNEL, _expect(gate, "a channel gate", torch.float32, width)
+        elif gate.shape != branch.shape:
+            raise ValueError("gate must have the branch's shape or be a vector of its width")
+        else:
+            d.gate_kind = GATE_ELEMENT
+            d.gate, d.ld_gate = _matrix(gate, "gate", (torch.bfloat16,))
+    if w_post is not None:
+        d.w_post = _expect(w_post, "w_post", torch.float32, width)
+    if w_pre is not None:
+        d.w_pre = _expect(w_pre, "w_pre", torch.float32, width)
+    return d
+
+
+def residual_norm_forward(branch, stream=None, w_post=None, w_pre=None, gate=None, gate_act=GATE_LINEAR,
+                          skip_scale: float = 1.0, branch_scale: float = 1.0, eps: float = 1e-5,
+                          stream_dtype=None, y=None, h=None):
+    """``mxfp4_residual_norm_forward``: ``y = skip_scale * stream + branch_scale * act(gate) * rms_norm(branch)
+    * w_post`` and ``h = rms_norm(y) * w_pre``; returns ``(y, h)``, h None without ``w_pre``.
+
+    ``branch`` bf16 [tokens, width]; ``stream`` bf16 or fp32 or None (nothing is added, y of type
+    ``stream_dtype``, bf16 by default); ``gate`` None, fp32 [width] or bf16 [tokens, width]; weights fp32
+    [width] or None (that norm is left out).  ``y`` may be ``stream``."""
+    dtype = stream.dtype if stream is not None else (stream_dtype or torch.bfloat16)
+    if dtype not in _STREAM_TYPES:
+        raise ValueError("the stream is bf16 or fp32")
+    d = _norm_desc(branch, stream, _STREAM_TYPES[dtype], w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps)
+    if y is None:
+        y = torch.empty(branch.shape, dtype=dtype, device=branch.device)
+    if h is None and w_pre is not None:
+        h = torch.empty(branch.shape, dtype=torch.bfloat16, device=branch.device)
+    if y.shape != branch.shape or (h is not None and h.shape != branch.shape):
+        raise ValueError("y and h must have the branch's shape")
+    y_ptr, ld_y = _matrix(y, "y", (dtype,))
+    h_ptr, ld_h = _matrix(h, "h", (torch.bfloat16,)) if h is not None else (None, 0)
+    _raise(load_library().mxfp4_residual_norm_forward(ctypes.byref(d), y_ptr, ld_y, h_ptr, ld_h, _stream()),
+           "mxfp4_residual_norm_forward")
+    return y, h
+
+
+def residual_norm_backward(dh, dy, branch, y, w_post=None, w_pre=None, gate=None, gate_act=GATE_LINEAR,
+                           skip_scale: float = 1.0, branch_scale: float = 1.0, eps: float = 1e-5, workspace=None,
+                           dstream=None, dbranch=None):
+    """``mxfp4_residual_norm_backward``: ``(dstream, dbranch, dgate, dw_post, dw_pre)`` from the gradients
+    ``dh`` (None without ``w_pre``) and ``dy`` (None: zero) and the forward's ``branch`` and ``y``; what
+    the forward did not have is None.  ``dstream`` may be ``dy`` and ``dbranch`` may be ``dh``."""
+    like = y if y is not None else dy
+    if like is None or like.dtype not in _STREAM_TYPES:
+        raise ValueError("y or dy is needed, bf16 or fp32")
+    dtype, shape, dev = like.dtype, branch.shape, branch.device
+    d = _norm_desc(branch, y, _STREAM_TYPES[dtype], w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps)
+    tokens, width = shape
+    if dstream is None:
+        dstream = torch.empty(shape, dtype=dtype, device=dev)
+    if dbranch is None:
+        dbranch = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    for t in (dh, dy, dstream, dbranch):
+        if t is not None and t.shape != shape:
+            raise ValueError("gradients must have the branch's shape")
+    vector = lambda like: torch.empty(width, dtype=torch.float32, device=dev) if like is not None else None
+    dw_post, dw_pre = vector(w_post), vector(w_pre)
+    dgate, ld_dgate = None, 0
+    if gate is not None:
+        dgate = vector(gate) if gate.dim() == 1 else torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        ld_dgate = width
+    lib = load_library()
+    sums = dw_post is not None or dw_pre is not None or (gate is not None and gate.dim() == 1)
+    if workspace is None and sums:
+        workspace = torch.empty(max(lib.mxfp4_residual_norm_workspace_bytes(tokens, width), 1), dtype=torch.uint8,
+                                device=dev)
+    opt = lambda t, name, kind: _matrix(t, name, (kind,)) if t is not None else (None, 0)
+    ptr = lambda t: _dev_ptr(t) if t is not None else None
+    rc = lib.mxfp4_residual_norm_backward(ctypes.byref(d), *opt(dh, "dh", torch.bfloat16), *opt(dy, "dy", dtype),
+                                          *_matrix(dstream, "dstream", (dtype,)),
+                                          *_matrix(dbranch, "dbranch", (torch.bfloat16,)), ptr(dgate), ld_dgate,
+                                          ptr(dw_post), ptr(dw_pre), ptr(workspace),
+                                          workspace.numel() if workspace is not None else 0, _stream())
+    _raise(rc, "mxfp4_residual_norm_backward")
+    return dstream, dbranch, dgate, dw_post, dw_pre
+
+
+# ---------------------------------------------------------------- token log probabilities
+def _logits(t: torch.Tensor) -> tuple:
+    ptr, ld = _matrix(t, "logits", tuple(_STREAM_TYPES))
+    return ptr, _STREAM_TYPES[t.dtype], t.shape[0], t.shape[1], ld
+
+
+def logprobs_forward(logits, targets=None, top_k: int = 0, scale: float = 1.0, workspace=None):
+    """``mxfp4_logprobs_forward`` on bf16 or fp32 logits [tokens, vocab] (rows may be strided).
+
+    Returns ``(logp, entropy, lse, top_logp, top_index)``: fp32 [tokens] each (logp None without
+    ``targets``, int64 [tokens], negative: no target) and the ``top_k`` <= 32 largest log probabilities
+    with their int64 indices, [tokens, top_k] (both None with ``top_k`` 0)."""
+    ptr, dtype, tokens, vocab, ld = _logits(logits)
+    lib = load_library()
+    dev = logits.device
+    row = lambda: torch.empty(tokens, dtype=torch.float32, device=dev)
+    logp, entropy, lse = row() if targets is not None else None, row(), row()
+    top_logp = top_index = None
+    if top_k > 0:
+        top_logp = torch.empty((tokens, top_k), dtype=torch.float32, device=dev)
+        top_index = torch.empty((tokens, top_k), dtype=torch.int64, device=dev)
+    need = lib.mxfp4_logprobs_workspace_bytes(tokens, vocab, top_k)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    opt = lambda t: _dev_ptr(t) if t is not None else None
+    rc = lib.mxfp4_logprobs_forward(
+        ptr, dtype, tokens, vocab, ld, _expect(targets, "targets", torch.int64, tokens) if targets is not None else None,
+        scale, opt(logp), _dev_ptr(entropy), _dev_ptr(lse), top_k, opt(top_logp), opt(top_index), opt(workspace),
+        workspace.numel() if workspace is not None else 0, _stream())
+    _raise(rc, "mxfp4_logprobs_forward")
+    return logp, entropy, lse, top_logp, top_index
+
+
+def logprobs_backward(logits, targets, lse, entropy=None, d_logp=None, d_entropy=None, scale: float = 1.0,
+                      dlogits=None):
+    """``mxfp4_logprobs_backward``: the gradient with respect to the logits from the forward's ``lse`` (and
+    ``entropy``) and the gradients of logp and entropy (fp32 [tokens], None: zero).  ``dlogits`` may be
+    the logits themselves."""
+    ptr, dtype, tokens, vocab, ld = _logits(logits)
+    if dlogits is None:
+        dlogits = torch.empty((tokens, vocab), dtype=logits.dtype, device=logits.device)
+    if dlogits.shape != logits.shape:
+        raise ValueError("dlogits must have the logits' shape")
+    d_ptr, ld_d = _matrix(dlogits, "dlogits", (logits.dtype,))
+    row = lambda t, name, kind=torch.float32: _expect(t, name, kind, tokens) if t is not None else None
+    rc = load_library().mxfp4_logprobs_backward(
+        ptr, dtype, tokens, vocab, ld, row(targets, "targets", torch.int64), scale, row(lse, "lse"),
+        row(entropy, "entropy"), row(d_logp, "d_logp"), row(d_entropy, "d_entropy"), d_ptr, ld_d, _stream())
+    _raise(rc, "mxfp4_logprobs_backward")
+    return dlogits
 
 
 def probe_mma_rate(iterations: int = 10000, random_operands: bool = True) -> float:

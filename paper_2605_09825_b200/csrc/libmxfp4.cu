@@ -1,6 +1,8 @@
-// C ABI of the library (see include/mxfp4.h).  Single translation unit: the kernels live in
-// the headers included below.  Host code here only validates arguments, builds TMA tensor
-// maps and launches; every step of the path runs in the kernels.
+// C ABI of the library (see include/mxfp4.h): the MXFP4 / MXFP8 quantizers, GEMMs and linear passes.
+// The kernels live in the headers included below; the operators around the linears have a
+// translation unit each (block128.cu, residual_norm.cu, logprobs.cu).  Host code here only
+// validates arguments, builds TMA tensor maps and launches; every step of the path runs in the
+// kernels.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -11,6 +13,7 @@
 #include "../../include/mxfp4.h"
 #include "ptx_sm100.cuh"
 #include "tma_host.cuh"
+#include "host_common.cuh"
 #include "quantize_kernel.cuh"
 #include "quantize_dual_kernel.cuh"
 #include "quantize_fp8_kernel.cuh"
@@ -18,71 +21,6 @@
 #include "mma_rate_probe.cuh"
 
 namespace mxfp4 {
-
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-constexpr int kMaxDevices = 64;      // size of the per-device tables below
-
-struct DeviceInfo {
-    int sm_count = 0;
-    int cc_major = 0;
-    bool ok = false;
-};
-
-// Per-device set-up that runs once however many host threads reach it at the same time: the
-// first caller on a device runs `f` (which returns a status code), the others wait for it, and
-// everybody gets that status.  One instance per table (device properties, a kernel's
-// shared-memory attribute, the copy streams of the host-buffer call, ...).
-struct PerDeviceOnce {
-    std::once_flag flag[kMaxDevices];
-    int status[kMaxDevices] = {};
-    template <class F>
-    int run(int dev, F&& f)
-    {
-        std::call_once(flag[dev], [&] { status[dev] = f(); });
-        return status[dev];
-    }
-};
-
-// Ordinal of the current device, or -1 if it cannot be had or lies beyond the tables.
-static int current_device()
-{
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
-    return dev;
-}
-
-static const DeviceInfo& device_info()
-{
-    static DeviceInfo info[kMaxDevices];
-    static PerDeviceOnce once;
-    static const DeviceInfo none;
-    const int dev = current_device();
-    if (dev < 0) return none;
-    once.run(dev, [&] {
-        cudaDeviceProp prop;
-        if (cudaGetDeviceProperties(&prop, dev) == cudaSuccess) {
-            info[dev].sm_count = prop.multiProcessorCount;
-            info[dev].cc_major = prop.major;
-            info[dev].ok = true;
-        }
-        return 0;
-    });
-    return info[dev];
-}
-
-// Raises a kernel's dynamic shared-memory limit on the current device, once per device.
-template <class Kernel>
-static int ensure_smem_attribute(PerDeviceOnce& once, Kernel kernel, size_t smem)
-{
-    const int dev = current_device();
-    if (dev < 0) return MXFP4_ERR_CUDA;
-    return once.run(dev, [&] {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) ==
-                       cudaSuccess
-                   ? MXFP4_OK : MXFP4_ERR_CUDA;
-    });
-}
 
 // Host copy of the counter-based generator, used only for the 32-bit sign mask of the
 // randomized rotation (counter (0,0,0,1), key = seed).
@@ -288,8 +226,6 @@ static int launch_quantize_dual(const QuantDualJob& job, int grid, cudaStream_t 
     return launch_quantize_dual_as<HMODE, SR, false>(job, grid, stream);
 }
 
-static size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
 // Self-test of the bounded-wait discipline: one warp waits on a barrier that nothing will ever
 // complete, with a spin limit of a few hundred attempts.  The wait gives up, records the
 // timeout status and the kernel returns normally.
@@ -342,7 +278,7 @@ static int gemm_checked(const void* a_codes, const void* a_scales, const void* b
 
 extern "C" {
 
-int mxfp4_version(void) { return 106; }   // 1.6: shared-space accesses in the quantizers, size limits checked on the host
+int mxfp4_version(void) { return 107; }   // 1.7: 128-block 8-bit product, residual norm, token log probabilities
 
 const char* mxfp4_status_string(int status)
 {
@@ -1025,14 +961,15 @@ int mxfp4_selftest_bounds(void* stream)
 int mxfp4_check(void* stream)
 {
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return MXFP4_ERR_CUDA;
-    int status = 0;
+    int status = 0, other = 0;
     if (cudaMemcpyFromSymbol(&status, g_device_status, sizeof(int)) != cudaSuccess)
         return MXFP4_ERR_CUDA;
     if (status != 0) {
         const int zero = 0;
         cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
     }
-    return status;
+    if (block128_take_status(&other) != MXFP4_OK) return MXFP4_ERR_CUDA;   // the 128-block kernels' own word
+    return status != 0 ? status : other;
 }
 
 }  // extern "C"

@@ -10,8 +10,8 @@
 namespace mxfp4 {
 
 // Sticky device-side status (0 = OK).  Written with atomicCAS so the first error wins.
-// The library is a single translation unit, so the definition lives here.
-__device__ int g_device_status = 0;
+// Every translation unit has its own word; mxfp4_check looks at those of all units with waits.
+static __device__ int g_device_status = 0;
 
 constexpr int kDevErrTimeout = -7;
 constexpr int kDevErrBounds = -10;
@@ -210,6 +210,15 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, const void* smem_
         : "memory");
 }
 
+// 3-D tiled store (the outermost coordinate picks one of several equally shaped matrices).
+__device__ __forceinline__ void tma_store_3d(const void* tmap, const void* smem_src, int32_t x, int32_t y, int32_t z)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+        ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(smem_src)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
 // L2 eviction-priority policies for cache-hinted TMA traffic.
 __device__ __forceinline__ uint64_t l2_policy_evict_first()
 {
@@ -369,6 +378,19 @@ __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t select
     return r;
 }
 
+// Four E4M3 codes (one 32-bit word) from four floats; v0 lands in bits 7:0.
+__device__ __forceinline__ uint32_t cvt_e4m3x4(float v0, float v1, float v2, float v3)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+        "mov.b32 %0, {lo, hi};\n\t}"
+        : "=r"(r)
+        : "f"(v0), "f"(v1), "f"(v2), "f"(v3));
+    return r;
+}
+
 // minimum of the two unsigned 16-bit halves
 __device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b)
 {
@@ -458,6 +480,18 @@ __device__ __forceinline__ void tcgen05_commit_pair(uint64_t* bar, uint16_t cta_
     asm volatile(
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
         ::"r"(smem_u32(bar)), "h"(cta_mask)
+        : "memory");
+}
+
+// Pair MMA on 8-bit operands without block scales, 256 x N x 32: D[tmem] (+)= A[smem] * B[smem]^T.
+__device__ __forceinline__ void tcgen05_mma_f8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                    uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred P;\n\t"
+        "setp.ne.b32 P, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, P;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 

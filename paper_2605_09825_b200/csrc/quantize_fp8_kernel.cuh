@@ -23,19 +23,6 @@ struct QuantFp8Smem {
     int abort_flag;
 };
 
-// Four E4M3 codes (one 32-bit word) from four floats; v0 lands in bits 7:0.
-__device__ __forceinline__ uint32_t cvt_e4m3x4(float v0, float v1, float v2, float v3)
-{
-    uint32_t r;
-    asm("{\n\t.reg .b16 lo, hi;\n\t"
-        "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
-        "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
-        "mov.b32 %0, {lo, hi};\n\t}"
-        : "=r"(r)
-        : "f"(v0), "f"(v1), "f"(v2), "f"(v3));
-    return r;
-}
-
 // One block: maximum, scale byte, scaling, conversion.  32 code bytes out.
 __device__ __forceinline__ void quantize_block_fp8(float2 (&P)[16], uint32_t (&packed)[8], uint32_t& byte)
 {

@@ -49,6 +49,22 @@ inline bool make_tmap_2d(CUtensorMap* map, CUtensorMapDataType dtype, uint32_t e
     return r == CUDA_SUCCESS;
 }
 
+// `count` matrices of the 2-D kind, `matrix_bytes` apart: boxes clip at every matrix's own edges.
+inline bool make_tmap_3d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, uint64_t count, uint64_t rows,
+                         uint64_t cols, uint64_t pitch_bytes, uint64_t matrix_bytes, uint32_t box_rows,
+                         uint32_t box_cols, CUtensorMapSwizzle swizzle)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {cols, rows, count};
+    cuuint64_t strides[2] = {pitch_bytes, matrix_bytes};
+    cuuint32_t box[3] = {box_cols, box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = fn(map, dtype, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 // Launch with the programmatic-stream-serialization attribute (see griddep_wait in
 // ptx_sm100.cuh).  MXFP4_PDL=0 in the environment turns the attribute off (plain stream order).
 inline bool pdl_enabled()
