@@ -190,15 +190,7 @@ static Pass128 pass128(int pass, int64_t T, int64_t in_f, int64_t out_f)
 }
 
 // Status word of this translation unit's kernels, cleared when it is set.
-int block128_take_status(int* status)
-{
-    if (cudaMemcpyFromSymbol(status, g_device_status, sizeof(int)) != cudaSuccess) return MXFP4_ERR_CUDA;
-    if (*status != 0) {
-        const int zero = 0;
-        cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
-    }
-    return MXFP4_OK;
-}
+int block128_take_status(int* status) { return take_device_status(status); }
 
 }  // namespace mxfp4
 

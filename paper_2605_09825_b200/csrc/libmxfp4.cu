@@ -961,15 +961,14 @@ int mxfp4_selftest_bounds(void* stream)
 int mxfp4_check(void* stream)
 {
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return MXFP4_ERR_CUDA;
-    int status = 0, other = 0;
-    if (cudaMemcpyFromSymbol(&status, g_device_status, sizeof(int)) != cudaSuccess)
+    // each translation unit whose kernels wait has a word of its own; the first one set is reported
+    int status = 0, more[2] = {0, 0};
+    if (take_device_status(&status) != 0 || block128_take_status(&more[0]) != 0 ||
+        residual_norm_take_status(&more[1]) != 0)
         return MXFP4_ERR_CUDA;
-    if (status != 0) {
-        const int zero = 0;
-        cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
-    }
-    if (block128_take_status(&other) != MXFP4_OK) return MXFP4_ERR_CUDA;   // the 128-block kernels' own word
-    return status != 0 ? status : other;
+    for (int m : more)
+        if (status == 0) status = m;
+    return status;
 }
 
 }  // extern "C"

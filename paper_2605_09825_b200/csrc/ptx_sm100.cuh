@@ -16,6 +16,17 @@ static __device__ int g_device_status = 0;
 constexpr int kDevErrTimeout = -7;
 constexpr int kDevErrBounds = -10;
 
+// This unit's status word into *status, cleared if it was set; 0 or -6 (a CUDA call failed).
+static inline int take_device_status(int* status)
+{
+    if (cudaMemcpyFromSymbol(status, g_device_status, sizeof(int)) != cudaSuccess) return -6;
+    if (*status != 0) {
+        const int zero = 0;
+        cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
+    }
+    return 0;
+}
+
 // Bounds discipline of the debug build (-DMXFP4_BOUNDS), the stand-in for a memory sanitizer: every
 // access whose address a kernel COMPUTES (shared-memory stages, staging tiles, scale tiles) goes
 // through smem_load / smem_store, which in that build check that the address lies inside the
@@ -164,6 +175,16 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     *abort_flag = 1;
     atomicCAS(&g_device_status, 0, kDevErrTimeout);
     return false;
+}
+
+// The same with the attempt that nearly always succeeds in line and the rest out of line.
+static __device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort_flag)
+{
+    return mbar_wait(bar, parity, abort_flag);
+}
+__device__ __forceinline__ bool mbar_wait_fast(uint64_t* bar, uint32_t parity, volatile int* abort_flag)
+{
+    return mbar_try_wait(bar, parity) || mbar_wait_slow(bar, parity, abort_flag);
 }
 
 // ---------------------------------------------------------------- async-proxy fences
@@ -417,6 +438,16 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
     return r;
+}
+
+// One word into the shared memory of a CTA of the cluster, counted in bytes on a barrier of that CTA: data and
+// signal in one, without the cluster-scope release that a barrier would need (which waits for all of the
+// thread's global stores).
+__device__ __forceinline__ void st_async_f32(uint32_t cluster_addr, float v, uint32_t bar_cluster_addr)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];"
+                 ::"r"(cluster_addr), "f"(v), "r"(bar_cluster_addr)
+                 : "memory");
 }
 
 __device__ __forceinline__ void cluster_sync_all()

@@ -10,11 +10,16 @@
 // root mean squares are formed again from rows that have to be read anyway, so nothing but y is
 // kept between the passes.
 //
-// One CTA walks whole rows: every tensor is read once in 16-byte loads and stays in registers
-// between the reductions over the row.  All arithmetic is fp32; the outputs are rounded once.
+// A row belongs to one CTA (up to 4096 columns, eight per thread) or to a cluster of two or four, which add up
+// their sums through distributed shared memory.  Bulk copies keep a ring of rows on their way into shared
+// memory while the row at hand goes through its reductions in registers; the vectors every row needs and
+// the sums of the weight gradients stay in registers for all of a CTA's rows.  All arithmetic is fp32;
+// the outputs are rounded once.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "../../include/mxfp4.h"
 #include "host_common.cuh"
@@ -25,7 +30,11 @@
 namespace mxfp4 {
 
 constexpr int kNormMaxWidth = 16384;
-constexpr int kNormMaxThreads = 1024;
+constexpr int kNormMaxThreads = 512;
+constexpr int kNormMaxCluster = 4;
+constexpr int kNormMaxStages = 8;
+constexpr int kNormWorkspaceSms = 160;
+constexpr int kNormRingBytes = 200 * 1024;       // per SM
 
 struct NormParams {
     const __nv_bfloat16* branch;
@@ -34,10 +43,15 @@ struct NormParams {
     const float* w_post;
     const float* w_pre;
     int64_t ld_branch, ld_stream, ld_gate;
-    int64_t tokens;
+    int32_t tokens;
     int32_t width;
-    int32_t gate_kind, gate_act;
+    int32_t cluster;                     // CTAs that share a row
+    int32_t cta_chunks;                  // 8-column chunks per CTA
+    int32_t gate_act;
     float skip_scale, branch_scale, eps;
+    // the ring of rows in shared memory: offsets of the tensors inside a stage, -1 where absent
+    int32_t at_stream, at_gate, at_dh, at_dy;
+    int32_t stage_bytes, stages;
 };
 
 struct NormForwardOut {
@@ -51,299 +65,494 @@ struct NormBackwardIo {
     const void* dy;
     void* dx;
     __nv_bfloat16* dbranch;
-    __nv_bfloat16* dgate;                // per element; the per-channel gradient goes through `partials`
-    float* partials;                     // [CTA][accumulated vector][width]
+    void* dgate;                         // bf16 per element; the per-channel gradient goes through `partials`
+    float* partials;                     // [cluster][accumulated vector][width]
     int64_t ld_dh, ld_dy, ld_dx, ld_dbranch, ld_dgate;
     int32_t acc_pre, acc_post, acc_gate; // index of the accumulated vector, -1 where none is wanted
     int32_t n_acc;
 };
 
-// Sum of up to three values over the CTA, the same in every thread.  `slot` alternates with every
-// call so that one barrier per reduction is enough: a slot is written again only after the
-// barrier of the reduction in between.
-template <int N>
-__device__ __forceinline__ void block_sum(float (&v)[N], float* red, int& slot)
+// What a kernel is compiled for: no gate, a gate per channel (its activation is applied once), or a gate per
+// element with one of the activations.
+enum NormGate { kGateNone, kGateChannel, kGateLinear, kGateSigmoid, kGateSilu };
+__host__ __device__ constexpr bool gate_per_element(int gate) { return gate >= kGateLinear; }
+
+// 1 / (1 + e^-x): the reciprocal of infinity is 0, so every finite x and both infinities are fine
+__device__ __forceinline__ float sigmoid(float x)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    float* r = red + slot * (3 * 32);
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) r[i * 32 + warp] = v[i];
-    slot ^= 1;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lane < warps ? r[i * 32 + lane] : 0.0f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
 }
 
-// 1 / (1 + e^-x): the quotient of 1 and infinity is 0, so every finite x and both infinities are fine
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
-
-__device__ __forceinline__ float gate_value(float g, int act)
+template <int GATE>
+__device__ __forceinline__ void gate_value_slope(float g, float& v, float& slope)
 {
-    if (act == MXFP4_GATE_LINEAR) return g;
-    const float s = sigmoid(g);
-    return act == MXFP4_GATE_SIGMOID ? s : g * s;
-}
-
-__device__ __forceinline__ void gate_value_slope(float g, int act, float& v, float& slope)
-{
-    if (act == MXFP4_GATE_LINEAR) {
+    if (GATE == kGateLinear) {
         v = g;
         slope = 1.0f;
         return;
     }
     const float s = sigmoid(g);
-    if (act == MXFP4_GATE_SIGMOID) {
+    if (GATE == kGateSigmoid) {
         v = s;
-        slope = s * (1.0f - s);
+        slope = fmaf(-s, s, s);
     } else {
         v = g * s;
-        slope = s * (1.0f + g * (1.0f - s));
+        slope = s * fmaf(g, 1.0f - s, 1.0f);
     }
 }
 
-// Gate of the eight columns of one chunk (1 without a gate).
-__device__ __forceinline__ void load_gate(const NormParams& p, int64_t row, int col, float (&g)[8])
+template <int GATE>
+__device__ __forceinline__ void gate_pair(const float2& g, float2& v, float2& slope)
 {
-    if (p.gate_kind == MXFP4_GATE_ELEMENT) {
-        load8(static_cast<const __nv_bfloat16*>(p.gate) + row * p.ld_gate + col, g);
-    } else if (p.gate_kind == MXFP4_GATE_CHANNEL) {
-        load8_cached(static_cast<const float*>(p.gate) + col, g);
-    }
+    gate_value_slope<GATE>(g.x, v.x, slope.x);
+    gate_value_slope<GATE>(g.y, v.y, slope.y);
 }
 
-template <class Stream, int C>
-__global__ void __launch_bounds__(C == 1 ? kNormMaxThreads / 2 : kNormMaxThreads, 1)
-residual_norm_forward_kernel(const NormParams p, const NormForwardOut out)
+// the same with the activation as a value (once per kernel)
+__device__ __forceinline__ void gate_pair_of(const float2& g, int act, float2& v, float2& slope)
 {
-    __shared__ float red[2 * 3 * 32];
+    if (act == MXFP4_GATE_LINEAR) gate_pair<kGateLinear>(g, v, slope);
+    else if (act == MXFP4_GATE_SIGMOID) gate_pair<kGateSigmoid>(g, v, slope);
+    else gate_pair<kGateSilu>(g, v, slope);
+}
+
+constexpr int kNormWarps = kNormMaxThreads / 32;
+
+struct NormShared {
+    float red[2][4][kNormMaxCluster * kNormWarps];   // [slot][value][CTA, warp]
+    uint64_t sums[2];                    // a slot's values from all CTAs of the cluster are here
+    uint64_t full[kNormMaxStages];
+    uint64_t empty[kNormMaxStages];
+    int abort_flag;
+};
+
+// Where a thread stands: its chunk of eight columns, and the rows its cluster walks.  A thread past the last
+// chunk works on the last one with the others and keeps its sums and results to itself.
+struct NormPlace {
+    int rank;             // of the CTA in its cluster
+    int local;            // chunk in the CTA's part of a row
+    int col;
+    bool active;
+    int first, step;      // rows first, first + step, ...
+};
+
+template <bool CLUSTER>
+__device__ __forceinline__ NormPlace norm_place(const NormParams& p)
+{
+    NormPlace t;
+    t.rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0;
+    const int here = min(p.cta_chunks, p.width / 8 - t.rank * p.cta_chunks);
+    t.active = static_cast<int>(threadIdx.x) < here;
+    t.local = t.active ? threadIdx.x : here - 1;
+    t.col = (t.rank * p.cta_chunks + t.local) * 8;
+    t.first = CLUSTER ? blockIdx.x / p.cluster : blockIdx.x;
+    t.step = CLUSTER ? gridDim.x / p.cluster : gridDim.x;
+    return t;
+}
+
+// Sums over a row of N values (2 or 4) at once, the same in every thread of the cluster.
+//
+// Inside a warp, exchanges with the lane 16 (and 8) away halve the number of values a lane holds, further
+// exchanges finish the one it is left with: value lane / (32 / N), the same in all lanes of that group.
+// Every warp leaves its sums in the shared memory of all CTAs of the cluster; then every warp adds all of
+// them.  `call` counts the calls: slots alternate, and a slot is written again only after every warp has
+// read it (it takes part in the call in between afterwards).
+template <int N, bool CLUSTER>
+__device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t& call, int cluster, int rank)
+{
+    static_assert(N == 2 || N == 4, "two or four values");
+    constexpr int kLanes = 32 / N;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int slot = call & 1, value = lane / kLanes, in_group = lane & (kLanes - 1);
+    float t;
+    if (N == 2) {
+        const bool up = lane & 16;
+        t = (up ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 16);
+    } else {
+        const bool up = lane & 16, right = lane & 8;
+        const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], 16);
+        const float b = (up ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, up ? v[1] : v[3], 16);
+        t = (right ? b : a) + __shfl_xor_sync(0xffffffffu, right ? a : b, 8);
+    }
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    const int n = CLUSTER ? cluster * warps : warps;
+    if (!CLUSTER) {
+        if (in_group == 0) sh.red[slot][value][warp] = t;
+        __syncthreads();
+    } else {
+        if (in_group < cluster)              // to CTA `in_group`
+            st_async_f32(map_to_cta(smem_u32(&sh.red[slot][value][rank * warps + warp]), in_group), t,
+                         map_to_cta(smem_u32(&sh.sums[slot]), in_group));
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&sh.sums[slot], n * N * 4);
+        (void)mbar_wait_fast(&sh.sums[slot], (call >> 1) & 1, &sh.abort_flag);
+    }
+    ++call;
+    t = 0.0f;
+    if (!CLUSTER) {
+        // at most sixteen warps: one or two entries per lane
+        if (in_group < n) t = sh.red[slot][value][in_group];
+        if (N == 4 && in_group + kLanes < n) t += sh.red[slot][value][in_group + kLanes];
+    } else {
+        for (int j = in_group; j < n; j += kLanes) t += sh.red[slot][value][j];
+    }
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, t, kLanes * i);
+}
+
+template <bool CLUSTER>
+__device__ __forceinline__ void norm_setup(NormShared& sh, const NormParams& p)
+{
+    if (threadIdx.x == 0) {
+        sh.abort_flag = 0;
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(&sh.full[s], 1);
+            mbar_init(&sh.empty[s], blockDim.x >> 5);
+        }
+        for (int s = 0; s < 2; ++s) mbar_init(&sh.sums[s], 1);
+        fence_barrier_init();
+    }
+    if (CLUSTER) cluster_sync_all();
+    else __syncthreads();
     griddep_launch_dependents();
     griddep_wait();
-    const int chunks = p.width >> 3;
-    const float inv_width = 1.0f / static_cast<float>(p.width);
-    int slot = 0;
-    for (int64_t row = blockIdx.x; row < p.tokens; row += gridDim.x) {
-        float u[C][8], x[C][8], g[C][8];
-        float ss[1] = {0.0f};
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int chunk = threadIdx.x + c * blockDim.x;
-            if (chunk < chunks) {
-                load8(p.branch + row * p.ld_branch + chunk * 8, u[c]);
-                if (p.stream) load8(static_cast<const Stream*>(p.stream) + row * p.ld_stream + chunk * 8, x[c]);
-                load_gate(p, row, chunk * 8, g[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ss[0] += u[c][i] * u[c][i];
-            }
-        }
-        float r = 1.0f;
-        if (p.w_post) {
-            block_sum(ss, red, slot);
-            r = rsqrtf(ss[0] * inv_width + p.eps);
-        }
-        ss[0] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int chunk = threadIdx.x + c * blockDim.x;
-            if (chunk < chunks) {
-                float w[8];
-                if (p.w_post) load8_cached(p.w_post + chunk * 8, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float b = u[c][i];
-                    if (p.w_post) b = b * r * w[i];
-                    if (p.gate_kind != MXFP4_GATE_NONE) b *= gate_value(g[c][i], p.gate_act);
-                    b *= p.branch_scale;
-                    if (p.stream) b = fmaf(p.skip_scale, x[c][i], b);
-                    u[c][i] = b;
-                }
-                store8(static_cast<Stream*>(out.y) + row * out.ld_y + chunk * 8, u[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    u[c][i] = as_stored<Stream>(u[c][i]);
-                    ss[0] += u[c][i] * u[c][i];
-                }
-            }
-        }
-        if (p.w_pre) {
-            block_sum(ss, red, slot);
-            r = rsqrtf(ss[0] * inv_width + p.eps);
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int chunk = threadIdx.x + c * blockDim.x;
-                if (chunk < chunks) {
-                    float w[8];
-                    load8_cached(p.w_pre + chunk * 8, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] *= u[c][i] * r;
-                    store8(out.h + row * out.ld_h + chunk * 8, w);
-                }
-            }
-        }
-    }
 }
 
-// Weight gradients: a column belongs to one thread, which adds its rows' terms to fp32 sums in
-// shared memory; each CTA leaves its sums in the workspace and `sum_partials_kernel` adds them in a
-// fixed order, so the result does not depend on scheduling.  (Two float4 planes per vector: with
-// the eight values of a chunk side by side every second bank would be hit twice.)
-__device__ __forceinline__ void accumulate8(float* acc, int chunks, int chunk, const float (&v)[8])
+// Eight values of a tensor's part of a stage.
+__device__ __forceinline__ void stage8(const uint8_t* at, const uint8_t* stage, int bytes, float2 (&v)[4], __nv_bfloat16)
 {
-    float4* lo = reinterpret_cast<float4*>(acc) + chunk;
-    float4* hi = lo + chunks;
-    float4 a = *lo, b = *hi;
-    a.x += v[0]; a.y += v[1]; a.z += v[2]; a.w += v[3];
-    b.x += v[4]; b.y += v[5]; b.z += v[6]; b.w += v[7];
-    *lo = a;
-    *hi = b;
+    unpack8(smem_load<uint4>(at, stage, bytes), v);
+}
+__device__ __forceinline__ void stage8(const uint8_t* at, const uint8_t* stage, int bytes, float2 (&v)[4], float)
+{
+    const float4 a = smem_load<float4>(at, stage, bytes), b = smem_load<float4>(at + 16, stage, bytes);
+    v[0] = make_float2(a.x, a.y);
+    v[1] = make_float2(a.z, a.w);
+    v[2] = make_float2(b.x, b.y);
+    v[3] = make_float2(b.z, b.w);
 }
 
-template <class Stream, int C>
-__global__ void __launch_bounds__(C == 1 ? kNormMaxThreads / 2 : kNormMaxThreads, 1)
-residual_norm_backward_kernel(const NormParams p, const NormBackwardIo io)
+// Starts the loads of one row's columns of this CTA into a stage (one thread): whole row pieces as bulk copies.
+template <class Stream, int GATE>
+__device__ __forceinline__ void norm_issue(const NormParams& p, const NormPlace& t, int row, uint8_t* stage, uint64_t* bar,
+                                           const NormBackwardIo* io)
 {
-    extern __shared__ __align__(16) float acc_all[];       // [accumulated vector][width]
-    __shared__ float red[2 * 3 * 32];
-    griddep_launch_dependents();
-    griddep_wait();
-    const int chunks = p.width >> 3;
-    const float inv_width = 1.0f / static_cast<float>(p.width);
-    int slot = 0;
-    float* acc_pre = acc_all + static_cast<int64_t>(io.acc_pre) * p.width;
-    float* acc_post = acc_all + static_cast<int64_t>(io.acc_post) * p.width;
-    float* acc_gate = acc_all + static_cast<int64_t>(io.acc_gate) * p.width;
-    for (int i = threadIdx.x; i < io.n_acc * p.width; i += blockDim.x) acc_all[i] = 0.0f;
-    __syncthreads();
+    const int col = t.rank * p.cta_chunks * 8;
+    const uint32_t n = static_cast<uint32_t>(min(p.cta_chunks * 8, p.width - col));
+    const uint32_t half = n * 2, full = n * sizeof(Stream);
+    const int64_t r = row;
+    uint32_t bytes = half;
+    if (p.at_stream >= 0) bytes += full;
+    if (gate_per_element(GATE)) bytes += half;
+    if (io && p.at_dh >= 0) bytes += half;
+    if (io && p.at_dy >= 0) bytes += full;
+    mbar_arrive_expect_tx(bar, bytes);
+    bulk_load_1d(stage, p.branch + r * p.ld_branch + col, half, bar);
+    if (p.at_stream >= 0)
+        bulk_load_1d(stage + p.at_stream, static_cast<const Stream*>(p.stream) + r * p.ld_stream + col, full, bar);
+    if (gate_per_element(GATE))
+        bulk_load_1d(stage + p.at_gate, static_cast<const __nv_bfloat16*>(p.gate) + r * p.ld_gate + col, half, bar);
+    if (io && p.at_dh >= 0) bulk_load_1d(stage + p.at_dh, io->dh + r * io->ld_dh + col, half, bar);
+    if (io && p.at_dy >= 0)
+        bulk_load_1d(stage + p.at_dy, static_cast<const Stream*>(io->dy) + r * io->ld_dy + col, full, bar);
+}
 
-    for (int64_t row = blockIdx.x; row < p.tokens; row += gridDim.x) {
-        float d[C][8], u[C][8], y[C][8], q[C][8];
-        float s[3] = {0.0f, 0.0f, 0.0f};           // sum u^2, sum y^2, sum dh w_pre y
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int chunk = threadIdx.x + c * blockDim.x;
-            if (chunk < chunks) {
-                const int64_t col = chunk * 8;
-                load8(p.branch + row * p.ld_branch + col, u[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[0] += u[c][i] * u[c][i];
-                if (p.w_pre) {
-                    load8(static_cast<const Stream*>(p.stream) + row * p.ld_stream + col, y[c]);
-                    load8(io.dh + row * io.ld_dh + col, q[c]);
-                    float w[8];
-                    load8_cached(p.w_pre + col, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        s[1] += y[c][i] * y[c][i];
-                        s[2] += q[c][i] * w[i] * y[c][i];
-                    }
-                }
-                if (io.dy) {
-                    load8(static_cast<const Stream*>(io.dy) + row * io.ld_dy + col, d[c]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[c][i] = 0.0f;
-                }
-            }
-        }
-        float r_u = 1.0f, r_y = 0.0f, mean_y = 0.0f;
-        if (p.w_post || p.w_pre) {
-            block_sum(s, red, slot);
-            if (p.w_post) r_u = rsqrtf(s[0] * inv_width + p.eps);
-            if (p.w_pre) {
-                r_y = rsqrtf(s[1] * inv_width + p.eps);
-                mean_y = r_y * s[2] * inv_width;                   // mean of dh w_pre y / rms(y)
-            }
-        }
-        float t[1] = {0.0f};                       // sum of the branch gradient's n term
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int chunk = threadIdx.x + c * blockDim.x;
-            if (chunk < chunks) {
-                const int64_t col = chunk * 8;
-                if (p.w_pre) {
-                    float w[8];
-                    load8_cached(p.w_pre + col, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float yh = y[c][i] * r_y;
-                        d[c][i] += r_y * (q[c][i] * w[i] - yh * mean_y);
-                        w[i] = q[c][i] * yh;
-                    }
-                    if (io.acc_pre >= 0) accumulate8(acc_pre, chunks, chunk, w);
-                }
-                float o[8];
-                if (io.dx) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = p.skip_scale * d[c][i];
-                    store8(static_cast<Stream*>(io.dx) + row * io.ld_dx + col, o);
-                }
-                float w[8];
-                if (p.w_post) load8_cached(p.w_post + col, w);
-                if (p.gate_kind != MXFP4_GATE_NONE) {
-                    load_gate(p, row, chunk * 8, o);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float v, slope;
-                        gate_value_slope(o[i], p.gate_act, v, slope);
-                        const float e = p.branch_scale * d[c][i];
-                        float b = u[c][i];
-                        if (p.w_post) b *= r_u * w[i];
-                        o[i] = e * b * slope;
-                        d[c][i] = e * v;
-                    }
-                    if (io.dgate) store8(io.dgate + row * io.ld_dgate + col, o);
-                    if (io.acc_gate >= 0) accumulate8(acc_gate, chunks, chunk, o);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[c][i] *= p.branch_scale;
-                }
-                if (p.w_post) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        u[c][i] *= r_u;
-                        o[i] = d[c][i] * u[c][i];
-                        d[c][i] *= w[i];
-                        t[0] += d[c][i] * u[c][i];
-                    }
-                    if (io.acc_post >= 0) accumulate8(acc_post, chunks, chunk, o);
-                }
-            }
-        }
-        float mean_u = 0.0f;
-        if (p.w_post) {
-            block_sum(t, red, slot);
-            mean_u = t[0] * inv_width;
-        }
-        if (io.dbranch) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int chunk = threadIdx.x + c * blockDim.x;
-                if (chunk < chunks) {
-                    if (p.w_post)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) d[c][i] = r_u * (d[c][i] - u[c][i] * mean_u);
-                    store8(io.dbranch + row * io.ld_dbranch + chunk * 8, d[c]);
-                }
-            }
+// This warp has its part of a stage in registers.
+__device__ __forceinline__ void norm_release(NormShared& sh, int s)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.empty[s]);
+}
+
+// Once all warps have: the row that takes the stage next (one thread).
+template <class Stream, int GATE>
+__device__ __forceinline__ void norm_refill(const NormParams& p, const NormPlace& t, int row, uint8_t* stage, NormShared& sh,
+                                            int s, uint32_t parity, const NormBackwardIo* io)
+{
+    if (threadIdx.x == 0 && row + static_cast<int64_t>(p.stages) * t.step < p.tokens &&
+        mbar_wait_fast(&sh.empty[s], parity, &sh.abort_flag))
+        norm_issue<Stream, GATE>(p, t, row + p.stages * t.step, stage, &sh.full[s], io);
+}
+
+// Walks a [tokens x width] matrix with the rows of a cluster.
+template <class T>
+struct RowWalk {
+    T* at;
+    int64_t step;
+    __device__ __forceinline__ RowWalk(void* base, int64_t ld, const NormPlace& t)
+        : at(static_cast<T*>(base) + t.first * ld + t.col), step(t.step * ld) {}
+    __device__ __forceinline__ void next() { at += step; }
+};
+
+// Position in the ring.
+struct RingPlace {
+    int s = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next(int stages)
+    {
+        if (++s == stages) {
+            s = 0;
+            parity ^= 1u;
         }
     }
-    // a thread wrote and reads only its own columns
-    for (int a = 0; a < io.n_acc; ++a) {
-        const float4* src = reinterpret_cast<const float4*>(acc_all + static_cast<int64_t>(a) * p.width);
-        float4* dst = reinterpret_cast<float4*>(io.partials + (static_cast<int64_t>(blockIdx.x) * io.n_acc + a) * p.width);
-        for (int chunk = threadIdx.x; chunk < chunks; chunk += blockDim.x) {
-            dst[2 * chunk] = src[chunk];
-            dst[2 * chunk + 1] = src[chunks + chunk];
+};
+
+template <class Stream, int GATE, bool CLUSTER>
+__global__ void __launch_bounds__(kNormMaxThreads, 2)
+residual_norm_forward_kernel(const __grid_constant__ NormParams p, const __grid_constant__ NormForwardOut out)
+{
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ NormShared sh;
+    norm_setup<CLUSTER>(sh, p);
+    const NormPlace t = norm_place<CLUSTER>(p);
+    const float inv_width = 1.0f / static_cast<float>(p.width);
+    const bool post = p.w_post != nullptr, pre = p.w_pre != nullptr;
+    if (threadIdx.x == 0)
+        for (int s = 0; s < p.stages && t.first + s * t.step < p.tokens; ++s)
+            norm_issue<Stream, GATE>(p, t, t.first + s * t.step, ring + s * p.stage_bytes, &sh.full[s], nullptr);
+    // vectors every row needs
+    float2 wb[4], wh[4], w[4];                // branch_scale * w_post * channel gate, w_pre
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        wb[i] = pair(p.branch_scale);
+        wh[i] = pair(1.0f);
+    }
+    if (post) {
+        load8(p.w_post + t.col, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wb[i] = __fmul2_rn(wb[i], w[i]);
+    }
+    if (GATE == kGateChannel) {
+        load8(static_cast<const float*>(p.gate) + t.col, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 v, slope;
+            gate_pair_of(w[i], p.gate_act, v, slope);
+            wb[i] = __fmul2_rn(wb[i], v);
         }
     }
+    if (pre) load8(p.w_pre + t.col, wh);
+    RowWalk<Stream> y(out.y, out.ld_y, t);
+    RowWalk<__nv_bfloat16> h(out.h, out.ld_h, t);
+    RingPlace at, ahead;                       // of the row at hand, of the one after it
+    uint32_t call = 0;
+    // One reduction per row: the sum the first norm of the NEXT row needs, and the one the second norm of this
+    // row needs.  The next row's part is read from its stage twice for that, which costs less than a second
+    // barrier in every row.
+    float sums[2];
+    auto look_ahead = [&](int row) {
+        sums[0] = 0.0f;
+        if (post && row < p.tokens) {
+            const uint8_t* stage = ring + ahead.s * p.stage_bytes;
+            (void)mbar_wait_fast(&sh.full[ahead.s], ahead.parity, &sh.abort_flag);   // given up: the status word says so
+            float2 u[4];
+            stage8(stage + t.local * 16, stage, p.stage_bytes, u, __nv_bfloat16());
+            float2 sq = __fmul2_rn(u[0], u[0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) sq = __ffma2_rn(u[i], u[i], sq);
+            sums[0] = t.active ? sq.x + sq.y : 0.0f;
+        }
+        ahead.next(p.stages);
+    };
+    look_ahead(t.first);
+    sums[1] = 0.0f;
+    if (post) row_sum<2, CLUSTER>(sums, sh, call, p.cluster, t.rank);
+    for (int row = t.first; row < p.tokens; row += t.step) {
+        const float r_u = post ? rsqrtf(sums[0] * inv_width + p.eps) : 1.0f;
+        look_ahead(row + t.step);
+        uint8_t* stage = ring + at.s * p.stage_bytes;
+        (void)mbar_wait_fast(&sh.full[at.s], at.parity, &sh.abort_flag);
+        float2 u[4], x[4], g[4];
+        stage8(stage + t.local * 16, stage, p.stage_bytes, u, __nv_bfloat16());
+        if (p.at_stream >= 0) {
+            stage8(stage + p.at_stream + t.local * (8 * sizeof(Stream)), stage, p.stage_bytes, x, Stream());
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = pair(0.0f);
+        }
+        if (gate_per_element(GATE)) stage8(stage + p.at_gate + t.local * 16, stage, p.stage_bytes, g, __nv_bfloat16());
+        norm_release(sh, at.s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 b = __fmul2_rn(__fmul2_rn(u[i], pair(r_u)), wb[i]);
+            if (gate_per_element(GATE)) {
+                float2 v, slope;
+                gate_pair<GATE>(g[i], v, slope);
+                b = __fmul2_rn(b, v);
+            }
+            u[i] = __ffma2_rn(pair(p.skip_scale), x[i], b);
+        }
+        store8_round(y.at, u, t.active);
+        y.next();
+        if (pre) {
+            float2 sq = __fmul2_rn(u[0], u[0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) sq = __ffma2_rn(u[i], u[i], sq);
+            sums[1] = t.active ? sq.x + sq.y : 0.0f;
+        }
+        if (post || pre) row_sum<2, CLUSTER>(sums, sh, call, p.cluster, t.rank);
+        norm_refill<Stream, GATE>(p, t, row, stage, sh, at.s, at.parity, nullptr);
+        if (pre) {
+            const float r = rsqrtf(sums[1] * inv_width + p.eps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = __fmul2_rn(__fmul2_rn(u[i], pair(r)), wh[i]);
+            if (t.active) store8(h.at, u);
+            h.next();
+        }
+        at.next(p.stages);
+    }
+    if (CLUSTER) cluster_sync_all();             // no CTA leaves while a peer may still write to its shared memory
+}
+
+// Weight gradients: a column belongs to one thread of a cluster, which adds its rows' terms in registers; each
+// cluster leaves its sums in the workspace and `sum_partials_kernel` adds them in a fixed order, so the
+// result does not depend on scheduling.
+template <class Stream, int GATE, bool CLUSTER>
+__global__ void __launch_bounds__(kNormMaxThreads, 1)
+residual_norm_backward_kernel(const __grid_constant__ NormParams p, const __grid_constant__ NormBackwardIo io)
+{
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ NormShared sh;
+    norm_setup<CLUSTER>(sh, p);
+    const NormPlace t = norm_place<CLUSTER>(p);
+    const float inv_width = 1.0f / static_cast<float>(p.width);
+    const bool post = p.w_post != nullptr, pre = p.w_pre != nullptr;
+    if (threadIdx.x == 0)
+        for (int s = 0; s < p.stages && t.first + s * t.step < p.tokens; ++s)
+            norm_issue<Stream, GATE>(p, t, t.first + s * t.step, ring + s * p.stage_bytes, &sh.full[s], &io);
+    // vectors every row needs, and the sums of the gradients of such vectors
+    float2 w_post[4], w_pre[4], gv[4], gs[4];
+    float2 acc_post[4], acc_pre[4], acc_gate[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w_post[i] = w_pre[i] = gv[i] = gs[i] = pair(1.0f);
+        acc_post[i] = acc_pre[i] = acc_gate[i] = pair(0.0f);
+    }
+    if (post) load8(p.w_post + t.col, w_post);
+    if (pre) load8(p.w_pre + t.col, w_pre);
+    if (GATE == kGateChannel) {
+        float2 w[4];
+        load8(static_cast<const float*>(p.gate) + t.col, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) gate_pair_of(w[i], p.gate_act, gv[i], gs[i]);
+    }
+    const bool want_dx = t.active && io.dx, want_dbranch = t.active && io.dbranch, want_dgate = t.active && io.dgate;
+    RowWalk<Stream> dx(io.dx, io.ld_dx, t);
+    RowWalk<__nv_bfloat16> dbranch(io.dbranch, io.ld_dbranch, t), dgate(io.dgate, io.ld_dgate, t);
+    RingPlace at, ahead;
+    uint32_t call = 0;
+    // One reduction per row, as in the forward kernel: sum u^2, sum y^2, sum dh w_pre y of the NEXT row, and the
+    // sum of this row's branch gradient times n.
+    float m[4];
+    auto look_ahead = [&](int row) {
+        m[0] = m[1] = m[2] = 0.0f;
+        if ((post || pre) && row < p.tokens) {
+            const uint8_t* stage = ring + ahead.s * p.stage_bytes;
+            (void)mbar_wait_fast(&sh.full[ahead.s], ahead.parity, &sh.abort_flag);   // given up: the status word says so
+            float2 u[4], y[4], q[4];
+            stage8(stage + t.local * 16, stage, p.stage_bytes, u, __nv_bfloat16());
+            float2 uu = __fmul2_rn(u[0], u[0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) uu = __ffma2_rn(u[i], u[i], uu);
+            if (t.active) m[0] = uu.x + uu.y;
+            if (pre) {
+                stage8(stage + p.at_stream + t.local * (8 * sizeof(Stream)), stage, p.stage_bytes, y, Stream());
+                stage8(stage + p.at_dh + t.local * 16, stage, p.stage_bytes, q, __nv_bfloat16());
+                float2 yy = pair(0.0f), qy = pair(0.0f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    yy = __ffma2_rn(y[i], y[i], yy);
+                    qy = __ffma2_rn(__fmul2_rn(q[i], w_pre[i]), y[i], qy);
+                }
+                if (t.active) {
+                    m[1] = yy.x + yy.y;
+                    m[2] = qy.x + qy.y;
+                }
+            }
+        }
+        ahead.next(p.stages);
+    };
+    look_ahead(t.first);
+    m[3] = 0.0f;
+    if (post || pre) row_sum<4, CLUSTER>(m, sh, call, p.cluster, t.rank);
+    for (int row = t.first; row < p.tokens; row += t.step) {
+        // a norm that is left out has r = 1, mean = 0 and weights of 1, which leave every value as it is
+        const float r_u = post ? rsqrtf(m[0] * inv_width + p.eps) : 1.0f;
+        const float r_y = pre ? rsqrtf(m[1] * inv_width + p.eps) : 0.0f;
+        const float mean_y = r_y * m[2] * inv_width;               // mean of dh w_pre y / rms(y)
+        look_ahead(row + t.step);
+        uint8_t* stage = ring + at.s * p.stage_bytes;
+        (void)mbar_wait_fast(&sh.full[at.s], at.parity, &sh.abort_flag);
+        float2 d[4], u[4], g[4], o[4];
+        stage8(stage + t.local * 16, stage, p.stage_bytes, u, __nv_bfloat16());
+        if (p.at_dy >= 0) {
+            stage8(stage + p.at_dy + t.local * (8 * sizeof(Stream)), stage, p.stage_bytes, d, Stream());
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = pair(0.0f);
+        }
+        if (gate_per_element(GATE)) stage8(stage + p.at_gate + t.local * 16, stage, p.stage_bytes, g, __nv_bfloat16());
+        if (pre) {
+            float2 y[4], q[4];
+            stage8(stage + p.at_stream + t.local * (8 * sizeof(Stream)), stage, p.stage_bytes, y, Stream());
+            stage8(stage + p.at_dh + t.local * 16, stage, p.stage_bytes, q, __nv_bfloat16());
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 yh = __fmul2_rn(y[i], pair(r_y));
+                acc_pre[i] = __ffma2_rn(q[i], yh, acc_pre[i]);
+                d[i] = __ffma2_rn(pair(r_y), __ffma2_rn(yh, pair(-mean_y), __fmul2_rn(q[i], w_pre[i])), d[i]);
+            }
+        }
+        norm_release(sh, at.s);
+        if (want_dx) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = __fmul2_rn(pair(p.skip_scale), d[i]);
+            store8(dx.at, o);
+        }
+        float2 un = pair(0.0f);                    // sum of the branch gradient's n term
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            d[i] = __fmul2_rn(d[i], pair(p.branch_scale));
+            u[i] = __fmul2_rn(u[i], pair(r_u));
+            if (GATE != kGateNone) {
+                float2 v = gv[i], slope = gs[i];
+                if (gate_per_element(GATE)) gate_pair<GATE>(g[i], v, slope);
+                o[i] = __fmul2_rn(__fmul2_rn(d[i], u[i]), w_post[i]);
+                if (GATE != kGateLinear) o[i] = __fmul2_rn(o[i], slope);
+                if (GATE == kGateChannel) acc_gate[i] = __fadd2_rn(acc_gate[i], o[i]);
+                d[i] = __fmul2_rn(d[i], v);
+            }
+            acc_post[i] = __ffma2_rn(d[i], u[i], acc_post[i]);
+            d[i] = __fmul2_rn(d[i], w_post[i]);
+            un = __ffma2_rn(d[i], u[i], un);
+        }
+        if (gate_per_element(GATE) && want_dgate) store8(dgate.at, o);
+        m[3] = t.active ? un.x + un.y : 0.0f;
+        if (post || pre) row_sum<4, CLUSTER>(m, sh, call, p.cluster, t.rank);
+        norm_refill<Stream, GATE>(p, t, row, stage, sh, at.s, at.parity, &io);
+        if (want_dbranch) {
+            const float mean_u = post ? m[3] * inv_width : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = __fmul2_rn(pair(r_u), __ffma2_rn(u[i], pair(-mean_u), d[i]));
+            store8(dbranch.at, d);
+        }
+        dx.next();
+        dbranch.next();
+        dgate.next();
+        at.next(p.stages);
+    }
+    if (t.active) {
+        float* part = io.partials + static_cast<int64_t>(t.first) * io.n_acc * p.width + t.col;
+        if (io.acc_pre >= 0) store8(part + static_cast<int64_t>(io.acc_pre) * p.width, acc_pre);
+        if (io.acc_post >= 0) store8(part + static_cast<int64_t>(io.acc_post) * p.width, acc_post);
+        if (io.acc_gate >= 0) store8(part + static_cast<int64_t>(io.acc_gate) * p.width, acc_gate);
+    }
+    if (CLUSTER) cluster_sync_all();             // no CTA leaves while a peer may still write to its shared memory
 }
 
 struct SumPartials {
@@ -380,53 +589,131 @@ __global__ void __launch_bounds__(kSumWarps * 32) sum_partials_kernel(const SumP
         }
         const int64_t col = at * 4;
         const int a = static_cast<int>(col / p.width);
-        *reinterpret_cast<float4*>(p.out[a] + (col - static_cast<int64_t>(a) * p.width)) = s;
+        float* out = a == 0 ? p.out[0] : a == 1 ? p.out[1] : p.out[2];
+        *reinterpret_cast<float4*>(out + (col - static_cast<int64_t>(a) * p.width)) = s;
     }
 }
 
-// Threads per row and 8-column chunks per thread: one chunk each up to 512 threads, two beyond.
-static int norm_chunks_per_thread(int width) { return width <= 4096 ? 1 : 2; }
+// Shape of a launch: up to 4096 columns per CTA (eight per thread), a cluster of CTAs for wider rows, and as
+// many CTAs per SM as their registers allow; the ring takes what shared memory that leaves.  Rows of 4096
+// split over two CTAs of half the threads (twice as many on an SM) measured slower: 16384 x 4096 backward
+// 253 us against 200, forward 146 against 137 -- the exchange between the CTAs costs more than the
+// independent barriers gain.
+struct NormShape {
+    int cluster, cta_chunks, threads, per_sm;
+};
 
-static int norm_threads(int width)
+static NormShape norm_shape(int width, bool backward)
 {
-    const int c = norm_chunks_per_thread(width);
-    const int need = (width / 8 + c - 1) / c;
-    return (need + 31) / 32 * 32;
+    NormShape n;
+    n.cluster = width <= 4096 ? 1 : width <= 8192 ? 2 : 4;
+    n.cta_chunks = (width / 8 + n.cluster - 1) / n.cluster;
+    n.threads = (n.cta_chunks + 31) / 32 * 32;
+    const int threads_per_sm = backward ? 512 : 1024;            // 128 / 64 registers each
+    n.per_sm = threads_per_sm / n.threads;
+    if (n.per_sm > 8) n.per_sm = 8;
+    return n;
 }
 
-static int norm_backward_ctas(int64_t tokens, int width, int n_acc, int sm_count)
+// Clusters of this size the device holds with one CTA per SM; a larger persistent grid would run its last
+// clusters as a second wave (of four CTAs, 33 fit on 148 SMs, not 37).
+static int resident_clusters(int cluster, int sm_count)
 {
-    // resident CTAs: 64 registers per thread and the shared accumulators
-    const int by_threads = 1024 / norm_threads(width);
-    const int by_smem = n_acc > 0 ? (200 * 1024) / (n_acc * width * 4 + 2048) : by_threads;
-    int per_sm = by_threads < by_smem ? by_threads : by_smem;
-    if (per_sm > 4) per_sm = 4;
-    if (per_sm < 1) per_sm = 1;
-    const int64_t ctas = static_cast<int64_t>(per_sm) * sm_count;
-    return static_cast<int>(tokens < ctas ? tokens : ctas);
+    if (cluster == 1) return sm_count;
+    static int count[kMaxDevices][2] = {};
+    static PerDeviceOnce once[2];
+    const int dev = current_device(), k = cluster == 2 ? 0 : 1;
+    if (dev < 0) return 0;
+    once[k].run(dev, [&] {
+        auto kernel = residual_norm_backward_kernel<__nv_bfloat16, kGateNone, true>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(sm_count / cluster * cluster), 1, 1);
+        cfg.blockDim = dim3(kNormMaxThreads, 1, 1);
+        cfg.dynamicSmemBytes = kNormRingBytes;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = static_cast<unsigned>(cluster);
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormRingBytes) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+            (void)cudaGetLastError();
+            n = sm_count / cluster;
+        }
+        count[dev][k] = n;
+        return MXFP4_OK;
+    });
+    return count[dev][k];
 }
 
-template <class Stream, int C>
-static int launch_norm_forward(const NormParams& p, const NormForwardOut& out, int sm_count, cudaStream_t st)
+// Clusters of a launch (one row at a time each).
+static int norm_clusters(const NormShape& n, int64_t tokens, int resident)
 {
-    const int64_t most = static_cast<int64_t>(sm_count) * 64;
-    const int grid = static_cast<int>(p.tokens < most ? p.tokens : most);
-    return launch_kernel_pdl(residual_norm_forward_kernel<Stream, C>, grid, norm_threads(p.width), 0, st, p, out) ==
-                   cudaSuccess
-               ? MXFP4_OK : MXFP4_ERR_CUDA;
+    const int64_t most = static_cast<int64_t>(n.per_sm) * resident;
+    return static_cast<int>(tokens < most ? tokens : most);
 }
 
-template <class Stream, int C>
-static int launch_norm_backward(const NormParams& p, const NormBackwardIo& io, int grid, cudaStream_t st)
+// Stage layout and ring depth.
+static void norm_ring(NormParams* p, const NormShape& n, int stream_bytes, bool gate, bool dh, bool dy)
 {
-    static PerDeviceOnce once;
-    const size_t most = static_cast<size_t>(3) * kNormMaxWidth * 4;
-    const int rc = ensure_smem_attribute(once, residual_norm_backward_kernel<Stream, C>, most);
+    const int cols = n.cta_chunks * 8;
+    int at = cols * 2;
+    auto take = [&](bool present, int bytes) {
+        const int here = present ? at : -1;
+        if (present) at += bytes;
+        return here;
+    };
+    p->cluster = n.cluster;
+    p->cta_chunks = n.cta_chunks;
+    p->at_stream = take(p->stream != nullptr, cols * stream_bytes);
+    p->at_gate = take(gate, cols * 2);
+    p->at_dh = take(dh, cols * 2);
+    p->at_dy = take(dy, cols * stream_bytes);
+    p->stage_bytes = (at + 127) / 128 * 128;
+    const int room = kNormRingBytes / n.per_sm / p->stage_bytes;
+    p->stages = room < kNormMaxStages ? room : kNormMaxStages;
+}
+
+template <class Kernel, class... Args>
+static int launch_norm(PerDeviceOnce& once, Kernel kernel, const NormParams& p, const NormShape& n, int clusters,
+                       cudaStream_t st, const Args&... args)
+{
+    const int rc = ensure_smem_attribute(once, kernel, kNormRingBytes);
     if (rc != MXFP4_OK) return rc;
-    const size_t smem = static_cast<size_t>(io.n_acc) * p.width * 4;
-    return launch_kernel_pdl(residual_norm_backward_kernel<Stream, C>, grid, norm_threads(p.width), smem, st, p, io) ==
-                   cudaSuccess
+    return launch_kernel_pdl_cluster(kernel, clusters * n.cluster, n.threads, static_cast<size_t>(p.stages) * p.stage_bytes,
+                                     n.cluster, st, p, args...) == cudaSuccess
                ? MXFP4_OK : MXFP4_ERR_CUDA;
+}
+
+template <class Stream, int GATE>
+static int launch_norm_forward(const NormParams& p, const NormForwardOut& out, const NormShape& n, int clusters,
+                               cudaStream_t st)
+{
+    static PerDeviceOnce once[2];
+    return n.cluster > 1 ? launch_norm(once[1], residual_norm_forward_kernel<Stream, GATE, true>, p, n, clusters, st, out)
+                         : launch_norm(once[0], residual_norm_forward_kernel<Stream, GATE, false>, p, n, clusters, st, out);
+}
+
+template <class Stream, int GATE>
+static int launch_norm_backward(const NormParams& p, const NormBackwardIo& io, const NormShape& n, int clusters,
+                                cudaStream_t st)
+{
+    static PerDeviceOnce once[2];
+    return n.cluster > 1 ? launch_norm(once[1], residual_norm_backward_kernel<Stream, GATE, true>, p, n, clusters, st, io)
+                         : launch_norm(once[0], residual_norm_backward_kernel<Stream, GATE, false>, p, n, clusters, st, io);
+}
+
+// Calls f with the NormGate of a (checked) description as a constant.
+template <class F>
+static int with_gate(const mxfp4_norm_desc* n, F&& f)
+{
+    if (n->gate_kind == MXFP4_GATE_NONE) return f(std::integral_constant<int, kGateNone>());
+    if (n->gate_kind == MXFP4_GATE_CHANNEL) return f(std::integral_constant<int, kGateChannel>());
+    if (n->gate_act == MXFP4_GATE_LINEAR) return f(std::integral_constant<int, kGateLinear>());
+    if (n->gate_act == MXFP4_GATE_SIGMOID) return f(std::integral_constant<int, kGateSigmoid>());
+    return f(std::integral_constant<int, kGateSilu>());
 }
 
 // What both directions check of the description; `stream` may be absent (forward: nothing is added;
@@ -439,7 +726,7 @@ static int norm_params(const mxfp4_norm_desc* n, NormParams* p)
     if (n->stream_dtype != MXFP4_OUT_BF16 && n->stream_dtype != MXFP4_OUT_FP32) return MXFP4_ERR_ENUM;
     if (!(n->eps >= 0.0f)) return MXFP4_ERR_ENUM;
     if ((n->gate_kind != MXFP4_GATE_NONE) != (n->gate != nullptr)) return MXFP4_ERR_NULL;
-    if (n->tokens <= 0 || n->width <= 0 || n->tokens > 0x7FFFFFFF) return MXFP4_ERR_SHAPE;
+    if (n->tokens <= 0 || n->width <= 0 || n->tokens > 0x7FFF0000) return MXFP4_ERR_SHAPE;
     if (n->width % 8 != 0 || n->width > kNormMaxWidth) return MXFP4_ERR_SHAPE;
     const bool element = n->gate_kind == MXFP4_GATE_ELEMENT;
     if (n->ld_branch < n->width || (n->stream && n->ld_stream < n->width) || (element && n->ld_gate < n->width))
@@ -457,15 +744,17 @@ static int norm_params(const mxfp4_norm_desc* n, NormParams* p)
     p->ld_branch = n->ld_branch;
     p->ld_stream = n->ld_stream;
     p->ld_gate = n->ld_gate;
-    p->tokens = n->tokens;
+    p->tokens = static_cast<int32_t>(n->tokens);
     p->width = static_cast<int32_t>(n->width);
-    p->gate_kind = n->gate_kind;
     p->gate_act = n->gate_act;
     p->skip_scale = n->skip_scale;
     p->branch_scale = n->branch_scale;
     p->eps = n->eps;
     return MXFP4_OK;
 }
+
+// Status word of this translation unit's kernels, cleared when it is set.
+int residual_norm_take_status(int* status) { return take_device_status(status); }
 
 // A [tokens x width] output or gradient: leading dimension and alignment.
 static int norm_matrix_ok(const void* t, int64_t ld, int64_t width)
@@ -493,21 +782,25 @@ int mxfp4_residual_norm_forward(const mxfp4_norm_desc* norm, void* y, int64_t ld
     if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
     const NormForwardOut out = {y, static_cast<__nv_bfloat16*>(h), ld_y, ld_h};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool one = norm_chunks_per_thread(p.width) == 1;
-    if (norm->stream_dtype == MXFP4_OUT_BF16)
-        return one ? launch_norm_forward<__nv_bfloat16, 1>(p, out, dev.sm_count, st)
-                   : launch_norm_forward<__nv_bfloat16, 2>(p, out, dev.sm_count, st);
-    return one ? launch_norm_forward<float, 1>(p, out, dev.sm_count, st)
-               : launch_norm_forward<float, 2>(p, out, dev.sm_count, st);
+    const bool bf16 = norm->stream_dtype == MXFP4_OUT_BF16;
+    const NormShape n = norm_shape(p.width, false);
+    norm_ring(&p, n, bf16 ? 2 : 4, norm->gate_kind == MXFP4_GATE_ELEMENT, false, false);
+    const int clusters = norm_clusters(n, p.tokens, resident_clusters(n.cluster, dev.sm_count));
+    return with_gate(norm, [&](auto gate) {
+        constexpr int kGate = decltype(gate)::value;
+        return bf16 ? launch_norm_forward<__nv_bfloat16, kGate>(p, out, n, clusters, st)
+                    : launch_norm_forward<float, kGate>(p, out, n, clusters, st);
+    });
 }
 
-// One partial vector per accumulated gradient and CTA; sized for the largest grid any device of
-// this kind runs, so that it needs no device.
+// One partial vector per accumulated gradient and cluster; sized for kNormWorkspaceSms SMs, so that it needs no
+// device (a launch never uses more).
 size_t mxfp4_residual_norm_workspace_bytes(int64_t tokens, int64_t width)
 {
     if (tokens <= 0 || width <= 0 || width % 8 != 0 || width > kNormMaxWidth) return 0;
-    const int64_t ctas = tokens < 4 * 160 ? tokens : 4 * 160;
-    return static_cast<size_t>(ctas) * 3 * static_cast<size_t>(width) * 4;
+    const NormShape n = norm_shape(static_cast<int>(width), true);
+    const int clusters = norm_clusters(n, tokens, kNormWorkspaceSms / n.cluster);
+    return static_cast<size_t>(clusters) * 3 * static_cast<size_t>(width) * 4;
 }
 
 int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, int64_t ld_dh, const void* dy,
@@ -518,10 +811,10 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
     NormParams p;
     int rc = norm_params(norm, &p);
     if (rc != MXFP4_OK) return rc;
+    const bool channel = norm->gate_kind == MXFP4_GATE_CHANNEL;
     if ((p.w_pre != nullptr) != (dh != nullptr) || (p.w_pre && !p.stream) || (!dh && !dy)) return MXFP4_ERR_NULL;
-    if ((dw_post && !p.w_post) || (dw_pre && !p.w_pre) || (dgate && p.gate_kind == MXFP4_GATE_NONE))
+    if ((dw_post && !p.w_post) || (dw_pre && !p.w_pre) || (dgate && norm->gate_kind == MXFP4_GATE_NONE))
         return MXFP4_ERR_NULL;
-    const bool channel = p.gate_kind == MXFP4_GATE_CHANNEL;
     if ((rc = norm_matrix_ok(dh, ld_dh, p.width)) != MXFP4_OK || (rc = norm_matrix_ok(dy, ld_dy, p.width)) != MXFP4_OK ||
         (rc = norm_matrix_ok(dx, ld_dx, p.width)) != MXFP4_OK ||
         (rc = norm_matrix_ok(dbranch, ld_dbranch, p.width)) != MXFP4_OK ||
@@ -534,7 +827,7 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
     io.dy = dy;
     io.dx = dx;
     io.dbranch = static_cast<__nv_bfloat16*>(dbranch);
-    io.dgate = channel ? nullptr : static_cast<__nv_bfloat16*>(dgate);
+    io.dgate = dgate;
     io.partials = static_cast<float*>(workspace);
     io.ld_dh = ld_dh;
     io.ld_dy = ld_dy;
@@ -551,15 +844,18 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
         return MXFP4_ERR_WORKSPACE;
     const DeviceInfo& dev = device_info();
     if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
-    const int sms = dev.sm_count < 160 ? dev.sm_count : 160;              // what the workspace is sized for
-    const int grid = norm_backward_ctas(p.tokens, p.width, io.n_acc, sms);
+    const bool bf16 = norm->stream_dtype == MXFP4_OUT_BF16;
+    const NormShape n = norm_shape(p.width, true);
+    if (!p.w_pre) p.stream = nullptr;            // y is only read for the second norm
+    norm_ring(&p, n, bf16 ? 2 : 4, norm->gate_kind == MXFP4_GATE_ELEMENT, dh != nullptr, dy != nullptr);
+    const int fit = resident_clusters(n.cluster, dev.sm_count), room = kNormWorkspaceSms / n.cluster;
+    const int grid = norm_clusters(n, p.tokens, fit < room ? fit : room);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool one = norm_chunks_per_thread(p.width) == 1;
-    if (norm->stream_dtype == MXFP4_OUT_BF16)
-        rc = one ? launch_norm_backward<__nv_bfloat16, 1>(p, io, grid, st)
-                 : launch_norm_backward<__nv_bfloat16, 2>(p, io, grid, st);
-    else
-        rc = one ? launch_norm_backward<float, 1>(p, io, grid, st) : launch_norm_backward<float, 2>(p, io, grid, st);
+    rc = with_gate(norm, [&](auto gate) {
+        constexpr int kGate = decltype(gate)::value;
+        return bf16 ? launch_norm_backward<__nv_bfloat16, kGate>(p, io, n, grid, st)
+                    : launch_norm_backward<float, kGate>(p, io, n, grid, st);
+    });
     if (rc != MXFP4_OK || io.n_acc == 0) return rc;
     sum.partials = io.partials;
     sum.parts = grid;

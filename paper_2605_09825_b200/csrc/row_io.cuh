@@ -1,5 +1,5 @@
-// Loads and stores of eight consecutive elements of a row (16 bytes of bf16, 32 of fp32) as fp32
-// values.  Streamed tensors are read past L1, which is left to the vectors every row needs again.
+// Loads and stores of eight consecutive elements of a row (16 bytes of bf16, 32 of fp32) as four pairs of
+// fp32 values, the operands of the packed fp32 instructions.  Streamed tensors pass L1 by.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -35,49 +35,51 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8])
+// eight bf16 of one 16-byte piece as four pairs
+__device__ __forceinline__ void unpack8(const uint4& w, float2 (&v)[4])
 {
-    const uint4 w = ld_stream(p);
-    v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x);
-    v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
-    v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z);
-    v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+    v[0] = make_float2(bf16_lo(w.x), bf16_hi(w.x));
+    v[1] = make_float2(bf16_lo(w.y), bf16_hi(w.y));
+    v[2] = make_float2(bf16_lo(w.z), bf16_hi(w.z));
+    v[3] = make_float2(bf16_lo(w.w), bf16_hi(w.w));
 }
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8])
-{
-    const uint4 a = ld_stream(p), b = ld_stream(p + 4);
-    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y);
-    v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
-    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y);
-    v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
-}
-
-// a vector every row reads: through L1
-__device__ __forceinline__ void load8_cached(const float* p, float (&v)[8])
+// a vector every row needs
+__device__ __forceinline__ void load8(const float* p, float2 (&v)[4])
 {
     const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = make_float2(a.x, a.y);
+    v[1] = make_float2(a.z, a.w);
+    v[2] = make_float2(b.x, b.y);
+    v[3] = make_float2(b.z, b.w);
 }
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8])
+__device__ __forceinline__ uint4 pack8(const float2 (&v)[4])
 {
-    st_stream(p, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+    return make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y),
+                      pack_bf16(v[3].x, v[3].y));
 }
 
-__device__ __forceinline__ void store8(float* p, const float (&v)[8])
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float2 (&v)[4]) { st_stream(p, pack8(v)); }
+
+__device__ __forceinline__ void store8(float* p, const float2 (&v)[4])
 {
-    st_stream(p, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-    st_stream(p + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+    st_stream(p, make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y)));
+    st_stream(p + 4, make_uint4(__float_as_uint(v[2].x), __float_as_uint(v[2].y), __float_as_uint(v[3].x), __float_as_uint(v[3].y)));
 }
 
-// the value a store to this type leaves behind
-template <class T>
-__device__ __forceinline__ float as_stored(float v);
-template <>
-__device__ __forceinline__ float as_stored<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float as_stored<__nv_bfloat16>(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
+// rounds to bf16, stores and leaves the stored values in v (fp32: stores)
+__device__ __forceinline__ void store8_round(__nv_bfloat16* p, float2 (&v)[4], bool store)
+{
+    const uint4 w = pack8(v);
+    if (store) st_stream(p, w);
+    unpack8(w, v);
+}
+__device__ __forceinline__ void store8_round(float* p, float2 (&v)[4], bool store)
+{
+    if (store) store8(p, v);
+}
+
+__device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
 
 }  // namespace mxfp4
