@@ -10,7 +10,15 @@
 //
 // Per SM and K-step: 512 cycles of MMA; 128 x 256 multiply-adds of the epilogue, packed in pairs, are 256
 // cycles of the FMA pipe (twice that when B has a scale per row, which costs a multiplication per
-// element more) and 256 cycles of tensor-memory reads beside it.
+// element more).  Neither bounds the kernel (8192 x 28672 x 4096: 890 us, 2.15 PFLOP/s; tensor pipe 51 %
+// busy): a K-step takes about 1000 cycles, most of which an epilogue warp spends waiting for one thing
+// after another -- a successful barrier wait costs some 150 cycles, a tensor-memory load of 32 columns
+// about as much -- with two warps per scheduler to cover for each other, which is what 128 sums per
+// thread leave room for.  Measured instead: handing the column halves of a buffer over separately
+// (1.85 PFLOP/s: the issuing warp's own waits and commits become the chain), 256 x 192 tiles with five
+// units of 96 columns in tensor memory and all 96 read ahead (1.63), both register sets loaded before
+// each wait (1.7), scales fetched by the epilogue warps from global memory (2.09).  With the scaling
+// left out the hand-over alone allows 2.15-2.2.
 //
 // Roles per CTA (384 threads): warps 0..7 epilogue (32 rows x 128 columns each), warp 8 TMA producer,
 // warp 9 MMA issuer (leader CTA only).  Barrier ownership as in the block-scaled kernel: full and
@@ -26,6 +34,7 @@
 
 #include "../../include/mxfp4.h"
 #include "ptx_sm100.cuh"
+#include "row_io.cuh"
 #include "tma_host.cuh"
 
 namespace mxfp4 {
@@ -34,6 +43,8 @@ constexpr int kBTile = 256;                       // both ways
 constexpr int kBHalf = 128;                       // rows of A, and of B, per CTA
 constexpr int kBBlockK = 128;                     // elements = bytes per stage and row
 constexpr int kBStages = 5;
+constexpr int kBGroup = 4;                        // K-steps whose scales travel together
+constexpr int kBGroups = 3;
 constexpr int kBOperandBytes = kBHalf * kBBlockK; // 16 KB
 constexpr int kBEpiWarps = 8;
 constexpr int kBProducerWarp = 8;
@@ -45,11 +56,14 @@ struct Gemm128Smem {
     alignas(1024) uint8_t a[kBStages][kBOperandBytes];
     alignas(1024) uint8_t b[kBStages][kBOperandBytes];
     alignas(1024) uint8_t out_stage[kBEpiWarps][kBStageBytes];
-    alignas(16) float sb[kBEpiWarps][2][kBHalf];  // this K-step's scales of the warp's 128 columns
+    alignas(128) float sa[kBGroups][kBGroup][kBHalf];     // scales of this CTA's rows
+    alignas(128) float sb[kBGroups][kBGroup][kBTile];     // of the tile's columns; of its two blocks (128 x 128)
+    alignas(32) uint64_t tmem_full[2];            // both, via multicast commit
+    alignas(32) uint64_t tmem_empty[2];           // leader's copy is the live one
     alignas(8) uint64_t full[kBStages];           // leader's copy is the live one
     uint64_t empty[kBStages];                     // both, via multicast commit
-    uint64_t tmem_full[2];                        // both, via multicast commit
-    uint64_t tmem_empty[2];                       // leader's copy is the live one
+    uint64_t scales_full[kBGroups];               // local
+    uint64_t scales_empty[kBGroups];              // local
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -105,7 +119,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
     extern __shared__ uint8_t smem_raw[];
     Gemm128Smem& sm = *reinterpret_cast<Gemm128Smem*>(smem_align_1024(smem_raw));
     const int warp = threadIdx.x >> 5;
-    const int lane = threadIdx.x & 31;
+    const int lane = lane_id();
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1;
     const int n_clusters = gridDim.x >> 1;
@@ -116,6 +130,10 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
         for (int s = 0; s < kBStages; ++s) {
             mbar_init(&sm.full[s], 2);                 // one arrive.expect_tx per CTA
             mbar_init(&sm.empty[s], 1);
+        }
+        for (int g = 0; g < kBGroups; ++g) {
+            mbar_init(&sm.scales_full[g], BROWS ? 1 : 33);       // bulk copies; a word per lane of the producer
+            mbar_init(&sm.scales_empty[g], kBEpiWarps);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sm.tmem_full[b], 1);
@@ -135,26 +153,34 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
     griddep_launch_dependents();
     griddep_wait();
 
-    // registers: 384 x 168 at launch = 256 x 208 (epilogue) + 128 x 88 (the others)
+    // registers: 384 x 168 at launch = 256 x 216 (epilogue) + 128 x 72 (the others)
     if (warp >= kBEpiWarps) {
-        setmaxnreg_dec<88>();
+        setmaxnreg_dec<72>();
         if (warp == kBProducerWarp) {
             // -------------------------------------------------------- TMA producer
             if (lane == 0) {
                 tma_prefetch_desc(&tm_a);
                 tma_prefetch_desc(&tm_b);
             }
-            int it = 0;
+            int s = 0, g = 0;
+            uint32_t parity = 1, scale_parity = 1;     // of the phase before: a fresh barrier passes
             bool alive = true;
             for (int item = cluster_id; alive && item < items; item += n_clusters) {
                 const Gemm128Work w = gemm128_work(p, item);
                 const int32_t ya = w.tm * kBTile + static_cast<int>(rank) * kBHalf;
                 // this CTA's share of the MMA's rows of B; the box is always 128 rows
                 const int32_t yb = w.tn * kBTile + static_cast<int>(rank) * (gemm128_width(p.N, w.tn) >> 1);
-                for (int k = w.k0; k < w.k1; ++k, ++it) {
-                    const int s = it % kBStages;
-                    const uint32_t round = it / kBStages;
-                    if (round > 0 && !mbar_wait(&sm.empty[s], (round - 1) & 1, &sm.abort_flag)) {
+                // scales: as far as the scale arrays reach (whole blocks of 128 rows); none for a CTA without rows, whose
+                // epilogue warps wait for none (a copy nobody waits for may land after the CTA is gone)
+                const bool rows = ya < p.M;
+                const uint32_t a_bytes = rows ? kBHalf * 4 : 0;
+                const uint32_t b_bytes =
+                    BROWS && rows ? static_cast<uint32_t>(min(static_cast<int64_t>(kBTile), p.pitch_b - w.tn * kBTile)) * 4
+                                  : 0;
+                for (int k = w.k0; k < w.k1; ++k) {
+                    const bool group = ((k - w.k0) & (kBGroup - 1)) == 0;
+                    if (!mbar_wait(&sm.empty[s], parity, &sm.abort_flag) ||
+                        (group && !mbar_wait(&sm.scales_empty[g], scale_parity, &sm.abort_flag))) {
                         alive = false;
                         break;
                     }
@@ -163,10 +189,47 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                         mbar_arrive_expect_tx_cluster(full_leader, 2 * kBOperandBytes);
                         tma_load_2d_pair(sm.a[s], &tm_a, full_leader, k * kBBlockK, ya);
                         tma_load_2d_pair(sm.b[s], &tm_b, full_leader, k * kBBlockK, yb);
+                        if (group) {
+                            const int n = min(kBGroup, w.k1 - k);
+                            mbar_arrive_expect_tx(&sm.scales_full[g], n * (a_bytes + b_bytes));
+                            for (int i = 0; i < n; ++i) {
+                                if (a_bytes)
+                                    bulk_load_1d(sm.sa[g][i], p.a_scales + (k + i) * p.pitch_a + ya, a_bytes,
+                                                 &sm.scales_full[g]);
+                                if (b_bytes)
+                                    bulk_load_1d(sm.sb[g][i], p.b_scales + (k + i) * p.pitch_b + w.tn * kBTile, b_bytes,
+                                                 &sm.scales_full[g]);
+                            }
+                        }
                     }
                     __syncwarp();
+                    if (!BROWS && group) {
+                        // the tile's columns are two blocks of 128: two words per K-step, one per lane
+                        const int i = lane >> 1, block = 2 * w.tn + (lane & 1);
+                        if (rows && i < min(kBGroup, w.k1 - k) && block < p.pitch_b)
+                            cp_async_word(&sm.sb[g][i][lane & 1], p.b_scales + (k + i) * p.pitch_b + block);
+                        cp_async_arrive(&sm.scales_full[g]);
+                    }
+                    if (++s == kBStages) {
+                        s = 0;
+                        parity ^= 1;
+                    }
+                    if (group && ++g == kBGroups) {
+                        g = 0;
+                        scale_parity ^= 1;
+                    }
                 }
             }
+            // the last stages' release signals: one that arrived after the CTA is gone would be counted on a barrier
+            // of the next launch
+            for (int i = 0; alive && i < kBStages; ++i) {
+                alive = mbar_wait(&sm.empty[s], parity, &sm.abort_flag);
+                if (++s == kBStages) {
+                    s = 0;
+                    parity ^= 1;
+                }
+            }
+            if (!alive) linger();      // given up: what is in flight lands before the CTA leaves
         } else if (warp == kBMmaWarp && rank == 0) {
             // -------------------------------------------------------- MMA issuer
             const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), 16, 1024, 2);
@@ -203,81 +266,141 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
         }
     } else {
         // ------------------------------------------------------------ epilogue warps
-        setmaxnreg_inc<208>();
+        setmaxnreg_inc<216>();
         const int quad = warp & 3;                     // TMEM lane quadrant of this warp
         const int half = warp >> 2;                    // which 128 columns
         uint8_t* stg = sm.out_stage[warp];
         const uint32_t taddr0 = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * kBHalf;
         const uint32_t tmem_empty_leader = map_to_cta(smem_u32(&sm.tmem_empty[0]), 0);
-        int it = 0;
+        // the buffer at hand: its columns, its barriers, the parity of its phase
+        uint32_t buf = 0, from = taddr0, parity = 0;
+        uint32_t full = smem_u32(&sm.tmem_full[0]), empty = tmem_empty_leader;
+        auto next_buffer = [&]() {
+            from ^= kBTile;                            // the two buffers start at a multiple of 512 columns
+            full ^= 8;                                 // two barriers, aligned to both
+            empty ^= 8;
+            parity ^= buf;
+            buf ^= 1;
+        };
+        int g = 0;                                     // scale group at hand
+        uint32_t scale_parity = 0;
+        auto release_group = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.scales_empty[g]);
+            if (++g == kBGroups) {
+                g = 0;
+                scale_parity ^= 1;
+            }
+        };
         bool alive = true;
         for (int item = cluster_id; alive && item < items; item += n_clusters) {
             const Gemm128Work w = gemm128_work(p, item);
             const int row0 = w.tm * kBTile + static_cast<int>(rank) * kBHalf + quad * 32;
             const int col0 = w.tn * kBTile + half * kBHalf;
-            const bool wanted = row0 < p.M && col0 < p.N;        // warp-uniform: something to keep here
             const bool row_ok = row0 + lane < p.M;
-            const float* sa_at = p.a_scales + row0 + lane;
-            const float* sb_at = p.b_scales + (BROWS ? col0 + lane * 4 : col0 / kBHalf);
+            if (row0 >= p.M || col0 >= p.N) {          // warp-uniform: nothing to keep here
+                for (int k = w.k0; alive && k < w.k1; ++k) {
+                    alive = mbar_wait_addr(full, parity, &sm.abort_flag);
+                    if (lane == 0) mbar_arrive_cluster(empty);
+                    next_buffer();
+                    if (((k - w.k0) & (kBGroup - 1)) == kBGroup - 1 || k + 1 == w.k1) release_group();
+                }
+                continue;
+            }
             float2 acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.0f, 0.0f);
-            // scales one K-step ahead of their use
-            float sa_next = 0.0f;
-            float4 sb_next = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            auto fetch = [&](int k) {
-                if (wanted && k < w.k1) {
-                    if (row_ok) sa_next = sa_at[k * p.pitch_a];
-                    if (BROWS) sb_next = *reinterpret_cast<const float4*>(sb_at + k * p.pitch_b);
-                    else sb_next.x = sb_at[k * p.pitch_b];
-                }
+            // a K-step's scale of this thread's row (times the one of the 128 columns)
+            auto scale_of = [&](int in_group) {
+                float v = smem_load<float>(sm.sa[g][in_group] + quad * 32 + lane, sm.sa[g], sizeof(sm.sa[0]));
+                if (!BROWS) v *= smem_load<float>(sm.sb[g][in_group] + half, sm.sb[g], sizeof(sm.sb[0]));
+                return v;
             };
-            fetch(w.k0);
-            for (int k = w.k0; k < w.k1; ++k, ++it) {
-                const int b = it & 1;
-                const float scale = BROWS ? sa_next : sa_next * sb_next.x;
-                float* sb = sm.sb[warp][b];
-                if (BROWS) {
-                    // the previous reader of this buffer is two steps back, with a warp barrier since
-                    smem_store(sb + lane * 4, sb_next, sb, sizeof(sm.sb[warp][b]));
+            alive = mbar_wait(&sm.scales_full[g], scale_parity, &sm.abort_flag);
+            float scale = scale_of(0);
+            uint32_t r0[32], r1[BROWS ? 1 : 32];
+            bool started = false;
+            for (int k = w.k0; k < w.k1; ++k) {
+                const int in_group = (k - w.k0) & (kBGroup - 1);
+                const bool more = k + 1 < w.k1;
+                const float* sb = sm.sb[g][in_group] + half * kBHalf;
+                const float2 scale2 = make_float2(scale, scale);
+                if (!started) {
+                    alive = mbar_wait_addr(full, parity, &sm.abort_flag) && alive;
+                    tcgen05_fence_after();
+                    if (!BROWS) tmem_ld_32x32b_x32(from, r0);
+                }
+                auto hand_back = [&]() {
+                    tcgen05_fence_before();
                     __syncwarp();
-                }
-                fetch(k + 1);
-                if (!mbar_wait(&sm.tmem_full[b], (it >> 1) & 1, &sm.abort_flag)) {
-                    alive = false;
-                    break;
-                }
-                tcgen05_fence_after();
-                if (wanted) {
-                    const float2 scale2 = make_float2(scale, scale);
+                    if (lane == 0) mbar_arrive_cluster(empty);
+                    next_buffer();
+                };
+                if constexpr (BROWS) {
+                    // a chunk's products and its columns' scales arrive together, while the other warp of the scheduler
+                    // works on its chunk
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t r[32];
-                        tmem_ld_32x32b_x32(taddr0 + b * kBTile + c * 32, r);
-                        tmem_ld_wait();
-                        if (c == 3) {
-                            tcgen05_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + b * 8);
-                        }
+                        tmem_ld_32x32b_x32(from + c * 32, r0);
+                        float4 e[4];                   // column scales, sixteen at a time
+                        auto load_scales = [&](float4 (&to)[4], int i0) {
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            float2 v0 = make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-                            float2 v1 = make_float2(__uint_as_float(r[2 * i + 2]), __uint_as_float(r[2 * i + 3]));
-                            if (BROWS) {
-                                const float4 q = smem_load<float4>(sb + c * 32 + i * 2, sb, sizeof(sm.sb[warp][b]));
-                                v0 = __fmul2_rn(v0, make_float2(q.x, q.y));
-                                v1 = __fmul2_rn(v1, make_float2(q.z, q.w));
+                            for (int i = 0; i < 4; ++i)
+                                to[i] = smem_load<float4>(sb + c * 32 + (i0 + i) * 4, sb, kBHalf * 4);
+                        };
+                        auto add = [&](const float4 (&e)[4], int i0) {
+#pragma unroll
+                            for (int i = i0; i < i0 + 4; ++i) {
+                                const float4& f = e[i - i0];
+                                const float2 v0 = __fmul2_rn(
+                                    make_float2(__uint_as_float(r0[4 * i]), __uint_as_float(r0[4 * i + 1])), make_float2(f.x, f.y));
+                                const float2 v1 = __fmul2_rn(
+                                    make_float2(__uint_as_float(r0[4 * i + 2]), __uint_as_float(r0[4 * i + 3])), make_float2(f.z, f.w));
+                                acc[c * 16 + 2 * i] = __ffma2_rn(v0, scale2, acc[c * 16 + 2 * i]);
+                                acc[c * 16 + 2 * i + 1] = __ffma2_rn(v1, scale2, acc[c * 16 + 2 * i + 1]);
                             }
-                            acc[c * 16 + i] = __ffma2_rn(v0, scale2, acc[c * 16 + i]);
-                            acc[c * 16 + i + 1] = __ffma2_rn(v1, scale2, acc[c * 16 + i + 1]);
-                        }
+                        };
+                        load_scales(e, 0);
+                        tmem_ld_wait_for(r0);
+                        if (c == 3) hand_back();
+                        add(e, 0);
+                        load_scales(e, 4);
+                        add(e, 4);
                     }
                 } else {
-                    if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + b * 8);
+                    // two register sets take turns: while one chunk of 32 columns is scaled and added, the next one is on
+                    // its way from tensor memory, across K-steps too where the next product is ready in time
+                    auto add = [&](int c, const uint32_t (&r)[32]) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[c * 16 + i] = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])),
+                                                         scale2, acc[c * 16 + i]);
+                    };
+                    tmem_ld_wait_for(r0);
+                    tmem_ld_32x32b_x32(from + 32, r1);
+                    add(0, r0);
+                    tmem_ld_wait_for(r1);
+                    tmem_ld_32x32b_x32(from + 64, r0);
+                    add(1, r1);
+                    tmem_ld_wait_for(r0);
+                    tmem_ld_32x32b_x32(from + 96, r1);
+                    add(2, r0);
+                    tmem_ld_wait_for(r1);
+                    hand_back();
+                    started = more && __all_sync(0xffffffffu, mbar_test_wait_addr(full, parity));
+                    if (started) {
+                        tcgen05_fence_after();
+                        tmem_ld_32x32b_x32(from, r0);
+                    }
+                    add(3, r1);
                 }
+                if (in_group == kBGroup - 1 || !more) {
+                    release_group();
+                    if (more) alive = mbar_wait(&sm.scales_full[g], scale_parity, &sm.abort_flag) && alive;
+                }
+                if (more) scale = scale_of((in_group + 1) & (kBGroup - 1));
             }
-            if (!alive || !wanted) continue;
+            if (!alive) break;                         // a wait was given up: nothing of this tile is stored
             // the warp's 32 rows x 128 columns leave in boxes of 128 bytes per row, staged in the 128-byte
             // swizzle for a TMA store that clips at the matrix edges
             constexpr int kBoxCols = OUT32 ? 32 : 64;
@@ -289,20 +412,16 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                 __syncwarp();
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    uint4 v;
+                    uint8_t* to = stg + lane * 128 + ((q ^ (lane & 7)) * 16);
                     if (OUT32) {
-                        const float2 x = acc[c * 16 + 2 * q], y = acc[c * 16 + 2 * q + 1];
-                        v = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(y.x), __float_as_uint(y.y));
+                        // two words at a time: four would have to sit in adjacent registers, which the sums' pairs do not
+                        smem_store(to, acc[c * 16 + 2 * q], stg, kBStageBytes);
+                        smem_store(to + 8, acc[c * 16 + 2 * q + 1], stg, kBStageBytes);
                     } else {
-                        uint32_t e[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(acc[c * 32 + 4 * q + j].x, acc[c * 32 + 4 * q + j].y);
-                            e[j] = *reinterpret_cast<const uint32_t*>(&h);
-                        }
-                        v = make_uint4(e[0], e[1], e[2], e[3]);
+                        const float2* x = &acc[c * 32 + 4 * q];
+                        smem_store(to, make_uint4(pack_bf16(x[0].x, x[0].y), pack_bf16(x[1].x, x[1].y),
+                                                  pack_bf16(x[2].x, x[2].y), pack_bf16(x[3].x, x[3].y)), stg, kBStageBytes);
                     }
-                    smem_store(stg + lane * 128 + ((q ^ (lane & 7)) * 16), v, stg, kBStageBytes);
                 }
                 fence_proxy_async_smem();
                 __syncwarp();

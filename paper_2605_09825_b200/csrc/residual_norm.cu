@@ -406,6 +406,7 @@ residual_norm_forward_kernel(const __grid_constant__ NormParams p, const __grid_
         }
         at.next(p.stages);
     }
+    if (*static_cast<volatile int*>(&sh.abort_flag)) linger();
     if (CLUSTER) cluster_sync_all();             // no CTA leaves while a peer may still write to its shared memory
 }
 
@@ -552,6 +553,7 @@ residual_norm_backward_kernel(const __grid_constant__ NormParams p, const __grid
         if (io.acc_post >= 0) store8(part + static_cast<int64_t>(io.acc_post) * p.width, acc_post);
         if (io.acc_gate >= 0) store8(part + static_cast<int64_t>(io.acc_gate) * p.width, acc_gate);
     }
+    if (*static_cast<volatile int*>(&sh.abort_flag)) linger();
     if (CLUSTER) cluster_sync_all();             // no CTA leaves while a peer may still write to its shared memory
 }
 
