@@ -128,7 +128,7 @@ static int gemm128_launch(const void* a_codes, const void* a_scales, const void*
     }
     if (!make_tmap_2d(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a_codes, M, K, K, kBHalf, kBBlockK,
                       CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_tmap_2d(&tm_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b_codes, N, K, K, kBHalf, kBBlockK,
+        !make_tmap_2d(&tm_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b_codes, N, K, K, kBHalf / 2, kBBlockK,
                       CU_TENSOR_MAP_SWIZZLE_128B))
         return MXFP4_ERR_CUDA;
     Gemm128Params p;

@@ -6,24 +6,27 @@
 // tensor cores cannot apply them: each K-step of 128 elements is a product of its own, formed in one
 // of two TMEM buffers (2 x 256 columns: all of TMEM) while the epilogue warps read the other one and add
 // it, scaled, to sums they keep in registers -- 128 rows x 256 columns per CTA, 128 sums per thread.
-// Four K = 32 instructions are the longest chain of the tensor cores' truncating additions.
+// Four K = 32 instructions are the longest chain of the tensor cores' truncating additions.  The two column
+// halves of a buffer are handed over separately, each by a warp of its own: the four warps that read one
+// half signal the issuer of that half.
 //
 // Per SM and K-step: 512 cycles of MMA; 128 x 256 multiply-adds of the epilogue, packed in pairs, are 256
 // cycles of the FMA pipe (twice that when B has a scale per row, which costs a multiplication per
-// element more).  Neither bounds the kernel (8192 x 28672 x 4096: 890 us, 2.15 PFLOP/s; tensor pipe 51 %
-// busy): a K-step takes about 1000 cycles, most of which an epilogue warp spends waiting for one thing
-// after another -- a successful barrier wait costs some 150 cycles, a tensor-memory load of 32 columns
-// about as much -- with two warps per scheduler to cover for each other, which is what 128 sums per
-// thread leave room for.  Measured instead: handing the column halves of a buffer over separately
-// (1.85 PFLOP/s: the issuing warp's own waits and commits become the chain), 256 x 192 tiles with five
-// units of 96 columns in tensor memory and all 96 read ahead (1.63), both register sets loaded before
-// each wait (1.7), scales fetched by the epilogue warps from global memory (2.09).  With the scaling
-// left out the hand-over alone allows 2.15-2.2.
+// element more).  Neither bounds the kernel (8192 x 28672 x 4096: 885 us, 2.2 PFLOP/s, a K-step in 900 to
+// 1000 cycles): a half buffer's way round does -- 256 cycles of MMA, about 200 until the epilogue has seen
+// the signal, 500 to 700 of reading and adding (two warps per scheduler, which is what 128 sums per
+// thread leave room for, cover little of each other's waits), 340 for the signal back across the pair,
+// 100 to issue -- with two K-steps of tensor memory to overlap it.  With the additions left out it runs
+// at 2.5-2.65 PFLOP/s.  Measured instead: one issuer for whole buffers (2.15), one issuer for both halves
+// (1.85: its waits and commits become the chain), 256 x 192 tiles with five units of 96 columns in tensor
+// memory and all 96 read ahead (1.63), both register sets loaded before each wait (1.7), scales fetched
+// by the epilogue warps from global memory (2.1), the next scale fetched a K-step ahead (2.1; 1.5 instead
+// of 1.7 with scales per row).
 //
 // Roles per CTA (384 threads): warps 0..7 epilogue (32 rows x 128 columns each), warp 8 TMA producer,
-// warp 9 MMA issuer (leader CTA only).  Barrier ownership as in the block-scaled kernel: full and
-// tmem_empty live in the leader, empty and tmem_full are signalled in both CTAs by a multicast
-// commit.  All waits are bounded.
+// warps 9 and 10 MMA issuers, one per column half (leader CTA only).  Barrier ownership as in the
+// block-scaled kernel: full and tmem_empty live in the leader, empty and tmem_full are signalled in both
+// CTAs by a multicast commit.  All waits are bounded.
 //
 // Products with few output tiles are split along K (`splits`): each split writes its fp32 sums to
 // the workspace and a second kernel adds them in a fixed order.
@@ -54,12 +57,12 @@ constexpr int kBStageBytes = 32 * 128;            // output staging per epilogue
 
 struct Gemm128Smem {
     alignas(1024) uint8_t a[kBStages][kBOperandBytes];
-    alignas(1024) uint8_t b[kBStages][kBOperandBytes];
+    alignas(1024) uint8_t b[kBStages][2][kBOperandBytes / 2];   // [column half][64 rows x 128 B]
     alignas(1024) uint8_t out_stage[kBEpiWarps][kBStageBytes];
     alignas(128) float sa[kBGroups][kBGroup][kBHalf];     // scales of this CTA's rows
     alignas(128) float sb[kBGroups][kBGroup][kBTile];     // of the tile's columns; of its two blocks (128 x 128)
-    alignas(32) uint64_t tmem_full[2];            // both, via multicast commit
-    alignas(32) uint64_t tmem_empty[2];           // leader's copy is the live one
+    alignas(32) uint64_t tmem_full[2][2];         // [column half][buffer]: both, via multicast commit
+    alignas(32) uint64_t tmem_empty[2][2];        // leader's copy is the live one
     alignas(8) uint64_t full[kBStages];           // leader's copy is the live one
     uint64_t empty[kBStages];                     // both, via multicast commit
     uint64_t scales_full[kBGroups];               // local
@@ -107,8 +110,12 @@ __device__ __forceinline__ Gemm128Work gemm128_work(const Gemm128Params& p, int 
     return w;
 }
 
-// Columns the MMAs of a tile column compute: what exists, rounded up to the instruction's granule.
-__device__ __forceinline__ int gemm128_width(int N, int tn) { return min(kBTile, (N - tn * kBTile + 15) & ~15); }
+// Columns the MMAs of a column half compute: what exists, rounded up to the instruction's granule (0: none).
+// CTA r of the pair supplies rows [r * n / 2, (r + 1) * n / 2) of the half's n rows of B.
+__device__ __forceinline__ int gemm128_width(int N, int tn, int half)
+{
+    return max(0, min(kBHalf, (N - tn * kBTile - half * kBHalf + 15) & ~15));
+}
 
 // BROWS: B has a scale per row and K-step (1 x 128 blocks); otherwise one per 128 rows.
 template <bool BROWS, bool OUT32>
@@ -129,15 +136,17 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
         sm.abort_flag = 0;
         for (int s = 0; s < kBStages; ++s) {
             mbar_init(&sm.full[s], 2);                 // one arrive.expect_tx per CTA
-            mbar_init(&sm.empty[s], 1);
+            mbar_init(&sm.empty[s], 2);                // one commit per column half
         }
         for (int g = 0; g < kBGroups; ++g) {
             mbar_init(&sm.scales_full[g], BROWS ? 1 : 33);       // bulk copies; a word per lane of the producer
             mbar_init(&sm.scales_empty[g], kBEpiWarps);
         }
         for (int b = 0; b < 2; ++b) {
-            mbar_init(&sm.tmem_full[b], 1);
-            mbar_init(&sm.tmem_empty[b], 2 * kBEpiWarps);
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(&sm.tmem_full[h][b], 1);
+                mbar_init(&sm.tmem_empty[h][b], kBEpiWarps);      // the half's four warps in each CTA
+            }
         }
         fence_barrier_init();
     }
@@ -168,8 +177,9 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
             for (int item = cluster_id; alive && item < items; item += n_clusters) {
                 const Gemm128Work w = gemm128_work(p, item);
                 const int32_t ya = w.tm * kBTile + static_cast<int>(rank) * kBHalf;
-                // this CTA's share of the MMA's rows of B; the box is always 128 rows
-                const int32_t yb = w.tn * kBTile + static_cast<int>(rank) * (gemm128_width(p.N, w.tn) >> 1);
+                // this CTA's share of each half's rows of B; the boxes are always 64 rows
+                const int32_t yb0 = w.tn * kBTile + static_cast<int>(rank) * (gemm128_width(p.N, w.tn, 0) >> 1);
+                const int32_t yb1 = w.tn * kBTile + kBHalf + static_cast<int>(rank) * (gemm128_width(p.N, w.tn, 1) >> 1);
                 // scales: as far as the scale arrays reach (whole blocks of 128 rows); none for a CTA without rows, whose
                 // epilogue warps wait for none (a copy nobody waits for may land after the CTA is gone)
                 const bool rows = ya < p.M;
@@ -188,7 +198,8 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                         const uint32_t full_leader = map_to_cta(smem_u32(&sm.full[s]), 0);
                         mbar_arrive_expect_tx_cluster(full_leader, 2 * kBOperandBytes);
                         tma_load_2d_pair(sm.a[s], &tm_a, full_leader, k * kBBlockK, ya);
-                        tma_load_2d_pair(sm.b[s], &tm_b, full_leader, k * kBBlockK, yb);
+                        tma_load_2d_pair(sm.b[s][0], &tm_b, full_leader, k * kBBlockK, yb0);
+                        tma_load_2d_pair(sm.b[s][1], &tm_b, full_leader, k * kBBlockK, yb1);
                         if (group) {
                             const int n = min(kBGroup, w.k1 - k);
                             mbar_arrive_expect_tx(&sm.scales_full[g], n * (a_bytes + b_bytes));
@@ -230,21 +241,24 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                 }
             }
             if (!alive) linger();      // given up: what is in flight lands before the CTA leaves
-        } else if (warp == kBMmaWarp && rank == 0) {
-            // -------------------------------------------------------- MMA issuer
+        } else if (warp < kBMmaWarp + 2 && rank == 0) {
+            // -------------------------------------------------------- MMA issuers, one per column half
+            const int half = warp - kBMmaWarp;
             const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), 16, 1024, 2);
-            const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), 16, 1024, 2);
-            int it = 0;
+            const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0][half]), 16, 1024, 2);
+            const uint32_t full = smem_u32(&sm.full[0]), tmem_empty = smem_u32(&sm.tmem_empty[half][0]);
+            int s = 0, b = 0;
+            uint32_t parity = 0, buf_parity = 1;       // a fresh tmem_empty passes for the phase before
             bool alive = true;
             for (int item = cluster_id; alive && item < items; item += n_clusters) {
                 const Gemm128Work w = gemm128_work(p, item);
+                const int width = gemm128_width(p.N, w.tn, half);
                 // instruction descriptor: fp32 accumulator, E4M3 x E4M3, K-major operands
-                const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(gemm128_width(p.N, w.tn) >> 3) << 17) |
+                const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(width >> 3) << 17) |
                                        (static_cast<uint32_t>(kBTile >> 4) << 24);
-                for (int k = w.k0; k < w.k1; ++k, ++it) {
-                    const int s = it % kBStages, b = it & 1;
-                    if (!mbar_wait(&sm.full[s], (it / kBStages) & 1, &sm.abort_flag) ||
-                        (it >= 2 && !mbar_wait(&sm.tmem_empty[b], ((it >> 1) - 1) & 1, &sm.abort_flag))) {
+                for (int k = w.k0; k < w.k1; ++k) {
+                    if (!mbar_wait_addr(full + s * 8, parity, &sm.abort_flag) ||
+                        !mbar_wait_addr(tmem_empty + b * 8, buf_parity, &sm.abort_flag)) {
                         alive = false;
                         break;
                     }
@@ -255,12 +269,19 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                         const uint64_t b_desc = b_desc0 + static_cast<uint64_t>(s * (kBOperandBytes >> 4));
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            if (j < nmma)
-                                tcgen05_mma_f8_pair(tmem + b * kBTile, a_desc + 2 * j, b_desc + 2 * j, idesc, j > 0);
+                            if (j < nmma && width > 0)
+                                tcgen05_mma_f8_pair(tmem + b * kBTile + half * kBHalf, a_desc + 2 * j, b_desc + 2 * j, idesc,
+                                                    j > 0);
                         tcgen05_commit_pair(&sm.empty[s], 3);
-                        tcgen05_commit_pair(&sm.tmem_full[b], 3);
+                        tcgen05_commit_pair(&sm.tmem_full[half][b], 3);
                     }
                     __syncwarp();
+                    if (++s == kBStages) {
+                        s = 0;
+                        parity ^= 1;
+                    }
+                    buf_parity ^= b;
+                    b ^= 1;
                 }
             }
         }
@@ -271,10 +292,10 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
         const int half = warp >> 2;                    // which 128 columns
         uint8_t* stg = sm.out_stage[warp];
         const uint32_t taddr0 = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * kBHalf;
-        const uint32_t tmem_empty_leader = map_to_cta(smem_u32(&sm.tmem_empty[0]), 0);
+        const uint32_t tmem_empty_leader = map_to_cta(smem_u32(&sm.tmem_empty[half][0]), 0);
         // the buffer at hand: its columns, its barriers, the parity of its phase
         uint32_t buf = 0, from = taddr0, parity = 0;
-        uint32_t full = smem_u32(&sm.tmem_full[0]), empty = tmem_empty_leader;
+        uint32_t full = smem_u32(&sm.tmem_full[half][0]), empty = tmem_empty_leader;
         auto next_buffer = [&]() {
             from ^= kBTile;                            // the two buffers start at a multiple of 512 columns
             full ^= 8;                                 // two barriers, aligned to both
