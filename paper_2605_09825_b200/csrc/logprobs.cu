@@ -8,12 +8,15 @@
 // The reference is the thread's first maximum and moves only when a later one is more than a factor
 // of 2^8 above it, so the sums are hardly ever rescaled on the way (a running maximum would make
 // some lane of a warp rescale at most vectors), and what the late step back to a common
-// reference can cost in precision stays within 8 * 2^-24 of a nat.
+// reference can cost in precision stays within 8 * 2^-24 of a nat.  Logits below -10^30 (masked ones) count
+// as -10^30 there, whose power is 0 in any row with a logit above -10^29; parts without one, or with a
+// largest logit near the other end of fp32, are summed again by a loop that takes every value as it is.
 //
 // Top alternatives: every thread remembers its largest logit and the first vector that held it.
 // The top_k-th best of those is a lower bound for the row's top_k-th best logit that exactly top_k
 // threads reach, so only their vectors are looked at again (they are still in L2), and what
-// reaches the bound -- a few dozen logits -- is ranked in shared memory.
+// reaches the bound -- a few dozen logits -- is ranked in shared memory, all by a warp of its own
+// beside the threads that stream the next row.
 //
 // A row is split over several CTAs when there are too few rows to fill the device; each split
 // leaves (m, S, A) and its own alternatives in the workspace and a second kernel joins them.
@@ -30,14 +33,41 @@
 
 namespace mxfp4 {
 
-constexpr int kLpThreads = 512;
+constexpr int kLpThreads = 256;
 constexpr int kLpMaxTop = 32;
 constexpr int kLpCandidates = 1024;          // ranked in shared memory; more take the slow way
-constexpr int kLpFillCtas = 296;             // two per SM of the device the kernel is tuned on
+constexpr int kLpHits = 512;
+constexpr int kLpUnroll = 4;                 // vectors a thread loads at once
+constexpr int kLpGroups = 16;                // per thread and row
+constexpr int kLpFillCtas = 592;             // four per SM of the device the kernel is tuned on
 constexpr int kLpMaxSplits = 74;
 constexpr float kLpReach = 8.0f;             // see above
+constexpr float kLpFloor = -1.0002555517425873e30f;     // the bf16 value 0xF14A
+constexpr float kLpLowest = -1e29f;             // the lowest reference
+constexpr float kLpHuge = 1e37f;                // bound of |m| c
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+
+// larger of the two, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 
 template <class T>
 struct LogitVec;
@@ -56,6 +86,18 @@ struct LogitVec<__nv_bfloat16> {
     {
         return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     }
+    // the largest value (NaN only if nothing else is there), and the values not below kLpFloor (NaN kept)
+    static __device__ __forceinline__ float top(const uint4& w)
+    {
+        const uint32_t m = max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w));
+        return fmaxf(bf16_lo(m), bf16_hi(m));
+    }
+    static __device__ __forceinline__ void get_floored(const uint4& w, float2 (&v)[4])
+    {
+        constexpr uint32_t f = 0xF14AF14Au;      // two bf16 of kLpFloor
+        const uint4 c = make_uint4(max_nan_bf16x2(w.x, f), max_nan_bf16x2(w.y, f), max_nan_bf16x2(w.z, f), max_nan_bf16x2(w.w, f));
+        unpack8(c, v);
+    }
     static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     static __device__ __forceinline__ void set(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 };
@@ -72,6 +114,15 @@ struct LogitVec<float> {
     {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
+    static __device__ __forceinline__ float top(const uint4& w)
+    {
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
+    static __device__ __forceinline__ void get_floored(const uint4& w, float2 (&v)[2])
+    {
+        v[0] = make_float2(max_nan(__uint_as_float(w.x), kLpFloor), max_nan(__uint_as_float(w.y), kLpFloor));
+        v[1] = make_float2(max_nan(__uint_as_float(w.z), kLpFloor), max_nan(__uint_as_float(w.w), kLpFloor));
+    }
     static __device__ __forceinline__ float one(const float* p) { return *p; }
     static __device__ __forceinline__ void set(float* p, float v) { *p = v; }
 };
@@ -80,14 +131,6 @@ __device__ __forceinline__ float exp2_approx(float x)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
-// larger of the two, NaN if either is
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 
@@ -129,13 +172,13 @@ struct LogprobsParams {
     uint64_t* part_keys;        // [row][split][top_k]
 };
 
-// (m, S, A) of part of a row
+// Sums of part of a row: S = sum 2^d, A = sum d 2^d with d = (x - m) c, c = scale * log2(e).  An empty part
+// has m = -infinity, and in s what a NaN left there.
 struct SoftSums {
     float m, s, a;
 };
 
-// The sums of two parts relative to a common reference.  An empty part (m = -infinity) adds nothing
-// but what a NaN left in its s.
+// The sums relative to a larger reference.
 __device__ __forceinline__ SoftSums rebase(const SoftSums& v, float m, float c)
 {
     if (m == -INFINITY) return {m, v.s, v.a};
@@ -208,25 +251,84 @@ __device__ __forceinline__ void write_top(const LogprobsParams& p, int64_t row, 
     p.top_index[at] = none ? -1 : static_cast<int64_t>(0xFFFFFFFFu - static_cast<uint32_t>(key));
 }
 
-// The largest key that at least `want` threads' keys (one per thread, compared above `low` bits)
-// reach; 0 when fewer than `want` threads have one.
-__device__ __forceinline__ uint32_t block_kth(uint32_t key, int want, int low)
-{
-    uint32_t found = 0;
-    for (int b = 31; b >= low; --b) {
-        const uint32_t probe = found | (1u << b);
-        if (__syncthreads_count(key >= probe) >= want) found = probe;
-    }
-    return found;
-}
+// What the threads of a row leave for the warp that finishes it.
+template <bool TOP>
+struct RowNotes {
+    SoftSums sums[kLpThreads / 32];
+    uint32_t key[kLpThreads], vec[kLpThreads];   // a thread's largest logit (as a key), first vector with it
+    uint16_t group[TOP ? kLpGroups : 1][kLpThreads];     // upper half of that key for each group of its vectors
+};
 
 struct TopScratch {
     uint64_t keys[kLpCandidates];
-    uint64_t best;
+    uint32_t hits[kLpHits];    // vectors whose largest logit reaches the bound
+    uint32_t groups[kLpHits];  // first vectors of groups that do
     int32_t owner[kLpMaxTop];
-    int32_t owners;
-    int32_t n;
+    int32_t n, n_hits, n_groups;
 };
+
+struct TopBound {
+    uint32_t kth, last_vec;    // the bound's value, and the last vector that counts where the value is equal
+    int32_t owners;
+};
+
+// One warp picks the threads whose best logits are the `want` largest (equal ones: of the first vectors).  Bits of the bound are tried from the top, as long as more
+// than `want` threads reach it.  The threads are left in the scratch.
+template <class T>
+__device__ __forceinline__ TopBound pick_owners(const RowNotes<true>& notes, TopScratch& sc, int want, int max_vec)
+{
+    constexpr int SHIFT = LogitVec<T>::kKeyShift;
+    constexpr int kEach = kLpThreads / 32;
+    const int lane = threadIdx.x & 31;
+    uint32_t key[kEach], vec[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        key[i] = notes.key[i * 32 + lane] >> SHIFT;
+        vec[i] = notes.vec[i * 32 + lane];
+    }
+    auto reach = [&](uint32_t bound) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) n += key[i] >= bound;
+        return __reduce_add_sync(0xffffffffu, n);
+    };
+    uint32_t bound = 0;
+    int n = kLpThreads;
+    for (int b = 31 - SHIFT; b >= 0 && n != want; --b) {
+        const int m = reach(bound | (1u << b));
+        if (m >= want) {
+            bound |= 1u << b;
+            n = m;
+        }
+    }
+    if (bound == 0) bound = 1;                       // fewer than `want` threads have a logit: all of those
+    uint32_t last = 0xFFFFFFFFu;
+    if (n > want) {
+        // more threads than wanted hold the bound itself: the first vectors among those
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) above += key[i] > bound;
+        above = __reduce_add_sync(0xffffffffu, above);
+        last = 0;                                    // largest vector number that fewer than the rest come before
+        for (int b = 31 - __clz(max_vec | 1); b >= 0; --b) {
+            const uint32_t probe = last | (1u << b);
+            int m = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) m += key[i] == bound && vec[i] < probe;
+            if (__reduce_add_sync(0xffffffffu, m) < want - above) last = probe;
+        }
+    }
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const bool mine = key[i] > bound || (key[i] == bound && vec[i] <= last);
+        const uint32_t who = __ballot_sync(0xffffffffu, mine);
+        const int place = at + __popc(who & ((1u << lane) - 1u));
+        if (mine && place < kLpMaxTop) sc.owner[place] = i * 32 + lane;
+        at += __popc(who);
+    }
+    return {bound, last, at < kLpMaxTop ? at : kLpMaxTop};
+}
 
 // The elements of a row a CTA owns: vectors first .. first + count, and the unaligned head or tail.
 template <class T>
@@ -237,6 +339,12 @@ struct RowPart {
     int loose0, n_loose0;      // single elements: at the row's head,
     int loose1, n_loose1;      // and at its end
     __device__ __forceinline__ int loose_index(int i) const { return i < n_loose0 ? loose0 + i : loose1 + i - n_loose0; }
+    // vectors per thread and group, in whole unrolled steps
+    __device__ __forceinline__ int group_steps() const
+    {
+        const int steps = (count + kLpUnroll * kLpThreads - 1) / (kLpUnroll * kLpThreads);
+        return (steps + kLpGroups - 1) / kLpGroups;
+    }
     __device__ __forceinline__ const T* vec(int v) const { return row + head + static_cast<int64_t>(v) * LogitVec<T>::kN; }
 };
 
@@ -258,115 +366,206 @@ __device__ __forceinline__ RowPart<T> row_part(const LogprobsParams& p, int64_t 
     return r;
 }
 
-// The part's `top_k` best keys in descending order; `emit(rank, key)` is called once for every rank
-// that exists.  `best` / `best_vec`: the thread's largest logit and the first vector with it.
+// The part's `top_k` best keys; `emit(rank, key)` is called once for every rank that exists.  One warp.
 template <class T, class Emit>
-__device__ __forceinline__ void block_top(const RowPart<T>& part, int top_k, float best, int best_vec, TopScratch& sc,
-                                          Emit emit)
+__device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, const RowNotes<true>& notes, TopScratch& sc, Emit emit)
 {
     constexpr int kN = LogitVec<T>::kN;
-    const int tid = threadIdx.x;
-    if (tid == 0) sc.owners = sc.n = 0;
-    // bound: value, then vector (all keys of threads that have one differ in the pair)
-    const uint32_t key = order_key(best);
-    const uint32_t kth = block_kth(key, top_k, LogitVec<T>::kKeyShift);
-    // bf16 keys of negative values end in ones: the bound found above has zeros there
-    const bool above = key != 0u && (key >> LogitVec<T>::kKeyShift) > (kth >> LogitVec<T>::kKeyShift);
-    const bool equal = key != 0u && (key >> LogitVec<T>::kKeyShift) == (kth >> LogitVec<T>::kKeyShift);
-    const int n_above = __syncthreads_count(above);
-    const int n_equal = __syncthreads_count(equal);
-    uint32_t vec_key = 0u;                      // of the vectors with a value equal to the bound: the first ones
-    if (n_above + n_equal > top_k)
-        vec_key = block_kth(equal ? 0x7FFFFFFFu - static_cast<uint32_t>(best_vec) : 0u, top_k - n_above, 0);
-    if (above || (equal && 0x7FFFFFFFu - static_cast<uint32_t>(best_vec) >= vec_key))
-        sc.owner[atomicAdd(&sc.owners, 1)] = tid;
-    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const TopBound bound = pick_owners<T>(notes, sc, top_k, part.first + part.count);
+    if (lane == 0) sc.n = sc.n_hits = sc.n_groups = 0;
+    __syncwarp();
     auto take = [&](float x, uint32_t index) {
         const uint64_t k = full_key(x, index);
         if (k == 0ull) return;
         const int at = atomicAdd(&sc.n, 1);
         if (at < kLpCandidates) sc.keys[at] = k;
     };
-    // the owners' vectors again, one warp per owner, a lane per vector
-    const int lane = tid & 31;
-    for (int o = tid >> 5; o < sc.owners; o += kLpThreads / 32) {
-        for (int v = sc.owner[o] + lane * kLpThreads; v < part.count; v += 32 * kLpThreads) {
-            const T* at = part.vec(part.first + v);
-            float x[kN];
-            LogitVec<T>::get(*reinterpret_cast<const uint4*>(at), x);
-            const bool late = 0x7FFFFFFFu - static_cast<uint32_t>(part.first + v) < vec_key;
-#pragma unroll
-            for (int i = 0; i < kN; ++i) {
-                const uint32_t k = order_key(x[i]) >> LogitVec<T>::kKeyShift, b = kth >> LogitVec<T>::kKeyShift;
-                if (k > b || (k == b && !late)) take(x[i], static_cast<uint32_t>(at - part.row) + i);
-            }
+    auto vector_at = [&](int v) { return *reinterpret_cast<const uint4*>(part.vec(part.first + v)); };
+    // the owners' groups that reach the bound, and of their vectors those that do: a lane per vector, several
+    // loads in flight
+    const int group_vecs = part.group_steps() * kLpUnroll;
+    auto in_reach = [&](uint32_t key, int first_vec) {
+        return key > bound.kth || (key == bound.kth && static_cast<uint32_t>(first_vec) <= bound.last_vec);
+    };
+    for (int i = lane; i < bound.owners * kLpGroups; i += 32) {
+        const int owner = sc.owner[i / kLpGroups], g = i % kLpGroups, v = owner + g * group_vecs * kLpThreads;
+        // an fp32 group whose upper half equals the bound's may or may not reach it
+        const uint32_t half = notes.group[g][owner], bound_half = bound.kth >> (16 - LogitVec<T>::kKeyShift);
+        if (v < part.count && (kN == 8 ? in_reach(half, part.first + v) : half >= bound_half)) {
+            const int at = atomicAdd(&sc.n_groups, 1);
+            if (at < kLpHits) sc.groups[at] = static_cast<uint32_t>(v);
         }
     }
-    for (int i = tid; i < part.n_loose0 + part.n_loose1; i += kLpThreads) {
+    __syncwarp();
+    const int n_groups = min(sc.n_groups, kLpHits), loads = n_groups * group_vecs;
+    constexpr int kBatch = 4;
+    for (int l = lane; l < loads; l += 32 * kBatch) {
+        uint4 w[kBatch];
+        int v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int i = l + 32 * j, o = i / group_vecs;
+            v[j] = i < loads ? static_cast<int>(sc.groups[o]) + (i - o * group_vecs) * kLpThreads : part.count;
+            if (v[j] < part.count) w[j] = vector_at(v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (v[j] < part.count && in_reach(order_key(LogitVec<T>::top(w[j])) >> LogitVec<T>::kKeyShift, part.first + v[j])) {
+                const int at = atomicAdd(&sc.n_hits, 1);
+                if (at < kLpHits) sc.hits[at] = static_cast<uint32_t>(v[j]);
+            }
+    }
+    __syncwarp();
+    const int n_hits = sc.n_hits;
+    for (int h = lane; h < n_hits && n_hits <= kLpHits; h += 32) {
+        const int v = static_cast<int>(sc.hits[h]), vec = part.first + v;
+        float x[kN];
+        LogitVec<T>::get(vector_at(v), x);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            if (in_reach(order_key(x[i]) >> LogitVec<T>::kKeyShift, vec))
+                take(x[i], static_cast<uint32_t>(part.head + vec * kN + i));
+        }
+    }
+    for (int i = lane; i < part.n_loose0 + part.n_loose1; i += 32) {
         const int at = part.loose_index(i);
         take(LogitVec<T>::one(part.row + at), static_cast<uint32_t>(at));
     }
-    __syncthreads();
-    const int n = sc.n;
+    __syncwarp();
+    const int n = n_hits <= kLpHits && sc.n_groups <= kLpHits ? sc.n : kLpCandidates + 1;
     if (n <= kLpCandidates) {
-        for (int i = tid; i < n; i += kLpThreads) {
+        for (int i = lane; i < n; i += 32) {
             const uint64_t k = sc.keys[i];
             int rank = 0;
             for (int j = 0; j < n; ++j) rank += sc.keys[j] > k;
             if (rank < top_k) emit(rank, k);
         }
     } else {
-        // thousands of logits above the bound: rank after rank, each from the whole part
+        // hundreds of vectors reach the bound: rank after rank, each from the whole part
         uint64_t last = ~0ull;
-        for (int rank = 0; rank < top_k; ++rank) {
-            if (tid == 0) sc.best = 0ull;
-            __syncthreads();
+        for (int rank = 0; rank < top_k && last; ++rank) {
             uint64_t mine = 0ull;
             auto look = [&](float x, uint32_t index) {
                 const uint64_t k = full_key(x, index);
                 if (k < last && k > mine) mine = k;
             };
-            for (int v = tid; v < part.count; v += kLpThreads) {
+            for (int v = lane; v < part.count; v += 32) {
                 const T* at = part.vec(part.first + v);
                 float x[kN];
                 LogitVec<T>::get(*reinterpret_cast<const uint4*>(at), x);
 #pragma unroll
                 for (int i = 0; i < kN; ++i) look(x[i], static_cast<uint32_t>(at - part.row) + i);
             }
-            for (int i = tid; i < part.n_loose0 + part.n_loose1; i += kLpThreads)
+            for (int i = lane; i < part.n_loose0 + part.n_loose1; i += 32)
                 look(LogitVec<T>::one(part.row + part.loose_index(i)), static_cast<uint32_t>(part.loose_index(i)));
-            atomicMax(reinterpret_cast<unsigned long long*>(&sc.best), static_cast<unsigned long long>(mine));
-            __syncthreads();
-            last = sc.best;
-            if (tid == 0 && last) emit(rank, last);
-            __syncthreads();
-            if (last == 0ull) break;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const uint64_t other = __shfl_xor_sync(0xffffffffu, mine, o);
+                if (other > mine) mine = other;
+            }
+            last = mine;
+            if (lane == 0 && last) emit(rank, last);
         }
     }
+    __syncwarp();
 }
 
+// Sums of a part with every value taken as it is, relative to the part's own largest logit: for parts whose
+// logits are all masked or lie at the ends of the type.  One warp; the same in every lane.
+template <class T>
+__device__ __noinline__ SoftSums careful_sums(const RowPart<T>& part, float c)
+{
+    const int n = part.count * LogitVec<T>::kN, all = n + part.n_loose0 + part.n_loose1;
+    const int lane = threadIdx.x & 31;
+    auto at = [&](int i) {
+        return LogitVec<T>::one(i < n ? part.vec(part.first) + i : part.row + part.loose_index(i - n));
+    };
+    SoftSums v = {-INFINITY, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int i = lane; i < all; i += 32) {
+        const float x = at(i);
+        v.m = fmaxf(v.m, x);
+        if (x != x) v.s = x;
+    }
+    v = warp_join(v, c);
+    if (v.m == -INFINITY) return v;
+    v.s = v.a = 0.0f;
+#pragma unroll 8
+    for (int i = lane; i < all; i += 32) {
+        const float d = max_nan((at(i) - v.m) * c, -300.0f), e = exp2_approx(d);
+        v.s += e;
+        v.a = fmaf(d, e, v.a);
+    }
+    return warp_join(v, c);
+}
+
+// A CTA walks items (a row, or a split of one): 256 threads stream the logits, and one more warp finishes an item
+// -- joins the sums, finds the alternatives, writes the results -- while they stream the next.  Named barriers
+// 1 and 2 hand a set of notes over, 3 and 4 hand it back; nobody waits for anything else.
+constexpr int kLpCtaThreads = kLpThreads + 32;
 template <class T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads, 2) logprobs_forward_kernel(const LogprobsParams p)
+__global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(const __grid_constant__ LogprobsParams p)
 {
     constexpr int kN = LogitVec<T>::kN;
-    __shared__ SoftSums red[kLpThreads / 32];
+    __shared__ RowNotes<TOP> notes[2];
     __shared__ TopScratch scratch;
     griddep_launch_dependents();
     griddep_wait();
-    const int64_t row = blockIdx.x / p.splits;
-    const int split = blockIdx.x % p.splits;
-    const RowPart<T> part = row_part<T>(p, row, split);
+    const int64_t items = p.tokens * p.splits;
     const float c = p.scale * kLog2e;
-    const float reach = kLpReach / c;
+    const int lane = threadIdx.x & 31;
+    int buf = 0;
 
-    float m = -INFINITY, limit = -INFINITY, ref = 0.0f;   // ref = m, or 0 while nothing but masked logits came
-    float2 s = make_float2(0.0f, 0.0f), a = make_float2(0.0f, 0.0f);
-    float best = -INFINITY;
-    int best_vec = 0;
-    auto add = [&](const float* x, int n) {               // n even, or 1
-        float top = x[0];
-        for (int i = 1; i < n; ++i) top = fmaxf(top, x[i]);
-        if (top > limit) {
+    if (threadIdx.x >= kLpThreads) {
+        // ---------------------------------------------------------------- finishing warp
+        for (int64_t item = blockIdx.x; item < items; item += gridDim.x, buf ^= 1) {
+            const int64_t row = item / p.splits;
+            const int split = static_cast<int>(item - row * p.splits);
+            const RowPart<T> part = row_part<T>(p, row, split);
+            bar_sync(1 + buf, kLpCtaThreads);
+            SoftSums sums = lane < kLpThreads / 32 ? notes[buf].sums[lane] : SoftSums{-INFINITY, 0.0f, 0.0f};
+            sums = warp_join(sums, c);
+            // (with scales beyond these, -10^30 times c is not far below everything, or not a number)
+            if (!(fabsf(sums.m) * c < kLpHuge) || c < 1e-26f || c > 1e7f) sums = careful_sums<T>(part, c);
+            if (p.splits == 1) {
+                float lse = 0.0f;
+                if (lane == 0) {
+                    lse = finish_row(p, row, sums);
+                    finish_target<T>(p, row, lse);
+                }
+                if constexpr (TOP) {
+                    lse = __shfl_sync(0xffffffffu, lse, 0);
+                    if (lane < p.top_k) write_top(p, row, lane, 0ull, lse);       // ranks that do not exist keep this
+                    __syncwarp();
+                    if (lse == lse && lse != -INFINITY)
+                        warp_top<T>(part, p.top_k, notes[buf], scratch,
+                                    [&](int rank, uint64_t key) { write_top(p, row, rank, key, lse); });
+                }
+            } else {
+                if (lane == 0) p.part_sums[item] = make_float4(sums.m, sums.s, sums.a, 0.0f);
+                if constexpr (TOP) {
+                    if (lane < p.top_k) p.part_keys[item * p.top_k + lane] = 0ull;
+                    __syncwarp();
+                    warp_top<T>(part, p.top_k, notes[buf], scratch,
+                                [&](int rank, uint64_t key) { p.part_keys[item * p.top_k + rank] = key; });
+                }
+            }
+            if (item + 2 * static_cast<int64_t>(gridDim.x) < items) bar_arrive(3 + buf, kLpCtaThreads);
+        }
+        return;
+    }
+
+    // -------------------------------------------------------------------- streaming threads
+    const float reach = kLpReach / c;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x, buf ^= 1) {
+        const int64_t row = item / p.splits;
+        const RowPart<T> part = row_part<T>(p, row, static_cast<int>(item - row * p.splits));
+        float m = -INFINITY, ref = 0.0f, limit = kLpLowest;  // ref = m, or 0 while no logit above kLpLowest came
+        float2 s = make_float2(0.0f, 0.0f), a = make_float2(0.0f, 0.0f);
+        float best = -INFINITY;
+        int best_vec = 0;
+        auto move_reference = [&](float top) {
             if (m > -INFINITY) {
                 const float d = fmaxf((m - top) * c, -1000.0f), f = exp2_approx(d);
                 a.x = f * fmaf(d, s.x, a.x);
@@ -376,80 +575,67 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprobs_forward_kernel(const L
             }
             m = ref = top;
             limit = top + reach;
-        }
-        return top;
-    };
-    auto accumulate = [&](const float (&x)[kN], int vec) {
-        const float top = add(x, kN);
-        if (TOP && top > best) {
-            best = top;
-            best_vec = vec;
-        }
+        };
+        float group_best = -INFINITY;
+        int step = 0, group = 0;
+        const int group_steps = TOP ? part.group_steps() : 0;
+        auto accumulate = [&](const uint4& w, int vec) {
+            const float top = LogitVec<T>::top(w);
+            if (top > limit) move_reference(top);
+            if (TOP) {
+                group_best = fmaxf(group_best, top);
+                if (top > best) {
+                    best = top;
+                    best_vec = vec;
+                }
+            }
+            float2 x[kN / 2];
+            LogitVec<T>::get_floored(w, x);
 #pragma unroll
-        for (int i = 0; i < kN; i += 2) {
-            float2 d = __fadd2_rn(make_float2(x[i], x[i + 1]), make_float2(-ref, -ref));
-            d = __fmul2_rn(d, make_float2(c, c));
-            d.x = max_nan(d.x, -300.0f);                // a masked logit: 2^-300 = 0, and 0 * -300 is 0
-            d.y = max_nan(d.y, -300.0f);
-            const float2 e = make_float2(exp2_approx(d.x), exp2_approx(d.y));
-            s = __fadd2_rn(s, e);
-            a = __ffma2_rn(d, e, a);
-        }
-    };
-    const T* base = part.vec(part.first);
-    constexpr int kUnroll = 4;
-    int v = threadIdx.x;
-    for (; v + (kUnroll - 1) * kLpThreads < part.count; v += kUnroll * kLpThreads) {
-        uint4 w[kUnroll];
+            for (int i = 0; i < kN / 2; ++i) {
+                const float2 d = __fmul2_rn(__fadd2_rn(x[i], pair(-ref)), pair(c));
+                const float2 e = make_float2(exp2_approx(d.x), exp2_approx(d.y));
+                s = __fadd2_rn(s, e);
+                a = __ffma2_rn(d, e, a);
+            }
+        };
+        // the notes of two items ago have been read
+        if (item >= 2 * static_cast<int64_t>(gridDim.x)) bar_sync(3 + buf, kLpCtaThreads);
+        auto close_group = [&](bool last) {
+            if (++step == group_steps || last) {
+                notes[buf].group[group][threadIdx.x] = static_cast<uint16_t>(order_key(group_best) >> 16);
+                group_best = -INFINITY;
+                step = 0;
+                ++group;
+            }
+        };
+        const T* base = part.vec(part.first);
+        int v = threadIdx.x;
+        for (; v + (kLpUnroll - 1) * kLpThreads < part.count; v += kLpUnroll * kLpThreads) {
+            uint4 w[kLpUnroll];
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j) w[j] = ld_stream(base + static_cast<int64_t>(v + j * kLpThreads) * kN);
+            for (int j = 0; j < kLpUnroll; ++j) w[j] = ld_stream(base + static_cast<int64_t>(v + j * kLpThreads) * kN);
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j) {
-            float x[kN];
-            LogitVec<T>::get(w[j], x);
-            accumulate(x, part.first + v + j * kLpThreads);
+            for (int j = 0; j < kLpUnroll; ++j) accumulate(w[j], part.first + v + j * kLpThreads);
+            if (TOP) close_group(false);
         }
-    }
-    for (; v < part.count; v += kLpThreads) {
-        float x[kN];
-        LogitVec<T>::get(ld_stream(base + static_cast<int64_t>(v) * kN), x);
-        accumulate(x, part.first + v);
-    }
-    if (static_cast<int>(threadIdx.x) < part.n_loose0 + part.n_loose1) {
-        const float x = LogitVec<T>::one(part.row + part.loose_index(threadIdx.x));
-        add(&x, 1);
-        const float d = max_nan((x - ref) * c, -300.0f), e = exp2_approx(d);
-        s.x += e;
-        a.x = fmaf(d, e, a.x);
-    }
-    const SoftSums sums = block_join({m, s.x + s.y, a.x + a.y}, c, red);
-
-    if (p.splits == 1) {
-        __shared__ float row_lse;
-        if (threadIdx.x == 0) {
-            const float lse = finish_row(p, row, sums);
-            finish_target<T>(p, row, lse);
-            row_lse = lse;
+        const bool rest = v < part.count;
+        for (; v < part.count; v += kLpThreads) accumulate(ld_stream(base + static_cast<int64_t>(v) * kN), part.first + v);
+        if (TOP && (rest || step > 0)) close_group(true);
+        if (static_cast<int>(threadIdx.x) < part.n_loose0 + part.n_loose1) {
+            const float x = LogitVec<T>::one(part.row + part.loose_index(threadIdx.x));
+            if (x > limit) move_reference(x);
+            const float d = (max_nan(x, kLpFloor) - ref) * c, e = exp2_approx(d);
+            s.x += e;
+            a.x = fmaf(d, e, a.x);
         }
+        const SoftSums sums = warp_join({m, s.x + s.y, a.x + a.y}, c);
+        if (lane == 0) notes[buf].sums[threadIdx.x >> 5] = sums;
         if (TOP) {
-            // ranks that do not exist keep this
-            __syncthreads();
-            const float lse = row_lse;
-            if (static_cast<int>(threadIdx.x) < p.top_k) write_top(p, row, threadIdx.x, 0ull, lse);
-            __syncthreads();
-            if (lse == lse && lse != -INFINITY)
-                block_top<T>(part, p.top_k, best, best_vec, scratch,
-                             [&](int rank, uint64_t key) { write_top(p, row, rank, key, lse); });
+            notes[buf].key[threadIdx.x] = order_key(best);
+            notes[buf].vec[threadIdx.x] = static_cast<uint32_t>(best_vec);
         }
-    } else {
-        const int64_t at = row * p.splits + split;
-        if (threadIdx.x == 0) p.part_sums[at] = make_float4(sums.m, sums.s, sums.a, 0.0f);
-        if (TOP) {
-            if (static_cast<int>(threadIdx.x) < p.top_k) p.part_keys[at * p.top_k + threadIdx.x] = 0ull;
-            __syncthreads();
-            block_top<T>(part, p.top_k, best, best_vec, scratch,
-                         [&](int rank, uint64_t key) { p.part_keys[at * p.top_k + rank] = key; });
-        }
+        bar_arrive(1 + buf, kLpCtaThreads);
     }
 }
 
@@ -487,16 +673,30 @@ __global__ void __launch_bounds__(kLpJoinThreads) logprobs_join_kernel(const Log
     if (static_cast<int>(threadIdx.x) < p.top_k) write_top(p, row, threadIdx.x, 0ull, lse);
     __syncthreads();
     if (lse != lse || lse == -INFINITY) return;
-    // a key's rank is the number of larger ones; each split's keys are in descending order
-    for (int i = threadIdx.x; i < n; i += kLpJoinThreads) {
-        const uint64_t k = keys[i];
-        if (k == 0ull) continue;
-        int rank = i % p.top_k;
-        for (int s = 0; s < p.splits && rank < p.top_k; ++s) {
-            if (s == i / p.top_k) continue;
-            for (int j = 0; j < p.top_k && keys[s * p.top_k + j] > k; ++j) ++rank;
+    // Each split's keys are in descending order: one warp takes the largest head, rank after rank.
+    if (threadIdx.x >= 32) return;
+    constexpr int kLists = (kLpMaxSplits + 31) / 32;
+    const int lane = threadIdx.x;
+    int at[kLists];
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) at[i] = 0;
+    for (int rank = 0; rank < p.top_k; ++rank) {
+        uint64_t head[kLists], best = 0ull;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) {
+            const int split = lane + 32 * i;
+            head[i] = split < p.splits && at[i] < p.top_k ? keys[split * p.top_k + at[i]] : 0ull;
+            if (head[i] > best) best = head[i];
         }
-        if (rank < p.top_k) write_top(p, row, rank, k, lse);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const uint64_t other = __shfl_xor_sync(0xffffffffu, best, o);
+            if (other > best) best = other;
+        }
+        if (best == 0ull) break;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) at[i] += head[i] == best;       // keys are unique
+        if (lane == 0) write_top(p, row, rank, best, lse);
     }
 }
 
@@ -613,12 +813,13 @@ static int logprobs_shape_ok(const void* logits, int dtype, int64_t tokens, int6
 }
 
 template <class T>
-static int launch_logprobs_forward(const LogprobsParams& p, cudaStream_t st)
+static int launch_logprobs_forward(const LogprobsParams& p, int sm_count, cudaStream_t st)
 {
-    const int grid = static_cast<int>(p.tokens * p.splits);
+    const int64_t items = p.tokens * p.splits, most = 4 * static_cast<int64_t>(sm_count);
+    const int grid = static_cast<int>(items < most ? items : most);
     const cudaError_t e = p.top_k > 0
-                              ? launch_kernel_pdl(logprobs_forward_kernel<T, true>, grid, kLpThreads, 0, st, p)
-                              : launch_kernel_pdl(logprobs_forward_kernel<T, false>, grid, kLpThreads, 0, st, p);
+                              ? launch_kernel_pdl(logprobs_forward_kernel<T, true>, grid, kLpCtaThreads, 0, st, p)
+                              : launch_kernel_pdl(logprobs_forward_kernel<T, false>, grid, kLpCtaThreads, 0, st, p);
     if (e != cudaSuccess) return MXFP4_ERR_CUDA;
     if (p.splits > 1 && launch_kernel_pdl(logprobs_join_kernel<T>, static_cast<int>(p.tokens), kLpJoinThreads, 0, st,
                                           p) != cudaSuccess)
@@ -673,8 +874,8 @@ int mxfp4_logprobs_forward(const void* logits, int dtype, int64_t tokens, int64_
     p.part_sums = static_cast<float4*>(workspace);
     p.part_keys = need ? reinterpret_cast<uint64_t*>(p.part_sums + tokens * p.splits) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return dtype == MXFP4_OUT_BF16 ? launch_logprobs_forward<__nv_bfloat16>(p, st)
-                                   : launch_logprobs_forward<float>(p, st);
+    return dtype == MXFP4_OUT_BF16 ? launch_logprobs_forward<__nv_bfloat16>(p, dev.sm_count, st)
+                                   : launch_logprobs_forward<float>(p, dev.sm_count, st);
 }
 
 int mxfp4_logprobs_backward(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld,

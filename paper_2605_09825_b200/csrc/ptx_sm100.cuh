@@ -113,6 +113,16 @@ __device__ __forceinline__ uint32_t elect_one_sync()
     return pred;
 }
 
+// ---------------------------------------------------------------- named CTA barriers
+__device__ __forceinline__ void bar_sync(int id, int threads)
+{
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(int id, int threads)
+{
+    asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
 // ---------------------------------------------------------------- mbarrier
 __device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count)
 {

@@ -164,6 +164,31 @@ def test_rising_and_spiked_rows():
     check_forward(x.bfloat16(), some_targets(4, vocab), 20, 0.01)
 
 
+@pytest.mark.parametrize("tokens", [4, 700])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [1e-28, 1e-6, 1e5, 1e9])
+def test_scales_far_from_one(tokens, dtype, scale):
+    x = logits(tokens, 3001, dtype, seed=11)
+    x[0, 100:200] = -INF
+    x[1] = -INF
+    x[2] *= 1e20
+    check_forward(x, some_targets(tokens, 3001), 5, scale)
+
+
+@pytest.mark.parametrize("tokens", [3, 700])
+def test_rows_at_the_ends_of_fp32(tokens):
+    """Largest logits whose scaled value leaves fp32, of either sign, beside ordinary rows."""
+    x = logits(tokens, 5003, torch.float32, seed=12)
+    x[0] = -3e38
+    x[0, 7::50] = -2.9e38
+    x[1] = 0.0
+    x[1, 4000:4003] = 3.3e38
+    x[2] = -2e30
+    x[2, 17] = -1.5e30
+    got = check_forward(x, some_targets(tokens, 5003), 7, 0.5)
+    assert abs(got[1][1].item() - math.log(3)) < 1e-5 and got[1][2] == 0
+
+
 def test_out_of_range_target_is_nan():
     x = logits(4, 100, seed=6)
     t = torch.tensor([0, 100, 1 << 40, -5], device="cuda")
