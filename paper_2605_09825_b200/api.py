@@ -514,19 +514,37 @@ def linear_static(pass_: int, a: torch.Tensor, b: torch.Tensor, T: int, in_f: in
 
 
 # ---------------------------------------------------------------- 8-bit product, 128-blocks
+# The calls below are used for single tokens too, where the host's time is what counts: one look at each
+# property, one tensor for outputs of a kind.
 def _matrix(t: torch.Tensor, name: str, dtypes) -> tuple:
     """Pointer and leading dimension of a 2-D CUDA tensor with contiguous rows."""
-    if t.dtype not in dtypes or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name} must be a 2-D tensor of {' or '.join(map(str, dtypes))} with contiguous rows")
-    rows, cols = t.shape
-    return _dev_ptr(t), t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    stride, shape = t.stride(), t.shape
+    if t.dtype not in dtypes or len(shape) != 2 or not t.is_cuda or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D CUDA tensor of {' or '.join(map(str, dtypes))} with contiguous rows")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else max(shape[1], stride[0])   # a single row's stride is arbitrary
 
 
 def _expect(t: torch.Tensor, name: str, dtype, numel: int) -> int:
     """Pointer of a contiguous CUDA tensor with at least ``numel`` elements."""
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} elements")
-    return _dev_ptr(t)
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of {numel} elements")
+    return t.data_ptr()
+
+
+def _raw_stream() -> int:
+    """The current stream of the current device (as ``_stream``, without building a stream object)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+_BF16, _FP32 = (torch.bfloat16,), (torch.float32,)
+
+
+def _block128_floats(outer: int, K: int, block_shape: int) -> int:
+    """Scales of an operand, 0 where the library would refuse it."""
+    if outer <= 0 or K <= 0 or K % 16:
+        return 0
+    blocks = -(-outer // 128) * -(-K // 128)
+    return blocks * 128 if block_shape == BLOCK_1X128 else blocks if block_shape == BLOCK_128X128 else 0
 
 
 def block128_scales_bytes(outer: int, K: int, block_shape: int) -> int:
@@ -541,21 +559,22 @@ def quantize_block128(src: torch.Tensor, axis: int = AXIS_COLS, block_shape: int
     Returns ``(codes uint8 [outer, K], scales float32 [ceil(K / 128), pitch])``, pitch = outer rounded up
     to 128 for ``BLOCK_1X128`` and the number of row blocks for ``BLOCK_128X128``.
     """
-    ptr, ld = _matrix(src, "src", (torch.bfloat16,))
+    ptr, ld = _matrix(src, "src", _BF16)
     rows, cols = src.shape
     outer, K = (rows, cols) if axis == AXIS_COLS else (cols, rows)
-    need = block128_scales_bytes(outer, K, block_shape)
+    need = _block128_floats(outer, K, block_shape)
     if need == 0:
         _raise(-2 if block_shape in (BLOCK_1X128, BLOCK_128X128) else -4, "mxfp4_quantize_block128")
     if codes is None:
         codes = torch.empty((outer, K), dtype=torch.uint8, device=src.device)
     if scales is None:
-        blocks = (K + 127) // 128
-        scales = torch.empty((blocks, need // (4 * blocks)), dtype=torch.float32, device=src.device)
+        blocks = -(-K // 128)
+        scales = torch.empty((blocks, need // blocks), dtype=torch.float32, device=src.device)
     rc = load_library().mxfp4_quantize_block128(ptr, rows, cols, ld, axis, block_shape,
                                                 _expect(codes, "codes", torch.uint8, outer * K),
-                                                _expect(scales, "scales", torch.float32, need // 4), _stream())
-    _raise(rc, "mxfp4_quantize_block128")
+                                                _expect(scales, "scales", torch.float32, need), _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_quantize_block128")
     return codes, scales
 
 
@@ -568,23 +587,28 @@ def gemm_block128(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     N, K2 = b_codes.shape
     if K != K2:
         raise ValueError("A and B disagree on K")
-    lib = load_library()
-    a_need = lib.mxfp4_block128_scales_bytes(M, K, BLOCK_1X128) // 4
-    b_need = lib.mxfp4_block128_scales_bytes(N, K, b_block_shape) // 4
+    a_need, b_need = _block128_floats(M, K, BLOCK_1X128), _block128_floats(N, K, b_block_shape)
     if a_need == 0 or b_need == 0:
         _raise(-2 if b_block_shape in (BLOCK_1X128, BLOCK_128X128) else -4, "mxfp4_gemm_block128")
+    lib = load_library()
     out = _out_tensor((M, N), out_dtype, a_codes.device, out)
-    need = lib.mxfp4_gemm_block128_workspace_bytes(M, N, K)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=a_codes.device)
+    if out.dtype != (torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32) or out.shape != (M, N):
+        raise ValueError("out must be [M, N] of the output type")
+    out_ptr, ld_out = _matrix(out, "out", (out.dtype,))
+    ws_ptr = ws_bytes = 0
+    if workspace is None:
+        ws_bytes = lib.mxfp4_gemm_block128_workspace_bytes(M, N, K)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=a_codes.device)
+    if workspace is not None:
+        ws_ptr, ws_bytes = _dev_ptr(workspace), workspace.numel()
     rc = lib.mxfp4_gemm_block128(_expect(a_codes, "a_codes", torch.uint8, M * K),
                                  _expect(a_scales, "a_scales", torch.float32, a_need),
                                  _expect(b_codes, "b_codes", torch.uint8, N * K),
-                                 _expect(b_scales, "b_scales", torch.float32, b_need), b_block_shape, M, N, K,
-                                 _dev_ptr(out), out_dtype, out.stride(0) if M > 1 else max(N, out.stride(0)),
-                                 _dev_ptr(workspace) if workspace is not None else None,
-                                 workspace.numel() if workspace is not None else 0, _stream())
-    _raise(rc, "mxfp4_gemm_block128")
+                                 _expect(b_scales, "b_scales", torch.float32, b_need), b_block_shape, M, N, K, out_ptr,
+                                 out_dtype, ld_out, ws_ptr or None, ws_bytes, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_gemm_block128")
     return out
 
 
@@ -608,9 +632,13 @@ def linear_pass_block128(pass_: int, a: torch.Tensor, b: torch.Tensor, out_dtype
         need = lib.mxfp4_linear_pass_block128_workspace_bytes(T, in_f, out_f, pass_)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=a.device)
     out = _out_tensor(shape, out_dtype, a.device, out)
+    if tuple(out.shape) != shape or not out.is_contiguous() or \
+            out.dtype != (torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32):
+        raise ValueError("out must be a contiguous tensor of the pass's output shape and type")
     rc = lib.mxfp4_linear_pass_block128(pass_, _dev_ptr(a), _dev_ptr(b), _dev_ptr(out), T, in_f, out_f, out_dtype,
-                                        _dev_ptr(workspace), workspace.numel(), _stream())
-    _raise(rc, "mxfp4_linear_pass_block128")
+                                        _dev_ptr(workspace), workspace.numel(), _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_linear_pass_block128")
     return out
 
 
@@ -619,27 +647,26 @@ _STREAM_TYPES = {torch.bfloat16: OUT_BF16, torch.float32: OUT_FP32}
 
 
 def _norm_desc(branch, stream, stream_dtype, w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps) -> NormDesc:
-    ptr, ld = _matrix(branch, "branch", (torch.bfloat16,))
-    tokens, width = branch.shape
-    d = NormDesc(tokens, width, ptr, ld, None, 0, None, 0, None, None, stream_dtype, GATE_NONE, gate_act, skip_scale,
-                 branch_scale, eps)
+    ptr, ld = _matrix(branch, "branch", _BF16)
+    shape = branch.shape
+    tokens, width = shape
+    s_ptr, ld_s, g_ptr, ld_g, kind = None, 0, None, 0, GATE_NONE
     if stream is not None:
-        if stream.shape != branch.shape:
+        if stream.shape != shape:
             raise ValueError("stream and branch must have the same shape")
-        d.stream, d.ld_stream = _matrix(stream, "stream", tuple(_STREAM_TYPES))
+        s_ptr, ld_s = _matrix(stream, "stream", _STREAM_TYPES)
     if gate is not None:
         if gate.dim() == 1:
-            d.gate_kind, d.gate = GATE_CHANNEL, _expect(gate, "a channel gate", torch.float32, width)
-        elif gate.shape != branch.shape:
+            kind, g_ptr = GATE_CHANNEL, _expect(gate, "a channel gate", torch.float32, width)
+        elif gate.shape != shape:
             raise ValueError("gate must have the branch's shape or be a vector of its width")
         else:
-            d.gate_kind = GATE_ELEMENT
-            d.gate, d.ld_gate = _matrix(gate, "gate", (torch.bfloat16,))
-    if w_post is not None:
-        d.w_post = _expect(w_post, "w_post", torch.float32, width)
-    if w_pre is not None:
-        d.w_pre = _expect(w_pre, "w_pre", torch.float32, width)
-    return d
+            kind = GATE_ELEMENT
+            g_ptr, ld_g = _matrix(gate, "gate", _BF16)
+    return NormDesc(tokens, width, ptr, ld, s_ptr, ld_s, g_ptr, ld_g,
+                    _expect(w_post, "w_post", torch.float32, width) if w_post is not None else None,
+                    _expect(w_pre, "w_pre", torch.float32, width) if w_pre is not None else None,
+                    stream_dtype, kind, gate_act, skip_scale, branch_scale, eps)
 
 
 def residual_norm_forward(branch, stream=None, w_post=None, w_pre=None, gate=None, gate_act=GATE_LINEAR,
@@ -655,16 +682,22 @@ def residual_norm_forward(branch, stream=None, w_post=None, w_pre=None, gate=Non
     if dtype not in _STREAM_TYPES:
         raise ValueError("the stream is bf16 or fp32")
     d = _norm_desc(branch, stream, _STREAM_TYPES[dtype], w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps)
+    shape = branch.shape
     if y is None:
-        y = torch.empty(branch.shape, dtype=dtype, device=branch.device)
-    if h is None and w_pre is not None:
-        h = torch.empty(branch.shape, dtype=torch.bfloat16, device=branch.device)
-    if y.shape != branch.shape or (h is not None and h.shape != branch.shape):
-        raise ValueError("y and h must have the branch's shape")
+        y = torch.empty(shape, dtype=dtype, device=branch.device)
+    elif y.shape != shape:
+        raise ValueError("y must have the branch's shape")
     y_ptr, ld_y = _matrix(y, "y", (dtype,))
-    h_ptr, ld_h = _matrix(h, "h", (torch.bfloat16,)) if h is not None else (None, 0)
-    _raise(load_library().mxfp4_residual_norm_forward(ctypes.byref(d), y_ptr, ld_y, h_ptr, ld_h, _stream()),
-           "mxfp4_residual_norm_forward")
+    h_ptr, ld_h = None, 0
+    if h is None and w_pre is not None:
+        h = torch.empty(shape, dtype=torch.bfloat16, device=branch.device)
+    if h is not None:
+        if h.shape != shape:
+            raise ValueError("h must have the branch's shape")
+        h_ptr, ld_h = _matrix(h, "h", _BF16)
+    rc = load_library().mxfp4_residual_norm_forward(ctypes.byref(d), y_ptr, ld_y, h_ptr, ld_h, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_residual_norm_forward")
     return y, h
 
 
@@ -684,35 +717,39 @@ def residual_norm_backward(dh, dy, branch, y, w_post=None, w_pre=None, gate=None
         dstream = torch.empty(shape, dtype=dtype, device=dev)
     if dbranch is None:
         dbranch = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-    for t in (dh, dy, dstream, dbranch):
-        if t is not None and t.shape != shape:
+
+    def part(t, name, kinds):
+        if t is None:
+            return None, 0
+        if t.shape != shape:
             raise ValueError("gradients must have the branch's shape")
-    vector = lambda like: torch.empty(width, dtype=torch.float32, device=dev) if like is not None else None
-    dw_post, dw_pre = vector(w_post), vector(w_pre)
-    dgate, ld_dgate = None, 0
-    if gate is not None:
-        dgate = vector(gate) if gate.dim() == 1 else torch.empty(shape, dtype=torch.bfloat16, device=dev)
-        ld_dgate = width
+        return _matrix(t, name, kinds)
+
+    channel = gate is not None and gate.dim() == 1
+    vector = lambda wanted: torch.empty(width, dtype=torch.float32, device=dev) if wanted else None
+    dw_post, dw_pre, dgate = vector(w_post is not None), vector(w_pre is not None), vector(channel)
+    if gate is not None and not channel:
+        dgate = torch.empty(shape, dtype=torch.bfloat16, device=dev)
     lib = load_library()
-    sums = dw_post is not None or dw_pre is not None or (gate is not None and gate.dim() == 1)
-    if workspace is None and sums:
+    if workspace is None and (dw_post is not None or dw_pre is not None or channel):
         workspace = torch.empty(max(lib.mxfp4_residual_norm_workspace_bytes(tokens, width), 1), dtype=torch.uint8,
                                 device=dev)
-    opt = lambda t, name, kind: _matrix(t, name, (kind,)) if t is not None else (None, 0)
-    ptr = lambda t: _dev_ptr(t) if t is not None else None
-    rc = lib.mxfp4_residual_norm_backward(ctypes.byref(d), *opt(dh, "dh", torch.bfloat16), *opt(dy, "dy", dtype),
-                                          *_matrix(dstream, "dstream", (dtype,)),
-                                          *_matrix(dbranch, "dbranch", (torch.bfloat16,)), ptr(dgate), ld_dgate,
-                                          ptr(dw_post), ptr(dw_pre), ptr(workspace),
-                                          workspace.numel() if workspace is not None else 0, _stream())
-    _raise(rc, "mxfp4_residual_norm_backward")
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    rc = lib.mxfp4_residual_norm_backward(ctypes.byref(d), *part(dh, "dh", _BF16), *part(dy, "dy", (dtype,)),
+                                          *part(dstream, "dstream", (dtype,)), *part(dbranch, "dbranch", _BF16),
+                                          ptr(dgate), width, ptr(dw_post), ptr(dw_pre),
+                                          _dev_ptr(workspace) if workspace is not None else None,
+                                          workspace.numel() if workspace is not None else 0, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_residual_norm_backward")
     return dstream, dbranch, dgate, dw_post, dw_pre
 
 
 # ---------------------------------------------------------------- token log probabilities
 def _logits(t: torch.Tensor) -> tuple:
-    ptr, ld = _matrix(t, "logits", tuple(_STREAM_TYPES))
-    return ptr, _STREAM_TYPES[t.dtype], t.shape[0], t.shape[1], ld
+    ptr, ld = _matrix(t, "logits", _STREAM_TYPES)
+    tokens, vocab = t.shape
+    return ptr, _STREAM_TYPES[t.dtype], tokens, vocab, ld
 
 
 def logprobs_forward(logits, targets=None, top_k: int = 0, scale: float = 1.0, workspace=None):
@@ -724,21 +761,29 @@ def logprobs_forward(logits, targets=None, top_k: int = 0, scale: float = 1.0, w
     ptr, dtype, tokens, vocab, ld = _logits(logits)
     lib = load_library()
     dev = logits.device
-    row = lambda: torch.empty(tokens, dtype=torch.float32, device=dev)
-    logp, entropy, lse = row() if targets is not None else None, row(), row()
-    top_logp = top_index = None
+    logp, entropy, lse = torch.empty((3, tokens), dtype=torch.float32, device=dev).unbind(0)
+    row_ptr = logp.data_ptr()
+    t_ptr = logp_ptr = None
+    if targets is not None:
+        t_ptr, logp_ptr = _expect(targets, "targets", torch.int64, tokens), row_ptr
+    else:
+        logp = None
+    top_logp = top_index = v_ptr = i_ptr = ws_ptr = None
     if top_k > 0:
         top_logp = torch.empty((tokens, top_k), dtype=torch.float32, device=dev)
         top_index = torch.empty((tokens, top_k), dtype=torch.int64, device=dev)
-    need = lib.mxfp4_logprobs_workspace_bytes(tokens, vocab, top_k)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    opt = lambda t: _dev_ptr(t) if t is not None else None
-    rc = lib.mxfp4_logprobs_forward(
-        ptr, dtype, tokens, vocab, ld, _expect(targets, "targets", torch.int64, tokens) if targets is not None else None,
-        scale, opt(logp), _dev_ptr(entropy), _dev_ptr(lse), top_k, opt(top_logp), opt(top_index), opt(workspace),
-        workspace.numel() if workspace is not None else 0, _stream())
-    _raise(rc, "mxfp4_logprobs_forward")
+        v_ptr, i_ptr = top_logp.data_ptr(), top_index.data_ptr()
+    ws_bytes = 0
+    if workspace is None:
+        ws_bytes = lib.mxfp4_logprobs_workspace_bytes(tokens, vocab, top_k)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        ws_ptr, ws_bytes = _dev_ptr(workspace), workspace.numel()
+    rc = lib.mxfp4_logprobs_forward(ptr, dtype, tokens, vocab, ld, t_ptr, scale, logp_ptr, row_ptr + 4 * tokens,
+                                    row_ptr + 8 * tokens, top_k, v_ptr, i_ptr, ws_ptr, ws_bytes, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_logprobs_forward")
     return logp, entropy, lse, top_logp, top_index
 
 
@@ -756,8 +801,9 @@ def logprobs_backward(logits, targets, lse, entropy=None, d_logp=None, d_entropy
     row = lambda t, name, kind=torch.float32: _expect(t, name, kind, tokens) if t is not None else None
     rc = load_library().mxfp4_logprobs_backward(
         ptr, dtype, tokens, vocab, ld, row(targets, "targets", torch.int64), scale, row(lse, "lse"),
-        row(entropy, "entropy"), row(d_logp, "d_logp"), row(d_entropy, "d_entropy"), d_ptr, ld_d, _stream())
-    _raise(rc, "mxfp4_logprobs_backward")
+        row(entropy, "entropy"), row(d_logp, "d_logp"), row(d_entropy, "d_entropy"), d_ptr, ld_d, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_logprobs_backward")
     return dlogits
 
 

@@ -135,7 +135,7 @@ def run_gemm(ops, square, out_dtype, out=None):
     return got
 
 
-SHAPES = [(256, 256, 128), (1, 8, 16), (1, 4096, 4096), (3, 520, 1040), (77, 200, 96), (128, 256, 2048), (129, 257 + 7, 400),
+SHAPES = [(8, 1000, 272), (9, 40, 4096), (16, 4096, 1040), (17, 520, 4096), (40, 4096, 2048), (256, 256, 128), (1, 8, 16), (1, 4096, 4096), (3, 520, 1040), (77, 200, 96), (128, 256, 2048), (129, 257 + 7, 400),
           (300, 392, 272), (512, 1000, 1184), (600, 24, 4112), (1100, 2056, 640), (2300, 4104, 256)]
 
 

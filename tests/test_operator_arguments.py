@@ -30,7 +30,7 @@ def test_sizes(lib):
     assert s(0, 128, 2) == s(128, 0, 2) == s(128, 120, 2) == s(128, 128, api.BLOCK_1X32) == 0
     w = lib.mxfp4_gemm_block128_workspace_bytes
     assert w(8192, 4096, 4096) == 0 and w(1, 4096, 128) == 0          # enough tiles; nothing to split
-    assert w(1, 4096, 14336) % (4096 * 4) == 0 and w(1, 4096, 14336) > 0
+    assert w(40, 4096, 14336) % (40 * 4096 * 4) == 0 and w(40, 4096, 14336) > 0 and w(1, 4096, 14336) == 0
     assert w(0, 8, 128) == w(8, 8, 100) == 0
     lw = lib.mxfp4_linear_pass_block128_workspace_bytes
     assert lw(8192, 4096, 6144, 0) >= 8192 * 4096 + 6144 * 4096
@@ -63,8 +63,8 @@ def test_gemm_block128(lib, p):
     assert call(shape=0) == call(dtype=2) == -4
     assert call(M=0) == call(N=0) == call(K=0) == call(K=120) == call(ld=120) == call(M=BIG, N=BIG, ld=BIG) == -2
     assert call(N=100, ld=100) == -3
-    assert call(M=1, N=4096, K=14336, ld=4096) == -5                   # split along K: needs its workspace
-    assert call(M=1, N=4096, K=14336, ld=4096, ws=p, n=64) == -5
+    assert call(M=40, N=4096, K=14336, ld=4096) == -5                  # split along K: needs its workspace
+    assert call(M=40, N=4096, K=14336, ld=4096, ws=p, n=64) == -5
 
 
 def test_linear_pass_block128(lib, p):
