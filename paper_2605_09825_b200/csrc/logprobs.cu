@@ -579,16 +579,22 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
         float group_best = -INFINITY;
         int step = 0, group = 0;
         const int group_steps = TOP ? part.group_steps() : 0;
-        auto accumulate = [&](const uint4& w, int vec) {
-            const float top = LogitVec<T>::top(w);
+        auto look = [&](const float* tops, int n, int vec) {    // n vectors from `vec` on, kLpThreads apart
+            float top = tops[0];
+#pragma unroll
+            for (int j = 1; j < n; ++j) top = fmaxf(top, tops[j]);
             if (top > limit) move_reference(top);
             if (TOP) {
                 group_best = fmaxf(group_best, top);
                 if (top > best) {
                     best = top;
-                    best_vec = vec;
+#pragma unroll
+                    for (int j = n - 1; j >= 0; --j)
+                        if (tops[j] == top) best_vec = vec + j * kLpThreads;     // the first of them stays
                 }
             }
+        };
+        auto accumulate = [&](const uint4& w) {
             float2 x[kN / 2];
             LogitVec<T>::get_floored(w, x);
 #pragma unroll
@@ -615,12 +621,21 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
             uint4 w[kLpUnroll];
 #pragma unroll
             for (int j = 0; j < kLpUnroll; ++j) w[j] = ld_stream(base + static_cast<int64_t>(v + j * kLpThreads) * kN);
+            float tops[kLpUnroll];
 #pragma unroll
-            for (int j = 0; j < kLpUnroll; ++j) accumulate(w[j], part.first + v + j * kLpThreads);
+            for (int j = 0; j < kLpUnroll; ++j) tops[j] = LogitVec<T>::top(w[j]);
+            look(tops, kLpUnroll, part.first + v);
+#pragma unroll
+            for (int j = 0; j < kLpUnroll; ++j) accumulate(w[j]);
             if (TOP) close_group(false);
         }
         const bool rest = v < part.count;
-        for (; v < part.count; v += kLpThreads) accumulate(ld_stream(base + static_cast<int64_t>(v) * kN), part.first + v);
+        for (; v < part.count; v += kLpThreads) {
+            const uint4 w = ld_stream(base + static_cast<int64_t>(v) * kN);
+            const float top = LogitVec<T>::top(w);
+            look(&top, 1, part.first + v);
+            accumulate(w);
+        }
         if (TOP && (rest || step > 0)) close_group(true);
         if (static_cast<int>(threadIdx.x) < part.n_loose0 + part.n_loose1) {
             const float x = LogitVec<T>::one(part.row + part.loose_index(threadIdx.x));
