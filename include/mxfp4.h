@@ -399,9 +399,9 @@ int mxfp4_linear_static(int pass, const void* a, const void* b, void* out, int64
  *
  * mxfp4_gemm_block128: out[m][n] = sum_t sa(m, t) * sb(n, t) * sum_{k in block t} A[m][k] * B[n][k]
  *   A always has 1 x 128 blocks, B the ones b_block_shape names.  out as in mxfp4_gemm.
- *   workspace   mxfp4_gemm_block128_workspace_bytes(M, N, K) bytes (0 for most shapes: only products with
- *               too few output tiles for the device are split along K and joined in a fixed order),
- *               16-byte aligned; free again once the call's work has run.
+ *   workspace   mxfp4_gemm_block128_workspace_bytes(M, N, K) bytes (at most 20 MB; may be 0: the output
+ *               tiles that do not fill a wave of the device are split along K and joined in a fixed
+ *               order), 16-byte aligned; free again once the call's work has run.
  *
  * mxfp4_linear_pass_block128: one pass of a linear with both operands quantized in the call;
  *   (a, b, out) as in mxfp4_linear_pass.  Activations and gradients get 1 x 128 blocks along the

@@ -61,14 +61,22 @@ static int64_t gemm128_tiles(int64_t M, int64_t N) { return ((M + kBTile - 1) / 
 // (1 x 4096 x 14336: RRR us against 22 + 5 us of the split kernel and its join).
 static bool gemm128_few_rows(int64_t M) { return M <= 8 * kRowsMaxTiles; }
 
-// Splits along K: as many as give every CTA pair a piece, with at least four K-steps in each.
-static int gemm128_splits(int64_t M, int64_t N, int64_t K)
+// Which tiles are split along K, and into how many pieces: those that do not fill a wave of the pairs, into as
+// many pieces as fit the wave, with at least four K-steps in each.
+struct Split128 {
+    int64_t whole;               // tiles of one piece
+    int64_t split;               // tiles after them
+    int64_t pieces;              // of each of these
+};
+
+static Split128 gemm128_split(int64_t M, int64_t N, int64_t K)
 {
-    if (gemm128_few_rows(M)) return 1;
     const int64_t tiles = gemm128_tiles(M, N), steps = blocks_of(K);
-    int64_t s = tiles > 0 ? kB128SplitPairs / tiles : 1;
-    if (s > steps / 4) s = steps / 4;
-    return static_cast<int>(s < 1 ? 1 : s);
+    const int64_t left = tiles % kB128SplitPairs;
+    int64_t pieces = left > 0 ? kB128SplitPairs / left : 1;
+    if (pieces > steps / 4) pieces = steps / 4;
+    if (gemm128_few_rows(M) || pieces < 2) return {tiles, 0, 1};
+    return {tiles - left, left, pieces};
 }
 
 static int gemm128_shape_ok(int64_t M, int64_t N, int64_t K)
@@ -81,7 +89,7 @@ static int gemm128_shape_ok(int64_t M, int64_t N, int64_t K)
 
 template <bool BROWS, bool OUT32>
 static int launch_gemm128(const CUtensorMap& tm_a, const CUtensorMap& tm_b, const CUtensorMap& tm_out,
-                          const Gemm128Params& p, int sm_count, cudaStream_t st)
+                          const CUtensorMap& tm_parts, const Gemm128Params& p, int sm_count, cudaStream_t st)
 {
     const size_t smem = sizeof(Gemm128Smem) + 1024;
     static PerDeviceOnce once;
@@ -107,9 +115,9 @@ static int launch_gemm128(const CUtensorMap& tm_a, const CUtensorMap& tm_b, cons
         return resident[dev] > 0 ? MXFP4_OK : MXFP4_ERR_CUDA;
     });
     if (rc != MXFP4_OK) return rc;
-    const int64_t items = static_cast<int64_t>(p.tiles_m) * p.tiles_n * p.splits;
-    const int clusters = static_cast<int>(items < resident[dev] ? items : resident[dev]);
-    return launch_kernel_pdl(kernel, 2 * clusters, kBThreads, smem, st, tm_a, tm_b, tm_out, p) == cudaSuccess
+    const int clusters = p.items < resident[dev] ? p.items : resident[dev];
+    return launch_kernel_pdl(kernel, 2 * clusters, kBThreads, smem, st, tm_a, tm_b, tm_out, tm_parts, p) ==
+                   cudaSuccess
                ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
@@ -148,21 +156,22 @@ static int gemm128_launch(const void* a_codes, const void* a_scales, const void*
 {
     if (gemm128_few_rows(M))
         return rows128_launch(a_codes, a_scales, b_codes, b_scales, brows, M, N, K, out, out_dtype, ld_out, st);
-    const int splits = gemm128_splits(M, N, K);
-    const bool out32 = splits > 1 || out_dtype == MXFP4_OUT_FP32;
-    // split products leave fp32 sums in the workspace, rows padded to whole 16-byte pieces
-    void* dst = splits > 1 ? workspace : out;
-    const int64_t ld = splits > 1 ? (N + 3) / 4 * 4 : ld_out;
+    const Split128 split = gemm128_split(M, N, K);
+    const bool out32 = out_dtype == MXFP4_OUT_FP32;
+    const int64_t part_rows = M < kBTile ? M : kBTile;
     const int64_t esz = out32 ? 4 : 2;
-    const int64_t n_tma = out32 ? (splits > 1 ? ld : N & ~static_cast<int64_t>(3)) : N & ~static_cast<int64_t>(7);
-    CUtensorMap tm_a, tm_b, tm_out;
-    if (n_tma > 0) {
-        if (!make_tmap_3d(&tm_out, out32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dst,
-                          splits, M, n_tma, ld * esz, M * ld * esz, 32, out32 ? 32 : 64, CU_TENSOR_MAP_SWIZZLE_128B))
-            return MXFP4_ERR_CUDA;
-    } else {
-        memset(&tm_out, 0, sizeof(tm_out));
-    }
+    const int64_t n_tma = N & ~static_cast<int64_t>(out32 ? 3 : 7);
+    CUtensorMap tm_a, tm_b, tm_out, tm_parts;
+    memset(&tm_out, 0, sizeof(tm_out));
+    memset(&tm_parts, 0, sizeof(tm_parts));
+    if (split.whole > 0 && n_tma > 0 &&
+        !make_tmap_3d(&tm_out, out32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, out, 1, M, n_tma,
+                      ld_out * esz, M * ld_out * esz, 32, out32 ? 32 : 64, CU_TENSOR_MAP_SWIZZLE_128B))
+        return MXFP4_ERR_CUDA;
+    if (split.split > 0 &&
+        !make_tmap_3d(&tm_parts, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, workspace, split.split * split.pieces, part_rows,
+                      kBTile, kBTile * 4, part_rows * kBTile * 4, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B))
+        return MXFP4_ERR_CUDA;
     if (!make_tmap_2d(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a_codes, M, K, K, kBHalf, kBBlockK,
                       CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_tmap_2d(&tm_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, b_codes, N, K, K, kBHalf / 2, kBBlockK,
@@ -171,9 +180,8 @@ static int gemm128_launch(const void* a_codes, const void* a_scales, const void*
     Gemm128Params p;
     p.a_scales = static_cast<const float*>(a_scales);
     p.b_scales = static_cast<const float*>(b_scales);
-    p.out = dst;
-    p.ld_out = ld;
-    p.split_stride = M * ld;
+    p.out = out;
+    p.ld_out = ld_out;
     p.pitch_a = blocks_of(M) * kB128;
     p.pitch_b = brows ? blocks_of(N) * kB128 : blocks_of(N);
     p.M = static_cast<int32_t>(M);
@@ -185,29 +193,33 @@ static int gemm128_launch(const void* a_codes, const void* a_scales, const void*
     if (band < 1) band = 1;
     p.band = static_cast<int32_t>(band < p.tiles_n ? band : p.tiles_n);
     p.k_steps = static_cast<int32_t>(blocks_of(K));
-    p.splits = splits;
+    p.whole = static_cast<int32_t>(split.whole);
+    p.splits = static_cast<int32_t>(split.pieces);
+    p.items = static_cast<int32_t>(split.whole + split.split * split.pieces);
     p.n_tma = static_cast<int32_t>(n_tma);
     int rc;
     if (brows)
-        rc = out32 ? launch_gemm128<true, true>(tm_a, tm_b, tm_out, p, sm_count, st)
-                   : launch_gemm128<true, false>(tm_a, tm_b, tm_out, p, sm_count, st);
+        rc = out32 ? launch_gemm128<true, true>(tm_a, tm_b, tm_out, tm_parts, p, sm_count, st)
+                   : launch_gemm128<true, false>(tm_a, tm_b, tm_out, tm_parts, p, sm_count, st);
     else
-        rc = out32 ? launch_gemm128<false, true>(tm_a, tm_b, tm_out, p, sm_count, st)
-                   : launch_gemm128<false, false>(tm_a, tm_b, tm_out, p, sm_count, st);
-    if (rc != MXFP4_OK || splits == 1) return rc;
+        rc = out32 ? launch_gemm128<false, true>(tm_a, tm_b, tm_out, tm_parts, p, sm_count, st)
+                   : launch_gemm128<false, false>(tm_a, tm_b, tm_out, tm_parts, p, sm_count, st);
+    if (rc != MXFP4_OK || split.split == 0) return rc;
     Gemm128JoinParams j;
     j.parts = static_cast<const float*>(workspace);
-    j.ld = ld;
-    j.split_stride = M * ld;
     j.out = out;
     j.ld_out = ld_out;
     j.M = p.M;
     j.N = p.N;
-    j.splits = splits;
-    j.out_fp32 = out_dtype == MXFP4_OUT_FP32;
-    const int64_t quads = M * (ld / 4);
-    return launch_kernel_pdl(gemm_block128_join_kernel, static_cast<int>((quads + 255) / 256), 256, 0, st, j) == cudaSuccess
-               ? MXFP4_OK : MXFP4_ERR_CUDA;
+    j.whole = p.whole;
+    j.splits = p.splits;
+    j.rows = static_cast<int32_t>(part_rows);
+    j.band = p.band;
+    j.tiles_m = p.tiles_m;
+    j.tiles_n = p.tiles_n;
+    j.out_fp32 = out32;
+    const int blocks = static_cast<int>(split.split * ((part_rows + kBJoinRows - 1) / kBJoinRows));
+    return launch_kernel_pdl(gemm_block128_join_kernel, blocks, 256, 0, st, j) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
 // (rows, cols, axis) of the pass's operands in their own row-major shapes, and the product's sizes
@@ -253,8 +265,8 @@ int mxfp4_quantize_block128(const void* src_bf16, int64_t rows, int64_t cols, in
 size_t mxfp4_gemm_block128_workspace_bytes(int64_t M, int64_t N, int64_t K)
 {
     if (gemm128_shape_ok(M, N, K) != MXFP4_OK) return 0;
-    const int splits = gemm128_splits(M, N, K);
-    return splits == 1 ? 0 : static_cast<size_t>(splits) * M * ((N + 3) / 4 * 4) * sizeof(float);
+    const Split128 split = gemm128_split(M, N, K);
+    return static_cast<size_t>(split.split * split.pieces) * (M < kBTile ? M : kBTile) * kBTile * sizeof(float);
 }
 
 int mxfp4_gemm_block128(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales,

@@ -28,12 +28,15 @@
 // block-scaled kernel: full and tmem_empty live in the leader, empty and tmem_full are signalled in both
 // CTAs by a multicast commit.  All waits are bounded.
 //
-// Products with few output tiles are split along K (`splits`): each split writes its fp32 sums to
-// the workspace and a second kernel adds them in a fixed order.
+// The output tiles that do not fill a wave of the 74 pairs -- all of them in a small product, the last ones in
+// a large one -- are split along K where two or more pieces of each fit the wave: every piece writes its
+// fp32 sums to the workspace, and a second kernel adds them in a fixed order.
 #pragma once
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "../../include/mxfp4.h"
 #include "ptx_sm100.cuh"
@@ -76,14 +79,15 @@ struct Gemm128Params {
     const float* b_scales;
     void* out;                   // for the columns past the last 16-byte granule
     int64_t ld_out;
-    int64_t split_stride;        // elements between the splits' outputs
     int64_t pitch_a;             // scales per K-step of A, of B
     int64_t pitch_b;
     int32_t M, N, K;
     int32_t tiles_m, tiles_n;
     int32_t band;                // tile columns per band of the tile order
     int32_t k_steps;             // ceil(K / 128)
-    int32_t splits;              // along K
+    int32_t whole;               // tiles with one piece; the others have `splits` along K
+    int32_t splits;
+    int32_t items;               // pieces of all tiles
     int32_t n_tma;               // columns written by TMA stores
 };
 
@@ -91,22 +95,36 @@ struct Gemm128Params {
 // `band` tile columns, sized so that its B panel stays in L2, and inside a band the tile column varies
 // fastest, so that the tiles in flight share A rows and B columns.
 struct Gemm128Work {
-    int tm, tn, split, k0, k1;
+    int tm, tn, slot, k0, k1;    // slot: place of the sums in the workspace; -1: they are the output
 };
+
+// Row and column of a tile, counted in tiles.
+__host__ __device__ __forceinline__ void gemm128_place(int tile, int band, int tiles_m, int tiles_n, int& tm, int& tn)
+{
+    const int per_band = band * tiles_m;
+    const int b = tile / per_band;
+    const int r = tile - b * per_band;
+    const int cols = min(band, tiles_n - b * band);
+    tm = r / cols;
+    tn = b * band + (r - tm * cols);
+}
 
 __device__ __forceinline__ Gemm128Work gemm128_work(const Gemm128Params& p, int item)
 {
     Gemm128Work w;
-    const int tile = item / p.splits;
-    w.split = item - tile * p.splits;
-    const int per_band = p.band * p.tiles_m;
-    const int b = tile / per_band;
-    const int r = tile - b * per_band;
-    const int cols = min(p.band, p.tiles_n - b * p.band);
-    w.tm = r / cols;
-    w.tn = b * p.band + (r - w.tm * cols);
-    w.k0 = static_cast<int>(static_cast<int64_t>(p.k_steps) * w.split / p.splits);
-    w.k1 = static_cast<int>(static_cast<int64_t>(p.k_steps) * (w.split + 1) / p.splits);
+    int tile = item;
+    w.slot = item - p.whole;
+    w.k0 = 0;
+    w.k1 = p.k_steps;
+    if (w.slot < 0) {
+        w.slot = -1;
+    } else {
+        const int t = w.slot / p.splits, split = w.slot - t * p.splits;
+        tile = p.whole + t;
+        w.k0 = static_cast<int>(static_cast<int64_t>(p.k_steps) * split / p.splits);
+        w.k1 = static_cast<int>(static_cast<int64_t>(p.k_steps) * (split + 1) / p.splits);
+    }
+    gemm128_place(tile, p.band, p.tiles_m, p.tiles_n, w.tm, w.tn);
     return w;
 }
 
@@ -121,7 +139,8 @@ __device__ __forceinline__ int gemm128_width(int N, int tn, int half)
 template <bool BROWS, bool OUT32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBThreads, 1)
 gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
-                          const __grid_constant__ CUtensorMap tm_out, const Gemm128Params p)
+                          const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ CUtensorMap tm_parts,
+                          const Gemm128Params p)
 {
     extern __shared__ uint8_t smem_raw[];
     Gemm128Smem& sm = *reinterpret_cast<Gemm128Smem*>(smem_align_1024(smem_raw));
@@ -130,7 +149,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1;
     const int n_clusters = gridDim.x >> 1;
-    const int items = p.tiles_m * p.tiles_n * p.splits;
+    const int items = p.items;
 
     if (threadIdx.x == 0) {
         sm.abort_flag = 0;
@@ -424,17 +443,13 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
             if (!alive) break;                         // a wait was given up: nothing of this tile is stored
             // the warp's 32 rows x 128 columns leave in boxes of 128 bytes per row, staged in the 128-byte
             // swizzle for a TMA store that clips at the matrix edges
-            constexpr int kBoxCols = OUT32 ? 32 : 64;
-            constexpr int kGranule = OUT32 ? 4 : 8;
-#pragma unroll
-            for (int c = 0; c < kBHalf / kBoxCols; ++c) {
-                const int col = col0 + c * kBoxCols;
+            auto stage_box = [&](auto fp32, int c) {
                 if (lane == 0) bulk_wait_group_read<0>();
                 __syncwarp();
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                     uint8_t* to = stg + lane * 128 + ((q ^ (lane & 7)) * 16);
-                    if (OUT32) {
+                    if constexpr (decltype(fp32)::value) {
                         // two words at a time: four would have to sit in adjacent registers, which the sums' pairs do not
                         smem_store(to, acc[c * 16 + 2 * q], stg, kBStageBytes);
                         smem_store(to + 8, acc[c * 16 + 2 * q + 1], stg, kBStageBytes);
@@ -446,12 +461,32 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
+            };
+            if (w.slot >= 0) {
+                // a piece of a tile: its sums have a place of their own in the workspace
+#pragma unroll
+                for (int c = 0; c < kBHalf / 32; ++c) {
+                    stage_box(std::true_type{}, c);
+                    if (lane == 0) {
+                        tma_store_3d(&tm_parts, stg, half * kBHalf + c * 32, static_cast<int>(rank) * kBHalf + quad * 32,
+                                     w.slot);
+                        bulk_commit_group();
+                    }
+                }
+                continue;
+            }
+            constexpr int kBoxCols = OUT32 ? 32 : 64;
+            constexpr int kGranule = OUT32 ? 4 : 8;
+#pragma unroll
+            for (int c = 0; c < kBHalf / kBoxCols; ++c) {
+                const int col = col0 + c * kBoxCols;
+                stage_box(std::bool_constant<OUT32>{}, c);
                 // columns past the last full 16-byte granule, one by one from the staged row
                 const int rc = p.n_tma - col;
                 if (p.n_tma < p.N && rc >= 0 && rc < kBoxCols && row_ok) {
                     const int q = rc / kGranule;
                     const uint4 v = smem_load<uint4>(stg + lane * 128 + ((q ^ (lane & 7)) * 16), stg, kBStageBytes);
-                    const int64_t at = w.split * p.split_stride + static_cast<int64_t>(row0 + lane) * p.ld_out + p.n_tma;
+                    const int64_t at = static_cast<int64_t>(row0 + lane) * p.ld_out + p.n_tma;
                     const uint32_t e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (int j = 0; j < kGranule; ++j)
@@ -461,7 +496,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                         }
                 }
                 if (lane == 0 && col < p.n_tma) {
-                    tma_store_3d(&tm_out, stg, col, row0, w.split);
+                    tma_store_3d(&tm_out, stg, col, row0, 0);
                     bulk_commit_group();
                 }
             }
@@ -479,35 +514,51 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
     }
 }
 
-// Sum of the splits' fp32 outputs, in the order of the splits; four columns per thread.
+// Sum of the pieces of the split tiles, in their order; four columns per thread.
 struct Gemm128JoinParams {
-    const float* parts;          // [split][M][ld]
-    int64_t ld;                  // a multiple of 4
-    int64_t split_stride;
+    const float* parts;          // [split tile][piece][rows][256]
     void* out;
     int64_t ld_out;
     int32_t M, N;
+    int32_t whole;               // the first split tile
     int32_t splits;
+    int32_t rows;                // min(M, 256)
+    int32_t band, tiles_m, tiles_n;
     int32_t out_fp32;
 };
+
+constexpr int kBJoinRows = 4;    // per block, four columns per thread
 
 __global__ void __launch_bounds__(256) gemm_block128_join_kernel(const Gemm128JoinParams p)
 {
     griddep_launch_dependents();
+    const int per_tile = (p.rows + kBJoinRows - 1) / kBJoinRows;
+    const int t = blockIdx.x / per_tile;
+    const int r = (blockIdx.x - t * per_tile) * kBJoinRows + threadIdx.x / (kBTile / 4);
+    const int c = threadIdx.x % (kBTile / 4) * 4;
+    int tm, tn;
+    gemm128_place(p.whole + t, p.band, p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t row = static_cast<int64_t>(tm) * kBTile + r;
+    const int64_t col = static_cast<int64_t>(tn) * kBTile + c;
+    if (r >= p.rows || row >= p.M || col >= p.N) return;
     griddep_wait();
-    const int64_t quads = p.ld / 4;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = at / quads;
-    const int col = static_cast<int>(at - row * quads) * 4;
-    if (row >= p.M || col >= p.N) return;
+    const int64_t piece = static_cast<int64_t>(p.rows) * kBTile;
+    const float* from = p.parts + t * p.splits * piece + r * kBTile + c;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
     for (int i = 0; i < p.splits; ++i) {
-        const float4 v = *reinterpret_cast<const float4*>(p.parts + i * p.split_stride + row * p.ld + col);
+        const float4 v = *reinterpret_cast<const float4*>(from + i * piece);
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
     const float e[4] = {s.x, s.y, s.z, s.w};
+    if (col + 3 < p.N) {                                     // rows start at multiples of 16 bytes
+        if (p.out_fp32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.ld_out + col) = s;
+        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * p.ld_out + col) =
+            make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+        return;
+    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 3; ++j)
         if (col + j < p.N) {
             if (p.out_fp32) static_cast<float*>(p.out)[row * p.ld_out + col + j] = e[j];
             else static_cast<__nv_bfloat16*>(p.out)[row * p.ld_out + col + j] = __float2bfloat16_rn(e[j]);

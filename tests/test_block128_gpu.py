@@ -165,6 +165,17 @@ def test_gemm_writes_its_matrix_and_nothing_else(M, N, K, out_dtype):
     assert (buf[0] == 7).all() and (buf[-1] == 7).all() and (buf[:, N:] == 7).all()
 
 
+# a full wave of tiles and a few left over, which are split along K; ragged in both directions
+@pytest.mark.parametrize("square", [True, False])
+@pytest.mark.parametrize("out_dtype", [api.OUT_FP32, api.OUT_BF16])
+@pytest.mark.parametrize("M,N,K", [(40, 75 * 256 + 8, 1040), (300, 38 * 256 - 8, 1536), (2049, 2304, 2064)])
+def test_gemm_left_over_tiles(M, N, K, out_dtype, square):
+    assert api.load_library().mxfp4_gemm_block128_workspace_bytes(M, N, K) > 0
+    test_gemm_random_codes(M, N, K, out_dtype, square)
+    if square:
+        test_gemm_writes_its_matrix_and_nothing_else(M, N - 5, K, out_dtype)
+
+
 def test_gemm_long_reduction_of_one_sign():
     """Products of one sign are where truncating additions show: with a chain of four instructions per
     block the error stays at the fp32 sum's own level however long the reduction is."""
