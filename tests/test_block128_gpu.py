@@ -168,7 +168,7 @@ def test_gemm_writes_its_matrix_and_nothing_else(M, N, K, out_dtype):
 # a full wave of tiles and a few left over, which are split along K; ragged in both directions
 @pytest.mark.parametrize("square", [True, False])
 @pytest.mark.parametrize("out_dtype", [api.OUT_FP32, api.OUT_BF16])
-@pytest.mark.parametrize("M,N,K", [(40, 75 * 256 + 8, 1040), (300, 38 * 256 - 8, 1536), (2049, 2304, 2064)])
+@pytest.mark.parametrize("M,N,K", [(40, 75 * 256 + 8, 2064), (300, 38 * 256 - 8, 2048), (2049, 2304, 2064)])
 def test_gemm_left_over_tiles(M, N, K, out_dtype, square):
     assert api.load_library().mxfp4_gemm_block128_workspace_bytes(M, N, K) > 0
     test_gemm_random_codes(M, N, K, out_dtype, square)
