@@ -58,7 +58,7 @@ static int quantize128_checked(const void* src, int64_t rows, int64_t cols, int6
 static int64_t gemm128_tiles(int64_t M, int64_t N) { return ((M + kBTile - 1) / kBTile) * ((N + kBTile - 1) / kBTile); }
 
 // Up to this many rows of A the product is bound by reading B and runs without the tensor cores' machinery
-// (1 x 4096 x 14336: RRR us against 22 + 5 us of the split kernel and its join).
+// (1 x 4096 x 14336: 13.4 us against 22 + 5 us of the split kernel and its join).
 static bool gemm128_few_rows(int64_t M) { return M <= 8 * kRowsMaxTiles; }
 
 // Which tiles are split along K, and into how many pieces: those that do not fill a wave of the pairs, into as

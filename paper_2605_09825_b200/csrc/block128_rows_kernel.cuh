@@ -7,7 +7,11 @@
 // both operands agree, so a lane's 16-byte pieces of a row go in as they come: a quad covers 64 contiguous
 // bytes of each row.  Every K-block is a product of its own, scaled and added in fp32.
 //
-// 1 x 4096 x 14336: 58.7 MB of codes.
+// Codes and scales of two K-blocks are loaded before the first product: two CTAs of eight warps keep 64 KB of B in
+// flight per SM.  1 x 4096 x 14336: 13.4 us (58.7 MB, 4.4 TB/s, with two launches' worth of latency in it),
+// 1 x 128256 x 4096: 92 us (5.7 TB/s); 16 rows: 16.8 and 120 us, the rows of A coming from L2 once per CTA.
+// Scales loaded where they are used: 14.0 and 98.6 us; four K-blocks in flight: 13.8 and 86 us, but 15.2
+// and 103 with a scale per row of B and 138 with 16 rows (registers); three or four CTAs per SM spill.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -77,46 +81,61 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 2) gemm_block128_rows_kernel(
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[m][i] = 0.0f;
 
-    constexpr int kUnroll = 2;                       // K-blocks in flight
+    constexpr int kUnroll = 2;                       // K-blocks in flight per warp
     for (int t0 = warp; t0 < p.k_blocks; t0 += kUnroll * kRowsWarps) {
-        uint4 w0[kUnroll][2], w1[kUnroll][2];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = (t0 + u * kRowsWarps) * 128 + h * 64 + q * 16;
-                w0[u][h] = ldg16_stream(b0 + k, row0 && k < p.K);
-                w1[u][h] = ldg16_stream(b1 + k, row1 && k < p.K);
-            }
+        uint4 w0[kUnroll][2], w1[kUnroll][2], x[kUnroll][TILES][2];
+        float2 sa[kUnroll][TILES];
+        float sb0[kUnroll], sb1[kUnroll];
+        // everything the blocks need is on its way before the first product
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int t = t0 + u * kRowsWarps;
-            if (t >= p.k_blocks) break;
-            float sb0, sb1;
-            if (BROWS) {
-                sb0 = row0 ? p.b_scales[t * p.pitch_b + n0 + g] : 0.0f;
-                sb1 = row1 ? p.b_scales[t * p.pitch_b + n0 + g + 8] : 0.0f;
-            } else {
-                sb0 = sb1 = p.b_scales[t * p.pitch_b + n0 / 128];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = t * 128 + h * 64 + q * 16;
+                w0[u][h] = ldg16_stream(b0 + k, row0 && k < p.K);
+                w1[u][h] = ldg16_stream(b1 + k, row1 && k < p.K);
             }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int t = t0 + u * kRowsWarps;
+            const bool in = t < p.k_blocks;
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int k = t * 128 + h * 64 + q * 16, row = m * 8 + g;
+                    x[u][m][h] = ldg16(p.a_codes + static_cast<int64_t>(row) * p.K + k, row < p.M && k < p.K);
+                }
+                // the scales of A reach to 128 rows
+                sa[u][m] = in ? __ldg(reinterpret_cast<const float2*>(p.a_scales + t * p.pitch_a + m * 8 + 2 * q))
+                              : make_float2(0.0f, 0.0f);
+            }
+            if (BROWS) {
+                sb0[u] = row0 && in ? __ldg(p.b_scales + t * p.pitch_b + n0 + g) : 0.0f;
+                sb1[u] = row1 && in ? __ldg(p.b_scales + t * p.pitch_b + n0 + g + 8) : 0.0f;
+            } else {
+                sb0[u] = sb1[u] = in ? __ldg(p.b_scales + t * p.pitch_b + n0 / 128) : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
             for (int m = 0; m < TILES; ++m) {
                 float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int k = t * 128 + h * 64 + q * 16, row = m * 8 + g;
-                    const uint4 x = ldg16(p.a_codes + static_cast<int64_t>(row) * p.K + k, row < p.M && k < p.K);
-                    mma_e4m3_16x8x32(c, w0[u][h].x, w1[u][h].x, w0[u][h].y, w1[u][h].y, x.x, x.y);
-                    mma_e4m3_16x8x32(c, w0[u][h].z, w1[u][h].z, w0[u][h].w, w1[u][h].w, x.z, x.w);
+                    const uint4 v = x[u][m][h];
+                    mma_e4m3_16x8x32(c, w0[u][h].x, w1[u][h].x, w0[u][h].y, w1[u][h].y, v.x, v.y);
+                    mma_e4m3_16x8x32(c, w0[u][h].z, w1[u][h].z, w0[u][h].w, w1[u][h].w, v.z, v.w);
                 }
-                // this lane's sums: rows g and g + 8 of B, rows 2 q and 2 q + 1 of A (the scales reach to 128 rows)
-                const float2 sa = *reinterpret_cast<const float2*>(p.a_scales + t * p.pitch_a + m * 8 + 2 * q);
-                acc[m][0] = fmaf(c[0], sa.x * sb0, acc[m][0]);
-                acc[m][1] = fmaf(c[1], sa.y * sb0, acc[m][1]);
-                acc[m][2] = fmaf(c[2], sa.x * sb1, acc[m][2]);
-                acc[m][3] = fmaf(c[3], sa.y * sb1, acc[m][3]);
+                // this lane's sums: rows g and g + 8 of B, rows 2 q and 2 q + 1 of A
+                acc[m][0] = fmaf(c[0], sa[u][m].x * sb0[u], acc[m][0]);
+                acc[m][1] = fmaf(c[1], sa[u][m].y * sb0[u], acc[m][1]);
+                acc[m][2] = fmaf(c[2], sa[u][m].x * sb1[u], acc[m][2]);
+                acc[m][3] = fmaf(c[3], sa[u][m].y * sb1[u], acc[m][3]);
             }
-        }
     }
 #pragma unroll
     for (int m = 0; m < TILES; ++m)
