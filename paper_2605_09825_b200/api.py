@@ -566,10 +566,10 @@ def quantize_block128(src: torch.Tensor, axis: int = AXIS_COLS, block_shape: int
     if need == 0:
         _raise(-2 if block_shape in (BLOCK_1X128, BLOCK_128X128) else -4, "mxfp4_quantize_block128")
     if codes is None:
-        codes = torch.empty((outer, K), dtype=torch.uint8, device=src.device)
+        codes = torch.empty(outer, K, dtype=torch.uint8, device=src.device)
     if scales is None:
         blocks = -(-K // 128)
-        scales = torch.empty((blocks, need // blocks), dtype=torch.float32, device=src.device)
+        scales = torch.empty(blocks, need // blocks, dtype=torch.float32, device=src.device)
     rc = load_library().mxfp4_quantize_block128(ptr, rows, cols, ld, axis, block_shape,
                                                 _expect(codes, "codes", torch.uint8, outer * K),
                                                 _expect(scales, "scales", torch.float32, need), _raw_stream())
@@ -591,8 +591,10 @@ def gemm_block128(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     if a_need == 0 or b_need == 0:
         _raise(-2 if b_block_shape in (BLOCK_1X128, BLOCK_128X128) else -4, "mxfp4_gemm_block128")
     lib = load_library()
-    out = _out_tensor((M, N), out_dtype, a_codes.device, out)
-    if out.dtype != (torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32) or out.shape != (M, N):
+    dtype = torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32
+    if out is None:
+        out = torch.empty(M, N, dtype=dtype, device=a_codes.device)
+    elif out.dtype != dtype or out.shape != (M, N):
         raise ValueError("out must be [M, N] of the output type")
     out_ptr, ld_out = _matrix(out, "out", (out.dtype,))
     ws_ptr = ws_bytes = 0
@@ -684,13 +686,13 @@ def residual_norm_forward(branch, stream=None, w_post=None, w_pre=None, gate=Non
     d = _norm_desc(branch, stream, _STREAM_TYPES[dtype], w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps)
     shape = branch.shape
     if y is None:
-        y = torch.empty(shape, dtype=dtype, device=branch.device)
+        y = torch.empty(*shape, dtype=dtype, device=branch.device)
     elif y.shape != shape:
         raise ValueError("y must have the branch's shape")
     y_ptr, ld_y = _matrix(y, "y", (dtype,))
     h_ptr, ld_h = None, 0
     if h is None and w_pre is not None:
-        h = torch.empty(shape, dtype=torch.bfloat16, device=branch.device)
+        h = torch.empty(*shape, dtype=torch.bfloat16, device=branch.device)
     if h is not None:
         if h.shape != shape:
             raise ValueError("h must have the branch's shape")
@@ -714,9 +716,9 @@ def residual_norm_backward(dh, dy, branch, y, w_post=None, w_pre=None, gate=None
     d = _norm_desc(branch, y, _STREAM_TYPES[dtype], w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps)
     tokens, width = shape
     if dstream is None:
-        dstream = torch.empty(shape, dtype=dtype, device=dev)
+        dstream = torch.empty(*shape, dtype=dtype, device=dev)
     if dbranch is None:
-        dbranch = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        dbranch = torch.empty(*shape, dtype=torch.bfloat16, device=dev)
 
     def part(t, name, kinds):
         if t is None:
@@ -729,7 +731,7 @@ def residual_norm_backward(dh, dy, branch, y, w_post=None, w_pre=None, gate=None
     vector = lambda wanted: torch.empty(width, dtype=torch.float32, device=dev) if wanted else None
     dw_post, dw_pre, dgate = vector(w_post is not None), vector(w_pre is not None), vector(channel)
     if gate is not None and not channel:
-        dgate = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        dgate = torch.empty(*shape, dtype=torch.bfloat16, device=dev)
     lib = load_library()
     if workspace is None and (dw_post is not None or dw_pre is not None or channel):
         workspace = torch.empty(max(lib.mxfp4_residual_norm_workspace_bytes(tokens, width), 1), dtype=torch.uint8,
@@ -761,7 +763,7 @@ def logprobs_forward(logits, targets=None, top_k: int = 0, scale: float = 1.0, w
     ptr, dtype, tokens, vocab, ld = _logits(logits)
     lib = load_library()
     dev = logits.device
-    logp, entropy, lse = torch.empty((3, tokens), dtype=torch.float32, device=dev).unbind(0)
+    logp, entropy, lse = torch.empty(3, tokens, dtype=torch.float32, device=dev).unbind(0)
     row_ptr = logp.data_ptr()
     t_ptr = logp_ptr = None
     if targets is not None:
@@ -770,8 +772,8 @@ def logprobs_forward(logits, targets=None, top_k: int = 0, scale: float = 1.0, w
         logp = None
     top_logp = top_index = v_ptr = i_ptr = ws_ptr = None
     if top_k > 0:
-        top_logp = torch.empty((tokens, top_k), dtype=torch.float32, device=dev)
-        top_index = torch.empty((tokens, top_k), dtype=torch.int64, device=dev)
+        top_logp = torch.empty(tokens, top_k, dtype=torch.float32, device=dev)
+        top_index = torch.empty(tokens, top_k, dtype=torch.int64, device=dev)
         v_ptr, i_ptr = top_logp.data_ptr(), top_index.data_ptr()
     ws_bytes = 0
     if workspace is None:
@@ -794,7 +796,7 @@ def logprobs_backward(logits, targets, lse, entropy=None, d_logp=None, d_entropy
     the logits themselves."""
     ptr, dtype, tokens, vocab, ld = _logits(logits)
     if dlogits is None:
-        dlogits = torch.empty((tokens, vocab), dtype=logits.dtype, device=logits.device)
+        dlogits = torch.empty(tokens, vocab, dtype=logits.dtype, device=logits.device)
     if dlogits.shape != logits.shape:
         raise ValueError("dlogits must have the logits' shape")
     d_ptr, ld_d = _matrix(dlogits, "dlogits", (logits.dtype,))
