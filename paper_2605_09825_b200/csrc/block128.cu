@@ -21,19 +21,9 @@ constexpr int kB128SplitPairs = 74;
 
 static int64_t blocks_of(int64_t n) { return (n + kB128 - 1) / kB128; }
 
-static int quantize128_checked(const void* src, int64_t rows, int64_t cols, int64_t ld, int axis, int block_shape,
-                               void* codes, void* scales, cudaStream_t st)
+static Quant128Params quantize128_params(const void* src, int64_t rows, int64_t cols, int64_t ld, int axis, bool square,
+                                         void* codes, void* scales)
 {
-    if (!src || !codes || !scales) return MXFP4_ERR_NULL;
-    if (axis != MXFP4_AXIS_ROWS && axis != MXFP4_AXIS_COLS) return MXFP4_ERR_ENUM;
-    if (block_shape != MXFP4_BLOCK_1X128 && block_shape != MXFP4_BLOCK_128X128) return MXFP4_ERR_ENUM;
-    if (rows <= 0 || cols <= 0 || ld < cols) return MXFP4_ERR_SHAPE;
-    if ((axis == MXFP4_AXIS_COLS ? cols : rows) % 16 != 0) return MXFP4_ERR_SHAPE;
-    if (rows > 0x7FFFFF00 || cols > 0x7FFFFF00 || blocks_of(rows) * blocks_of(cols) > 0x3FFFFFFF) return MXFP4_ERR_SHAPE;
-    if (!aligned16(src) || !aligned16(codes) || !aligned16(scales) || ld % 8 != 0) return MXFP4_ERR_ALIGN;
-    const int rc = device_status_code(device_info());
-    if (rc != MXFP4_OK) return rc;
-    const bool square = block_shape == MXFP4_BLOCK_128X128;
     Quant128Params p;
     p.src = static_cast<const __nv_bfloat16*>(src);
     p.codes = static_cast<uint8_t*>(codes);
@@ -44,16 +34,10 @@ static int quantize128_checked(const void* src, int64_t rows, int64_t cols, int6
     p.tiles_c = static_cast<int32_t>(blocks_of(cols));
     const int64_t outer = axis == MXFP4_AXIS_COLS ? rows : cols;
     p.pitch = static_cast<int32_t>(square ? blocks_of(outer) : blocks_of(outer) * kB128);
-    const int grid = static_cast<int>(blocks_of(rows) * blocks_of(cols));
-    cudaError_t e;
-    if (axis == MXFP4_AXIS_COLS)
-        e = square ? launch_kernel_pdl(quantize_block128_kernel<1, true>, grid, kB128Threads, 0, st, p)
-                   : launch_kernel_pdl(quantize_block128_kernel<1, false>, grid, kB128Threads, 0, st, p);
-    else
-        e = square ? launch_kernel_pdl(quantize_block128_kernel<0, true>, grid, kB128Threads, 0, st, p)
-                   : launch_kernel_pdl(quantize_block128_kernel<0, false>, grid, kB128Threads, 0, st, p);
-    return e == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
+    return p;
 }
+
+static int64_t quantize128_tiles(int64_t rows, int64_t cols) { return blocks_of(rows) * blocks_of(cols); }
 
 static int64_t gemm128_tiles(int64_t M, int64_t N) { return ((M + kBTile - 1) / kBTile) * ((N + kBTile - 1) / kBTile); }
 
@@ -260,8 +244,23 @@ size_t mxfp4_block128_scales_bytes(int64_t outer, int64_t K, int block_shape)
 int mxfp4_quantize_block128(const void* src_bf16, int64_t rows, int64_t cols, int64_t ld_src, int axis,
                             int block_shape, void* codes, void* scales, void* stream)
 {
-    return quantize128_checked(src_bf16, rows, cols, ld_src, axis, block_shape, codes, scales,
-                               static_cast<cudaStream_t>(stream));
+    if (!src_bf16 || !codes || !scales) return MXFP4_ERR_NULL;
+    if (axis != MXFP4_AXIS_ROWS && axis != MXFP4_AXIS_COLS) return MXFP4_ERR_ENUM;
+    if (block_shape != MXFP4_BLOCK_1X128 && block_shape != MXFP4_BLOCK_128X128) return MXFP4_ERR_ENUM;
+    if (rows <= 0 || cols <= 0 || ld_src < cols) return MXFP4_ERR_SHAPE;
+    if ((axis == MXFP4_AXIS_COLS ? cols : rows) % 16 != 0) return MXFP4_ERR_SHAPE;
+    if (rows > 0x7FFFFF00 || cols > 0x7FFFFF00 || quantize128_tiles(rows, cols) > 0x3FFFFFFF) return MXFP4_ERR_SHAPE;
+    if (!aligned16(src_bf16) || !aligned16(codes) || !aligned16(scales) || ld_src % 8 != 0) return MXFP4_ERR_ALIGN;
+    const int rc = device_status_code(device_info());
+    if (rc != MXFP4_OK) return rc;
+    const bool square = block_shape == MXFP4_BLOCK_128X128;
+    const Quant128Params p = quantize128_params(src_bf16, rows, cols, ld_src, axis, square, codes, scales);
+    const int grid = static_cast<int>(quantize128_tiles(rows, cols));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    auto kernel = axis == MXFP4_AXIS_COLS
+                      ? (square ? quantize_block128_kernel<1, true> : quantize_block128_kernel<1, false>)
+                      : (square ? quantize_block128_kernel<0, true> : quantize_block128_kernel<0, false>);
+    return launch_kernel_pdl(kernel, grid, kB128Threads, 0, st, p) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
 size_t mxfp4_gemm_block128_workspace_bytes(int64_t M, int64_t N, int64_t K)
@@ -317,8 +316,8 @@ int mxfp4_linear_pass_block128(int pass, const void* a, const void* b, void* out
     const Pass128 q = pass128(pass, T, in_features, out_features);
     int rc = gemm128_shape_ok(q.M, q.N, q.K);
     if (rc != MXFP4_OK) return rc;
-    if (blocks_of(q.ar) * blocks_of(q.ac) > 0x3FFFFFFF || blocks_of(q.br) * blocks_of(q.bc) > 0x3FFFFFFF)
-        return MXFP4_ERR_SHAPE;
+    const int64_t a_tiles = quantize128_tiles(q.ar, q.ac), b_tiles = quantize128_tiles(q.br, q.bc);
+    if (a_tiles > 0x3FFFFFFF || b_tiles > 0x3FFFFFFF) return MXFP4_ERR_SHAPE;
     const size_t need = mxfp4_linear_pass_block128_workspace_bytes(T, in_features, out_features, pass);
     if (!workspace || workspace_bytes < need) return MXFP4_ERR_WORKSPACE;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) || !aligned16(a) || !aligned16(b) || !aligned16(out))
@@ -331,10 +330,16 @@ int mxfp4_linear_pass_block128(int pass, const void* a, const void* b, void* out
     uint8_t* b_codes = a_scales + round_up(mxfp4_block128_scales_bytes(q.M, q.K, MXFP4_BLOCK_1X128), 256);
     uint8_t* b_scales = b_codes + round_up(static_cast<size_t>(q.N) * q.K, 256);
     uint8_t* parts = b_scales + round_up(mxfp4_block128_scales_bytes(q.N, q.K, q.b_shape), 256);
-    rc = quantize128_checked(a, q.ar, q.ac, q.ac, q.a_axis, MXFP4_BLOCK_1X128, a_codes, a_scales, st);
-    if (rc != MXFP4_OK) return rc;
-    rc = quantize128_checked(b, q.br, q.bc, q.bc, q.b_axis, q.b_shape, b_codes, b_scales, st);
-    if (rc != MXFP4_OK) return rc;
+    // every reduction size is a multiple of 16 by now: one launch quantizes both operands
+    const bool square = q.b_shape == MXFP4_BLOCK_128X128;
+    const Quant128Params pa = quantize128_params(a, q.ar, q.ac, q.ac, q.a_axis, false, a_codes, a_scales);
+    const Quant128Params pb = quantize128_params(b, q.br, q.bc, q.bc, q.b_axis, square, b_codes, b_scales);
+    auto kernel = pass == MXFP4_PASS_FPROP ? quantize_block128_both_kernel<1, 1, true>
+                  : pass == MXFP4_PASS_DGRAD ? quantize_block128_both_kernel<1, 0, true>
+                                             : quantize_block128_both_kernel<0, 0, false>;
+    if (launch_kernel_pdl(kernel, static_cast<int>(a_tiles + b_tiles), kB128Threads, 0, st, pa, pb,
+                          static_cast<int>(a_tiles)) != cudaSuccess)
+        return MXFP4_ERR_CUDA;
     return gemm128_launch(a_codes, a_scales, b_codes, b_scales, q.b_shape == MXFP4_BLOCK_1X128, q.M, q.N, q.K, out,
                           out_dtype, q.N, parts, dev.sm_count, st);
 }

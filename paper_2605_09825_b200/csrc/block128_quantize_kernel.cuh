@@ -9,10 +9,10 @@
 // staged in shared memory (word index XOR-ed with the column group: no bank conflicts either way)
 // and written as 16-byte pieces of 128-byte operand rows.
 //
-// Bound by memory, 3 bytes per element: 8192 x 14336 in 60 to 68 us by itself (5.2 to 5.9 TB/s; three CTAs per SM
-// and maxima in fp32: 64 to 79 us), 8192 x 4096 in 23 to 27 us.  Maxima are kept as pairs of 16-bit words
-// and the maxima of two rows share a shuffle: the instructions per element, not the loads in flight,
-// kept the row-wise form behind the square one.
+// Bound by memory, 3 bytes per element: 8192 x 14336 in 57 (square), 59 (row-wise) and 64 us (transposed) by itself, 5.5
+// to 6.1 TB/s; 8192 x 4096 in 23 to 25 us.  What was in the way was the number of instructions per element:
+// maxima in fp32, a division per row in each of its sixteen lanes and three CTAs per SM took 64, 79 and 70 us.
+// Now maxima are pairs of 16-bit words, two rows share a shuffle, and each lane divides for one row.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -81,16 +81,14 @@ __device__ __forceinline__ uint2 piece_codes(const uint4& w, float inv)
 
 // AXIS 1: operand row = source row; AXIS 0: operand row = source column.  SQUARE: 128 x 128 blocks.
 template <int AXIS, bool SQUARE>
-__global__ void __launch_bounds__(kB128Threads, kB128Ctas) quantize_block128_kernel(const Quant128Params p)
+__device__ __forceinline__ void quantize_block128_tile(const Quant128Params& p, int tile)
 {
     __shared__ __align__(16) uint8_t codes_t[AXIS == 0 ? kB128 * kB128 : 16];      // [source column][source row]
     __shared__ __align__(16) uint32_t part[AXIS == 0 && !SQUARE ? 16 * kB128 / 2 : 16];    // maxima
     __shared__ __align__(16) float inverse[AXIS == 0 && !SQUARE ? kB128 : 4];              // 448 / maximum, per column
-    griddep_launch_dependents();
-    griddep_wait();
     const int tid = threadIdx.x;
     const int cg = tid & 15, rg = tid >> 4;              // column group of 8, row group
-    const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x % p.tiles_c;
+    const int tr = tile / p.tiles_c, tc = tile % p.tiles_c;
     const int row0 = tr * kB128, col0 = tc * kB128;
     // row-wise: rows rg, rg + 16, ...; transposed: rows 8 * rg ... 8 * rg + 7
     auto row_of = [&](int i) { return AXIS == 1 ? rg + 16 * i : 8 * rg + i; };
@@ -120,21 +118,25 @@ __global__ void __launch_bounds__(kB128Threads, kB128Ctas) quantize_block128_ker
             w[i].y = c.y;
         }
     } else if (AXIS == 1) {
+        // two rows' maxima travel in one word; lane cg of a row's sixteen keeps the one of row cg (mod 8) and divides for it
+        uint32_t mine = 0;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            // two rows' maxima travel in one word
             uint32_t m = fold(piece_amax(w[i])) | (fold(piece_amax(w[i + 1])) << 16);
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if ((cg & 6) == i) mine = (cg & 1) ? m >> 16 : m & 0xFFFFu;
+        }
+        const float amax = magnitude(mine), inv = block_inverse(amax);
+        if (cg < 8) {
+            const int row = row0 + row_of(cg);
+            p.scales[static_cast<int64_t>(tc) * p.pitch + row] = row < p.rows ? block_scale(amax) : 0.0f;
+        }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float amax = magnitude(j ? m >> 16 : m & 0xFFFFu);
-                const int row = row0 + row_of(i + j);
-                if (cg == 0) p.scales[static_cast<int64_t>(tc) * p.pitch + row] = row < p.rows ? block_scale(amax) : 0.0f;
-                const uint2 c = piece_codes(w[i + j], block_inverse(amax));
-                w[i + j].x = c.x;
-                w[i + j].y = c.y;
-            }
+        for (int i = 0; i < 8; ++i) {
+            const uint2 c = piece_codes(w[i], __shfl_sync(0xffffffffu, inv, i, 16));
+            w[i].x = c.x;
+            w[i].y = c.y;
         }
     } else {
         // maximum of each column: this thread's eight rows, then the sixteen row groups
@@ -210,6 +212,27 @@ __global__ void __launch_bounds__(kB128Threads, kB128Ctas) quantize_block128_ker
                 *reinterpret_cast<uint4*>(p.codes + static_cast<int64_t>(o) * p.rows + k) = make_uint4(lo.x, lo.y, hi.x, hi.y);
         }
     }
+}
+
+template <int AXIS, bool SQUARE>
+__global__ void __launch_bounds__(kB128Threads, kB128Ctas)
+quantize_block128_kernel(const Quant128Params p)
+{
+    griddep_launch_dependents();
+    griddep_wait();
+    quantize_block128_tile<AXIS, SQUARE>(p, blockIdx.x);
+}
+
+// Both operands of a linear's pass in one launch: 1 x 128 blocks of a, then b.
+template <int AXIS_A, int AXIS_B, bool SQUARE_B>
+__global__ void __launch_bounds__(kB128Threads, kB128Ctas)
+quantize_block128_both_kernel(const __grid_constant__ Quant128Params a, const __grid_constant__ Quant128Params b, int a_tiles)
+{
+    griddep_launch_dependents();
+    griddep_wait();
+    const int tile = blockIdx.x;
+    if (tile < a_tiles) quantize_block128_tile<AXIS_A, false>(a, tile);
+    else quantize_block128_tile<AXIS_B, SQUARE_B>(b, tile - a_tiles);
 }
 
 }  // namespace mxfp4
