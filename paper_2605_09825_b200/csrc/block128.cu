@@ -46,9 +46,10 @@ static int64_t gemm128_tiles(int64_t M, int64_t N) { return ((M + kBTile - 1) / 
 static bool gemm128_few_rows(int64_t M) { return M <= 8 * kRowsMaxTiles; }
 
 // Which tiles are split along K, and into how many pieces: those that do not fill a wave of the pairs, into as
-// many pieces as fit the wave, with at least four K-steps in each.  Not below 16 K-steps, where the second
-// kernel takes what the shorter wave gives (333 x 28672 x 1024: 24 us whole, 26 us split; with K 4096: 84 us
-// whole, 71 us split; 40 x 4096 x 2048: 15 us in two pieces, 10 us in four).
+// many pieces as fit the wave, with at least four K-steps in each -- where that makes the wave at least 12 K-steps
+// shorter, which is what the second kernel and the traffic of the sums cost: 4096 x 4096 x 2048 in two pieces (8
+// K-steps less) 44 us, whole 41 us; 333 x 28672 x 1024 (4 less) 26 and 24 us; 4096 x 4096 x 4096 with a
+// scale per row (16 less) 93.5 and 95.6 us; 333 x 28672 x 4096 (28 less) 71 and 84 us.
 struct Split128 {
     int64_t whole;               // tiles of one piece
     int64_t split;               // tiles after them
@@ -61,7 +62,7 @@ static Split128 gemm128_split(int64_t M, int64_t N, int64_t K)
     const int64_t left = tiles % kB128SplitPairs;
     int64_t pieces = left > 0 ? kB128SplitPairs / left : 1;
     if (pieces > steps / 4) pieces = steps / 4;
-    if (gemm128_few_rows(M) || steps < 16 || pieces < 2) return {tiles, 0, 1};
+    if (gemm128_few_rows(M) || pieces < 2 || steps - steps / pieces < 12) return {tiles, 0, 1};
     return {tiles - left, left, pieces};
 }
 
