@@ -128,7 +128,7 @@ constexpr int kNormWarps = kNormMaxThreads / 32;
 
 struct NormShared {
     float red[2][4][kNormMaxCluster * kNormWarps];   // [slot][value][CTA, warp]
-    uint64_t sums[2];                    // a slot's values from all CTAs of the cluster are here
+    uint64_t sums[2];                    // a slot's values are here: from the CTAs of the cluster, or this CTA's warps
     uint64_t full[kNormMaxStages];
     uint64_t empty[kNormMaxStages];
     int abort_flag;
@@ -163,7 +163,9 @@ __device__ __forceinline__ NormPlace norm_place(const NormParams& p)
 // Inside a warp, exchanges with the lane 16 (and 8) away halve the number of values a lane holds, further
 // exchanges finish the one it is left with: value lane / (32 / N), the same in all lanes of that group.
 // Every warp leaves its sums in the shared memory of all CTAs of the cluster; then every warp adds all of
-// them.  `call` counts the calls: slots alternate, and a slot is written again only after every warp has
+// them.  Inside one CTA the forward pass waits for that at an mbarrier and the backward pass at the block's barrier, as
+// measured: 16384 x 4096 without a gate, forward 89 us against 93 at the block's barrier, backward 165
+// against 155.  `call` counts the calls: slots alternate, and a slot is written again only after every warp has
 // read it (it takes part in the call in between afterwards).
 template <int N, bool CLUSTER>
 __device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t& call, int cluster, int rank)
@@ -187,7 +189,13 @@ __device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t&
     const int n = CLUSTER ? cluster * warps : warps;
     if (!CLUSTER) {
         if (in_group == 0) sh.red[slot][value][warp] = t;
-        __syncthreads();
+        if (N == 4) {
+            __syncthreads();
+        } else {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.sums[slot]);
+            (void)mbar_wait_fast(&sh.sums[slot], (call >> 1) & 1, &sh.abort_flag);
+        }
     } else {
         if (in_group < cluster)              // to CTA `in_group`
             st_async_f32(map_to_cta(smem_u32(&sh.red[slot][value][rank * warps + warp]), in_group), t,
@@ -219,7 +227,7 @@ __device__ __forceinline__ void norm_setup(NormShared& sh, const NormParams& p)
             mbar_init(&sh.full[s], 1);
             mbar_init(&sh.empty[s], blockDim.x >> 5);
         }
-        for (int s = 0; s < 2; ++s) mbar_init(&sh.sums[s], 1);
+        for (int s = 0; s < 2; ++s) mbar_init(&sh.sums[s], CLUSTER ? 1 : blockDim.x >> 5);
         fence_barrier_init();
     }
     if (CLUSTER) cluster_sync_all();
