@@ -11,7 +11,9 @@
 // flight per SM.  1 x 4096 x 14336: 13.4 us (58.7 MB, 4.4 TB/s, with two launches' worth of latency in it),
 // 1 x 128256 x 4096: 92 us (5.7 TB/s); 16 rows: 16.8 and 120 us, the rows of A coming from L2 once per CTA.
 // Scales loaded where they are used: 14.0 and 98.6 us; four K-blocks in flight: 13.8 and 86 us, but 15.2
-// and 103 with a scale per row of B and 138 with 16 rows (registers); three or four CTAs per SM spill.
+// and 103 with a scale per row of B and 138 with 16 rows (registers); three or four CTAs per SM spill; 32 rows of B
+// per CTA: 20 and 88 us; a persistent grid with a ring of asynchronous copies in shared memory: 17 to 25 and
+// 101 to 127 us.
 #pragma once
 
 #include <cuda_bf16.h>
