@@ -277,3 +277,17 @@ def test_calls_repeat_bit_for_bit_and_follow_their_stream():
         got = [api.logprobs_forward(x, t, 20) for _ in range(3)]
     side.synchronize()
     assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("tokens", [2, 700])
+def test_scaled_logits_below_the_range_keep_their_place(tokens):
+    """Finite logits whose scaled value is below fp32's range have probability 0 but stay alternatives; a row of nothing
+    else counts as masked entirely."""
+    low = torch.finfo(torch.float32).min
+    x = torch.full((tokens, 40), low, device="cuda")
+    x[::2, 7], x[::2, 9], x[:, 3] = 1.0, 0.0, float("-inf")
+    logp, entropy, lse, top_logp, top_index = api.logprobs_forward(x, None, 4, 2.0)
+    api.check()
+    assert (top_index[::2] == torch.tensor([7, 9, 0, 1], device="cuda")).all()
+    assert torch.isinf(top_logp[::2, 2:]).all() and torch.isfinite(top_logp[::2, :2]).all()
+    assert (top_index[1::2] == -1).all() and (lse[1::2] == float("-inf")).all() and (entropy[1::2] == 0).all()
