@@ -227,7 +227,8 @@ __device__ __forceinline__ float finish_row(const LogprobsParams& p, int64_t row
     const float log_s = kLn2 * log2f(v.s);
     const float lse = v.m == -INFINITY ? v.s : fmaf(v.m, p.scale, log_s);
     p.lse[row] = lse;
-    if (p.entropy) p.entropy[row] = v.m == -INFINITY ? v.s : log_s - kLn2 * (v.a / v.s);
+    // (no logit's z reached fp32's range: a row masked entirely)
+    if (p.entropy) p.entropy[row] = v.m == -INFINITY ? v.s : lse == -INFINITY ? 0.0f : log_s - kLn2 * (v.a / v.s);
     return lse;
 }
 
