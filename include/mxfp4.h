@@ -495,7 +495,7 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
  * have are (-infinity, -1).  A row masked entirely has lse -infinity, logp -infinity, entropy 0 and
  * a zero gradient.  A finite logit whose z is below fp32's range has probability 0 and log
  * probability -infinity and keeps its place among the alternatives; a row of nothing else counts as
- * masked entirely.  A NaN or +infinity makes its row's results NaN (index -1).
+ * masked entirely.  A NaN, +infinity or z above the range makes its row's results NaN (index -1).
  *
  * lse is an fp32 number: where it is beyond about 2^20 in magnitude (a row of the type's lowest value,
  * say) it no longer resolves the row's probabilities, which the backward pass takes from it; logp,

@@ -225,10 +225,11 @@ __device__ __forceinline__ float finish_row(const LogprobsParams& p, int64_t row
         return -INFINITY;
     }
     const float log_s = kLn2 * log2f(v.s);
-    const float lse = v.m == -INFINITY ? v.s : fmaf(v.m, p.scale, log_s);
+    float lse = v.m == -INFINITY ? v.s : fmaf(v.m, p.scale, log_s);
+    if (lse == INFINITY) lse = NAN;                  // a z above fp32's range counts as an infinite logit
     p.lse[row] = lse;
-    // (no logit's z reached fp32's range: a row masked entirely)
-    if (p.entropy) p.entropy[row] = v.m == -INFINITY ? v.s : lse == -INFINITY ? 0.0f : log_s - kLn2 * (v.a / v.s);
+    // all z below the range: a row masked entirely
+    if (p.entropy) p.entropy[row] = lse != lse ? lse : lse == -INFINITY ? 0.0f : log_s - kLn2 * (v.a / v.s);
     return lse;
 }
 

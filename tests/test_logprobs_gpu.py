@@ -291,3 +291,15 @@ def test_scaled_logits_below_the_range_keep_their_place(tokens):
     assert (top_index[::2] == torch.tensor([7, 9, 0, 1], device="cuda")).all()
     assert torch.isinf(top_logp[::2, 2:]).all() and torch.isfinite(top_logp[::2, :2]).all()
     assert (top_index[1::2] == -1).all() and (lse[1::2] == float("-inf")).all() and (entropy[1::2] == 0).all()
+
+
+@pytest.mark.parametrize("tokens", [2, 700])
+def test_scaled_logits_above_the_range_poison_their_row_alone(tokens):
+    x = torch.zeros((tokens, 40), device="cuda")
+    x[::2, 5] = torch.finfo(torch.float32).max
+    targets = torch.full((tokens,), 5, device="cuda")
+    logp, entropy, lse, top_logp, top_index = api.logprobs_forward(x, targets, 3, 2.0)
+    api.check()
+    for v in (logp, entropy, lse, top_logp):
+        assert torch.isnan(v[::2]).all() and torch.isfinite(v[1::2]).all()
+    assert (top_index[::2] == -1).all() and (top_index[1::2] == torch.arange(3, device="cuda")).all()
