@@ -497,9 +497,10 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
  * probability -infinity and keeps its place among the alternatives; a row of nothing else counts as
  * masked entirely.  A NaN, +infinity or z above the range makes its row's results NaN (index -1).
  *
- * lse is an fp32 number: where it is beyond about 2^20 in magnitude (a row of the type's lowest value,
- * say) it no longer resolves the row's probabilities, which the backward pass takes from it; logp,
- * entropy and the alternatives' order do not depend on that.
+ * logp, top_logp and entropy are formed from differences to a logit of the row, so a common offset of the
+ * row's logits does not cost them accuracy.  lse is an fp32 number, and the backward pass takes the row's
+ * probabilities from it, as exp(z - lse), with a relative error of up to 2^-24 * |lse|: 6 % at 2^20,
+ * and beyond about 2^23 (a row of the type's lowest value, say) log vocab is lost in it altogether.
  *
  * Backward: dlogits[t][i] = scale * (d_logp[t] * (delta(i, target) - p_i)
  *                                    - d_entropy[t] * p_i * (z_i - lse + entropy[t]))

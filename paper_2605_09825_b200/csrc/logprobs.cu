@@ -4,7 +4,7 @@
 // Forward: one pass over the logits.  A thread keeps a reference m, S = sum 2^a and A = sum a 2^a
 // with a = (x - m) * scale * log2(e) over its vectors; at the end the CTA brings all threads to a
 // common m, and then
-//     lse = scale * m + ln S,   entropy = ln S - ln 2 * A / S.
+//     lse = scale * m + ln S,   logp = (x - m) * scale - ln S,   entropy = ln S - ln 2 * A / S.
 // The reference is the thread's first maximum and moves only when a later one is more than a factor
 // of 2^8 above it, so the sums are hardly ever rescaled on the way (a running maximum would make
 // some lane of a warp rescale at most vectors), and what the late step back to a common
@@ -216,13 +216,28 @@ __device__ __forceinline__ SoftSums block_join(SoftSums v, float c, SoftSums* re
     return warp_join(v, c);
 }
 
+// What a row's log probabilities are formed from: z - lse = (x - m) * scale - ln S.  The rounded lse itself will not do:
+// far from zero its last bit is worth more than ln S.
+struct RowNorm {
+    float lse, m, log_s;
+};
+
+__device__ __forceinline__ float log_prob(const RowNorm& n, float x, float scale)
+{
+    if (n.lse != n.lse) return NAN;
+    if (n.lse == -INFINITY || x * scale == -INFINITY) return -INFINITY;
+    const float d = x - n.m;
+    // a difference past fp32's range between two logits whose z are in it: both are far too large for ln S to count
+    return fabsf(d) < INFINITY ? fmaf(d, scale, -n.log_s) : fmaf(x, scale, -n.lse);
+}
+
 // Row results of one thread.
-__device__ __forceinline__ float finish_row(const LogprobsParams& p, int64_t row, const SoftSums& v)
+__device__ __forceinline__ RowNorm finish_row(const LogprobsParams& p, int64_t row, const SoftSums& v)
 {
     if (v.m == -INFINITY && v.s == 0.0f) {           // nothing but masked logits
         p.lse[row] = -INFINITY;
         if (p.entropy) p.entropy[row] = 0.0f;
-        return -INFINITY;
+        return {-INFINITY, 0.0f, 0.0f};
     }
     const float log_s = kLn2 * log2f(v.s);
     float lse = v.m == -INFINITY ? v.s : fmaf(v.m, p.scale, log_s);
@@ -230,30 +245,26 @@ __device__ __forceinline__ float finish_row(const LogprobsParams& p, int64_t row
     p.lse[row] = lse;
     // all z below the range: a row masked entirely
     if (p.entropy) p.entropy[row] = lse != lse ? lse : lse == -INFINITY ? 0.0f : log_s - kLn2 * (v.a / v.s);
-    return lse;
+    return {lse, v.m, log_s};
 }
 
 template <class T>
-__device__ __forceinline__ void finish_target(const LogprobsParams& p, int64_t row, float lse)
+__device__ __forceinline__ void finish_target(const LogprobsParams& p, int64_t row, const RowNorm& norm)
 {
     if (!p.logp) return;
     const int64_t t = p.targets[row];
     float r = 0.0f;
-    if (t >= p.vocab) {
-        r = NAN;
-    } else if (t >= 0) {
-        const float x = LogitVec<T>::one(static_cast<const T*>(p.logits) + row * p.ld + t);
-        r = lse == -INFINITY ? -INFINITY : fmaf(x, p.scale, -lse);
-    }
+    if (t >= p.vocab) r = NAN;
+    else if (t >= 0) r = log_prob(norm, LogitVec<T>::one(static_cast<const T*>(p.logits) + row * p.ld + t), p.scale);
     p.logp[row] = r;
 }
 
-__device__ __forceinline__ void write_top(const LogprobsParams& p, int64_t row, int rank, uint64_t key, float lse)
+__device__ __forceinline__ void write_top(const LogprobsParams& p, int64_t row, int rank, uint64_t key, const RowNorm& norm)
 {
     const int64_t at = row * p.top_k + rank;
-    const bool bad = lse != lse;
+    const bool bad = norm.lse != norm.lse;
     const bool none = bad || key == 0ull;
-    p.top_logp[at] = bad ? NAN : none ? -INFINITY : fmaf(key_value(static_cast<uint32_t>(key >> 32)), p.scale, -lse);
+    p.top_logp[at] = bad ? NAN : none ? -INFINITY : log_prob(norm, key_value(static_cast<uint32_t>(key >> 32)), p.scale);
     p.top_index[at] = none ? -1 : static_cast<int64_t>(0xFFFFFFFFu - static_cast<uint32_t>(key));
 }
 
@@ -271,6 +282,8 @@ struct TopScratch {
     uint32_t groups[kLpHits];  // first vectors of groups that do
     int32_t owner[kLpMaxTop];
     int32_t n, n_hits, n_groups;
+    RowNorm norm;              // of the row at hand (in registers it would cost the alternatives spills)
+    uint64_t top[kLpMaxTop];   // its alternatives
 };
 
 struct TopBound {
@@ -372,14 +385,15 @@ __device__ __forceinline__ RowPart<T> row_part(const LogprobsParams& p, int64_t 
     return r;
 }
 
-// The part's `top_k` best keys; `emit(rank, key)` is called once for every rank that exists.  One warp.
-template <class T, class Emit>
-__device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, const RowNotes<true>& notes, TopScratch& sc, Emit emit)
+// The part's `top_k` best keys, in the scratch's `top`; 0 for ranks that do not exist.  One warp.
+template <class T>
+__device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, const RowNotes<true>& notes, TopScratch& sc)
 {
     constexpr int kN = LogitVec<T>::kN;
     const int lane = threadIdx.x & 31;
     const TopBound bound = pick_owners<T>(notes, sc, top_k, part.first + part.count);
     if (lane == 0) sc.n = sc.n_hits = sc.n_groups = 0;
+    sc.top[lane] = 0ull;
     __syncwarp();
     auto take = [&](float x, uint32_t index) {
         const uint64_t k = full_key(x, index);
@@ -445,7 +459,7 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
             const uint64_t k = sc.keys[i];
             int rank = 0;
             for (int j = 0; j < n; ++j) rank += sc.keys[j] > k;
-            if (rank < top_k) emit(rank, k);
+            if (rank < top_k) sc.top[rank] = k;
         }
     } else {
         // hundreds of vectors reach the bound: rank after rank, each from the whole part
@@ -471,7 +485,7 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
                 if (other > mine) mine = other;
             }
             last = mine;
-            if (lane == 0 && last) emit(rank, last);
+            if (lane == 0) sc.top[rank] = last;
         }
     }
     __syncwarp();
@@ -535,26 +549,22 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
             // (with scales beyond these, -10^30 times c is not far below everything, or not a number)
             if (!(fabsf(sums.m) * c < kLpHuge) || c < 1e-26f || c > 1e7f) sums = careful_sums<T>(part, c);
             if (p.splits == 1) {
-                float lse = 0.0f;
                 if (lane == 0) {
-                    lse = finish_row(p, row, sums);
-                    finish_target<T>(p, row, lse);
+                    scratch.norm = finish_row(p, row, sums);
+                    finish_target<T>(p, row, scratch.norm);
                 }
                 if constexpr (TOP) {
-                    lse = __shfl_sync(0xffffffffu, lse, 0);
-                    if (lane < p.top_k) write_top(p, row, lane, 0ull, lse);       // ranks that do not exist keep this
                     __syncwarp();
-                    if (lse == lse && lse != -INFINITY)
-                        warp_top<T>(part, p.top_k, notes[buf], scratch,
-                                    [&](int rank, uint64_t key) { write_top(p, row, rank, key, lse); });
+                    const float lse = scratch.norm.lse;
+                    const bool any = lse == lse && lse != -INFINITY;
+                    if (any) warp_top<T>(part, p.top_k, notes[buf], scratch);
+                    if (lane < p.top_k) write_top(p, row, lane, any ? scratch.top[lane] : 0ull, scratch.norm);
                 }
             } else {
                 if (lane == 0) p.part_sums[item] = make_float4(sums.m, sums.s, sums.a, 0.0f);
                 if constexpr (TOP) {
-                    if (lane < p.top_k) p.part_keys[item * p.top_k + lane] = 0ull;
-                    __syncwarp();
-                    warp_top<T>(part, p.top_k, notes[buf], scratch,
-                                [&](int rank, uint64_t key) { p.part_keys[item * p.top_k + rank] = key; });
+                    warp_top<T>(part, p.top_k, notes[buf], scratch);
+                    if (lane < p.top_k) p.part_keys[item * p.top_k + lane] = scratch.top[lane];
                 }
             }
             if (item + 2 * static_cast<int64_t>(gridDim.x) < items) bar_arrive(3 + buf, kLpCtaThreads);
@@ -667,7 +677,7 @@ __global__ void __launch_bounds__(kLpJoinThreads) logprobs_join_kernel(const Log
 {
     __shared__ SoftSums red[kLpJoinThreads / 32];
     __shared__ uint64_t keys[kLpMaxSplits * kLpMaxTop];
-    __shared__ float row_lse;
+    __shared__ RowNorm row_norm;
     griddep_launch_dependents();
     griddep_wait();
     const int64_t row = blockIdx.x;
@@ -682,26 +692,25 @@ __global__ void __launch_bounds__(kLpJoinThreads) logprobs_join_kernel(const Log
     }
     v = block_join(v, c, red);
     if (threadIdx.x == 0) {
-        const float lse = finish_row(p, row, v);
-        finish_target<T>(p, row, lse);
-        row_lse = lse;
+        row_norm = finish_row(p, row, v);
+        finish_target<T>(p, row, row_norm);
     }
     if (p.top_k == 0) return;
     const int n = p.splits * p.top_k;
     for (int i = threadIdx.x; i < n; i += kLpJoinThreads) keys[i] = p.part_keys[row * n + i];
     __syncthreads();
-    const float lse = row_lse;
-    if (static_cast<int>(threadIdx.x) < p.top_k) write_top(p, row, threadIdx.x, 0ull, lse);
-    __syncthreads();
-    if (lse != lse || lse == -INFINITY) return;
-    // Each split's keys are in descending order: one warp takes the largest head, rank after rank.
+    const RowNorm norm = row_norm;
+    // Each split's keys are in descending order: one warp takes the largest head, rank after rank, and keeps the
+    // key of rank r in lane r.
     if (threadIdx.x >= 32) return;
     constexpr int kLists = (kLpMaxSplits + 31) / 32;
     const int lane = threadIdx.x;
     int at[kLists];
 #pragma unroll
     for (int i = 0; i < kLists; ++i) at[i] = 0;
-    for (int rank = 0; rank < p.top_k; ++rank) {
+    uint64_t mine = 0ull;
+    const bool any = norm.lse == norm.lse && norm.lse != -INFINITY;
+    for (int rank = 0; any && rank < p.top_k; ++rank) {
         uint64_t head[kLists], best = 0ull;
 #pragma unroll
         for (int i = 0; i < kLists; ++i) {
@@ -717,8 +726,9 @@ __global__ void __launch_bounds__(kLpJoinThreads) logprobs_join_kernel(const Log
         if (best == 0ull) break;
 #pragma unroll
         for (int i = 0; i < kLists; ++i) at[i] += head[i] == best;       // keys are unique
-        if (lane == 0) write_top(p, row, rank, best, lse);
+        if (lane == rank) mine = best;
     }
+    if (lane < p.top_k) write_top(p, row, lane, mine, norm);
 }
 
 struct LogprobsGradParams {

@@ -303,3 +303,38 @@ def test_scaled_logits_above_the_range_poison_their_row_alone(tokens):
     for v in (logp, entropy, lse, top_logp):
         assert torch.isnan(v[::2]).all() and torch.isfinite(v[1::2]).all()
     assert (top_index[::2] == -1).all() and (top_index[1::2] == torch.arange(3, device="cuda")).all()
+
+
+def far_reference(x, targets, top, scale):
+    """logp, entropy, top alternatives in 64 bits from differences to the row's largest logit, which stay exact
+    whatever the rows' common offset; lse loses log n there in any precision."""
+    z = x.double() * f32(scale)
+    d = z - z.amax(1, keepdim=True)
+    logp = d - torch.logsumexp(d, 1, keepdim=True)
+    entropy = -(logp.exp() * torch.where(torch.isinf(logp), 0.0, logp)).sum(1)
+    v, i = torch.sort(logp, dim=1, descending=True, stable=True)
+    return torch.where(targets < 0, 0.0, logp.gather(1, targets.clamp(min=0)[:, None])[:, 0]), entropy, v[:, :top], i[:, :top]
+
+
+@pytest.mark.parametrize("tokens,vocab", [(3, 1000), (3, 40001), (700, 1003)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("offset", [2.0 ** 12, -2.0 ** 20, 2.0 ** 24, -1e30, "lowest"])
+def test_log_probabilities_do_not_depend_on_a_common_offset(tokens, vocab, dtype, offset):
+    """Rows far from zero: the difference of two logits is what counts.  The tolerance is 2^-20 of the sizes of
+    that difference and of the logarithm (a rounding of the difference, one of the sum, and the logarithm's eight
+    units), not of the logits."""
+    low = torch.finfo(dtype).min
+    x = (logits(tokens, vocab, torch.float32, seed=21) + (low if offset == "lowest" else offset)).clamp(min=low).to(dtype)
+    x[0] = x[0, 0]                               # uniform
+    x[-1, : vocab // 3] = -INF
+    t = some_targets(tokens, vocab)
+    t[0], t[-1] = 5, vocab - 1
+    for scale in (1.0, 0.5):
+        logp, entropy, _, top_logp, top_index = api.logprobs_forward(x, t, 20, scale)
+        api.check()
+        w_logp, w_entropy, w_top, w_index = far_reference(x, t, 20, scale)
+        near(logp, w_logp, 1.0 + w_logp.abs() + math.log(vocab), "logp")
+        assert torch.equal(top_index, w_index)
+        near(top_logp, w_top, 1.0 + w_top.abs() + math.log(vocab), "top")
+        near(entropy, w_entropy, 8.0 + 4.0 * w_entropy.abs(), "entropy")
+        assert abs(logp[0].item() + math.log(vocab)) < 1e-5
