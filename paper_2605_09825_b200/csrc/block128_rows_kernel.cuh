@@ -83,7 +83,9 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 2) gemm_block128_rows_kernel(
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[m][i] = 0.0f;
 
-    constexpr int kUnroll = 2;                       // K-blocks in flight per warp
+    // K-blocks in flight per warp.  A step's second block may start past K; its number is 8 to 15 modulo 16 and its first
+    // block's at most 2^24 - 3, so it is below 2^24, and element numbers stay below 2^31
+    constexpr int kUnroll = 2;
     for (int t0 = warp; t0 < p.k_blocks; t0 += kUnroll * kRowsWarps) {
         uint4 w0[kUnroll][2], w1[kUnroll][2], x[kUnroll][TILES][2];
         float2 sa[kUnroll][TILES];

@@ -93,3 +93,22 @@ def test_gemm_long_k_and_what_fp32_accumulation_costs(K, same_sign):
     elif K <= 28672:
         assert (np.abs(err) <= 1e-5 * S).all()         # the stated tolerance, with room: mixed signs
         assert (np.abs(err) <= 3e-6 * S).all()
+
+
+@pytest.mark.parametrize("square", [True, False])
+def test_block128_product_at_the_longest_reduction(square):
+    """K at the limit of the argument check, in the kernel for few rows: the last step's element numbers come within 16
+    of 2^31."""
+    M, N, K = 1, 3, 0x7FFFFF00
+    blocks = K // 128
+    a = torch.zeros(M, K, dtype=torch.uint8, device="cuda")
+    b = torch.zeros(N, K, dtype=torch.uint8, device="cuda")
+    for part in (slice(0, 16), slice(K - 16, K)):
+        a[:, part] = 0x38                                                     # 1.0
+        b[:, part] = torch.tensor([[0x38], [0x40], [0x44]], dtype=torch.uint8)   # 1, 2, 3
+    out = api.gemm_block128(a, torch.ones(blocks, 128, device="cuda"), b,
+                            torch.ones(blocks, 1 if square else 128, device="cuda"),
+                            api.BLOCK_128X128 if square else api.BLOCK_1X128, api.OUT_FP32,
+                            torch.empty(1, 4, device="cuda")[:, :N])
+    api.check()
+    assert out.tolist() == [[32.0, 64.0, 96.0]]
