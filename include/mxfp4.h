@@ -395,7 +395,8 @@ int mxfp4_linear_static(int pass, const void* a, const void* b, void* out, int64
  *                the scale of (row o, block t) is at t * pitch + o, pitch = 128 * ceil(outer / 128), for
  *                1 x 128 (entries of rows past `outer` are written as 0) and at
  *                t * ceil(outer / 128) + o / 128 for 128 x 128.
- *   ld_src a multiple of 8; src 16-byte aligned; inputs finite.
+ *   ld_src a multiple of 8; src 16-byte aligned.  A NaN makes its block's scale and codes NaN, an infinity
+ *   its block's scale infinite and its own code NaN; either way every product of the block is NaN.
  *
  * mxfp4_gemm_block128: out[m][n] = sum_t sa(m, t) * sb(n, t) * sum_{k in block t} A[m][k] * B[n][k]
  *   A always has 1 x 128 blocks, B the ones b_block_shape names.  out as in mxfp4_gemm.

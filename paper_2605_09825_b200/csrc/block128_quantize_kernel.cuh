@@ -59,7 +59,8 @@ __device__ __forceinline__ uint32_t word_of(const uint4& w, int i)
     return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
 }
 
-// Magnitudes of bf16 numbers order as their bits do: maxima are taken on pairs of 16-bit words.
+// Magnitudes of bf16 numbers order as their bits do: maxima are taken on pairs of 16-bit words.  A NaN's are above all
+// others, and max_nan keeps it: one NaN makes its block's scale and codes NaN.
 __device__ __forceinline__ uint32_t magnitudes(uint32_t pair) { return pair & 0x7FFF7FFFu; }
 __device__ __forceinline__ uint32_t fold(uint32_t m) { return __vmaxu2(m, m >> 16) & 0xFFFFu; }
 __device__ __forceinline__ float magnitude(uint32_t m) { return __uint_as_float(m << 16); }
@@ -70,8 +71,8 @@ __device__ __forceinline__ uint32_t piece_amax(const uint4& w)
     return __vmaxu2(__vmaxu2(magnitudes(w.x), magnitudes(w.y)), __vmaxu2(magnitudes(w.z), magnitudes(w.w)));
 }
 
-__device__ __forceinline__ float block_inverse(float amax) { return __fdiv_rn(kE4m3Max, fmaxf(amax, kBlockTiny)); }
-__device__ __forceinline__ float block_scale(float amax) { return __fdiv_rn(fmaxf(amax, kBlockTiny), kE4m3Max); }
+__device__ __forceinline__ float block_inverse(float amax) { return __fdiv_rn(kE4m3Max, max_nan(amax, kBlockTiny)); }
+__device__ __forceinline__ float block_scale(float amax) { return __fdiv_rn(max_nan(amax, kBlockTiny), kE4m3Max); }
 
 __device__ __forceinline__ uint2 piece_codes(const uint4& w, float inv)
 {

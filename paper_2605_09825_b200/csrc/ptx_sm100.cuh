@@ -495,6 +495,14 @@ __device__ __forceinline__ uint32_t cvt_e4m3x4(float v0, float v1, float v2, flo
     return r;
 }
 
+// larger of the two, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // minimum of the two unsigned 16-bit halves
 __device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b)
 {

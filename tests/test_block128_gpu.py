@@ -215,3 +215,54 @@ def test_pass_on_a_stream_of_its_own():
         got = api.linear_pass_block128(api.PASS_FPROP, X, W)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def with_value(bits, places, value):
+    """A copy with a bf16 pattern put in some places."""
+    out = bits.copy()
+    for r, c in places:
+        out[r, c] = value
+    return out
+
+
+@pytest.mark.parametrize("square", [False, True])
+@pytest.mark.parametrize("axis", [1, 0])
+@pytest.mark.parametrize("nan", [0x7FC0, 0xFF81])
+def test_quantize_nan_takes_its_block_and_no_other(axis, square, nan):
+    """One NaN makes its block's scale and codes NaN; all other blocks are what they are without it."""
+    bits = random_bits(np.random.default_rng(4), 304, 416, 3)
+    clean = api.quantize_block128(to_dev(bits), axis, api.BLOCK_128X128 if square else api.BLOCK_1X128)
+    at = [(17, 140), (303, 415)]
+    codes, scales = api.quantize_block128(to_dev(with_value(bits, at, nan)), axis,
+                                          api.BLOCK_128X128 if square else api.BLOCK_1X128)
+    api.check()
+    blocks_hit = torch.zeros_like(scales, dtype=torch.bool)
+    codes_hit = torch.zeros_like(codes, dtype=torch.bool)
+    for r, c in at:
+        o, k = (r, c) if axis == 1 else (c, r)
+        t, row = k // 128, o // 128 if square else o
+        blocks_hit[t, row] = True
+        rows = slice(row * 128, row * 128 + 128) if square else slice(o, o + 1)
+        codes_hit[rows, t * 128: t * 128 + 128] = True
+    assert torch.isnan(scales[blocks_hit]).all() and torch.equal(scales[~blocks_hit], clean[1][~blocks_hit])
+    assert ((codes[codes_hit] & 0x7F) == 0x7F).all() and torch.equal(codes[~codes_hit], clean[0][~codes_hit])
+
+
+@pytest.mark.parametrize("M", [3, 40])
+@pytest.mark.parametrize("value", [0x7FC0, 0x7F80, 0xFF80])
+def test_nan_and_infinity_reach_every_product_of_their_block(M, value):
+    """A row of A, and the 128 columns that share a block of B, are NaN; everything else is as without them."""
+    rng = np.random.default_rng(M)
+    a, b = random_bits(rng, M, 272, 2), random_bits(rng, 400, 272, 2)
+    mul = lambda x, y: api.gemm_block128(*api.quantize_block128(to_dev(x)),
+                                         *api.quantize_block128(to_dev(y), api.AXIS_COLS, api.BLOCK_128X128), out_dtype=api.OUT_FP32)
+    clean = mul(a, b)
+    got = mul(with_value(a, [(2, 270)], value), b)
+    assert torch.isnan(got[2]).all()
+    got[2] = clean[2]
+    assert torch.equal(got, clean)
+    got = mul(a, with_value(b, [(130, 3)], value))
+    api.check()
+    assert torch.isnan(got[:, 128:256]).all()
+    got[:, 128:256] = clean[:, 128:256]
+    assert torch.equal(got, clean)
