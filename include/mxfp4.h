@@ -486,7 +486,7 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
  *   logits   [tokens x vocab] bf16 or fp32 (dtype, MXFP4_OUT_*), leading dimension ld >= vocab; any
  *            vocab, any ld, aligned to the element only
  *   targets  int64 [tokens].  A negative target is a position without one: logp 0, and no gradient
- *            through it.  A target >= vocab gives NaN in logp and in the row's gradient.
+ *            through it.  A target >= vocab gives NaN in logp and in the row's gradient, masked rows included.
  *   scale    finite, > 0 (1 / temperature)
  *   logp, entropy, lse  fp32 [tokens]; logp (with targets) and entropy may be NULL
  *   top_logp fp32, top_index int64, [tokens x top_k]; 0 <= top_k <= 32

@@ -754,10 +754,11 @@ __global__ void __launch_bounds__(kLpGradThreads) logprobs_backward_kernel(const
     const int64_t target = p.targets ? p.targets[row] : -1;
     const float lse = p.lse[row];
     float gl = p.d_logp && target >= 0 ? p.d_logp[row] : 0.0f;
-    if (p.d_logp && target >= p.vocab) gl = NAN;
+    const bool bad = p.d_logp && target >= p.vocab;
+    if (bad) gl = NAN;
     const float ge = p.d_entropy ? p.d_entropy[row] : 0.0f;
     const float base = fmaf(ge, p.entropy && p.d_entropy ? p.entropy[row] : 0.0f, gl);
-    const bool zero = (gl == 0.0f && ge == 0.0f) || lse == -INFINITY;
+    const bool zero = (gl == 0.0f && ge == 0.0f) || (lse == -INFINITY && !bad);
     // the gradient without the target's own term: -scale * p * (base + ge * (z - lse))
     auto grad = [&](float x, int index) {
         const float l = fmaf(x, p.scale, -lse);

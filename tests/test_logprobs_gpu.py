@@ -338,3 +338,14 @@ def test_log_probabilities_do_not_depend_on_a_common_offset(tokens, vocab, dtype
         near(top_logp, w_top, 1.0 + w_top.abs() + math.log(vocab), "top")
         near(entropy, w_entropy, 8.0 + 4.0 * w_entropy.abs(), "entropy")
         assert abs(logp[0].item() + math.log(vocab)) < 1e-5
+
+
+def test_out_of_range_target_is_nan_in_a_masked_row_too():
+    x = logits(3, 100, seed=6)
+    x[0], x[1] = -INF, -INF
+    t = torch.tensor([100, 7, 3], device="cuda")
+    logp, entropy, lse, _, _ = api.logprobs_forward(x, t)
+    d = api.logprobs_backward(x, t, lse, entropy, torch.ones(3, device="cuda"))
+    api.check()
+    assert torch.isnan(logp).tolist() == [True, False, False]
+    assert torch.isnan(d[0]).all() and (d[1] == 0).all() and torch.isfinite(d[2]).all()
