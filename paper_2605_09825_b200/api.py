@@ -582,7 +582,8 @@ def gemm_block128(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
                   b_block_shape: int = BLOCK_128X128, out_dtype: int = OUT_BF16, out: torch.Tensor | None = None,
                   workspace: torch.Tensor | None = None):
     """``mxfp4_gemm_block128``: ``A B^T`` from E4M3 codes [M, K], [N, K] and their fp32 scales; A has
-    1 x 128 blocks, B those ``b_block_shape`` names."""
+    1 x 128 blocks, B those ``b_block_shape`` names.  Rows of the output start at multiples of 16 bytes: where N
+    elements do not fill those, the [M, N] tensor returned is a view of a wider one."""
     M, K = a_codes.shape
     N, K2 = b_codes.shape
     if K != K2:
@@ -593,7 +594,10 @@ def gemm_block128(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     lib = load_library()
     dtype = torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32
     if out is None:
-        out = torch.empty(M, N, dtype=dtype, device=a_codes.device)
+        granule = 8 if out_dtype == OUT_BF16 else 4
+        out = torch.empty(M, -(-N // granule) * granule, dtype=dtype, device=a_codes.device)
+        if N % granule:
+            out = out[:, :N]
     elif out.dtype != dtype or out.shape != (M, N):
         raise ValueError("out must be [M, N] of the output type")
     out_ptr, ld_out = _matrix(out, "out", (out.dtype,))

@@ -266,3 +266,14 @@ def test_nan_and_infinity_reach_every_product_of_their_block(M, value):
     assert torch.isnan(got[:, 128:256]).all()
     got[:, 128:256] = clean[:, 128:256]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 515, 144), (3, 1, 272), (40, 515, 272), (300, 1001, 400)])
+@pytest.mark.parametrize("out_dtype", [api.OUT_FP32, api.OUT_BF16])
+def test_gemm_makes_room_for_ragged_columns(M, N, K, out_dtype):
+    """Without `out` any number of columns works: the binding pads the rows it allocates."""
+    ops = random_operands(np.random.default_rng(N + K), M, N, K, True)
+    got = run_gemm(ops, True, out_dtype)
+    assert got.shape == (M, N)
+    ref, S = product(*ops, True)
+    assert (np.abs(got.double().cpu().numpy() - ref) <= tolerance(ref, S, K, out_dtype == api.OUT_BF16)).all()

@@ -67,3 +67,15 @@ def test_decoder(batch):
         assert ((top_logp - ref.gather(1, top_index)).abs() <= 0.62).all()
         assert (top_logp[:, 0] >= ref.max(1).values - 0.62).all()
         assert ((entropy + (ref.exp() * ref).sum(1)).abs() <= 0.62).all()
+
+
+@pytest.mark.parametrize("batch", [2, 40])
+def test_decoder_with_an_odd_vocabulary(batch):
+    w = block_step.make_weights(128, 1203)
+    ids = torch.arange(batch, device="cuda")
+    top_logp, top_index, entropy = block_step.Decoder(w, batch, 4).step(ids)
+    api.check()
+    ref = torch.log_softmax(logits_of({k: v.double() for k, v in w.items()}, ids), -1)
+    assert ((top_logp - ref.gather(1, top_index)).abs() <= 0.62).all()
+    assert (top_logp[:, 0] >= ref.max(1).values - 0.62).all()
+    assert ((entropy + (ref.exp() * ref).sum(1)).abs() <= 0.62).all()
