@@ -521,7 +521,7 @@ def _matrix(t: torch.Tensor, name: str, dtypes) -> tuple:
     stride, shape = t.stride(), t.shape
     if t.dtype not in dtypes or len(shape) != 2 or not t.is_cuda or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be a 2-D CUDA tensor of {' or '.join(map(str, dtypes))} with contiguous rows")
-    return t.data_ptr(), stride[0] if shape[0] > 1 else max(shape[1], stride[0])   # a single row's stride is arbitrary
+    return t.data_ptr(), stride[0] if shape[0] > 1 else (shape[1] + 7) // 8 * 8    # a single row's stride is arbitrary
 
 
 def _expect(t: torch.Tensor, name: str, dtype, numel: int) -> int:
