@@ -525,10 +525,25 @@ def _matrix(t: torch.Tensor, name: str, dtypes) -> tuple:
 
 
 def _expect(t: torch.Tensor, name: str, dtype, numel: int) -> int:
-    """Pointer of a contiguous CUDA tensor with at least ``numel`` elements."""
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel or not t.is_cuda:
+    """Pointer of a contiguous CUDA tensor of ``numel`` elements."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() != numel or not t.is_cuda:
         raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of {numel} elements")
     return t.data_ptr()
+
+
+def _buffer(t: torch.Tensor, name: str, dtype, numel: int) -> int:
+    """Pointer of a contiguous CUDA tensor with room for ``numel`` elements."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of at least {numel} elements")
+    return t.data_ptr()
+
+
+def _scales(t: torch.Tensor, name: str, blocks: int, numel: int) -> int:
+    """Pointer of an operand's scales: [blocks, pitch] as the quantizer returns them, or a flat buffer.  Scales of another
+    operand size or block shape, whose pitch would be misread, have another shape."""
+    if len(t.shape) != 1 and t.shape != (blocks, numel // blocks):
+        raise ValueError(f"{name} must be a flat tensor or of shape [{blocks}, {numel // blocks}]")
+    return _buffer(t, name, torch.float32, numel)
 
 
 def _raw_stream() -> int:
@@ -571,8 +586,8 @@ def quantize_block128(src: torch.Tensor, axis: int = AXIS_COLS, block_shape: int
         blocks = -(-K // 128)
         scales = torch.empty(blocks, need // blocks, dtype=torch.float32, device=src.device)
     rc = load_library().mxfp4_quantize_block128(ptr, rows, cols, ld, axis, block_shape,
-                                                _expect(codes, "codes", torch.uint8, outer * K),
-                                                _expect(scales, "scales", torch.float32, need), _raw_stream())
+                                                _buffer(codes, "codes", torch.uint8, outer * K),
+                                                _buffer(scales, "scales", torch.float32, need), _raw_stream())
     if rc:
         _raise(rc, "mxfp4_quantize_block128")
     return codes, scales
@@ -609,9 +624,9 @@ def gemm_block128(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     if workspace is not None:
         ws_ptr, ws_bytes = _dev_ptr(workspace), workspace.numel()
     rc = lib.mxfp4_gemm_block128(_expect(a_codes, "a_codes", torch.uint8, M * K),
-                                 _expect(a_scales, "a_scales", torch.float32, a_need),
+                                 _scales(a_scales, "a_scales", -(-K // 128), a_need),
                                  _expect(b_codes, "b_codes", torch.uint8, N * K),
-                                 _expect(b_scales, "b_scales", torch.float32, b_need), b_block_shape, M, N, K, out_ptr,
+                                 _scales(b_scales, "b_scales", -(-K // 128), b_need), b_block_shape, M, N, K, out_ptr,
                                  out_dtype, ld_out, ws_ptr or None, ws_bytes, _raw_stream())
     if rc:
         _raise(rc, "mxfp4_gemm_block128")
@@ -622,8 +637,8 @@ def linear_pass_block128(pass_: int, a: torch.Tensor, b: torch.Tensor, out_dtype
                          out=None):
     """``mxfp4_linear_pass_block128``: one pass in 8 bits with 128-blocks; (a, b) = (X, W) / (dY, W) / (dY, X)."""
     for t in (a, b):
-        if t.dtype != torch.bfloat16 or not t.is_contiguous():
-            raise ValueError("inputs must be contiguous bf16 tensors")
+        if t.dtype != torch.bfloat16 or t.dim() != 2 or not t.is_contiguous():
+            raise ValueError("inputs must be contiguous 2-D bf16 tensors")
     if pass_ == PASS_FPROP:
         T, in_f, out_f, shape = a.shape[0], a.shape[1], b.shape[0], (a.shape[0], b.shape[0])
     elif pass_ == PASS_DGRAD:
