@@ -696,10 +696,12 @@ def residual_norm_forward(branch, stream=None, w_post=None, w_pre=None, gate=Non
     """``mxfp4_residual_norm_forward``: ``y = skip_scale * stream + branch_scale * act(gate) * rms_norm(branch)
     * w_post`` and ``h = rms_norm(y) * w_pre``; returns ``(y, h)``, h None without ``w_pre``.
 
-    ``branch`` bf16 [tokens, width]; ``stream`` bf16 or fp32 or None (nothing is added, y of type
-    ``stream_dtype``, bf16 by default); ``gate`` None, fp32 [width] or bf16 [tokens, width]; weights fp32
-    [width] or None (that norm is left out).  ``y`` may be ``stream``."""
+    ``branch`` bf16 [tokens, width]; ``stream`` bf16 or fp32, which is y's type too, or None (nothing is
+    added, y of type ``stream_dtype``, bf16 by default); ``gate`` None, fp32 [width] or bf16 [tokens, width];
+    weights fp32 [width] or None (that norm is left out).  ``y`` may be ``stream``."""
     dtype = stream.dtype if stream is not None else (stream_dtype or torch.bfloat16)
+    if stream_dtype not in (None, dtype):
+        raise ValueError("stream_dtype is for calls without a stream; with one, y has the stream's type")
     if dtype not in _STREAM_TYPES:
         raise ValueError("the stream is bf16 or fp32")
     d = _norm_desc(branch, stream, _STREAM_TYPES[dtype], w_post, w_pre, gate, gate_act, skip_scale, branch_scale, eps)

@@ -145,3 +145,12 @@ def test_python_binding_checks_types_and_shapes_on_the_host():
                  lambda: api.residual_norm_forward(x), lambda: api.linear_pass_block128(0, x, x)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_stream_dtype_against_a_given_stream():
+    """The type of the result follows a given stream; asking for another one is refused, not ignored."""
+    import torch
+    u = torch.zeros(4, 64, dtype=torch.bfloat16)
+    for stream, dtype in ((u, torch.float32), (u.float(), torch.bfloat16)):
+        with pytest.raises(ValueError, match="stream_dtype"):
+            api.residual_norm_forward(u, stream, stream_dtype=dtype)
