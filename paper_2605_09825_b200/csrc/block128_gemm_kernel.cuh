@@ -236,7 +236,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
                     if (!BROWS && group) {
                         // the tile's columns are two blocks of 128: two words per K-step, one per lane
                         const int i = lane >> 1, block = 2 * w.tn + (lane & 1);
-                        if (rows && i < min(kBGroup, w.k1 - k) && block < p.pitch_b)
+                        if (rows && i < min(kBGroup, w.k1 - k) && block < p.pitch_b && smem_within(sm.sb[g], i))
                             cp_async_word(&sm.sb[g][i][lane & 1], p.b_scales + (k + i) * p.pitch_b + block);
                         cp_async_arrive(&sm.scales_full[g]);
                     }

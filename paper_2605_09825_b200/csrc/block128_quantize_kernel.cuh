@@ -102,11 +102,11 @@ __device__ __forceinline__ void quantize_block128_tile(const Quant128Params& p, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = __vmaxu2(m, piece_amax(w[i]));
         m = __reduce_max_sync(0xffffffffu, fold(m));
-        if ((tid & 31) == 0) part[tid >> 5] = m;
+        if ((tid & 31) == 0) smem_put(part, tid >> 5, m);
         __syncthreads();
-        m = part[0];
+        m = smem_get(part, 0);
 #pragma unroll
-        for (int i = 1; i < kB128Threads / 32; ++i) m = max(m, part[i]);
+        for (int i = 1; i < kB128Threads / 32; ++i) m = max(m, smem_get(part, i));
         const float amax = magnitude(m), inv = block_inverse(amax);
         if (tid == 0) {
             const int ob = AXIS == 1 ? tr : tc, kb = AXIS == 1 ? tc : tr;
@@ -148,20 +148,20 @@ __device__ __forceinline__ void quantize_block128_tile(const Quant128Params& p, 
 #pragma unroll
             for (int i = 0; i < 8; ++i) m[j] = __vmaxu2(m[j], magnitudes(word_of(w[i], j)));
         }
-        *reinterpret_cast<uint4*>(&part[rg * (kB128 / 2) + cg * 4]) = make_uint4(m[0], m[1], m[2], m[3]);
+        smem_store(part + rg * (kB128 / 2) + cg * 4, make_uint4(m[0], m[1], m[2], m[3]), part, sizeof(part));
         __syncthreads();
         if (tid < kB128) {
             uint32_t a = 0;
 #pragma unroll
-            for (int g = 0; g < 16; ++g) a = __vmaxu2(a, part[g * (kB128 / 2) + (tid >> 1)]);
+            for (int g = 0; g < 16; ++g) a = __vmaxu2(a, smem_get(part, g * (kB128 / 2) + (tid >> 1)));
             const float amax = magnitude((tid & 1) ? a >> 16 : a & 0xFFFFu);
             const int col = col0 + tid;
             p.scales[static_cast<int64_t>(tr) * p.pitch + col] = col < p.cols ? block_scale(amax) : 0.0f;
-            inverse[tid] = block_inverse(amax);
+            smem_put(inverse, tid, block_inverse(amax));
         }
         __syncthreads();
-        const float4 lo = *reinterpret_cast<const float4*>(&inverse[cg * 8]);
-        const float4 hi = *reinterpret_cast<const float4*>(&inverse[cg * 8 + 4]);
+        const float4 lo = smem_load<float4>(inverse + cg * 8, inverse, sizeof(inverse));
+        const float4 hi = smem_load<float4>(inverse + cg * 8 + 4, inverse, sizeof(inverse));
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint4 v = w[i];

@@ -144,13 +144,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 2) gemm_block128_rows_kernel(
 #pragma unroll
     for (int m = 0; m < TILES; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[warp][m][i][lane] = acc[m][i];
+        for (int i = 0; i < 4; ++i) smem_store(&part[warp][m][i][lane], acc[m][i], part, sizeof(part));
     __syncthreads();
     for (int e = threadIdx.x; e < TILES * 128; e += kRowsWarps * 32) {
         const int m = e >> 7, i = (e >> 5) & 3, l = e & 31;
         float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kRowsWarps; ++w) s += part[w][m][i][l];
+        for (int w = 0; w < kRowsWarps; ++w) s += smem_load<float>(&part[w][m][i][l], part, sizeof(part));
         const int row = m * 8 + 2 * (l & 3) + (i & 1), col = n0 + (l >> 2) + 8 * (i >> 1);
         if (row < p.M && col < p.N) {
             const int64_t at = row * p.ld_out + col;

@@ -86,9 +86,9 @@ static inline int device_status_code(const DeviceInfo& dev)
     return dev.cc_major == 10 ? MXFP4_OK : MXFP4_ERR_DEVICE;
 }
 
-// Read and clear the device status words of the other translation units whose kernels wait (each unit has
-// its own word).
+// Read and clear the device status words of the other translation units (each has its own).
 int block128_take_status(int* status);
 int residual_norm_take_status(int* status);
+int logprobs_take_status(int* status);
 
 }  // namespace mxfp4

@@ -248,7 +248,7 @@ __global__ void selftest_bounds_kernel()
 {
     __shared__ uint32_t buf[8];
     uint32_t* past = buf + 8;
-    if (bounds_ok(past, sizeof(uint32_t), buf, sizeof(buf))) *past = 1u;
+    if (bounds_ok(past, sizeof(uint32_t), alignof(uint32_t), buf, sizeof(buf))) *past = 1u;
 }
 
 }  // namespace mxfp4
@@ -961,11 +961,13 @@ int mxfp4_selftest_bounds(void* stream)
 int mxfp4_check(void* stream)
 {
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return MXFP4_ERR_CUDA;
-    // each translation unit whose kernels wait has a word of its own; the first one set is reported
-    int status = 0, more[2] = {0, 0};
+    // each translation unit has a word of its own; the first one set is reported
+    int status = 0, more[3] = {0, 0, 0};
     if (take_device_status(&status) != 0 || block128_take_status(&more[0]) != 0 ||
         residual_norm_take_status(&more[1]) != 0)
         return MXFP4_ERR_CUDA;
+    // the log probabilities' kernels have no wait that could run out: only the bounds-checking build sets their word
+    if (mxfp4_bounds_checked() && logprobs_take_status(&more[2]) != 0) return MXFP4_ERR_CUDA;
     for (int m : more)
         if (status == 0) status = m;
     return status;

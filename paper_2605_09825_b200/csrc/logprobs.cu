@@ -198,13 +198,14 @@ __device__ __forceinline__ SoftSums warp_join(SoftSums v, float c)
 }
 
 // Over the CTA; every thread gets the result.  Ends with every thread past a barrier.
-__device__ __forceinline__ SoftSums block_join(SoftSums v, float c, SoftSums* red)
+template <size_t N>
+__device__ __forceinline__ SoftSums block_join(SoftSums v, float c, SoftSums (&red)[N])
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     v = warp_join(v, c);
-    if (lane == 0) red[warp] = v;
+    if (lane == 0) smem_put(red, warp, v);
     __syncthreads();
-    v = lane < static_cast<int>(blockDim.x >> 5) ? red[lane] : SoftSums{-INFINITY, 0.0f, 0.0f};
+    v = lane < static_cast<int>(blockDim.x >> 5) ? smem_get(red, lane) : SoftSums{-INFINITY, 0.0f, 0.0f};
     return warp_join(v, c);
 }
 
@@ -294,8 +295,8 @@ __device__ __forceinline__ TopBound pick_owners(const RowNotes<true>& notes, Top
     uint32_t key[kEach], vec[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        key[i] = notes.key[i * 32 + lane] >> SHIFT;
-        vec[i] = notes.vec[i * 32 + lane];
+        key[i] = smem_get(notes.key, i * 32 + lane) >> SHIFT;
+        vec[i] = smem_get(notes.vec, i * 32 + lane);
     }
     auto reach = [&](uint32_t bound) {
         int n = 0;
@@ -335,7 +336,7 @@ __device__ __forceinline__ TopBound pick_owners(const RowNotes<true>& notes, Top
         const bool mine = key[i] > bound || (key[i] == bound && vec[i] <= last);
         const uint32_t who = __ballot_sync(0xffffffffu, mine);
         const int place = at + __popc(who & ((1u << lane) - 1u));
-        if (mine && place < kLpMaxTop) sc.owner[place] = i * 32 + lane;
+        if (mine && place < kLpMaxTop) smem_put(sc.owner, place, i * 32 + lane);
         at += __popc(who);
     }
     return {bound, last, at < kLpMaxTop ? at : kLpMaxTop};
@@ -385,13 +386,13 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
     const int lane = threadIdx.x & 31;
     const TopBound bound = pick_owners<T>(notes, sc, top_k, part.first + part.count);
     if (lane == 0) sc.n = sc.n_hits = sc.n_groups = 0;
-    sc.top[lane] = 0ull;
+    smem_put(sc.top, lane, uint64_t{0});
     __syncwarp();
     auto take = [&](float x, uint32_t index) {
         const uint64_t k = full_key(x, index);
         if (k == 0ull) return;
         const int at = atomicAdd(&sc.n, 1);
-        if (at < kLpCandidates) sc.keys[at] = k;
+        if (at < kLpCandidates) smem_put(sc.keys, at, k);
     };
     auto vector_at = [&](int v) { return *reinterpret_cast<const uint4*>(part.vec(part.first + v)); };
     // the owners' groups that reach the bound, and of their vectors those that do: a lane per vector, several
@@ -401,12 +402,13 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
         return key > bound.kth || (key == bound.kth && static_cast<uint32_t>(first_vec) <= bound.last_vec);
     };
     for (int i = lane; i < bound.owners * kLpGroups; i += 32) {
-        const int owner = sc.owner[i / kLpGroups], g = i % kLpGroups, v = owner + g * group_vecs * kLpThreads;
+        const int owner = smem_get(sc.owner, i / kLpGroups), g = i % kLpGroups, v = owner + g * group_vecs * kLpThreads;
         // an fp32 group whose upper half equals the bound's may or may not reach it
-        const uint32_t half = notes.group[g][owner], bound_half = bound.kth >> (16 - LogitVec<T>::kKeyShift);
+        const uint32_t half = smem_load<uint16_t>(&notes.group[g][owner], notes.group, sizeof(notes.group));
+        const uint32_t bound_half = bound.kth >> (16 - LogitVec<T>::kKeyShift);
         if (v < part.count && (kN == 8 ? in_reach(half, part.first + v) : half >= bound_half)) {
             const int at = atomicAdd(&sc.n_groups, 1);
-            if (at < kLpHits) sc.groups[at] = static_cast<uint32_t>(v);
+            if (at < kLpHits) smem_put(sc.groups, at, static_cast<uint32_t>(v));
         }
     }
     __syncwarp();
@@ -418,20 +420,20 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const int i = l + 32 * j, o = i / group_vecs;
-            v[j] = i < loads ? static_cast<int>(sc.groups[o]) + (i - o * group_vecs) * kLpThreads : part.count;
+            v[j] = i < loads ? static_cast<int>(smem_get(sc.groups, o)) + (i - o * group_vecs) * kLpThreads : part.count;
             if (v[j] < part.count) w[j] = vector_at(v[j]);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
             if (v[j] < part.count && in_reach(order_key(LogitVec<T>::top(w[j])) >> LogitVec<T>::kKeyShift, part.first + v[j])) {
                 const int at = atomicAdd(&sc.n_hits, 1);
-                if (at < kLpHits) sc.hits[at] = static_cast<uint32_t>(v[j]);
+                if (at < kLpHits) smem_put(sc.hits, at, static_cast<uint32_t>(v[j]));
             }
     }
     __syncwarp();
     const int n_hits = sc.n_hits;
     for (int h = lane; h < n_hits && n_hits <= kLpHits; h += 32) {
-        const int v = static_cast<int>(sc.hits[h]), vec = part.first + v;
+        const int v = static_cast<int>(smem_get(sc.hits, h)), vec = part.first + v;
         float x[kN];
         LogitVec<T>::get(vector_at(v), x);
 #pragma unroll
@@ -448,10 +450,10 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
     const int n = n_hits <= kLpHits && sc.n_groups <= kLpHits ? sc.n : kLpCandidates + 1;
     if (n <= kLpCandidates) {
         for (int i = lane; i < n; i += 32) {
-            const uint64_t k = sc.keys[i];
+            const uint64_t k = smem_get(sc.keys, i);
             int rank = 0;
-            for (int j = 0; j < n; ++j) rank += sc.keys[j] > k;
-            if (rank < top_k) sc.top[rank] = k;
+            for (int j = 0; j < n; ++j) rank += smem_get(sc.keys, j) > k;
+            if (rank < top_k) smem_put(sc.top, rank, k);
         }
     } else {
         // hundreds of vectors reach the bound: rank after rank, each from the whole part
@@ -477,7 +479,7 @@ __device__ __forceinline__ void warp_top(const RowPart<T>& part, int top_k, cons
                 if (other > mine) mine = other;
             }
             last = mine;
-            if (lane == 0) sc.top[rank] = last;
+            if (lane == 0) smem_put(sc.top, rank, last);
         }
     }
     __syncwarp();
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
             const int split = static_cast<int>(item - row * p.splits);
             const RowPart<T> part = row_part<T>(p, row, split);
             bar_sync(1 + buf, kLpCtaThreads);
-            SoftSums sums = lane < kLpThreads / 32 ? notes[buf].sums[lane] : SoftSums{-INFINITY, 0.0f, 0.0f};
+            SoftSums sums = lane < kLpThreads / 32 ? smem_get(notes[buf].sums, lane) : SoftSums{-INFINITY, 0.0f, 0.0f};
             sums = warp_join(sums, c);
             // (with scales beyond these, -10^30 times c is not far below everything, or not a number)
             if (!(fabsf(sums.m) * c < kLpHuge) || c < 1e-26f || c > 1e7f) sums = careful_sums<T>(part, c);
@@ -550,13 +552,13 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
                     const float lse = scratch.norm.lse;
                     const bool any = lse == lse && lse != -INFINITY;
                     if (any) warp_top<T>(part, p.top_k, notes[buf], scratch);
-                    if (lane < p.top_k) write_top(p, row, lane, any ? scratch.top[lane] : 0ull, scratch.norm);
+                    if (lane < p.top_k) write_top(p, row, lane, any ? smem_get(scratch.top, lane) : 0ull, scratch.norm);
                 }
             } else {
                 if (lane == 0) p.part_sums[item] = make_float4(sums.m, sums.s, sums.a, 0.0f);
                 if constexpr (TOP) {
                     warp_top<T>(part, p.top_k, notes[buf], scratch);
-                    if (lane < p.top_k) p.part_keys[item * p.top_k + lane] = scratch.top[lane];
+                    if (lane < p.top_k) p.part_keys[item * p.top_k + lane] = smem_get(scratch.top, lane);
                 }
             }
             if (item + 2 * static_cast<int64_t>(gridDim.x) < items) bar_arrive(3 + buf, kLpCtaThreads);
@@ -617,7 +619,8 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
         if (item >= 2 * static_cast<int64_t>(gridDim.x)) bar_sync(3 + buf, kLpCtaThreads);
         auto close_group = [&](bool last) {
             if (++step == group_steps || last) {
-                notes[buf].group[group][threadIdx.x] = static_cast<uint16_t>(order_key(group_best) >> 16);
+                smem_store(&notes[buf].group[group][threadIdx.x], static_cast<uint16_t>(order_key(group_best) >> 16),
+                           notes[buf].group, sizeof(notes[buf].group));
                 group_best = -INFINITY;
                 step = 0;
                 ++group;
@@ -653,10 +656,10 @@ __global__ void __launch_bounds__(kLpCtaThreads, 4) logprobs_forward_kernel(cons
             a.x = fmaf(d, e, a.x);
         }
         const SoftSums sums = warp_join({m, s.x + s.y, a.x + a.y}, c);
-        if (lane == 0) notes[buf].sums[threadIdx.x >> 5] = sums;
+        if (lane == 0) smem_put(notes[buf].sums, threadIdx.x >> 5, sums);
         if (TOP) {
-            notes[buf].key[threadIdx.x] = order_key(best);
-            notes[buf].vec[threadIdx.x] = static_cast<uint32_t>(best_vec);
+            smem_put(notes[buf].key, threadIdx.x, order_key(best));
+            smem_put(notes[buf].vec, threadIdx.x, static_cast<uint32_t>(best_vec));
         }
         bar_arrive(1 + buf, kLpCtaThreads);
     }
@@ -689,7 +692,7 @@ __global__ void __launch_bounds__(kLpJoinThreads) logprobs_join_kernel(const Log
     }
     if (p.top_k == 0) return;
     const int n = p.splits * p.top_k;
-    for (int i = threadIdx.x; i < n; i += kLpJoinThreads) keys[i] = p.part_keys[row * n + i];
+    for (int i = threadIdx.x; i < n; i += kLpJoinThreads) smem_put(keys, i, p.part_keys[row * n + i]);
     __syncthreads();
     const RowNorm norm = row_norm;
     // Each split's keys are in descending order: one warp takes the largest head, rank after rank, and keeps the
@@ -707,7 +710,7 @@ __global__ void __launch_bounds__(kLpJoinThreads) logprobs_join_kernel(const Log
 #pragma unroll
         for (int i = 0; i < kLists; ++i) {
             const int split = lane + 32 * i;
-            head[i] = split < p.splits && at[i] < p.top_k ? keys[split * p.top_k + at[i]] : 0ull;
+            head[i] = split < p.splits && at[i] < p.top_k ? smem_get(keys, split * p.top_k + at[i]) : 0ull;
             if (head[i] > best) best = head[i];
         }
 #pragma unroll
@@ -824,6 +827,9 @@ static int logprobs_splits(int64_t tokens, int64_t vocab)
     if (s > kLpMaxSplits) s = kLpMaxSplits;
     return static_cast<int>(s < 1 ? 1 : s);
 }
+
+// Status word of this translation unit's kernels, cleared when it is set.
+int logprobs_take_status(int* status) { return take_device_status(status); }
 
 static int logprobs_shape_ok(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld, float scale)
 {

@@ -33,10 +33,10 @@ static inline int take_device_status(int* status)
 // buffer it was derived from and is naturally aligned; a miss records kDevErrBounds in the status
 // word and the access is skipped (a load returns zeros) -- nothing traps.  In the normal build the
 // helpers are plain loads and stores.
-__device__ __forceinline__ bool bounds_ok(const void* p, size_t bytes, const void* base, size_t size)
+__device__ __forceinline__ bool bounds_ok(const void* p, size_t bytes, size_t align, const void* base, size_t size)
 {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(base);
-    if (a >= b && a + bytes <= b + size && a % bytes == 0) return true;
+    if (a >= b && a + bytes <= b + size && a % align == 0) return true;
     atomicCAS(&g_device_status, 0, kDevErrBounds);
     return false;
 }
@@ -45,7 +45,7 @@ template <class T>
 __device__ __forceinline__ T smem_load(const void* p, const void* base, size_t size)
 {
 #ifdef MXFP4_BOUNDS
-    if (!bounds_ok(p, sizeof(T), base, size)) return T{};
+    if (!bounds_ok(p, sizeof(T), alignof(T), base, size)) return T{};
 #endif
     return *static_cast<const T*>(p);
 }
@@ -54,9 +54,32 @@ template <class T>
 __device__ __forceinline__ void smem_store(void* p, const T& v, const void* base, size_t size)
 {
 #ifdef MXFP4_BOUNDS
-    if (!bounds_ok(p, sizeof(T), base, size)) return;
+    if (!bounds_ok(p, sizeof(T), alignof(T), base, size)) return;
 #endif
     *static_cast<T*>(p) = v;
+}
+
+// Elements of a shared array.
+template <class T, size_t N>
+__device__ __forceinline__ T smem_get(const T (&a)[N], int i)
+{
+    return smem_load<T>(a + i, a, sizeof(a));
+}
+template <class T, size_t N>
+__device__ __forceinline__ void smem_put(T (&a)[N], int i, const T& v)
+{
+    smem_store<T>(a + i, v, a, sizeof(a));
+}
+
+// For a copy instruction that takes the address of element i itself; always true in the normal build.
+template <class T, size_t N>
+__device__ __forceinline__ bool smem_within(const T (&a)[N], int i)
+{
+#ifdef MXFP4_BOUNDS
+    return bounds_ok(a + i, sizeof(T), alignof(T), a, sizeof(a));
+#else
+    return true;
+#endif
 }
 
 // Spin limit for one wait.  A try_wait suspends for a hardware-defined slice, so this many

@@ -188,7 +188,7 @@ __device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t&
     for (int o = kLanes / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     const int n = CLUSTER ? cluster * warps : warps;
     if (!CLUSTER) {
-        if (in_group == 0) sh.red[slot][value][warp] = t;
+        if (in_group == 0) smem_put(sh.red[slot][value], warp, t);
         if (N == 4) {
             __syncthreads();
         } else {
@@ -197,7 +197,7 @@ __device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t&
             (void)mbar_wait_fast(&sh.sums[slot], (call >> 1) & 1, &sh.abort_flag);
         }
     } else {
-        if (in_group < cluster)              // to CTA `in_group`
+        if (in_group < cluster && smem_within(sh.red[slot][value], rank * warps + warp))     // to CTA `in_group`
             st_async_f32(map_to_cta(smem_u32(&sh.red[slot][value][rank * warps + warp]), in_group), t,
                          map_to_cta(smem_u32(&sh.sums[slot]), in_group));
         if (threadIdx.x == 0) mbar_arrive_expect_tx(&sh.sums[slot], n * N * 4);
@@ -207,10 +207,10 @@ __device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t&
     t = 0.0f;
     if (!CLUSTER) {
         // at most sixteen warps: one or two entries per lane
-        if (in_group < n) t = sh.red[slot][value][in_group];
-        if (N == 4 && in_group + kLanes < n) t += sh.red[slot][value][in_group + kLanes];
+        if (in_group < n) t = smem_get(sh.red[slot][value], in_group);
+        if (N == 4 && in_group + kLanes < n) t += smem_get(sh.red[slot][value], in_group + kLanes);
     } else {
-        for (int j = in_group; j < n; j += kLanes) t += sh.red[slot][value][j];
+        for (int j = in_group; j < n; j += kLanes) t += smem_get(sh.red[slot][value], j);
     }
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
@@ -595,11 +595,11 @@ __global__ void __launch_bounds__(kSumWarps * 32) sum_partials_kernel(const SumP
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
     }
-    part[warp][lane] = s;
+    smem_put(part[warp], lane, s);
     __syncthreads();
     if (warp == 0 && at < row4) {
         for (int w = 1; w < kSumWarps; ++w) {
-            const float4 v = part[w][lane];
+            const float4 v = smem_get(part[w], lane);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
         const int64_t col = at * 4;
