@@ -6,9 +6,11 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "../../include/mxfp4.h"
+#include "ptx_sm100.cuh"
 
 namespace mxfp4 {
 
@@ -45,6 +47,14 @@ static inline int current_device()
     return dev;
 }
 
+// Whether this translation unit has been called on a device.  Every entry point asks for device_info() before it
+// launches anything, which sets it; until then the unit's status word cannot be set either.
+static inline std::atomic<bool>& unit_used(int dev)
+{
+    static std::atomic<bool> used[kMaxDevices];
+    return used[dev];
+}
+
 static inline const DeviceInfo& device_info()
 {
     static DeviceInfo info[kMaxDevices];
@@ -53,6 +63,7 @@ static inline const DeviceInfo& device_info()
     const int dev = current_device();
     if (dev < 0) return none;
     once.run(dev, [&] {
+        unit_used(dev) = true;
         cudaDeviceProp prop;
         if (cudaGetDeviceProperties(&prop, dev) == cudaSuccess) {
             info[dev].sm_count = prop.multiProcessorCount;
@@ -86,7 +97,16 @@ static inline int device_status_code(const DeviceInfo& dev)
     return dev.cc_major == 10 ? MXFP4_OK : MXFP4_ERR_DEVICE;
 }
 
-// Read and clear the device status words of the other translation units (each has its own).
+// The status of this translation unit's kernels, cleared if it was set; 0 without a look at the device where the
+// unit has not been called (a look costs a copy of its own, 11 us).
+static inline int take_unit_status(int* status)
+{
+    const int dev = current_device();
+    *status = 0;
+    return dev >= 0 && !unit_used(dev) ? 0 : take_device_status(status);
+}
+
+// The same of the other translation units (each has its own status word).
 int block128_take_status(int* status);
 int residual_norm_take_status(int* status);
 int logprobs_take_status(int* status);
