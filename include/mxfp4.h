@@ -483,8 +483,8 @@ int mxfp4_residual_norm_backward(const mxfp4_norm_desc* norm, const void* dh, in
  *     z = scale * logits,  lse = log sum exp z,  logp = z[target] - lse,
  *     entropy = lse - sum_i p_i z_i  (p = exp(z - lse)),
  *     top_logp / top_index: the top_k largest z - lse, descending, equal ones by lowest index.
- *   logits   [tokens x vocab] bf16 or fp32 (dtype, MXFP4_OUT_*), leading dimension ld >= vocab; any
- *            vocab, any ld, aligned to the element only
+ *   logits   [tokens x vocab] bf16 or fp32 (dtype, MXFP4_OUT_*), leading dimension ld >= vocab; vocab
+ *            below 2^30, up to 3621388 tokens, any ld, aligned to the element only
  *   targets  int64 [tokens].  A negative target is a position without one: logp 0, and no gradient
  *            through it.  A target >= vocab gives NaN in logp and in the row's gradient, masked rows included.
  *   scale    finite, > 0 (1 / temperature)

@@ -728,8 +728,9 @@ def residual_norm_backward(dh, dy, branch, y, w_post=None, w_pre=None, gate=None
                            skip_scale: float = 1.0, branch_scale: float = 1.0, eps: float = 1e-5, workspace=None,
                            dstream=None, dbranch=None):
     """``mxfp4_residual_norm_backward``: ``(dstream, dbranch, dgate, dw_post, dw_pre)`` from the gradients
-    ``dh`` (None without ``w_pre``) and ``dy`` (None: zero) and the forward's ``branch`` and ``y``; what
-    the forward did not have is None.  ``dstream`` may be ``dy`` and ``dbranch`` may be ``dh``."""
+    ``dh`` (None without ``w_pre``) and ``dy`` (None: zero) and the forward's ``branch`` and ``y``; gradients of a
+    gate or weight that the forward did not have are None (``dstream`` is always formed: without a stream it is
+    ``skip_scale`` times the gradient of y).  ``dstream`` may be ``dy`` and ``dbranch`` may be ``dh``."""
     like = y if y is not None else dy
     if like is None or like.dtype not in _STREAM_TYPES:
         raise ValueError("y or dy is needed, bf16 or fp32")

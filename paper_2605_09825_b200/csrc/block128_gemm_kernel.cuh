@@ -12,8 +12,10 @@
 //
 // Per SM and K-step: 512 cycles of MMA; 128 x 256 multiply-adds of the epilogue, packed in pairs, are 256
 // cycles of the FMA pipe (twice that when B has a scale per row, which costs a multiplication per
-// element more).  Neither bounds the kernel (8192 x 28672 x 4096: 885 us, 2.2 PFLOP/s, a K-step in 900 to
-// 1000 cycles): a half buffer's way round does -- 256 cycles of MMA, about 200 until the epilogue has seen
+// element more).  Neither bounds the kernel (8192 x 28672 x 4096 by itself: 848 us, 2.3 PFLOP/s, 1.9 back to back, where the
+// power cap holds 1.5 GHz; 28672 x 4096 x 8192 with a scale per row of B: 1202 us, 1.6, and 1.45 back to back at
+// 1.64 GHz; 4096 x 4096 x 4096 with its join: 82 and 115 us.  A K-step takes 900 to 1000 cycles, 1400 with scales per
+// row): a half buffer's way round does -- 256 cycles of MMA, about 200 until the epilogue has seen
 // the signal, 500 to 700 of reading and adding (two warps per scheduler, which is what 128 sums per
 // thread leave room for, cover little of each other's waits), 340 for the signal back across the pair,
 // 100 to issue -- with two K-steps of tensor memory to overlap it.  With the additions left out it runs

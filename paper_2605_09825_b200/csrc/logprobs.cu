@@ -21,9 +21,12 @@
 // A row is split over several CTAs when there are too few rows to fill the device; each split
 // leaves (m, S, A) and its own alternatives in the workspace and a second kernel joins them.
 //
-// 8192 x 128256 in bf16 (2.10 GB): 349 us (6.0 TB/s), 405 with 5 alternatives, 420 with 20; the issue slots (54 %) and
-// the multifunction unit (one exponential per logit, 53 %) bound it, not memory.  Backward 649 us for 4.20 GB,
-// 6.5 TB/s.
+// 8192 x 128256 in bf16 (2.10 GB), a call by itself after a flush of L2: 360 us (5.8 TB/s), 416 with 5 alternatives, 432 with
+// 20, whatever the spread of the logits; calls back to back, where the power cap holds the clock at 1.7 to 1.8 GHz, 394 and
+// (5 alternatives) 436.  The issue slots (54 %) and the multifunction unit (one exponential per logit, 53 %) bound it, not
+// memory.  The 56 registers that four CTAs of 288 threads leave spill 112 bytes (bf16) and 120 (fp32) with
+// alternatives, none without.  Rows without a logit above -10^29 are summed by one warp: 8192 x 32001 masked entirely
+// take 5.2 ms, of the type's lowest value 8.1, ordinary ones 0.11.  Backward 652 us for 4.20 GB, 6.4 TB/s; 677 back to back.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>

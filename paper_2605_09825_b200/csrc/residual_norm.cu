@@ -16,10 +16,12 @@
 // the sums of the weight gradients stay in registers for all of a CTA's rows.  All arithmetic is fp32;
 // the outputs are rounded once.
 //
-// Bound by memory forward (16384 x 4096, bf16 stream, gate per element: 108 us for 671 MB, 6.2 TB/s).  Backward the
+// Bound by memory forward (16384 x 4096, bf16 stream, sigmoid gate per element: 117 us for 671 MB, 5.7 TB/s).  Backward the
 // registers of the weight gradients leave one CTA of 512 threads per SM, and the one reduction per row stands between its
-// loads and stores: 198 us for 1.07 GB (5.4 TB/s), a row in 1.8 us; 1003 x 14336 with an fp32 stream, where
-// the reduction crosses four CTAs, 71 us for 259 MB (3.6 TB/s), a row in 2.1 us.
+// loads and stores: 203 to 210 us for 1.07 GB (SiLU gate per element; 5.1 to 5.3 TB/s), a row in 1.8 us; 1003 x 14336 with an
+// fp32 stream, where the reduction crosses four CTAs, 73 us for 259 MB (3.6 TB/s), a row in 2.1 us.  Rows that take a
+// cluster, 4096 x 14336: forward 125 us for 470 MB (bf16 stream) and 160 for 705 (fp32), backward 256 and 260 for 705
+// and 1057 MB.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -164,8 +166,8 @@ __device__ __forceinline__ NormPlace norm_place(const NormParams& p)
 // exchanges finish the one it is left with: value lane / (32 / N), the same in all lanes of that group.
 // Every warp leaves its sums in the shared memory of all CTAs of the cluster; then every warp adds all of
 // them.  Inside one CTA the forward pass waits for that at an mbarrier and the backward pass at the block's barrier, as
-// measured: 16384 x 4096 without a gate, forward 89 us against 93 at the block's barrier, backward 165
-// against 155.  `call` counts the calls: slots alternate, and a slot is written again only after every warp has
+// measured (16384 x 4096 without a gate, both forms in one run): forward 89 us against 93 at the block's barrier,
+// backward 165 against 155.  `call` counts the calls: slots alternate, and a slot is written again only after every warp has
 // read it (it takes part in the call in between afterwards).
 template <int N, bool CLUSTER>
 __device__ __forceinline__ void row_sum(float (&v)[N], NormShared& sh, uint32_t& call, int cluster, int rank)
