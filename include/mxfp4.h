@@ -455,6 +455,9 @@ int mxfp4_linear_pass_block128(int pass, const void* a, const void* b, void* out
 #define MXFP4_GATE_LINEAR 0
 #define MXFP4_GATE_SIGMOID 1
 #define MXFP4_GATE_SILU 2
+#define MXFP4_GATE_GELU 3         /* _GELU, _GELU_TANH, _RELU: the gated projections' (below) only */
+#define MXFP4_GATE_GELU_TANH 4
+#define MXFP4_GATE_RELU 5
 typedef struct mxfp4_norm_desc {
     int64_t tokens, width;
     const void* branch;
@@ -517,6 +520,80 @@ int mxfp4_logprobs_forward(const void* logits, int dtype, int64_t tokens, int64_
 int mxfp4_logprobs_backward(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld,
                             const int64_t* targets, float scale, const float* lse, const float* entropy,
                             const float* d_logp, const float* d_entropy, void* dlogits, int64_t ld_d, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * The first half of a gated feed-forward block that stays in 16 bits:
+ *     g = x Wg^T,   u = x Wu^T,   h = act(g) * u
+ * Both projections, the activation and the product are one kernel; sums in fp32, act and product on the sums
+ * before they are rounded.
+ *   x               bf16 [tokens x in_features], ld_x
+ *   w_gate, w_up    bf16 [features x in_features], ld_gate, ld_up (two halves of one matrix are two such pointers)
+ *   act             MXFP4_GATE_LINEAR, _SIGMOID, _SILU, _GELU (x * normal distribution function), _GELU_TANH (its usual
+ *                   approximation by tanh), _RELU
+ * in_features and features multiples of 8; matrices 16-byte aligned with leading dimensions that are multiples of 8;
+ * nothing an output overlaps may be read.  The struct is a HOST struct of DEVICE pointers.
+ *
+ * Forward: h bf16 [tokens x features], ld_h; gate and up (both or neither NULL): g and u rounded to bf16, [tokens x
+ *   features], ld_kept, as the backward pass wants them.
+ * Backward, from dh and the stored g and u:
+ *     dg = dh * u * act'(g),   du = dh * act(g)            rounded to bf16 (the products' operands)
+ *     dx = dg Wg + du Wu,      dWg = dg^T x,   dWu = du^T x
+ *   dx bf16 [tokens x in_features]; dw_gate, dw_up (dw_dtype, MXFP4_OUT_*) [features x in_features], ld_dw; dx, or
+ *   both weight gradients, may be NULL: not wanted.  act' of _RELU at 0 is 0.
+ *   workspace: mxfp4_gated_linear_workspace_bytes bytes (dg and du), 16-byte aligned.
+ * Calls repeat bit for bit.
+ */
+typedef struct mxfp4_gated_desc {
+    int64_t tokens, in_features, features;
+    const void* x;
+    int64_t ld_x;
+    const void* w_gate;
+    int64_t ld_gate;
+    const void* w_up;
+    int64_t ld_up;
+    int32_t act;
+} mxfp4_gated_desc;
+int mxfp4_gated_linear_forward(const mxfp4_gated_desc* gated, void* h, int64_t ld_h, void* gate, void* up,
+                               int64_t ld_kept, void* stream);
+size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t features);
+int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, int64_t ld_dh, const void* gate,
+                                const void* up, int64_t ld_kept, void* dx, int64_t ld_dx, void* dw_gate, void* dw_up,
+                                int64_t ld_dw, int dw_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Log probabilities of given tokens straight from an output layer's input and weight (softmax cross entropy), in
+ * pieces of the vocabulary: the logits are never stored.
+ *     z = scale * x W^T,   lse = log sum exp z,   logp = z[target] - lse
+ *   x        bf16 [tokens x in_features], ld_x;  w bf16 [vocab x in_features], ld_w; in_features a multiple of 8,
+ *            any vocab; 16-byte aligned, leading dimensions multiples of 8
+ *   targets  int64 [tokens], as in mxfp4_logprobs_forward: negative: none (logp 0, no gradient through it); >= vocab: NaN
+ *   scale    finite, > 0
+ *   logp (with targets; both may be NULL), lse   fp32 [tokens]
+ * A NaN or +infinity among a row's z makes its lse NaN.
+ *
+ * Backward: dz = scale * (d_logp * (delta(target) - p) + d_lse * p),  p = exp(z - lse), from the forward's lse (or that of
+ *   a vocabulary split over devices), rounded to bf16 (the products' operand);
+ *     dx = dz W,   dW = dz^T x
+ *   d_logp, d_lse fp32 [tokens], one of them may be NULL (zero; targets may then be NULL with d_logp);
+ *   dx bf16 [tokens x in_features]; dw (dw_dtype, MXFP4_OUT_*) [vocab x in_features]; either may be NULL: not wanted.
+ *   A position whose two gradients are 0 adds nothing, whatever its z; its x must be finite all the same, since dW
+ *   sums 0 * x.
+ * workspace: mxfp4_linear_logprobs_workspace_bytes(..., backward 0 / 1) bytes, 16-byte aligned: forward 131 MB at most at a
+ *   vocabulary of 128256; backward the gradients of 2^27 / tokens logits per token (at least 8192), and dx in fp32 where
+ *   the vocabulary takes more than one piece.
+ * Calls repeat bit for bit.
+ */
+size_t mxfp4_linear_logprobs_workspace_bytes(int64_t tokens, int64_t in_features, int64_t vocab, int backward);
+int mxfp4_linear_logprobs_forward(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t tokens,
+                                  int64_t in_features, int64_t vocab, const int64_t* targets, float scale, float* logp,
+                                  float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t tokens,
+                                   int64_t in_features, int64_t vocab, const int64_t* targets, float scale,
+                                   const float* lse, const float* d_logp, const float* d_lse, void* dx, int64_t ld_dx,
+                                   void* dw, int64_t ld_dw, int dw_dtype, void* workspace, size_t workspace_bytes,
+                                   void* stream);
 
 /*
  * Synchronises `stream` and returns the sticky device-side status of the current device:

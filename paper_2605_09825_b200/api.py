@@ -24,6 +24,7 @@ PASS_FPROP, PASS_DGRAD, PASS_WGRAD = 0, 1, 2
 AXIS_ROWS, AXIS_COLS = 0, 1
 GATE_NONE, GATE_CHANNEL, GATE_ELEMENT = 0, 1, 2      # kinds
 GATE_LINEAR, GATE_SIGMOID, GATE_SILU = 0, 1, 2       # activations
+GATE_GELU, GATE_GELU_TANH, GATE_RELU = 3, 4, 5       # of the gated projections only
 
 EXPORTS = (
     "mxfp4_version", "mxfp4_status_string", "mxfp4_codes_bytes", "mxfp4_scales_bytes",
@@ -37,6 +38,8 @@ EXPORTS = (
     "mxfp4_gemm_block128", "mxfp4_linear_pass_block128_workspace_bytes", "mxfp4_linear_pass_block128",
     "mxfp4_residual_norm_forward", "mxfp4_residual_norm_workspace_bytes", "mxfp4_residual_norm_backward",
     "mxfp4_logprobs_workspace_bytes", "mxfp4_logprobs_forward", "mxfp4_logprobs_backward",
+    "mxfp4_gated_linear_forward", "mxfp4_gated_linear_workspace_bytes", "mxfp4_gated_linear_backward",
+    "mxfp4_linear_logprobs_workspace_bytes", "mxfp4_linear_logprobs_forward", "mxfp4_linear_logprobs_backward",
 )
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 
@@ -56,6 +59,14 @@ class NormDesc(ctypes.Structure):
                 ("w_pre", ctypes.c_void_p), ("stream_dtype", ctypes.c_int32), ("gate_kind", ctypes.c_int32),
                 ("gate_act", ctypes.c_int32), ("skip_scale", ctypes.c_float), ("branch_scale", ctypes.c_float),
                 ("eps", ctypes.c_float)]
+
+
+class GatedDesc(ctypes.Structure):
+    """``mxfp4_gated_desc``: what both directions of ``mxfp4_gated_linear_*`` read."""
+    _fields_ = [("tokens", ctypes.c_int64), ("in_features", ctypes.c_int64), ("features", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64), ("w_gate", ctypes.c_void_p),
+                ("ld_gate", ctypes.c_int64), ("w_up", ctypes.c_void_p), ("ld_up", ctypes.c_int64),
+                ("act", ctypes.c_int32)]
 
 
 class Mxfp4Error(RuntimeError):
@@ -127,7 +138,7 @@ def load_library() -> ctypes.CDLL:
     lib.mxfp4_linear_static.argtypes = [ci, vp, vp, vp, i64, i64, i64, ci, ci, u64, ci, vp]
     lib.mxfp4_linear_static.restype = ci
     lib.mxfp4_check.argtypes, lib.mxfp4_check.restype = [vp], ci
-    f32, norm = ctypes.c_float, ctypes.POINTER(NormDesc)
+    f32, norm, gated = ctypes.c_float, ctypes.POINTER(NormDesc), ctypes.POINTER(GatedDesc)
     for name, args, res in (
             ("mxfp4_block128_scales_bytes", [i64, i64, ci], sz),
             ("mxfp4_quantize_block128", [vp, i64, i64, i64, ci, ci, vp, vp, vp], ci),
@@ -140,7 +151,14 @@ def load_library() -> ctypes.CDLL:
             ("mxfp4_residual_norm_backward", [norm] + [vp, i64] * 5 + [vp, vp, vp, sz, vp], ci),
             ("mxfp4_logprobs_workspace_bytes", [i64, i64, ci], sz),
             ("mxfp4_logprobs_forward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, ci, vp, vp, vp, sz, vp], ci),
-            ("mxfp4_logprobs_backward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp], ci)):
+            ("mxfp4_logprobs_backward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp], ci),
+            ("mxfp4_gated_linear_forward", [gated, vp, i64, vp, vp, i64, vp], ci),
+            ("mxfp4_gated_linear_workspace_bytes", [i64, i64], sz),
+            ("mxfp4_gated_linear_backward", [gated, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, ci, vp, sz, vp], ci),
+            ("mxfp4_linear_logprobs_workspace_bytes", [i64, i64, i64, ci], sz),
+            ("mxfp4_linear_logprobs_forward", [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, sz, vp], ci),
+            ("mxfp4_linear_logprobs_backward",
+             [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, vp, i64, vp, i64, ci, vp, sz, vp], ci)):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, res
     lib.mxfp4_selftest_wait_timeout.argtypes, lib.mxfp4_selftest_wait_timeout.restype = [vp], ci
@@ -829,6 +847,152 @@ def logprobs_backward(logits, targets, lse, entropy=None, d_logp=None, d_entropy
     if rc:
         _raise(rc, "mxfp4_logprobs_backward")
     return dlogits
+
+
+# ---------------------------------------------------------------- gated projections, loss from the output layer's input
+def _on_current_device(*tensors) -> None:
+    """All CUDA tensors of a call live on the current device, whose current stream the call runs on."""
+    index = torch._C._cuda_getDevice() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != index:
+            raise ValueError(f"tensors must be on the current device (cuda:{index})")
+
+
+def _output(t, name: str, shape: tuple, dtype, device) -> torch.Tensor:
+    """The caller's output tensor, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {list(shape)}")
+    return t
+
+
+def _gated_desc(x, w_gate, w_up, act) -> GatedDesc:
+    x_ptr, ld_x = _matrix(x, "x", _BF16)
+    g_ptr, ld_gate = _matrix(w_gate, "w_gate", _BF16)
+    u_ptr, ld_up = _matrix(w_up, "w_up", _BF16)
+    if w_gate.shape != w_up.shape or w_gate.shape[1] != x.shape[1]:
+        raise ValueError("w_gate and w_up must have the same shape, [features, in_features] with x's in_features")
+    return GatedDesc(x.shape[0], x.shape[1], w_gate.shape[0], x_ptr, ld_x, g_ptr, ld_gate, u_ptr, ld_up, act)
+
+
+def _kept(gate, up, shape: tuple) -> tuple:
+    """Pointers and the common leading dimension of the stored projections."""
+    if tuple(gate.shape) != shape or tuple(up.shape) != shape:
+        raise ValueError(f"the kept projections must have shape {list(shape)}")
+    (g_ptr, ld), (u_ptr, ld_u) = _matrix(gate, "gate", _BF16), _matrix(up, "up", _BF16)
+    if ld != ld_u:
+        raise ValueError("the kept projections must have the same row stride")
+    return g_ptr, u_ptr, ld
+
+
+def gated_linear_forward(x, w_gate, w_up, act: int = GATE_SILU, keep: bool = True, h=None):
+    """``mxfp4_gated_linear_forward``: ``h = act(x w_gate^T) * (x w_up^T)`` of bf16 matrices, x [tokens,
+    in_features], weights [features, in_features].  Returns ``(h, kept)``; ``kept``, the two projections as
+    ``gated_linear_backward`` takes them, is None without ``keep``."""
+    d = _gated_desc(x, w_gate, w_up, act)
+    shape, dev = (x.shape[0], w_gate.shape[0]), x.device
+    h = _output(h, "h", shape, torch.bfloat16, dev)
+    _on_current_device(x, w_gate, w_up, h)
+    kept, g_ptr, u_ptr, ld_kept = None, None, None, 0
+    if keep:
+        kept = torch.empty(2, *shape, dtype=torch.bfloat16, device=dev).unbind(0)
+        g_ptr, u_ptr, ld_kept = _kept(*kept, shape)
+    h_ptr, ld_h = _matrix(h, "h", _BF16)
+    rc = load_library().mxfp4_gated_linear_forward(ctypes.byref(d), h_ptr, ld_h, g_ptr, u_ptr, ld_kept, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_gated_linear_forward")
+    return h, kept
+
+
+def gated_linear_backward(dh, x, w_gate, w_up, kept, act: int = GATE_SILU, dw_dtype: int = OUT_BF16, want_dx: bool = True,
+                          want_dw: bool = True, dx=None, dw_gate=None, dw_up=None, workspace=None):
+    """``mxfp4_gated_linear_backward``: ``(dx, dw_gate, dw_up)`` from the gradient of h and the ``(gate, up)`` that the
+    forward call kept; dx bf16, the weights' of type ``dw_dtype``.  What is not wanted is None."""
+    d = _gated_desc(x, w_gate, w_up, act)
+    (T, D), F, dev = x.shape, w_gate.shape[0], x.device
+    gate, up = kept
+    g_ptr, u_ptr, ld_kept = _kept(gate, up, (T, F))
+    if tuple(dh.shape) != (T, F):
+        raise ValueError("dh must have the shape of h")
+    dh_ptr, ld_dh = _matrix(dh, "dh", _BF16)
+    lib = load_library()
+    dx_ptr = dg_ptr = du_ptr = None
+    ld_dx = ld_dw = 0
+    if want_dx:
+        dx = _output(dx, "dx", (T, D), torch.bfloat16, dev)
+        dx_ptr, ld_dx = _matrix(dx, "dx", _BF16)
+    if want_dw:
+        kind = torch.float32 if dw_dtype == OUT_FP32 else torch.bfloat16
+        dw_gate, dw_up = _output(dw_gate, "dw_gate", (F, D), kind, dev), _output(dw_up, "dw_up", (F, D), kind, dev)
+        (dg_ptr, ld_dw), (du_ptr, ld_du) = _matrix(dw_gate, "dw_gate", (kind,)), _matrix(dw_up, "dw_up", (kind,))
+        if ld_dw != ld_du:
+            raise ValueError("dw_gate and dw_up must have the same row stride")
+    if workspace is None:
+        workspace = torch.empty(max(lib.mxfp4_gated_linear_workspace_bytes(T, F), 1), dtype=torch.uint8, device=dev)
+    _on_current_device(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, workspace)
+    rc = lib.mxfp4_gated_linear_backward(ctypes.byref(d), dh_ptr, ld_dh, g_ptr, u_ptr, ld_kept, dx_ptr, ld_dx, dg_ptr, du_ptr,
+                                         ld_dw, dw_dtype, _dev_ptr(workspace), workspace.numel(), _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_gated_linear_backward")
+    return (dx if want_dx else None, dw_gate if want_dw else None, dw_up if want_dw else None)
+
+
+def _loss_operands(x, w, targets) -> tuple:
+    x_ptr, ld_x = _matrix(x, "x", _BF16)
+    w_ptr, ld_w = _matrix(w, "w", _BF16)
+    (T, D), V = x.shape, w.shape[0]
+    if w.shape[1] != D:
+        raise ValueError("x and w disagree on in_features")
+    return (x_ptr, ld_x, w_ptr, ld_w, T, D, V, _expect(targets, "targets", torch.int64, T) if targets is not None else None)
+
+
+def linear_logprobs_workspace_bytes(tokens: int, in_features: int, vocab: int, backward: bool) -> int:
+    return int(load_library().mxfp4_linear_logprobs_workspace_bytes(tokens, in_features, vocab, int(backward)))
+
+
+def linear_logprobs_forward(x, w, targets=None, scale: float = 1.0, workspace=None):
+    """``mxfp4_linear_logprobs_forward``: ``(logp, lse)``, fp32 [tokens] each, of ``targets`` (int64 [tokens], negative:
+    none; without them logp is None) under the logits ``scale * x w^T``, which are not stored; x bf16 [tokens,
+    in_features], w bf16 [vocab, in_features]."""
+    args = _loss_operands(x, w, targets)
+    T, D, V = args[4:7]
+    logp, lse = torch.empty(2, T, dtype=torch.float32, device=x.device).unbind(0)
+    if workspace is None:
+        workspace = torch.empty(max(linear_logprobs_workspace_bytes(T, D, V, False), 1), dtype=torch.uint8, device=x.device)
+    _on_current_device(x, w, targets, workspace)
+    rc = load_library().mxfp4_linear_logprobs_forward(*args, scale, logp.data_ptr() if targets is not None else None,
+                                                      lse.data_ptr(), _dev_ptr(workspace), workspace.numel(), _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_linear_logprobs_forward")
+    return (logp if targets is not None else None), lse
+
+
+def linear_logprobs_backward(x, w, targets, lse, d_logp=None, d_lse=None, scale: float = 1.0, dw_dtype: int = OUT_BF16,
+                             want_dx: bool = True, want_dw: bool = True, dx=None, dw=None, workspace=None):
+    """``mxfp4_linear_logprobs_backward``: ``(dx, dw)`` from the forward's ``lse`` and the gradients of logp and lse (fp32
+    [tokens], None: zero); dx bf16, dw of type ``dw_dtype``.  What is not wanted is None."""
+    args = _loss_operands(x, w, targets)
+    (T, D, V), dev = args[4:7], x.device
+    row = lambda t, name: _expect(t, name, torch.float32, T) if t is not None else None
+    dx_ptr = dw_ptr = None
+    ld_dx = ld_dw = 0
+    if want_dx:
+        dx = _output(dx, "dx", (T, D), torch.bfloat16, dev)
+        dx_ptr, ld_dx = _matrix(dx, "dx", _BF16)
+    if want_dw:
+        kind = torch.float32 if dw_dtype == OUT_FP32 else torch.bfloat16
+        dw = _output(dw, "dw", (V, D), kind, dev)
+        dw_ptr, ld_dw = _matrix(dw, "dw", (kind,))
+    if workspace is None:
+        workspace = torch.empty(max(linear_logprobs_workspace_bytes(T, D, V, True), 1), dtype=torch.uint8, device=dev)
+    _on_current_device(x, w, targets, lse, d_logp, d_lse, dx, dw, workspace)
+    rc = load_library().mxfp4_linear_logprobs_backward(
+        *args, scale, row(lse, "lse"), row(d_logp, "d_logp"), row(d_lse, "d_lse"), dx_ptr, ld_dx, dw_ptr, ld_dw, dw_dtype,
+        _dev_ptr(workspace), workspace.numel(), _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_linear_logprobs_backward")
+    return (dx if want_dx else None), (dw if want_dw else None)
 
 
 def probe_mma_rate(iterations: int = 10000, random_operands: bool = True) -> float:

@@ -1,0 +1,75 @@
+// Activations of a gate and their derivatives, in fp32.  Sigmoid and tanh come from the exponential of the
+// hardware (2 units in the last place and one division): far below the 2^-9 of a bf16 result.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "../../include/mxfp4.h"
+
+namespace mxfp4 {
+
+__device__ __forceinline__ float exp_neg(float x) { return __expf(-x); }
+
+// 1 / (1 + exp(-x)).  The fast quotient is 0 for a divisor above 2^126: the result is below 2^-126 there.
+__device__ __forceinline__ float logistic(float x) { return __fdividef(1.0f, 1.0f + exp_neg(x)); }
+
+constexpr float kSqrtHalf = 0.70710678118654752f;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+constexpr float kGeluC = 0.79788456080286536f;       // sqrt(2 / pi)
+constexpr float kGeluCubic = 0.044715f;
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float g)
+{
+    if constexpr (ACT == MXFP4_GATE_SIGMOID) return logistic(g);
+    if constexpr (ACT == MXFP4_GATE_SILU) return g * logistic(g);
+    if constexpr (ACT == MXFP4_GATE_GELU) return 0.5f * g * erfcf(-g * kSqrtHalf);
+    // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))
+    if constexpr (ACT == MXFP4_GATE_GELU_TANH) return g * logistic(2.0f * kGeluC * (g + kGeluCubic * g * g * g));
+    if constexpr (ACT == MXFP4_GATE_RELU) return g < 0.0f ? 0.0f : g;         // NaN stays
+    return g;
+}
+
+// value and derivative
+template <int ACT>
+__device__ __forceinline__ float2 act_both(float g)
+{
+    if constexpr (ACT == MXFP4_GATE_SIGMOID) {
+        const float s = logistic(g);
+        return make_float2(s, s * (1.0f - s));
+    }
+    if constexpr (ACT == MXFP4_GATE_SILU) {
+        const float s = logistic(g);
+        return make_float2(g * s, s * (1.0f + g * (1.0f - s)));
+    }
+    if constexpr (ACT == MXFP4_GATE_GELU) {
+        const float cdf = 0.5f * erfcf(-g * kSqrtHalf);
+        return make_float2(g * cdf, cdf + g * kInvSqrt2Pi * __expf(-0.5f * g * g));
+    }
+    if constexpr (ACT == MXFP4_GATE_GELU_TANH) {
+        const float s = logistic(2.0f * kGeluC * (g + kGeluCubic * g * g * g));
+        const float slope = kGeluC * (1.0f + 3.0f * kGeluCubic * g * g);
+        return make_float2(g * s, s + 2.0f * g * s * (1.0f - s) * slope);
+    }
+    if constexpr (ACT == MXFP4_GATE_RELU) return make_float2(g < 0.0f ? 0.0f : g, g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g);
+    return make_float2(g, 1.0f);
+}
+
+// Calls f with the activation as a compile-time constant: one uniform branch for a stretch of elements.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f)
+{
+    switch (act) {
+        case MXFP4_GATE_SIGMOID: f(std::integral_constant<int, MXFP4_GATE_SIGMOID>{}); break;
+        case MXFP4_GATE_SILU: f(std::integral_constant<int, MXFP4_GATE_SILU>{}); break;
+        case MXFP4_GATE_GELU: f(std::integral_constant<int, MXFP4_GATE_GELU>{}); break;
+        case MXFP4_GATE_GELU_TANH: f(std::integral_constant<int, MXFP4_GATE_GELU_TANH>{}); break;
+        case MXFP4_GATE_RELU: f(std::integral_constant<int, MXFP4_GATE_RELU>{}); break;
+        default: f(std::integral_constant<int, MXFP4_GATE_LINEAR>{}); break;
+    }
+}
+
+}  // namespace mxfp4

@@ -1,0 +1,428 @@
+// Product of 16-bit matrices with a fused epilogue: D[m][n] = sum_k A[m][k] * B[n][k], fp32 sums in tensor memory.
+//
+// CTA-pair kernel (tcgen05 cta_group::2, kind::f16) on 256 x 256 output tiles: each CTA holds 128 rows of A and 128
+// rows of B per K-step of 64 elements (32 KB), six steps in flight, two accumulators of 256 columns (all of
+// tensor memory), so that the epilogue of one tile runs under the products of the next.
+//
+// Either operand may be stored along K (rows of A, of B) or along its own rows (the transposed matrix, as the
+// gradients need it): a K-step is then fetched as two boxes of 64 columns x 64 rows, and the shared-memory
+// descriptor names the transposed layout.  No transposed copy exists anywhere.
+//
+// Two matrices of the same shape may stand in for one along M (both weight gradients of a pair of projections in
+// one launch) or along K (the input's gradient, a sum of two products).
+//
+// Epilogues:
+//   kDenseBf16, kDenseF32   the sums, rounded or not
+//   kDenseAddF32            added to the fp32 output by the copy engine; one addition per element and launch,
+//                           so results do not depend on scheduling
+//   kDenseGated             columns 0..127 of a tile are a gate's, 128..255 the other projection's of the same features
+//                           (the pair's first CTA loads the rows of one weight, the second those of the other): act(g) * u,
+//                           and g and u on request
+//   kDensePartials          maximum and sum of exponentials of each row's 128 columns, and the target's value
+//   kDenseLogitGrad         gradient of the log probabilities with respect to the logits, rounded to bf16
+//
+// Roles per CTA (320 threads): warps 0..7 epilogue (32 rows x 128 columns each), warp 8 TMA producer, warp 9 MMA
+// issuer (leader CTA only).  Barrier ownership: full and tmem_empty live in the leader, empty and tmem_full are signalled
+// in both CTAs by a multicast commit.  All waits are bounded.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <type_traits>
+
+#include "../../include/mxfp4.h"
+#include "activations.cuh"
+#include "dense_gemm.cuh"
+#include "ptx_sm100.cuh"
+#include "row_io.cuh"
+
+namespace mxfp4 {
+
+constexpr int kDTile = 256;                        // both ways
+constexpr int kDHalf = 128;                        // rows of A, and of B, per CTA
+constexpr int kDBlockK = 64;                       // elements: 128 bytes
+constexpr int kDStages = 6;
+constexpr int kDOperandBytes = kDHalf * kDBlockK * 2;
+constexpr int kDBoxBytes = kDOperandBytes / 2;     // 64 columns x 64 rows of a transposed operand
+constexpr int kDEpiWarps = 8;
+constexpr int kDProducerWarp = 8;
+constexpr int kDMmaWarp = 9;
+constexpr int kDThreads = 320;
+constexpr int kDStageBytes = 32 * 128;             // output staging per epilogue warp
+
+struct DenseSmem {
+    alignas(1024) uint8_t a[kDStages][kDOperandBytes];
+    alignas(1024) uint8_t b[kDStages][kDOperandBytes];
+    alignas(1024) uint8_t out_stage[kDEpiWarps][kDStageBytes];
+    alignas(16) uint64_t full[kDStages];           // leader's copy is the live one
+    uint64_t empty[kDStages];                      // both, via multicast commit
+    uint64_t tmem_full[2];                         // both, via multicast commit
+    uint64_t tmem_empty[2];                        // leader's copy is the live one
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+struct DenseMaps {
+    CUtensorMap a[2], b[2], out[3];
+};
+
+// Row and column of a tile.  Tiles are numbered band by band: a band is `band` tile columns, and inside it the tile
+// column varies fastest, so that the tiles in flight share rows of A and of B.
+__device__ __forceinline__ void dense_place(const DenseParams& p, int tile, int& tm, int& tn)
+{
+    const int per_band = p.band * p.tiles_m;
+    const int b = tile / per_band;
+    const int r = tile - b * per_band;
+    const int cols = min(p.band, p.tiles_n - b * p.band);
+    tm = r / cols;
+    tn = b * p.band + (r - tm * cols);
+}
+
+// One operand of a K-step: 128 rows x 64 elements of K, or the transposed 64 x 128 in two boxes.
+template <bool MN>
+__device__ __forceinline__ void dense_load(uint8_t* to, const CUtensorMap* map, uint32_t bar, int row, int k)
+{
+    if (MN) {
+        tma_load_2d_pair(to, map, bar, row, k);
+        tma_load_2d_pair(to + kDBoxBytes, map, bar, row + 64, k);
+    } else {
+        tma_load_2d_pair(to, map, bar, k, row);
+    }
+}
+
+// eight sums as bf16
+__device__ __forceinline__ uint4 dense_pack8(const uint32_t* v)
+{
+    auto two = [&](int i) { return pack_bf16(__uint_as_float(v[i]), __uint_as_float(v[i + 1])); };
+    return make_uint4(two(0), two(2), two(4), two(6));
+}
+
+// exp(x) of a difference to a maximum or a normaliser
+__device__ __forceinline__ float dense_exp(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+    return r;
+}
+
+template <int EPI, bool A_MN, bool B_MN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDThreads, 1)
+dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    DenseSmem& sm = *reinterpret_cast<DenseSmem*>(smem_align_1024(smem_raw));
+    const int warp = threadIdx.x >> 5;
+    const int lane = lane_id();
+    const uint32_t rank = cluster_ctarank();
+    const int cluster_id = blockIdx.x >> 1;
+    const int n_clusters = gridDim.x >> 1;
+    const int tiles = p.tiles_m * p.tiles_n;
+    constexpr bool kGated = EPI == kDenseGated;
+
+    if (threadIdx.x == 0) {
+        sm.abort_flag = 0;
+        for (int s = 0; s < kDStages; ++s) {
+            mbar_init(&sm.full[s], 2);                 // one arrive.expect_tx per CTA
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sm.tmem_full[b], 1);
+            mbar_init(&sm.tmem_empty[b], 2 * kDEpiWarps);
+        }
+        fence_barrier_init();
+    }
+    if (warp == kDMmaWarp) {
+        tmem_alloc_pair(&sm.tmem_base, 512);
+        tmem_relinquish_pair();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync_all();           // both CTAs' barriers exist before anyone signals across the pair
+    tcgen05_fence_after();
+    const uint32_t tmem = sm.tmem_base;
+    griddep_launch_dependents();
+    griddep_wait();
+
+    if (warp == kDProducerWarp) {
+        // ------------------------------------------------------------ TMA producer
+        if (elect_one_sync()) {
+            int s = 0;
+            uint32_t parity = 1;                       // of the phase before: a fresh barrier passes
+            bool alive = true;
+            for (int tile = cluster_id; alive && tile < tiles; tile += n_clusters) {
+                int tm, tn;
+                dense_place(p, tile, tm, tn);
+                const int seg_m = tm >= p.seg_tiles_m;
+                const int ya = (tm - seg_m * p.seg_tiles_m) * kDTile + static_cast<int>(rank) * kDHalf;
+                const int yb = kGated ? tn * kDHalf : tn * kDTile + static_cast<int>(rank) * kDHalf;
+                for (int k = 0; k < p.k_steps; ++k) {
+                    if (!mbar_wait(&sm.empty[s], parity, &sm.abort_flag)) {
+                        alive = false;
+                        break;
+                    }
+                    const int seg_k = k >= p.seg_k_steps;
+                    const int kk = (k - seg_k * p.seg_k_steps) * kDBlockK;
+                    const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
+                    mbar_arrive_expect_tx_cluster(full, 2 * kDOperandBytes);
+                    dense_load<A_MN>(sm.a[s], &maps.a[seg_m + seg_k], full, ya, kk);
+                    dense_load<B_MN>(sm.b[s], &maps.b[kGated ? rank : seg_k], full, yb, kk);
+                    if (++s == kDStages) {
+                        s = 0;
+                        parity ^= 1;
+                    }
+                }
+            }
+            // the last stages' release signals: one that arrived after the CTA is gone would be counted on a barrier
+            // of the next launch
+            for (int i = 0; alive && i < kDStages; ++i) {
+                alive = mbar_wait(&sm.empty[s], parity, &sm.abort_flag);
+                if (++s == kDStages) {
+                    s = 0;
+                    parity ^= 1;
+                }
+            }
+            if (!alive) linger();      // given up: what is in flight lands before the CTA leaves
+        }
+        __syncwarp();
+    } else if (warp == kDMmaWarp) {
+        // ------------------------------------------------------------ MMA issuer
+        if (rank == 0 && elect_one_sync()) {
+            // fp32 accumulator, bf16 x bf16, 256 x 256 x 16
+            constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                                       (static_cast<uint32_t>(kDTile >> 3) << 17) | (static_cast<uint32_t>(kDTile >> 4) << 24);
+            // along K: 8-row groups 1024 bytes apart, an instruction's 16 elements are 32 bytes; transposed: 64-column boxes
+            // 8 KB apart, 8-row groups of K 1024 bytes apart, 16 rows are 2 KB
+            const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), A_MN ? kDBoxBytes : 16, 1024, 2);
+            const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), B_MN ? kDBoxBytes : 16, 1024, 2);
+            constexpr int kStepA = A_MN ? 128 : 2, kStepB = B_MN ? 128 : 2;
+            int s = 0, b = 0;
+            uint32_t parity = 0, buf_parity = 1;       // a fresh tmem_empty passes for the phase before
+            bool alive = true;
+            for (int tile = cluster_id; alive && tile < tiles; tile += n_clusters) {
+                if (!mbar_wait(&sm.tmem_empty[b], buf_parity, &sm.abort_flag)) break;
+                tcgen05_fence_after();
+                for (int k = 0; k < p.k_steps; ++k) {
+                    if (!mbar_wait(&sm.full[s], parity, &sm.abort_flag)) {
+                        alive = false;
+                        break;
+                    }
+                    tcgen05_fence_after();
+                    const int kk = (k >= p.seg_k_steps ? k - p.seg_k_steps : k) * kDBlockK;
+                    const int nmma = (min(kDBlockK, p.K - kk) + 15) / 16;      // what lies past K is filled with zeros
+                    const uint64_t a_desc = a_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
+                    const uint64_t b_desc = b_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
+#pragma unroll
+                    for (int j = 0; j < kDBlockK / 16; ++j)
+                        if (j < nmma)
+                            tcgen05_mma_f16_pair(tmem + b * kDTile, a_desc + kStepA * j, b_desc + kStepB * j, idesc, (k | j) > 0);
+                    tcgen05_commit_pair(&sm.empty[s], 3);
+                    if (++s == kDStages) {
+                        s = 0;
+                        parity ^= 1;
+                    }
+                }
+                if (alive) tcgen05_commit_pair(&sm.tmem_full[b], 3);
+                buf_parity ^= b;
+                b ^= 1;
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ epilogue warps
+        const int quad = warp & 3;                     // TMEM lane quadrant of this warp
+        const int half = warp >> 2;                    // which 128 columns
+        uint8_t* stg = sm.out_stage[warp];
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t tmem_empty_leader = map_to_cta(smem_u32(&sm.tmem_empty[0]), 0);
+        // 32 rows x 128 bytes, staged in the 128-byte swizzle for a TMA store that clips at the matrix edges
+        auto stage_wait = [&]() {
+            if (lane == 0) bulk_wait_group_read<0>();
+            __syncwarp();
+        };
+        auto stage_put = [&](int q, const uint4& v) {
+            smem_store(stg + lane * 128 + ((q ^ (lane & 7)) * 16), v, stg, kDStageBytes);
+        };
+        auto stage_store = [&](const CUtensorMap* map, int col, int row) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (EPI == kDenseAddF32) tma_add_2d(map, stg, col, row);
+                else tma_store_2d(map, stg, col, row);
+                bulk_commit_group();
+            }
+        };
+        int b = 0;
+        uint32_t parity = 0;
+        for (int tile = cluster_id; tile < tiles; tile += n_clusters) {
+            int tm, tn;
+            dense_place(p, tile, tm, tn);
+            const int seg_m = tm >= p.seg_tiles_m;
+            const int row0 = (tm - seg_m * p.seg_tiles_m) * kDTile + static_cast<int>(rank) * kDHalf + quad * 32;
+            const int row = row0 + lane;
+            if (!mbar_wait(&sm.tmem_full[b], parity, &sm.abort_flag)) break;       // given up: nothing more is stored
+            tcgen05_fence_after();
+            const uint32_t from = lanes + b * kDTile;
+            auto hand_back = [&]() {
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + b * 8);
+            };
+            uint32_t r[32];
+            auto read = [&](int col) {
+                tmem_ld_32x32b_x32(from + col, r);
+                tmem_ld_wait_for(r);
+            };
+            if (row0 >= p.M) {                         // warp-uniform: no rows here
+                hand_back();
+            } else if constexpr (EPI == kDenseBf16 || EPI == kDenseF32 || EPI == kDenseAddF32) {
+                const int col0 = tn * kDTile + half * kDHalf;
+                constexpr bool k32 = EPI != kDenseBf16;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int col = col0 + c * 32;
+                    if (col < p.N) {
+                        read(half * kDHalf + c * 32);
+                        if (k32 || (c & 1) == 0) stage_wait();
+#pragma unroll
+                        for (int q = 0; q < (k32 ? 8 : 4); ++q) {
+                            const uint32_t* v = r + q * (k32 ? 4 : 8);
+                            if constexpr (k32) stage_put(q, make_uint4(v[0], v[1], v[2], v[3]));
+                            else stage_put((c & 1) * 4 + q, dense_pack8(v));
+                        }
+                    }
+                    if (k32 ? col < p.N : (c & 1) != 0 && col - 32 < p.N)
+                        stage_store(&maps.out[seg_m], k32 ? col : col - 32, row0);
+                }
+                hand_back();
+            } else if constexpr (EPI == kDenseGated) {
+                const int col0 = tn * kDHalf + half * 64;
+                if (col0 < p.N) {
+                    uint4 gate[8], up[8];              // as stored, eight features each
+                    stage_wait();
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t u[32];
+                        tmem_ld_32x32b_x32(from + kDHalf + half * 64 + c * 32, u);
+                        read(half * 64 + c * 32);
+                        tmem_ld_wait_for(u);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            gate[c * 4 + q] = dense_pack8(r + 8 * q);
+                            up[c * 4 + q] = dense_pack8(u + 8 * q);
+                        }
+                        with_act(p.act, [&](auto act) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                r[i] = __float_as_uint(act_value<decltype(act)::value>(__uint_as_float(r[i])) *
+                                                       __uint_as_float(u[i]));
+                        });
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) stage_put(c * 4 + q, dense_pack8(r + 8 * q));
+                    }
+                    hand_back();
+                    stage_store(&maps.out[0], col0, row0);
+                    if (p.keep) {
+                        stage_wait();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) stage_put(q, gate[q]);
+                        stage_store(&maps.out[1], col0, row0);
+                        stage_wait();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) stage_put(q, up[q]);
+                        stage_store(&maps.out[2], col0, row0);
+                    }
+                } else {
+                    hand_back();
+                }
+            } else {
+                // rows of logits
+                const int col0 = tn * kDTile + half * kDHalf;
+                const bool row_ok = row < p.M;
+                const int64_t target = row_ok && p.targets ? p.targets[row] : -1;
+                const int at = target >= p.col_base + col0 && target < p.col_base + col0 + kDHalf
+                                   ? static_cast<int>(target - p.col_base - col0) : -1;
+                const bool any_here = __any_sync(0xffffffffu, at >= 0);
+                if constexpr (EPI == kDensePartials) {
+                    if (col0 < p.N) {
+                        float m = -INFINITY, sum = 0.0f, picked = 0.0f;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            read(half * kDHalf + c * 32);
+                            float z[32], top = m;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                z[i] = __uint_as_float(r[i]) * p.scale;
+                                if (col0 + c * 32 + i >= p.N) z[i] = -INFINITY;
+                                top = fmaxf(top, z[i]);
+                            }
+                            if (any_here) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (c * 32 + i == at) picked = z[i];
+                            }
+                            // a row of nothing but -infinity so far has sum 0; a NaN passes the maximum by and enters the sum
+                            const float ref = top == -INFINITY ? 0.0f : top;
+                            sum *= dense_exp(m - ref);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) sum += dense_exp(z[i] - ref);
+                            m = top;
+                        }
+                        hand_back();
+                        if (row_ok) {
+                            p.parts[static_cast<int64_t>(tn * 2 + half) * p.ld_parts + row] = make_float2(m, sum);
+                            if (at >= 0 && target < p.col_base + p.N) p.picked[row] = picked;
+                        }
+                    } else {
+                        hand_back();
+                    }
+                } else {
+                    const float lse = row_ok ? p.lse[row] : 0.0f;
+                    float gl = row_ok && p.d_logp && target >= 0 ? p.d_logp[row] : 0.0f;
+                    const float gn = row_ok && p.d_lse ? p.d_lse[row] : 0.0f;
+                    if (target >= p.vocab) gl = NAN;
+                    const bool zero = (gl == 0.0f && gn == 0.0f);
+                    const float coef = p.scale * (gn - gl);
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        const int col = col0 + c * 32;
+                        if (col < p.ld_grad) {
+                            read(half * kDHalf + c * 32);
+                            if ((c & 1) == 0) stage_wait();
+                            float z[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                z[i] = coef * dense_exp(__uint_as_float(r[i]) * p.scale - lse);
+                                if (zero || col + i >= p.N) z[i] = 0.0f;
+                            }
+                            if (any_here) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (c * 32 + i == at) z[i] += p.scale * gl;
+                            }
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                stage_put((c & 1) * 4 + q, dense_pack8(reinterpret_cast<uint32_t*>(z) + 8 * q));
+                        }
+                        if ((c & 1) != 0 && col - 32 < p.ld_grad) stage_store(&maps.out[0], col - 32, row0);
+                    }
+                    hand_back();
+                }
+            }
+            parity ^= b;
+            b ^= 1;
+        }
+        if (lane == 0) bulk_wait_group<0>();
+    }
+
+    // neither CTA may leave (or free TMEM) while its peer can still signal it or read its memory
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == kDMmaWarp) {
+        tcgen05_fence_after();
+        tmem_dealloc_pair(tmem, 512);
+    }
+}
+
+}  // namespace mxfp4

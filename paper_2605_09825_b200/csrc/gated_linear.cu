@@ -1,0 +1,184 @@
+// Gated projections of a feed-forward block kept in 16 bits (see include/mxfp4.h): argument checks, the products
+// (dense_gemm_kernel.cuh) and the elementwise step of the backward pass.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/mxfp4.h"
+#include "activations.cuh"
+#include "dense_gemm.cuh"
+#include "host_common.cuh"
+#include "row_io.cuh"
+#include "ptx_sm100.cuh"
+#include "tma_host.cuh"
+
+namespace mxfp4 {
+
+// dg = dh * u * act'(g), du = dh * act(g), rounded to bf16: they are operands of the tensor cores' products, whose sums
+// over hundreds of them are off by about 2^-9 / sqrt(3) of their value, less than the rounding of a bf16 result.
+// Eight elements per thread and step, bound by memory: 10 bytes per element.
+struct GatedGradParams {
+    const __nv_bfloat16* dh;
+    const __nv_bfloat16* gate;
+    const __nv_bfloat16* up;
+    __nv_bfloat16* dg;           // [tokens x features]
+    __nv_bfloat16* du;
+    int64_t ld_dh, ld_kept;
+    int64_t items;               // tokens * features / 8
+    int32_t per_row;             // features / 8
+    int32_t act;
+};
+
+constexpr int kGradThreads = 256;
+
+__global__ void __launch_bounds__(kGradThreads) gated_grad_kernel(const GatedGradParams p)
+{
+    griddep_launch_dependents();
+    griddep_wait();
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kGradThreads;
+    with_act(p.act, [&](auto act) {
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kGradThreads + threadIdx.x; i < p.items; i += stride) {
+            const int64_t row = i / p.per_row;
+            const int64_t col = (i - row * p.per_row) * 8;
+            float2 dh[4], g[4], u[4], a[4], b[4];
+            const uint4 w0 = ld_stream(p.dh + row * p.ld_dh + col);
+            const uint4 w1 = ld_stream(p.gate + row * p.ld_kept + col);
+            const uint4 w2 = ld_stream(p.up + row * p.ld_kept + col);
+            unpack8(w0, dh);
+            unpack8(w1, g);
+            unpack8(w2, u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 x = act_both<decltype(act)::value>(g[j].x), y = act_both<decltype(act)::value>(g[j].y);
+                a[j] = make_float2(dh[j].x * u[j].x * x.y, dh[j].y * u[j].y * y.y);
+                b[j] = make_float2(dh[j].x * x.x, dh[j].y * y.x);
+            }
+            *reinterpret_cast<uint4*>(p.dg + i * 8) = pack8(a);
+            *reinterpret_cast<uint4*>(p.du + i * 8) = pack8(b);
+        }
+    });
+}
+
+// Sizes, leading dimensions and alignment of what both directions read.
+static int gated_check(const mxfp4_gated_desc* d)
+{
+    if (!d || !d->x || !d->w_gate || !d->w_up) return MXFP4_ERR_NULL;
+    if (d->act < MXFP4_GATE_LINEAR || d->act > MXFP4_GATE_RELU) return MXFP4_ERR_ENUM;
+    if (d->tokens <= 0 || d->in_features <= 0 || d->features <= 0 || d->in_features % 8 != 0 || d->features % 8 != 0)
+        return MXFP4_ERR_SHAPE;
+    if (d->tokens > kDenseMaxDim || d->in_features > kDenseMaxDim || d->features > kDenseMaxDim) return MXFP4_ERR_SHAPE;
+    if (d->ld_x < d->in_features || d->ld_gate < d->in_features || d->ld_up < d->in_features) return MXFP4_ERR_SHAPE;
+    if (!aligned16(d->x) || !aligned16(d->w_gate) || !aligned16(d->w_up) || d->ld_x % 8 != 0 || d->ld_gate % 8 != 0 ||
+        d->ld_up % 8 != 0)
+        return MXFP4_ERR_ALIGN;
+    return MXFP4_OK;
+}
+
+}  // namespace mxfp4
+
+using namespace mxfp4;
+
+extern "C" {
+
+int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h, void* gate, void* up, int64_t ld_kept,
+                               void* stream)
+{
+    int rc = gated_check(d);
+    if (rc != MXFP4_OK) return rc;
+    if (!h || (gate == nullptr) != (up == nullptr)) return MXFP4_ERR_NULL;
+    if (ld_h < d->features || (gate && ld_kept < d->features)) return MXFP4_ERR_SHAPE;
+    if (!aligned16(h) || ld_h % 8 != 0 || (gate && (!aligned16(gate) || !aligned16(up) || ld_kept % 8 != 0)))
+        return MXFP4_ERR_ALIGN;
+    const DeviceInfo& dev = device_info();
+    if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
+    DenseCall c;
+    c.epilogue = kDenseGated;
+    c.a[0] = {d->x, d->ld_x};
+    c.b[0] = {d->w_gate, d->ld_gate};
+    c.b[1] = {d->w_up, d->ld_up};
+    c.out[0] = {h, ld_h};
+    c.out[1] = {gate, ld_kept};
+    c.out[2] = {up, ld_kept};
+    c.p.M = static_cast<int32_t>(d->tokens);
+    c.p.N = static_cast<int32_t>(d->features);
+    c.p.K = static_cast<int32_t>(d->in_features);
+    c.p.act = d->act;
+    c.p.keep = gate != nullptr;
+    return dense_launch(c, dev.sm_count, static_cast<cudaStream_t>(stream));
+}
+
+size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t features)
+{
+    if (tokens <= 0 || features <= 0 || features % 8 != 0 || tokens > kDenseMaxDim || features > kDenseMaxDim) return 0;
+    return 2 * round_up(static_cast<size_t>(tokens) * features * 2, 256);
+}
+
+int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64_t ld_dh, const void* gate, const void* up,
+                                int64_t ld_kept, void* dx, int64_t ld_dx, void* dw_gate, void* dw_up, int64_t ld_dw,
+                                int dw_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = gated_check(d);
+    if (rc != MXFP4_OK) return rc;
+    if (!dh || !gate || !up || (dw_gate == nullptr) != (dw_up == nullptr) || (!dx && !dw_gate)) return MXFP4_ERR_NULL;
+    if (dw_dtype != MXFP4_OUT_BF16 && dw_dtype != MXFP4_OUT_FP32) return MXFP4_ERR_ENUM;
+    if (ld_dh < d->features || ld_kept < d->features || (dx && ld_dx < d->in_features) || (dw_gate && ld_dw < d->in_features))
+        return MXFP4_ERR_SHAPE;
+    if (!aligned16(dh) || !aligned16(gate) || !aligned16(up) || ld_dh % 8 != 0 || ld_kept % 8 != 0 ||
+        (dx && (!aligned16(dx) || ld_dx % 8 != 0)) || (dw_gate && (!aligned16(dw_gate) || !aligned16(dw_up) || ld_dw % 8 != 0)))
+        return MXFP4_ERR_ALIGN;
+    const size_t need = mxfp4_gated_linear_workspace_bytes(d->tokens, d->features);
+    if (!workspace || workspace_bytes < need) return MXFP4_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return MXFP4_ERR_ALIGN;
+    const DeviceInfo& dev = device_info();
+    if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+
+    GatedGradParams g;
+    g.dh = static_cast<const __nv_bfloat16*>(dh);
+    g.gate = static_cast<const __nv_bfloat16*>(gate);
+    g.up = static_cast<const __nv_bfloat16*>(up);
+    g.dg = static_cast<__nv_bfloat16*>(workspace);
+    g.du = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(workspace) + need / 2);
+    g.ld_dh = ld_dh;
+    g.ld_kept = ld_kept;
+    g.items = d->tokens * (d->features / 8);
+    g.per_row = static_cast<int32_t>(d->features / 8);
+    g.act = d->act;
+    const int64_t blocks = (g.items + kGradThreads - 1) / kGradThreads;
+    const int64_t most = 8 * static_cast<int64_t>(dev.sm_count);
+    if (launch_kernel_pdl(gated_grad_kernel, static_cast<int>(blocks < most ? blocks : most), kGradThreads, 0, st, g) !=
+        cudaSuccess)
+        return MXFP4_ERR_CUDA;
+    const DenseMatrix mg = {g.dg, d->features}, mu = {g.du, d->features};
+    if (dx) {
+        DenseCall c;                       // dx = dg Wg + du Wu
+        c.epilogue = kDenseBf16;
+        c.b_mn = c.stack_k = true;
+        c.a[0] = mg;
+        c.a[1] = mu;
+        c.b[0] = {d->w_gate, d->ld_gate};
+        c.b[1] = {d->w_up, d->ld_up};
+        c.out[0] = {dx, ld_dx};
+        c.p.M = static_cast<int32_t>(d->tokens);
+        c.p.N = static_cast<int32_t>(d->in_features);
+        c.p.K = static_cast<int32_t>(d->features);
+        if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+    }
+    if (dw_gate) {
+        DenseCall c;                       // dWg = dg^T x, dWu = du^T x
+        c.epilogue = dw_dtype == MXFP4_OUT_FP32 ? kDenseF32 : kDenseBf16;
+        c.a_mn = c.b_mn = c.stack_m = true;
+        c.a[0] = mg;
+        c.a[1] = mu;
+        c.b[0] = {d->x, d->ld_x};
+        c.out[0] = {dw_gate, ld_dw};
+        c.out[1] = {dw_up, ld_dw};
+        c.p.M = static_cast<int32_t>(d->features);
+        c.p.N = static_cast<int32_t>(d->in_features);
+        c.p.K = static_cast<int32_t>(d->tokens);
+        if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+    }
+    return MXFP4_OK;
+}
+
+}  // extern "C"

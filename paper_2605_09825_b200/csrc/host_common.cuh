@@ -110,5 +110,6 @@ static inline int take_unit_status(int* status)
 int block128_take_status(int* status);
 int residual_norm_take_status(int* status);
 int logprobs_take_status(int* status);
+int dense_take_status(int* status);
 
 }  // namespace mxfp4

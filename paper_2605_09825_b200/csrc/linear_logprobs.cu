@@ -1,0 +1,269 @@
+// Log probabilities of given tokens from an output layer's input and weight (see include/mxfp4.h).
+//
+// Forward: the logits' product leaves only a maximum and a sum of exponentials per row and 128 columns, and the target's
+// value; a second kernel joins them.  Backward, piece by piece of the vocabulary: the piece's logits again, whose
+// epilogue forms their gradient (bf16, in the workspace), then its product with the piece of the weight, added to the
+// input's gradient in fp32, and with the input, which is the piece of the weight's gradient.
+//
+// The gradient of the logits is rounded to bf16 because it is an operand of the tensor cores' products: sums over
+// hundreds of them are off by about 2^-9 / sqrt(3) of their value, less than the rounding of a bf16 result.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/mxfp4.h"
+#include "dense_gemm.cuh"
+#include "host_common.cuh"
+#include "row_io.cuh"
+#include "ptx_sm100.cuh"
+#include "tma_host.cuh"
+
+namespace mxfp4 {
+
+// Rows per forward product: bounds the partial results' memory (131 MB at a vocabulary of 128256) with tens of thousands
+// of tiles in a launch.
+constexpr int64_t kLossRows = 16384;
+
+struct LossJoinParams {
+    const float2* parts;         // [pieces][ld_parts]
+    const float* picked;
+    const int64_t* targets;
+    float* logp;
+    float* lse;
+    int64_t ld_parts, vocab;
+    int32_t rows, pieces;
+};
+
+constexpr int kJoinWarps = 8;
+
+// 32 rows per CTA, one per lane; the warps take every eighth partial result and are joined in their order.
+__global__ void __launch_bounds__(kJoinWarps * 32) loss_join_kernel(const LossJoinParams p)
+{
+    __shared__ float2 part[kJoinWarps][32];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row = blockIdx.x * 32 + lane;
+    // sums are relative to the maximum so far; while that is -infinity they are 0
+    auto join = [](float2& a, const float2& b) {
+        const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.0f : m;
+        a = make_float2(m, a.y * __expf(a.x - ref) + b.y * __expf(b.x - ref));
+    };
+    float2 v = make_float2(-INFINITY, 0.0f);
+    if (row < p.rows) {
+#pragma unroll 4
+        for (int i = warp; i < p.pieces; i += kJoinWarps) join(v, p.parts[i * p.ld_parts + row]);
+    }
+    smem_store(&part[warp][lane], v, part, sizeof(part));
+    __syncthreads();
+    if (warp != 0 || row >= p.rows) return;
+    for (int w = 1; w < kJoinWarps; ++w) join(v, smem_load<float2>(&part[w][lane], part, sizeof(part)));
+    const float total = logf(v.y);
+    p.lse[row] = v.x + total;                              // -infinity - infinity where all are masked
+    if (!p.logp) return;
+    const int64_t t = p.targets[row];
+    float logp = 0.0f;
+    if (t >= p.vocab) logp = NAN;
+    else if (t >= 0) logp = v.y == 0.0f ? -INFINITY : (p.picked[row] - v.x) - total;
+    p.logp[row] = logp;
+}
+
+struct RoundRowsParams {
+    const float* from;           // [rows x cols]
+    __nv_bfloat16* to;
+    int64_t ld, items;           // items: rows * cols / 8
+    int32_t per_row;
+};
+
+__global__ void __launch_bounds__(256) round_rows_kernel(const RoundRowsParams p)
+{
+    griddep_launch_dependents();
+    griddep_wait();
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < p.items; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = i / p.per_row, col = (i - row * p.per_row) * 8;
+        const float4 a = *reinterpret_cast<const float4*>(p.from + i * 8), b = *reinterpret_cast<const float4*>(p.from + i * 8 + 4);
+        const float2 v[4] = {make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)};
+        *reinterpret_cast<uint4*>(p.to + row * p.ld + col) = pack8(v);
+    }
+}
+
+// Columns of the vocabulary per piece of the backward pass: 256 MB of gradients, at least 8192 columns, so that the fp32
+// sums of dx, which every piece reads and writes once, stay a small part of the traffic.
+static int64_t loss_piece(int64_t tokens, int64_t vocab)
+{
+    int64_t cols = (int64_t{1} << 27) / tokens / 256 * 256;
+    if (cols < 8192) cols = 8192;
+    return cols < vocab ? cols : vocab;
+}
+
+static size_t loss_grad_bytes(int64_t tokens, int64_t vocab)
+{
+    return round_up(static_cast<size_t>(tokens) * round_up(loss_piece(tokens, vocab), 8) * 2, 256);
+}
+
+static int loss_check(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t tokens, int64_t in_features,
+                      int64_t vocab, float scale)
+{
+    if (!x || !w) return MXFP4_ERR_NULL;
+    if (!(scale > 0.0f) || isinf(scale)) return MXFP4_ERR_ENUM;
+    if (tokens <= 0 || in_features <= 0 || vocab <= 0 || in_features % 8 != 0 || tokens > kDenseMaxDim ||
+        in_features > kDenseMaxDim || vocab > kDenseMaxDim)
+        return MXFP4_ERR_SHAPE;
+    if (ld_x < in_features || ld_w < in_features) return MXFP4_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(w) || ld_x % 8 != 0 || ld_w % 8 != 0) return MXFP4_ERR_ALIGN;
+    return MXFP4_OK;
+}
+
+}  // namespace mxfp4
+
+using namespace mxfp4;
+
+extern "C" {
+
+size_t mxfp4_linear_logprobs_workspace_bytes(int64_t tokens, int64_t in_features, int64_t vocab, int backward)
+{
+    if (tokens <= 0 || in_features <= 0 || vocab <= 0 || in_features % 8 != 0 || tokens > kDenseMaxDim ||
+        in_features > kDenseMaxDim || vocab > kDenseMaxDim)
+        return 0;
+    if (backward) {
+        const bool one = loss_piece(tokens, vocab) == vocab;
+        return loss_grad_bytes(tokens, vocab) + (one ? 0 : static_cast<size_t>(tokens) * in_features * 4);
+    }
+    const size_t rows = round_up(static_cast<size_t>(tokens < kLossRows ? tokens : kLossRows), 32);
+    return rows * static_cast<size_t>(dense_tiles(vocab, 128)) * sizeof(float2) + rows * sizeof(float);
+}
+
+int mxfp4_linear_logprobs_forward(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t tokens,
+                                  int64_t in_features, int64_t vocab, const int64_t* targets, float scale, float* logp,
+                                  float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = loss_check(x, ld_x, w, ld_w, tokens, in_features, vocab, scale);
+    if (rc != MXFP4_OK) return rc;
+    if (!lse || (targets == nullptr) != (logp == nullptr)) return MXFP4_ERR_NULL;
+    const size_t need = mxfp4_linear_logprobs_workspace_bytes(tokens, in_features, vocab, 0);
+    if (!workspace || workspace_bytes < need) return MXFP4_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return MXFP4_ERR_ALIGN;
+    const DeviceInfo& dev = device_info();
+    if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int64_t pitch = round_up(static_cast<size_t>(tokens < kLossRows ? tokens : kLossRows), 32);
+    const int64_t pieces = dense_tiles(vocab, 128);
+    for (int64_t r = 0; r < tokens; r += kLossRows) {
+        const int64_t rows = tokens - r < kLossRows ? tokens - r : kLossRows;
+        DenseCall c;
+        c.epilogue = kDensePartials;
+        c.a[0] = {static_cast<const __nv_bfloat16*>(x) + r * ld_x, ld_x};
+        c.b[0] = {w, ld_w};
+        c.p.M = static_cast<int32_t>(rows);
+        c.p.N = static_cast<int32_t>(vocab);
+        c.p.K = static_cast<int32_t>(in_features);
+        c.p.vocab = vocab;
+        c.p.targets = targets ? targets + r : nullptr;
+        c.p.scale = scale;
+        c.p.parts = static_cast<float2*>(workspace);
+        c.p.ld_parts = pitch;
+        c.p.picked = reinterpret_cast<float*>(c.p.parts + pitch * pieces);
+        if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        LossJoinParams j;
+        j.parts = c.p.parts;
+        j.picked = c.p.picked;
+        j.targets = c.p.targets;
+        j.logp = logp ? logp + r : nullptr;
+        j.lse = lse + r;
+        j.ld_parts = pitch;
+        j.vocab = vocab;
+        j.rows = c.p.M;
+        j.pieces = static_cast<int32_t>(pieces);
+        if (launch_kernel_pdl(loss_join_kernel, (j.rows + 31) / 32, kJoinWarps * 32, 0, st, j) != cudaSuccess)
+            return MXFP4_ERR_CUDA;
+    }
+    return MXFP4_OK;
+}
+
+int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t tokens,
+                                   int64_t in_features, int64_t vocab, const int64_t* targets, float scale,
+                                   const float* lse, const float* d_logp, const float* d_lse, void* dx, int64_t ld_dx,
+                                   void* dw, int64_t ld_dw, int dw_dtype, void* workspace, size_t workspace_bytes,
+                                   void* stream)
+{
+    int rc = loss_check(x, ld_x, w, ld_w, tokens, in_features, vocab, scale);
+    if (rc != MXFP4_OK) return rc;
+    if (!lse || (!d_logp && !d_lse) || (d_logp && !targets) || (!dx && !dw)) return MXFP4_ERR_NULL;
+    if (dw_dtype != MXFP4_OUT_BF16 && dw_dtype != MXFP4_OUT_FP32) return MXFP4_ERR_ENUM;
+    if ((dx && ld_dx < in_features) || (dw && ld_dw < in_features)) return MXFP4_ERR_SHAPE;
+    if ((dx && (!aligned16(dx) || ld_dx % 8 != 0)) || (dw && (!aligned16(dw) || ld_dw % 8 != 0))) return MXFP4_ERR_ALIGN;
+    const size_t need = mxfp4_linear_logprobs_workspace_bytes(tokens, in_features, vocab, 1);
+    if (!workspace || workspace_bytes < need) return MXFP4_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return MXFP4_ERR_ALIGN;
+    const DeviceInfo& dev = device_info();
+    if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+
+    const int64_t piece = loss_piece(tokens, vocab);
+    const int64_t ld_grad = round_up(piece, 8);
+    __nv_bfloat16* grad = static_cast<__nv_bfloat16*>(workspace);
+    float* sums = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + loss_grad_bytes(tokens, vocab));
+    for (int64_t v = 0; v < vocab; v += piece) {
+        const int64_t cols = vocab - v < piece ? vocab - v : piece;
+        const DenseMatrix wp = {static_cast<const __nv_bfloat16*>(w) + v * ld_w, ld_w};
+        const DenseMatrix gp = {grad, ld_grad};
+        {
+            DenseCall c;
+            c.epilogue = kDenseLogitGrad;
+            c.a[0] = {x, ld_x};
+            c.b[0] = wp;
+            c.out[0] = gp;
+            c.p.M = static_cast<int32_t>(tokens);
+            c.p.N = static_cast<int32_t>(cols);
+            c.p.K = static_cast<int32_t>(in_features);
+            c.p.vocab = vocab;
+            c.p.col_base = v;
+            c.p.targets = targets;
+            c.p.scale = scale;
+            c.p.lse = lse;
+            c.p.d_logp = d_logp;
+            c.p.d_lse = d_lse;
+            c.p.ld_grad = static_cast<int32_t>(round_up(cols, 8));
+            if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        }
+        if (dx) {
+            DenseCall c;                   // dx (+)= dz W
+            c.epilogue = piece == vocab ? kDenseBf16 : v == 0 ? kDenseF32 : kDenseAddF32;
+            c.b_mn = true;
+            c.a[0] = gp;
+            c.b[0] = wp;
+            c.out[0] = piece == vocab ? DenseMatrix{dx, ld_dx} : DenseMatrix{sums, in_features};
+            c.p.M = static_cast<int32_t>(tokens);
+            c.p.N = static_cast<int32_t>(in_features);
+            c.p.K = static_cast<int32_t>(cols);
+            if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        }
+        if (dw) {
+            DenseCall c;                   // dW = dz^T x
+            c.epilogue = dw_dtype == MXFP4_OUT_FP32 ? kDenseF32 : kDenseBf16;
+            c.a_mn = c.b_mn = true;
+            c.a[0] = gp;
+            c.b[0] = {x, ld_x};
+            c.out[0] = {static_cast<uint8_t*>(dw) + v * ld_dw * (dw_dtype == MXFP4_OUT_FP32 ? 4 : 2), ld_dw};
+            c.p.M = static_cast<int32_t>(cols);
+            c.p.N = static_cast<int32_t>(in_features);
+            c.p.K = static_cast<int32_t>(tokens);
+            if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        }
+    }
+    if (dx && piece != vocab) {
+        RoundRowsParams p;
+        p.from = sums;
+        p.to = static_cast<__nv_bfloat16*>(dx);
+        p.ld = ld_dx;
+        p.items = tokens * (in_features / 8);
+        p.per_row = static_cast<int32_t>(in_features / 8);
+        const int64_t blocks = (p.items + 255) / 256, most = 8 * static_cast<int64_t>(dev.sm_count);
+        if (launch_kernel_pdl(round_rows_kernel, static_cast<int>(blocks < most ? blocks : most), 256, 0, st, p) != cudaSuccess)
+            return MXFP4_ERR_CUDA;
+    }
+    return MXFP4_OK;
+}
+
+}  // extern "C"

@@ -321,6 +321,15 @@ __device__ __forceinline__ void tma_store_3d(const void* tmap, const void* smem_
         : "memory");
 }
 
+// 2-D tiled addition shared -> global of fp32 elements.
+__device__ __forceinline__ void tma_add_2d(const void* tmap, const void* smem_src, int32_t x, int32_t y)
+{
+    asm volatile(
+        "cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];"
+        ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(smem_src)), "r"(x), "r"(y)
+        : "memory");
+}
+
 // L2 eviction-priority policies for cache-hinted TMA traffic.
 __device__ __forceinline__ uint64_t l2_policy_evict_first()
 {
@@ -458,9 +467,11 @@ __device__ __forceinline__ void tmem_ld_wait()
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// Shared-memory matrix descriptor (K-major operand).  Fields: start address >> 4 in bits
+// Shared-memory matrix descriptor.  Fields: start address >> 4 in bits
 // 0..13, leading byte offset >> 4 in 16..29, stride byte offset >> 4 in 32..45, descriptor
-// version 1 in 46..47, swizzle mode in 61..63 (0 none, 2 = 128 B, 4 = 64 B, 6 = 32 B).
+// version 1 in 46..47, swizzle mode in 61..63 (0 none, 2 = 128 B, 4 = 64 B, 6 = 32 B).  With the 128-byte
+// swizzle, an operand stored along K has its 8-row groups a stride offset apart (the leading offset is not
+// used); a transposed one has 8-row groups of K a stride offset and its 128-byte columns a leading offset apart.
 __device__ __forceinline__ uint64_t make_smem_desc(uint32_t smem_addr, uint32_t lbo_bytes,
                                                    uint32_t sbo_bytes, uint32_t swizzle_mode)
 {
@@ -636,6 +647,18 @@ __device__ __forceinline__ void tcgen05_mma_f8_pair(uint32_t d_tmem, uint64_t a_
         "{\n\t.reg .pred P;\n\t"
         "setp.ne.b32 P, %4, 0;\n\t"
         "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, P;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Pair MMA on 16-bit operands of one type, 256 x N x 16.
+__device__ __forceinline__ void tcgen05_mma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                     uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred P;\n\t"
+        "setp.ne.b32 P, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, P;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
