@@ -596,6 +596,50 @@ int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, i
                                    void* stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------
+ * Token embeddings: scaled lookup, and the gradient of the table.
+ *     out[t] = scale * table[ids[t]]
+ *     d_table[v] (+)= scale * sum over t with ids[t] = v, ascending, of d_out[t]
+ *   ids      int64 [tokens].  A negative one is a position without a token: its output is 0 and its gradient goes
+ *            nowhere.  One >= vocab gives a row of NaN, and its gradient goes nowhere.
+ *   table, d_table  [vocab x width], out, d_out [tokens x width]: each bf16 or fp32 (its dtype, MXFP4_OUT_*), 16-byte
+ *            aligned, leading dimension a multiple of 8; width a multiple of 8; vocab, tokens below 2^30
+ *   scale    finite
+ * Backward: sums in fp32, rounded once.  accumulate 0: every row of d_table is written, those without a token with 0;
+ *   otherwise the sums are added to the rows that have tokens and no other row is touched.  d_table may not overlap
+ *   d_out.  workspace: mxfp4_embedding_workspace_bytes bytes (at most 4096 partial rows, two per piece of the sorted
+ *   positions), 16-byte aligned.  Calls repeat bit for bit.
+ */
+int mxfp4_embedding_forward(const int64_t* ids, int64_t tokens, const void* table, int table_dtype, int64_t vocab,
+                            int64_t width, int64_t ld_table, float scale, void* out, int out_dtype, int64_t ld_out,
+                            void* stream);
+size_t mxfp4_embedding_workspace_bytes(int64_t tokens, int64_t width);
+int mxfp4_embedding_backward(const int64_t* ids, int64_t tokens, const void* d_out, int d_out_dtype, int64_t ld_d_out,
+                             int64_t vocab, int64_t width, float scale, void* d_table, int d_table_dtype,
+                             int64_t ld_d_table, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * The global norm of many gradient tensors, and clipping by it:
+ *     norm = sqrt(sum of the squares of all elements of all tensors)
+ *     factor = min(1, max_norm / (norm + eps)),   out[i] = factor * tensors[i]
+ *   tensors, numel, dtypes   HOST arrays of `count` device pointers, element counts (0 allowed) and types (MXFP4_OUT_*);
+ *            each tensor contiguous, aligned to its element only.  They are read before the call returns.
+ *   out, out_dtypes          likewise; out[i] may be tensors[i] with its type (clipped in place) and overlaps nothing
+ *            else of the call (found on the host: MXFP4_ERR_SHAPE).  Results are rounded once.
+ *   norm     fp32 [1], on the device; max_norm >= 0 (infinity: the norm alone decides nothing), eps >= 0
+ * Squares are added so that neither large nor small elements of fp32's range are lost (fp64 beyond 16 bytes of elements).  Where the norm
+ * is not finite in fp32, the factor is 1: gradients stay as they are, and the norm tells the caller.
+ * workspace: mxfp4_grad_norm_workspace_bytes bytes, 16-byte aligned.  Calls repeat bit for bit.
+ */
+size_t mxfp4_grad_norm_workspace_bytes(int64_t count);
+int mxfp4_grad_norm(const void* const* tensors, const int64_t* numel, const int32_t* dtypes, int64_t count, float* norm,
+                    void* workspace, size_t workspace_bytes, void* stream);
+int mxfp4_clip_grads(const void* const* tensors, const int64_t* numel, const int32_t* dtypes, int64_t count, float max_norm,
+                     float eps, void* const* out, const int32_t* out_dtypes, float* norm, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/*
  * Synchronises `stream` and returns the sticky device-side status of the current device:
  * MXFP4_OK, MXFP4_ERR_TIMEOUT (a kernel gave up a bounded wait; its output is invalid) or
  * MXFP4_ERR_CUDA.  The status word is cleared by the call.

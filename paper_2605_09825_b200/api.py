@@ -6,6 +6,7 @@ if the shared library is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -40,6 +41,8 @@ EXPORTS = (
     "mxfp4_logprobs_workspace_bytes", "mxfp4_logprobs_forward", "mxfp4_logprobs_backward",
     "mxfp4_gated_linear_forward", "mxfp4_gated_linear_workspace_bytes", "mxfp4_gated_linear_backward",
     "mxfp4_linear_logprobs_workspace_bytes", "mxfp4_linear_logprobs_forward", "mxfp4_linear_logprobs_backward",
+    "mxfp4_embedding_forward", "mxfp4_embedding_workspace_bytes", "mxfp4_embedding_backward",
+    "mxfp4_grad_norm_workspace_bytes", "mxfp4_grad_norm", "mxfp4_clip_grads",
 )
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 
@@ -158,7 +161,13 @@ def load_library() -> ctypes.CDLL:
             ("mxfp4_linear_logprobs_workspace_bytes", [i64, i64, i64, ci], sz),
             ("mxfp4_linear_logprobs_forward", [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, sz, vp], ci),
             ("mxfp4_linear_logprobs_backward",
-             [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, vp, i64, vp, i64, ci, vp, sz, vp], ci)):
+             [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, vp, i64, vp, i64, ci, vp, sz, vp], ci),
+            ("mxfp4_embedding_forward", [vp, i64, vp, ci, i64, i64, i64, f32, vp, ci, i64, vp], ci),
+            ("mxfp4_embedding_workspace_bytes", [i64, i64], sz),
+            ("mxfp4_embedding_backward", [vp, i64, vp, ci, i64, i64, i64, f32, vp, ci, i64, ci, vp, sz, vp], ci),
+            ("mxfp4_grad_norm_workspace_bytes", [i64], sz),
+            ("mxfp4_grad_norm", [vp, vp, vp, i64, vp, vp, sz, vp], ci),
+            ("mxfp4_clip_grads", [vp, vp, vp, i64, f32, f32, vp, vp, vp, vp, sz, vp], ci)):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, res
     lib.mxfp4_selftest_wait_timeout.argtypes, lib.mxfp4_selftest_wait_timeout.restype = [vp], ci
@@ -993,6 +1002,116 @@ def linear_logprobs_backward(x, w, targets, lse, d_logp=None, d_lse=None, scale:
     if rc:
         _raise(rc, "mxfp4_linear_logprobs_backward")
     return (dx if want_dx else None), (dw if want_dw else None)
+
+
+# ---------------------------------------------------------------- token embeddings
+_TYPE_OF = {OUT_BF16: torch.bfloat16, OUT_FP32: torch.float32}
+
+
+def embedding_forward(ids, table, scale: float = 1.0, out_dtype=None, out=None):
+    """``mxfp4_embedding_forward``: ``scale * table[ids]``, [tokens, width], of a bf16 or fp32 table [vocab, width] and
+    int64 ``ids`` [tokens] (negative: a row of zeros); of the table's type unless ``out_dtype`` names another."""
+    t_ptr, ld_table = _matrix(table, "table", _STREAM_TYPES)
+    vocab, width = table.shape
+    tokens = ids.numel()
+    id_ptr = _expect(ids, "ids", torch.int64, tokens)
+    kind = _STREAM_TYPES[table.dtype] if out_dtype is None else out_dtype
+    if kind not in _TYPE_OF:
+        _raise(-4, "mxfp4_embedding_forward")
+    out = _output(out, "out", (tokens, width), _TYPE_OF[kind], table.device)
+    _on_current_device(ids, table, out)
+    out_ptr, ld_out = _matrix(out, "out", (out.dtype,))
+    rc = load_library().mxfp4_embedding_forward(id_ptr, tokens, t_ptr, _STREAM_TYPES[table.dtype], vocab, width, ld_table, scale,
+                                                out_ptr, kind, ld_out, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_embedding_forward")
+    return out
+
+
+def embedding_backward(ids, d_out, vocab: int, scale: float = 1.0, out_dtype: int = OUT_FP32, d_table=None,
+                       accumulate: bool = False, workspace=None):
+    """``mxfp4_embedding_backward``: the gradient of the table [vocab, width] from that of the output, d_out [tokens,
+    width] bf16 or fp32.  With ``accumulate`` it is added to ``d_table``, whose other rows are not touched."""
+    d_ptr, ld_d = _matrix(d_out, "d_out", _STREAM_TYPES)
+    tokens, width = d_out.shape
+    id_ptr = _expect(ids, "ids", torch.int64, tokens)
+    if accumulate and d_table is None:
+        raise ValueError("accumulate adds to a d_table")
+    if d_table is not None:
+        out_dtype = _STREAM_TYPES.get(d_table.dtype, out_dtype)
+    if out_dtype not in _TYPE_OF:
+        _raise(-4, "mxfp4_embedding_backward")
+    d_table = _output(d_table, "d_table", (vocab, width), _TYPE_OF[out_dtype], d_out.device)
+    lib = load_library()
+    if workspace is None:
+        workspace = torch.empty(max(lib.mxfp4_embedding_workspace_bytes(tokens, width), 1), dtype=torch.uint8, device=d_out.device)
+    _on_current_device(ids, d_out, d_table, workspace)
+    t_ptr, ld_t = _matrix(d_table, "d_table", (d_table.dtype,))
+    rc = lib.mxfp4_embedding_backward(id_ptr, tokens, d_ptr, _STREAM_TYPES[d_out.dtype], ld_d, vocab, width, scale, t_ptr,
+                                      out_dtype, ld_t, int(accumulate), _dev_ptr(workspace), workspace.numel(), _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_embedding_backward")
+    return d_table
+
+
+# ---------------------------------------------------------------- gradient norm and clipping
+# Called with hundreds of tensors: each property of all of them in one pass.
+def _tensor_list(tensors, name: str) -> tuple:
+    """Arrays of the pointers, element counts and types of contiguous CUDA tensors on the current device."""
+    index = torch._C._cuda_getDevice() if torch.cuda.is_available() else -1
+    kinds = [_STREAM_TYPES.get(t.dtype) for t in tensors]
+    if None in kinds or not all(map(torch.Tensor.is_contiguous, tensors)) or any(i != index for i in map(torch.Tensor.get_device, tensors)):
+        raise ValueError(f"{name} must be contiguous bf16 or fp32 tensors on the current device")
+    return (array.array("q", map(torch.Tensor.data_ptr, tensors)), array.array("q", map(torch.Tensor.numel, tensors)),
+            array.array("i", kinds))
+
+
+def _norm_buffers(count: int, lib, device, workspace) -> tuple:
+    """The norm, and the workspace's pointer and size (one allocation where the caller brings none)."""
+    need = lib.mxfp4_grad_norm_workspace_bytes(count)
+    if workspace is None:
+        both = torch.empty(need // 4 + 4, dtype=torch.float32, device=device)
+        return both[need // 4], both.data_ptr(), need, both
+    return torch.empty((), dtype=torch.float32, device=device), _dev_ptr(workspace), workspace.numel(), workspace
+
+
+def grad_norm(tensors, workspace=None) -> torch.Tensor:
+    """``mxfp4_grad_norm``: the root of the sum of the squares of all elements of all ``tensors`` (contiguous, bf16 or
+    fp32), an fp32 tensor of no dimensions."""
+    tensors = list(tensors)
+    ptrs, numel, kinds = _tensor_list(tensors, "tensors")
+    if not tensors:
+        _raise(-2, "mxfp4_grad_norm")
+    lib = load_library()
+    norm, ws_ptr, ws_bytes, _keep = _norm_buffers(len(tensors), lib, tensors[0].device, workspace)
+    at = lambda a: a.buffer_info()[0]
+    rc = lib.mxfp4_grad_norm(at(ptrs), at(numel), at(kinds), len(tensors), norm.data_ptr(), ws_ptr, ws_bytes, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_grad_norm")
+    return norm
+
+
+def clip_grads(tensors, max_norm: float, out=None, eps: float = 1e-6, workspace=None) -> torch.Tensor:
+    """``mxfp4_clip_grads``: scales ``tensors`` by ``min(1, max_norm / (norm + eps))``, in place or into the tensors of
+    ``out`` (as many elements each, bf16 or fp32), and returns the norm as ``grad_norm`` does.  A norm that is not
+    finite leaves the gradients as they are."""
+    tensors = list(tensors)
+    ptrs, numel, kinds = _tensor_list(tensors, "tensors")
+    to, to_kinds = ptrs, kinds
+    if out is not None:
+        to, to_numel, to_kinds = _tensor_list(list(out), "out")
+        if to_numel != numel:
+            raise ValueError("out must have a tensor of the same number of elements for each of tensors")
+    if not tensors:
+        _raise(-2, "mxfp4_clip_grads")
+    lib = load_library()
+    norm, ws_ptr, ws_bytes, _keep = _norm_buffers(len(tensors), lib, tensors[0].device, workspace)
+    at = lambda a: a.buffer_info()[0]
+    rc = lib.mxfp4_clip_grads(at(ptrs), at(numel), at(kinds), len(tensors), max_norm, eps, at(to), at(to_kinds), norm.data_ptr(),
+                              ws_ptr, ws_bytes, _raw_stream())
+    if rc:
+        _raise(rc, "mxfp4_clip_grads")
+    return norm
 
 
 def probe_mma_rate(iterations: int = 10000, random_operands: bool = True) -> float:

@@ -1,0 +1,441 @@
+// The global norm of many gradient tensors, and clipping by it (see include/mxfp4.h).
+//
+// The tensors are cut into blocks of 16384 elements, which the CTAs take in turn; their descriptors travel as a kernel
+// argument, so a call copies nothing to the device and can be captured.  Squares are added in fp32 over the eight or four
+// elements of a 16-byte piece and in fp64 beyond that; a piece whose sum leaves fp32's range, or falls where fp32's squares
+// lose bits, is added in fp64 throughout.  Every CTA writes one partial sum, and whoever needs the norm adds them in their
+// order: results do not depend on scheduling.
+//
+// Clipping reads the gradients a second time, last blocks first: what the first pass read last is still in L2.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include "../../include/mxfp4.h"
+#include "host_common.cuh"
+#include "ptx_sm100.cuh"
+#include "row_io.cuh"
+#include "tma_host.cuh"
+
+namespace mxfp4 {
+
+constexpr int kNormBlock = 16384;                  // elements
+constexpr int kNormThreads = 512;
+constexpr int kNormWarps = kNormThreads / 32;
+constexpr int kNormUnroll = 4;                     // 16-byte pieces in flight per thread
+constexpr int kNormCtas = 296;                     // two per SM; a constant, so that results do not depend on the device
+constexpr int kNormMostTensors = 640;              // per launch: 30 KB of arguments
+
+struct NormTensor {
+    const void* in;
+    void* out;
+    int64_t numel;
+    int32_t in32, out32;         // fp32, otherwise bf16
+    int32_t first_block;
+};
+
+template <int N>
+struct NormParams {
+    double* parts;               // of this launch: [kNormCtas]
+    const double* all;           // of all launches
+    int32_t launches;            // whose partial sums are in `all`
+    int32_t count, blocks;
+    float* norm;
+    float max_norm, eps;
+    int32_t write_norm;
+    NormTensor t[N];
+};
+
+// The tensor a block belongs to.
+template <int N>
+__device__ __forceinline__ int norm_tensor_of(const NormParams<N>& p, int block)
+{
+    int lo = 0, hi = p.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.t[mid].first_block <= block) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double square64(float v) { return static_cast<double>(v) * static_cast<double>(v); }
+
+// Sum of squares of a piece's elements; `any`: whether a bit other than a sign is set in it.
+template <int N>
+__device__ __forceinline__ double piece_squares(const float (&v)[N], bool any)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
+    if ((s > 0x1p-80f && s < INFINITY) || !any) return static_cast<double>(s);
+    double d = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) d += square64(v[i]);
+    return d;
+}
+
+__device__ __forceinline__ double piece_squares_bf16(const uint4& w)
+{
+    float2 q[4];
+    unpack8(w, q);
+    const float v[8] = {q[0].x, q[0].y, q[1].x, q[1].y, q[2].x, q[2].y, q[3].x, q[3].y};
+    return piece_squares(v, ((w.x | w.y | w.z | w.w) & 0x7FFF7FFFu) != 0);
+}
+
+__device__ __forceinline__ double piece_squares_fp32(const uint4& w)
+{
+    const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+    return piece_squares(v, ((w.x | w.y | w.z | w.w) & 0x7FFFFFFFu) != 0);
+}
+
+template <class T>
+__device__ __forceinline__ float as_float(T v)
+{
+    if constexpr (sizeof(T) == 2) return __bfloat162float(v);
+    else return v;
+}
+
+// Elements before the first 16-byte boundary.
+template <class T>
+__device__ __forceinline__ int head_of(const T* p, int n)
+{
+    return min(n, static_cast<int>(((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / sizeof(T)));
+}
+
+template <class T>
+__device__ __forceinline__ double block_squares(const T* x, int n)
+{
+    constexpr int kPer = 16 / sizeof(T);
+    double sum = 0.0;
+    const int head = head_of(x, n), pieces = (n - head) / kPer, tail = head + pieces * kPer;
+    const T* body = x + head;
+    for (int i = threadIdx.x; i < pieces; i += kNormThreads * kNormUnroll) {
+        uint4 w[kNormUnroll];
+#pragma unroll
+        for (int u = 0; u < kNormUnroll; ++u)
+            w[u] = i + u * kNormThreads < pieces ? ld_stream(body + (i + u * kNormThreads) * kPer) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int u = 0; u < kNormUnroll; ++u) sum += sizeof(T) == 2 ? piece_squares_bf16(w[u]) : piece_squares_fp32(w[u]);
+    }
+    if (threadIdx.x < head) sum += square64(as_float(x[threadIdx.x]));
+    if (tail + static_cast<int>(threadIdx.x) < n) sum += square64(as_float(x[tail + threadIdx.x]));
+    return sum;
+}
+
+__device__ __forceinline__ double warp_sum(double v)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kNormThreads, 2) norm_kernel(const __grid_constant__ NormParams<N> p)
+{
+    __shared__ double part[kNormWarps];
+    griddep_launch_dependents();
+    griddep_wait();
+    double sum = 0.0;
+    for (int b = blockIdx.x; b < p.blocks; b += kNormCtas) {
+        const NormTensor& t = p.t[norm_tensor_of(p, b)];
+        const int64_t at = static_cast<int64_t>(b - t.first_block) * kNormBlock;
+        const int n = static_cast<int>(min(t.numel - at, static_cast<int64_t>(kNormBlock)));
+        sum += t.in32 ? block_squares(static_cast<const float*>(t.in) + at, n)
+                      : block_squares(static_cast<const __nv_bfloat16*>(t.in) + at, n);
+    }
+    sum = warp_sum(sum);
+    if ((threadIdx.x & 31) == 0) smem_put(part, threadIdx.x >> 5, sum);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kNormWarps; ++w) sum += smem_get(part, w);
+        p.parts[blockIdx.x] = sum;
+    }
+}
+
+// The norm from the partial sums, the same in every CTA.
+template <int N>
+__device__ __forceinline__ float norm_of(const NormParams<N>& p, double (&part)[kNormWarps])
+{
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < p.launches * kNormCtas; i += kNormThreads) sum += p.all[i];
+    sum = warp_sum(sum);
+    if ((threadIdx.x & 31) == 0) smem_put(part, threadIdx.x >> 5, sum);
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < kNormWarps; ++w) sum += smem_get(part, w);
+    return static_cast<float>(sqrt(sum));
+}
+
+template <class In, class Out>
+__device__ __forceinline__ void block_scale(const In* x, Out* y, int n, float factor)
+{
+    constexpr int kPer = 16 / (sizeof(In) < sizeof(Out) ? sizeof(In) : sizeof(Out));       // elements per step: 16 or 32 bytes
+    const int head = head_of(x, n);
+    const bool vectors = kPer == 8 ? (reinterpret_cast<uintptr_t>(y + head) & 15u) == 0 && (reinterpret_cast<uintptr_t>(x + head) & 15u) == 0
+                                   : (reinterpret_cast<uintptr_t>(y + head) & 15u) == 0;
+    if (!vectors) {
+        for (int i = threadIdx.x; i < n; i += kNormThreads) {
+            const float v = as_float(x[i]) * factor;
+            if constexpr (sizeof(Out) == 2) y[i] = __float2bfloat16_rn(v);
+            else y[i] = v;
+        }
+        return;
+    }
+    const int pieces = (n - head) / kPer, tail = head + pieces * kPer;
+    for (int i = threadIdx.x; i < pieces; i += kNormThreads * kNormUnroll) {
+        uint4 w[kNormUnroll][sizeof(In) * kPer / 16];
+#pragma unroll
+        for (int u = 0; u < kNormUnroll; ++u) {
+            if (i + u * kNormThreads >= pieces) break;
+#pragma unroll
+            for (int h = 0; h < static_cast<int>(sizeof(In)) * kPer / 16; ++h)
+                w[u][h] = ld_stream(reinterpret_cast<const uint4*>(x + head + (i + u * kNormThreads) * kPer) + h);
+        }
+#pragma unroll
+        for (int u = 0; u < kNormUnroll; ++u) {
+            if (i + u * kNormThreads >= pieces) break;
+            float v[kPer];
+            if constexpr (sizeof(In) == 2) {
+                float2 q[4];
+                unpack8(w[u][0], q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] = q[j].x * factor;
+                    v[2 * j + 1] = q[j].y * factor;
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < kPer / 4; ++h) {
+                    v[4 * h] = __uint_as_float(w[u][h].x) * factor;
+                    v[4 * h + 1] = __uint_as_float(w[u][h].y) * factor;
+                    v[4 * h + 2] = __uint_as_float(w[u][h].z) * factor;
+                    v[4 * h + 3] = __uint_as_float(w[u][h].w) * factor;
+                }
+            }
+            uint4* to = reinterpret_cast<uint4*>(y + head + (i + u * kNormThreads) * kPer);
+            if constexpr (sizeof(Out) == 2) {
+                st_stream(to, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+            } else {
+#pragma unroll
+                for (int h = 0; h < kPer / 4; ++h)
+                    st_stream(to + h, make_uint4(__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]),
+                                                 __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])));
+            }
+        }
+    }
+    auto one = [&](int i) {
+        const float v = as_float(x[i]) * factor;
+        if constexpr (sizeof(Out) == 2) y[i] = __float2bfloat16_rn(v);
+        else y[i] = v;
+    };
+    if (static_cast<int>(threadIdx.x) < head) one(threadIdx.x);
+    if (tail + static_cast<int>(threadIdx.x) < n) one(tail + threadIdx.x);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kNormThreads, 2) clip_kernel(const __grid_constant__ NormParams<N> p)
+{
+    __shared__ double part[kNormWarps];
+    griddep_launch_dependents();
+    griddep_wait();
+    const float norm = norm_of(p, part);
+    if (p.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+    const float share = p.max_norm / (norm + p.eps);
+    const float factor = norm <= 3.402823466e38f && share < 1.0f ? share : 1.0f;       // not finite: as they are
+    for (int b = p.blocks - 1 - static_cast<int>(blockIdx.x); b >= 0; b -= gridDim.x) {
+        const NormTensor& t = p.t[norm_tensor_of(p, b)];
+        if (factor == 1.0f && t.in == t.out && t.in32 == t.out32) continue;
+        const int64_t at = static_cast<int64_t>(b - t.first_block) * kNormBlock;
+        const int n = static_cast<int>(min(t.numel - at, static_cast<int64_t>(kNormBlock)));
+        const float* x32 = static_cast<const float*>(t.in) + at;
+        const __nv_bfloat16* x16 = static_cast<const __nv_bfloat16*>(t.in) + at;
+        float* y32 = static_cast<float*>(t.out) + at;
+        __nv_bfloat16* y16 = static_cast<__nv_bfloat16*>(t.out) + at;
+        if (t.in32) {
+            if (t.out32) block_scale(x32, y32, n, factor);
+            else block_scale(x32, y16, n, factor);
+        } else {
+            if (t.out32) block_scale(x16, y32, n, factor);
+            else block_scale(x16, y16, n, factor);
+        }
+    }
+}
+
+// The norm alone.
+__global__ void __launch_bounds__(kNormThreads) norm_join_kernel(const __grid_constant__ NormParams<1> p)
+{
+    __shared__ double part[kNormWarps];
+    griddep_launch_dependents();
+    griddep_wait();
+    const float norm = norm_of(p, part);
+    if (threadIdx.x == 0) *p.norm = norm;
+}
+
+struct NormCall {
+    const void* const* in;
+    void* const* out;            // NULL: the norm alone
+    const int64_t* numel;
+    const int32_t* in_dtype;
+    const int32_t* out_dtype;
+    int64_t count;
+};
+
+// Fills a launch's descriptors from tensor `first` on; returns how many tensors it took.  Empty ones are passed by.
+template <int N>
+static int64_t norm_fill(NormParams<N>& p, const NormCall& c, int64_t first)
+{
+    p.count = p.blocks = 0;
+    int64_t i = first;
+    for (; i < c.count && p.count < N; ++i) {
+        if (c.numel[i] == 0) continue;
+        const int64_t blocks = (c.numel[i] + kNormBlock - 1) / kNormBlock;
+        if (blocks > 0x7FFFFFFF - p.blocks) break;
+        NormTensor& t = p.t[p.count++];
+        t.in = c.in[i];
+        t.out = c.out ? c.out[i] : nullptr;
+        t.numel = c.numel[i];
+        t.in32 = c.in_dtype[i] == MXFP4_OUT_FP32;
+        t.out32 = c.out && c.out_dtype[i] == MXFP4_OUT_FP32;
+        t.first_block = p.blocks;
+        p.blocks += static_cast<int32_t>(blocks);
+    }
+    return i - first;
+}
+
+static int64_t norm_launches(int64_t count) { return (count + kNormMostTensors - 1) / kNormMostTensors; }
+
+template <int N>
+static int norm_run(const NormCall& c, float max_norm, float eps, float* norm, double* parts, cudaStream_t st)
+{
+    NormParams<N> p;
+    memset(&p, 0, offsetof(NormParams<N>, t));
+    p.all = parts;
+    p.norm = norm;
+    p.max_norm = max_norm;
+    p.eps = eps;
+    int64_t launches = 0;
+    for (int64_t i = 0; i < c.count;) {
+        i += norm_fill(p, c, i);
+        p.parts = parts + launches++ * kNormCtas;
+        if (launch_kernel_pdl(norm_kernel<N>, kNormCtas, kNormThreads, 0, st, p) != cudaSuccess) return MXFP4_ERR_CUDA;
+    }
+    if (!c.out) {
+        NormParams<1> q;
+        memset(&q, 0, sizeof(q));
+        q.all = parts;
+        q.norm = norm;
+        q.launches = static_cast<int32_t>(launches);
+        return launch_kernel_pdl(norm_join_kernel, 1, kNormThreads, 0, st, q) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
+    }
+    p.launches = static_cast<int32_t>(launches);
+    p.write_norm = 1;
+    for (int64_t i = 0; i < c.count; p.write_norm = 0) {
+        i += norm_fill(p, c, i);
+        const int ctas = p.blocks < kNormCtas ? (p.blocks > 0 ? p.blocks : 1) : kNormCtas;
+        if (launch_kernel_pdl(clip_kernel<N>, ctas, kNormThreads, 0, st, p) != cudaSuccess) return MXFP4_ERR_CUDA;
+    }
+    return MXFP4_OK;
+}
+
+// Whether an output overlaps another tensor of the call.
+struct NormSpan {
+    uintptr_t begin, end;
+    int32_t tensor, written;
+};
+
+static int span_order(const void* a, const void* b)
+{
+    const NormSpan* x = static_cast<const NormSpan*>(a);
+    const NormSpan* y = static_cast<const NormSpan*>(b);
+    return x->begin < y->begin ? -1 : x->begin > y->begin;
+}
+
+static int norm_overlap(const NormCall& c)
+{
+    NormSpan* s = static_cast<NormSpan*>(malloc(sizeof(NormSpan) * 2 * static_cast<size_t>(c.count)));
+    if (!s) return MXFP4_ERR_WORKSPACE;
+    size_t n = 0;
+    for (int64_t i = 0; i < c.count; ++i) {
+        if (c.numel[i] == 0) continue;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(c.in[i]), b = reinterpret_cast<uintptr_t>(c.out[i]);
+        const int32_t t = static_cast<int32_t>(i);
+        s[n++] = {b, b + c.numel[i] * (c.out_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), t, 1};
+        if (a != b || c.in_dtype[i] != c.out_dtype[i])
+            s[n++] = {a, a + c.numel[i] * (c.in_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), t, 0};
+    }
+    qsort(s, n, sizeof(NormSpan), span_order);
+    uintptr_t all = 0, written = 0;    // ends of what began so far, and of what of it is written
+    int rc = MXFP4_OK;
+    for (size_t i = 0; i < n && rc == MXFP4_OK; ++i) {
+        if (s[i].begin < (s[i].written ? all : written)) rc = MXFP4_ERR_SHAPE;
+        if (s[i].end > all) all = s[i].end;
+        if (s[i].written && s[i].end > written) written = s[i].end;
+    }
+    free(s);
+    return rc;
+}
+
+int grad_norm_take_status(int* status) { return take_unit_status(status); }
+
+}  // namespace mxfp4
+
+using namespace mxfp4;
+
+extern "C" {
+
+size_t mxfp4_grad_norm_workspace_bytes(int64_t count)
+{
+    if (count <= 0 || count > 0x3FFFFFFF) return 0;
+    return static_cast<size_t>(norm_launches(count)) * kNormCtas * sizeof(double);
+}
+
+static int norm_call(const NormCall& c, float max_norm, float eps, float* norm, void* workspace, size_t workspace_bytes,
+                     void* stream)
+{
+    if (c.count <= 0 || c.count > 0x3FFFFFFF) return MXFP4_ERR_SHAPE;
+    for (int64_t i = 0; i < c.count; ++i) {
+        if (c.numel[i] < 0 || c.numel[i] > (int64_t{1} << 44)) return MXFP4_ERR_SHAPE;
+        for (int o = 0; o < (c.out ? 2 : 1); ++o) {
+            const int type = o ? c.out_dtype[i] : c.in_dtype[i];
+            const void* ptr = o ? c.out[i] : c.in[i];
+            if (type != MXFP4_OUT_BF16 && type != MXFP4_OUT_FP32) return MXFP4_ERR_ENUM;
+            if (c.numel[i] > 0 && !ptr) return MXFP4_ERR_NULL;
+            if ((reinterpret_cast<uintptr_t>(ptr) & (type == MXFP4_OUT_FP32 ? 3u : 1u)) != 0) return MXFP4_ERR_ALIGN;
+        }
+    }
+    int rc = MXFP4_OK;
+    if (c.out && (rc = norm_overlap(c)) != MXFP4_OK) return rc;
+    if (!workspace || workspace_bytes < mxfp4_grad_norm_workspace_bytes(c.count)) return MXFP4_ERR_WORKSPACE;
+    if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(norm) & 3u)) return MXFP4_ERR_ALIGN;
+    if ((rc = device_status_code(device_info())) != MXFP4_OK) return rc;
+    double* parts = static_cast<double*>(workspace);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // a launch's arguments are copied when it is queued: as few as the call needs
+    if (c.count <= 16) return norm_run<16>(c, max_norm, eps, norm, parts, st);
+    if (c.count <= 128) return norm_run<128>(c, max_norm, eps, norm, parts, st);
+    return norm_run<kNormMostTensors>(c, max_norm, eps, norm, parts, st);
+}
+
+int mxfp4_grad_norm(const void* const* tensors, const int64_t* numel, const int32_t* dtypes, int64_t count, float* norm,
+                    void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!tensors || !numel || !dtypes || !norm) return MXFP4_ERR_NULL;
+    const NormCall c = {tensors, nullptr, numel, dtypes, nullptr, count};
+    return norm_call(c, 0.0f, 0.0f, norm, workspace, workspace_bytes, stream);
+}
+
+int mxfp4_clip_grads(const void* const* tensors, const int64_t* numel, const int32_t* dtypes, int64_t count, float max_norm,
+                     float eps, void* const* out, const int32_t* out_dtypes, float* norm, void* workspace,
+                     size_t workspace_bytes, void* stream)
+{
+    if (!tensors || !numel || !dtypes || !out || !out_dtypes || !norm) return MXFP4_ERR_NULL;
+    if (!(max_norm >= 0.0f) || !(eps >= 0.0f) || isinf(eps)) return MXFP4_ERR_ENUM;
+    const NormCall c = {tensors, out, numel, dtypes, out_dtypes, count};
+    return norm_call(c, max_norm, eps, norm, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

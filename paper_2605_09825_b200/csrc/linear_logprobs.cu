@@ -115,6 +115,8 @@ static int loss_check(const void* x, int64_t ld_x, const void* w, int64_t ld_w, 
     return MXFP4_OK;
 }
 
+int linear_logprobs_take_status(int* status) { return take_unit_status(status); }
+
 }  // namespace mxfp4
 
 using namespace mxfp4;
