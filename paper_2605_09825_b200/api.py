@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
 import os
 
 import torch
@@ -1056,11 +1057,14 @@ def embedding_backward(ids, d_out, vocab: int, scale: float = 1.0, out_dtype: in
 
 # ---------------------------------------------------------------- gradient norm and clipping
 # Called with hundreds of tensors: each property of all of them in one pass.
+_DTYPE = operator.attrgetter("dtype")
+
+
 def _tensor_list(tensors, name: str) -> tuple:
     """Arrays of the pointers, element counts and types of contiguous CUDA tensors on the current device."""
-    index = torch._C._cuda_getDevice() if torch.cuda.is_available() else -1
-    kinds = [_STREAM_TYPES.get(t.dtype) for t in tensors]
-    if None in kinds or not all(map(torch.Tensor.is_contiguous, tensors)) or any(i != index for i in map(torch.Tensor.get_device, tensors)):
+    index = torch._C._cuda_getDevice() if torch.cuda.is_available() else -2
+    kinds = list(map(_STREAM_TYPES.get, map(_DTYPE, tensors)))
+    if None in kinds or not all(map(torch.Tensor.is_contiguous, tensors)) or not set(map(torch.Tensor.get_device, tensors)) <= {index}:
         raise ValueError(f"{name} must be contiguous bf16 or fp32 tensors on the current device")
     return (array.array("q", map(torch.Tensor.data_ptr, tensors)), array.array("q", map(torch.Tensor.numel, tensors)),
             array.array("i", kinds))

@@ -7,6 +7,7 @@
 #include "../../include/mxfp4.h"
 #include "activations.cuh"
 #include "dense_gemm.cuh"
+#include "gated_rows_kernel.cuh"
 #include "host_common.cuh"
 #include "row_io.cuh"
 #include "ptx_sm100.cuh"
@@ -91,6 +92,28 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
         return MXFP4_ERR_ALIGN;
     const DeviceInfo& dev = device_info();
     if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
+    if (d->tokens <= 8 * kGRowsMaxTiles) {
+        GatedRowsParams p;
+        p.x = static_cast<const __nv_bfloat16*>(d->x);
+        p.w_gate = static_cast<const __nv_bfloat16*>(d->w_gate);
+        p.w_up = static_cast<const __nv_bfloat16*>(d->w_up);
+        p.h = static_cast<__nv_bfloat16*>(h);
+        p.gate = static_cast<__nv_bfloat16*>(gate);
+        p.up = static_cast<__nv_bfloat16*>(up);
+        p.ld_x = d->ld_x;
+        p.ld_gate = d->ld_gate;
+        p.ld_up = d->ld_up;
+        p.ld_h = ld_h;
+        p.ld_kept = ld_kept;
+        p.tokens = static_cast<int32_t>(d->tokens);
+        p.features = static_cast<int32_t>(d->features);
+        p.K = static_cast<int32_t>(d->in_features);
+        p.act = d->act;
+        auto kernel = d->tokens <= 8 ? gated_rows_kernel<1> : gated_rows_kernel<2>;
+        return launch_kernel_pdl(kernel, static_cast<int>(d->features / kGRowsFeatures), kGRowsWarps * 32, 0,
+                                 static_cast<cudaStream_t>(stream), p) == cudaSuccess
+                   ? MXFP4_OK : MXFP4_ERR_CUDA;
+    }
     DenseCall c;
     c.epilogue = kDenseGated;
     c.a[0] = {d->x, d->ld_x};

@@ -14,6 +14,8 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "../../include/mxfp4.h"
 #include "host_common.cuh"
 #include "ptx_sm100.cuh"
@@ -344,15 +346,8 @@ static int norm_run(const NormCall& c, float max_norm, float eps, float* norm, d
 // Whether an output overlaps another tensor of the call.
 struct NormSpan {
     uintptr_t begin, end;
-    int32_t tensor, written;
+    bool written;
 };
-
-static int span_order(const void* a, const void* b)
-{
-    const NormSpan* x = static_cast<const NormSpan*>(a);
-    const NormSpan* y = static_cast<const NormSpan*>(b);
-    return x->begin < y->begin ? -1 : x->begin > y->begin;
-}
 
 static int norm_overlap(const NormCall& c)
 {
@@ -362,12 +357,11 @@ static int norm_overlap(const NormCall& c)
     for (int64_t i = 0; i < c.count; ++i) {
         if (c.numel[i] == 0) continue;
         const uintptr_t a = reinterpret_cast<uintptr_t>(c.in[i]), b = reinterpret_cast<uintptr_t>(c.out[i]);
-        const int32_t t = static_cast<int32_t>(i);
-        s[n++] = {b, b + c.numel[i] * (c.out_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), t, 1};
+        s[n++] = {b, b + c.numel[i] * (c.out_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), true};
         if (a != b || c.in_dtype[i] != c.out_dtype[i])
-            s[n++] = {a, a + c.numel[i] * (c.in_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), t, 0};
+            s[n++] = {a, a + c.numel[i] * (c.in_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), false};
     }
-    qsort(s, n, sizeof(NormSpan), span_order);
+    std::sort(s, s + n, [](const NormSpan& x, const NormSpan& y) { return x.begin < y.begin; });
     uintptr_t all = 0, written = 0;    // ends of what began so far, and of what of it is written
     int rc = MXFP4_OK;
     for (size_t i = 0; i < n && rc == MXFP4_OK; ++i) {
