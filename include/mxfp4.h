@@ -607,13 +607,13 @@ int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, i
  *   scale    finite
  * Backward: sums in fp32, rounded once.  accumulate 0: every row of d_table is written, those without a token with 0;
  *   otherwise the sums are added to the rows that have tokens and no other row is touched.  d_table may not overlap
- *   d_out.  workspace: mxfp4_embedding_workspace_bytes bytes (at most 4096 partial rows, two per piece of the sorted
- *   positions), 16-byte aligned.  Calls repeat bit for bit.
+ *   d_out.  workspace: mxfp4_embedding_workspace_bytes bytes (16 per position, 4 per row of the table, two fp32
+ *   rows per share of the positions, 10 MB at most up to a million columns), 16-byte aligned.  Calls repeat bit for bit.
  */
 int mxfp4_embedding_forward(const int64_t* ids, int64_t tokens, const void* table, int table_dtype, int64_t vocab,
                             int64_t width, int64_t ld_table, float scale, void* out, int out_dtype, int64_t ld_out,
                             void* stream);
-size_t mxfp4_embedding_workspace_bytes(int64_t tokens, int64_t width);
+size_t mxfp4_embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width);
 int mxfp4_embedding_backward(const int64_t* ids, int64_t tokens, const void* d_out, int d_out_dtype, int64_t ld_d_out,
                              int64_t vocab, int64_t width, float scale, void* d_table, int d_table_dtype,
                              int64_t ld_d_table, int accumulate, void* workspace, size_t workspace_bytes, void* stream);

@@ -164,7 +164,7 @@ def load_library() -> ctypes.CDLL:
             ("mxfp4_linear_logprobs_backward",
              [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, vp, i64, vp, i64, ci, vp, sz, vp], ci),
             ("mxfp4_embedding_forward", [vp, i64, vp, ci, i64, i64, i64, f32, vp, ci, i64, vp], ci),
-            ("mxfp4_embedding_workspace_bytes", [i64, i64], sz),
+            ("mxfp4_embedding_workspace_bytes", [i64, i64, i64], sz),
             ("mxfp4_embedding_backward", [vp, i64, vp, ci, i64, i64, i64, f32, vp, ci, i64, ci, vp, sz, vp], ci),
             ("mxfp4_grad_norm_workspace_bytes", [i64], sz),
             ("mxfp4_grad_norm", [vp, vp, vp, i64, vp, vp, sz, vp], ci),
@@ -1045,7 +1045,7 @@ def embedding_backward(ids, d_out, vocab: int, scale: float = 1.0, out_dtype: in
     d_table = _output(d_table, "d_table", (vocab, width), _TYPE_OF[out_dtype], d_out.device)
     lib = load_library()
     if workspace is None:
-        workspace = torch.empty(max(lib.mxfp4_embedding_workspace_bytes(tokens, width), 1), dtype=torch.uint8, device=d_out.device)
+        workspace = torch.empty(max(lib.mxfp4_embedding_workspace_bytes(tokens, vocab, width), 1), dtype=torch.uint8, device=d_out.device)
     _on_current_device(ids, d_out, d_table, workspace)
     t_ptr, ld_t = _matrix(d_table, "d_table", (d_table.dtype,))
     rc = lib.mxfp4_embedding_backward(id_ptr, tokens, d_ptr, _STREAM_TYPES[d_out.dtype], ld_d, vocab, width, scale, t_ptr,

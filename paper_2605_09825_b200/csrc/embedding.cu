@@ -1,22 +1,26 @@
 // Token embeddings: scaled lookup, and the gradient of the table (see include/mxfp4.h).
 //
-// Backward, three launches:
-//   1. the first cluster sorts the token ids (below) while all other CTAs set the rows that no token has to zero, which
-//      for a large vocabulary is most of the bytes: a CTA learns which of its rows those are by reading all ids;
-//   2. sums: the sorted positions in chunks, a warp per chunk and 256 columns, gradients added in fp32 in the order of
-//      their positions; a row whose positions all lie in one chunk is written at once, a part of a row that goes on
-//      in another chunk becomes a partial sum;
-//   3. partial sums are joined in the order of their chunks.
+// Backward.  The positions are sorted by their ids, positions of the same id in their order, and the first of each id's
+// run is noted (a note counts only where the sorted ids confirm it, so the notes need no clearing).  Then
+//   - the sorted positions are shared out evenly, and gradients of equal ids are added in fp32 in the order of their
+//     positions; where a run spans shares, its partial sums are joined in the order of the shares;
+//   - the rows without tokens of a dense gradient are set to zero.  Small CTAs in the device's own order keep the rows being
+//     written close together: 128256 rows of 16 KB take 273 us that way (7.3 TB/s), 338 from CTAs that stay and take rows
+//     in turn.  Zeros first and sums after them cost 16 us more at 16384 tokens: what the zeros leave in L2 has to be written
+//     back before anything else finds room there.
 // No floating-point atomics: results depend on the inputs alone.
 //
-// The sort: a cluster of eight CTAs, 9 bits per pass from the lowest.  Each CTA counts the digits of its eighth of the
-// positions, reads the other CTAs' counts through distributed shared memory and places its positions, 1024 at a time,
-// behind the smaller digits, the earlier CTAs' and its own earlier ones: equal ids stay in the order of their
-// positions.  Ids without a row sort behind all others.
+// Up to 4096 positions are sorted by counting, for each, the smaller ones: 2 T^2 comparisons over the whole device, one
+// launch without any exchange.  Longer texts take a radix sort by a cluster of eight CTAs, 9 bits per pass from the lowest:
+// each CTA counts the digits of its eighth of the positions, reads the other CTAs' counts through distributed shared
+// memory and places its positions, 4096 at a time, behind the smaller digits, the earlier CTAs' and its own earlier ones.
+// Ids without a row sort behind all others.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "../../include/mxfp4.h"
 #include "host_common.cuh"
@@ -84,37 +88,78 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupPara
     }
 }
 
-// ------------------------------------------------------------------ sort and rows without tokens
-constexpr int kSortCtas = 8;                       // one cluster
-constexpr int kSortThreads = 1024;
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortBits = 9;
-constexpr int kSortBins = 1 << kSortBits;
-constexpr int kFillRows = 1 << 16;                 // rows a CTA looks up at a time
-
+// ------------------------------------------------------------------ sort
 struct SortParams {
     const int64_t* ids;
     uint2* a;                    // (id, position), in turn source and destination; the result is in a
     uint2* b;
+    uint32_t* first;             // [vocab]: where the id's run begins
     int32_t tokens;
     int32_t passes;
     int64_t vocab;
-    // rows without tokens
-    uint8_t* table;
-    int64_t pitch;               // bytes
-    int32_t row_vectors;         // 16-byte pieces per row
 };
+
+__device__ __forceinline__ uint32_t sort_key(const SortParams& p, int64_t id)
+{
+    return static_cast<uint32_t>(id < 0 || id >= p.vocab ? p.vocab : id);
+}
+
+constexpr int kRankMost = 4096;                    // positions
+constexpr int kRankWarps = 8;
+
+// 32 positions per CTA, one per lane; every warp compares them with an eighth of all.
+__global__ void __launch_bounds__(kRankWarps * 32) rank_kernel(const __grid_constant__ SortParams p)
+{
+    __shared__ uint4 keys[kRankMost / 4];
+    __shared__ uint32_t less[kRankWarps][32], same[kRankWarps][32];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int quads = (p.tokens + 3) / 4;
+    for (int i = threadIdx.x; i < quads; i += kRankWarps * 32) {
+        uint32_t k[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = 4 * i + j < p.tokens ? sort_key(p, p.ids[4 * i + j]) : 0xFFFFFFFFu;
+        smem_put(keys, i, make_uint4(k[0], k[1], k[2], k[3]));
+    }
+    __syncthreads();
+    const int mine = blockIdx.x * 32 + lane;
+    const uint32_t key = mine < p.tokens ? sort_key(p, p.ids[mine]) : 0u;
+    const int share = (quads + kRankWarps - 1) / kRankWarps;
+    const int begin = warp * share, end = min(quads, begin + share);
+    uint32_t n_less = 0, n_same = 0;               // smaller ids; equal ones at earlier positions
+#pragma unroll 4
+    for (int i = begin; i < end; ++i) {
+        const uint4 k = smem_get(keys, i);
+        n_less += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+        n_same += (k.x == key && 4 * i < mine) + (k.y == key && 4 * i + 1 < mine) + (k.z == key && 4 * i + 2 < mine) +
+                  (k.w == key && 4 * i + 3 < mine);
+    }
+    smem_store(&less[warp][lane], n_less, less, sizeof(less));
+    smem_store(&same[warp][lane], n_same, same, sizeof(same));
+    __syncthreads();
+    if (warp != 0 || mine >= p.tokens) return;
+    n_less = n_same = 0;
+    for (int w = 0; w < kRankWarps; ++w) {
+        n_less += smem_load<uint32_t>(&less[w][lane], less, sizeof(less));
+        n_same += smem_load<uint32_t>(&same[w][lane], same, sizeof(same));
+    }
+    p.a[n_less + n_same] = make_uint2(key, static_cast<uint32_t>(mine));
+    if (n_same == 0 && key < p.vocab) p.first[key] = n_less;
+}
+
+constexpr int kSortCtas = 8;                       // one cluster
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortItems = 4;                      // positions per thread and round
+constexpr int kSortBits = 9;
+constexpr int kSortBins = 1 << kSortBits;
 
 struct SortSmem {
     uint32_t counts[kSortBins];                    // of this CTA's positions
     uint32_t start[kSortBins];                     // where the next position with this digit goes
     uint32_t warp_counts[kSortWarps][kSortBins];   // digits of a round, then where each warp's start
     uint32_t sums[kSortWarps];
-};
-
-union SortFillSmem {
-    SortSmem sort;
-    uint32_t touched[kFillRows / 32];
 };
 
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr)
@@ -124,8 +169,13 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr)
     return v;
 }
 
-__device__ void sort_ids(const SortParams& p, SortSmem& s, uint32_t rank)
+__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads, 1) sort_kernel(const __grid_constant__ SortParams p)
 {
+    extern __shared__ uint8_t smem_raw[];
+    SortSmem& s = *reinterpret_cast<SortSmem*>(smem_align_1024(smem_raw));
+    griddep_launch_dependents();
+    griddep_wait();
+    const uint32_t rank = cluster_ctarank();
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     const int share = (p.tokens + kSortCtas - 1) / kSortCtas;
     const int begin = min(p.tokens, static_cast<int>(rank) * share), end = min(p.tokens, begin + share);
@@ -135,8 +185,7 @@ __device__ void sort_ids(const SortParams& p, SortSmem& s, uint32_t rank)
         const int shift = pass * kSortBits;
         auto entry = [&](int i) {
             if (from) return from[i];
-            const int64_t id = p.ids[i];
-            return make_uint2(static_cast<uint32_t>(id < 0 || id >= p.vocab ? p.vocab : id), static_cast<uint32_t>(i));
+            return make_uint2(sort_key(p, p.ids[i]), static_cast<uint32_t>(i));
         };
         auto digit_of = [&](const uint2& e) { return static_cast<int>((e.x >> shift) & (kSortBins - 1)); };
         if (t < kSortBins) smem_put(s.counts, t, 0u);
@@ -169,18 +218,35 @@ __device__ void sort_ids(const SortParams& p, SortSmem& s, uint32_t rank)
             for (int w = 0; w < warp; ++w) base += smem_get(s.sums, w);
             smem_put(s.start, t, base + upto - all + before);
         }
-        // 1024 positions at a time
-        for (int i0 = begin; i0 < end; i0 += kSortThreads) {
+        // a round of positions: 128 consecutive ones per warp, four per lane
+        constexpr int kRound = kSortThreads * kSortItems;
+        uint2 e[kSortItems];
+        auto load = [&](int i0) {
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j) {
+                const int i = i0 + (warp * kSortItems + j) * 32 + lane;
+                e[j] = i < end ? entry(i) : make_uint2(0u, 0u);
+            }
+        };
+        load(begin);
+        for (int i0 = begin; i0 < end; i0 += kRound) {
             for (int i = t; i < kSortWarps * kSortBins; i += kSortThreads) smem_store(&s.warp_counts[0][0] + i, 0u, s.warp_counts, sizeof(s.warp_counts));
             __syncthreads();
-            const int i = i0 + t;
-            const bool in = i < end;
-            const uint2 e = in ? entry(i) : make_uint2(0u, 0u);
-            const int d = digit_of(e);
-            // lanes with the same digit (those past the end among themselves)
-            const uint32_t same = __match_any_sync(0xffffffffu, in ? d : kSortBins + lane);
-            const int ahead = __popc(same & ((1u << lane) - 1));
-            if (in && ahead == 0) smem_store(&s.warp_counts[warp][d], static_cast<uint32_t>(__popc(same)), s.warp_counts, sizeof(s.warp_counts));
+            int at_digit[kSortItems];
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j) {
+                const bool in = i0 + (warp * kSortItems + j) * 32 + lane < end;
+                const int d = digit_of(e[j]);
+                // lanes with the same digit (those past the end among themselves)
+                const uint32_t same = __match_any_sync(0xffffffffu, in ? d : kSortBins + lane);
+                const int ahead = __popc(same & ((1u << lane) - 1));
+                uint32_t* count = &s.warp_counts[warp][d];
+                const uint32_t n = smem_load<uint32_t>(count, s.warp_counts, sizeof(s.warp_counts));
+                __syncwarp();
+                if (in && ahead == 0) smem_store(count, n + __popc(same), s.warp_counts, sizeof(s.warp_counts));
+                __syncwarp();
+                at_digit[j] = in ? static_cast<int>(n) + ahead : -1;
+            }
             __syncthreads();
             if (t < kSortBins) {
                 uint32_t at = smem_get(s.start, t);
@@ -194,49 +260,21 @@ __device__ void sort_ids(const SortParams& p, SortSmem& s, uint32_t rank)
                 smem_put(s.start, t, at);
             }
             __syncthreads();
-            if (in) {
-                const uint32_t at = smem_load<uint32_t>(&s.warp_counts[warp][d], s.warp_counts, sizeof(s.warp_counts)) + ahead;
-                if (at < static_cast<uint32_t>(p.tokens)) to[at] = e;
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j) {
+                const uint32_t at = smem_load<uint32_t>(&s.warp_counts[warp][digit_of(e[j])], s.warp_counts, sizeof(s.warp_counts)) + at_digit[j];
+                if (at_digit[j] >= 0 && at < static_cast<uint32_t>(p.tokens)) to[at] = e[j];
             }
+            load(i0 + kRound);
             __syncthreads();
         }
         cluster_sync_all();      // everything is placed, and the counts have been read
         from = to;
     }
-}
-
-__device__ void fill_rows(const SortParams& p, uint32_t (&touched)[kFillRows / 32], int cta, int ctas)
-{
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t share = (p.vocab + ctas - 1) / ctas;
-    const int64_t last = min(p.vocab, (cta + 1) * share);
-    for (int64_t v0 = cta * share; v0 < last; v0 += kFillRows) {
-        const int rows = static_cast<int>(min(last - v0, static_cast<int64_t>(kFillRows)));
-        for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) smem_put(touched, i, 0u);
-        __syncthreads();
-        for (int i = threadIdx.x; i < p.tokens; i += kSortThreads) {
-            const int64_t r = p.ids[i] - v0;
-            if (r >= 0 && r < rows && smem_within(touched, static_cast<int>(r >> 5)))
-                atomicOr(touched + (r >> 5), 1u << (r & 31));
-        }
-        __syncthreads();
-        for (int r = warp; r < rows; r += kSortWarps) {
-            if (smem_get(touched, r >> 5) >> (r & 31) & 1) continue;
-            uint8_t* to = p.table + (v0 + r) * p.pitch;
-            for (int i = lane; i < p.row_vectors; i += 32) st_stream(to + i * 16, make_uint4(0u, 0u, 0u, 0u));
-        }
-        __syncthreads();
+    for (int i = begin + t; i < end; i += kSortThreads) {
+        const uint32_t id = p.a[i].x;
+        if (id < p.vocab && (i == 0 || p.a[i - 1].x != id)) p.first[id] = static_cast<uint32_t>(i);
     }
-}
-
-__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads, 2) sort_fill_kernel(const __grid_constant__ SortParams p)
-{
-    extern __shared__ uint8_t smem_raw[];
-    SortFillSmem& sm = *reinterpret_cast<SortFillSmem*>(smem_align_1024(smem_raw));
-    griddep_launch_dependents();
-    griddep_wait();
-    if (blockIdx.x < kSortCtas) sort_ids(p, sm.sort, cluster_ctarank());
-    else fill_rows(p, sm.touched, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
 }
 
 // ------------------------------------------------------------------ sums
@@ -244,122 +282,260 @@ struct SumParams {
     const uint2* sorted;         // (id, position)
     const void* grads;
     void* table;
-    float* parts;                // [chunk][first, last][width]
+    float* parts;                // [share][goes on, begins][width]
     int64_t ld_grads, ld_table;
     int32_t tokens, width;
-    int32_t chunk;               // positions per chunk
-    int32_t chunks;
+    int32_t share;               // sorted positions per warp
+    int32_t shares;
     uint32_t vocab;
-    int32_t slabs;               // pieces of 256 columns
+    int32_t slabs;               // pieces of kSlab columns
     int32_t accumulate;
     float scale;
 };
 
 constexpr int kSumWarps = 8;
-constexpr int kSumUnroll = 8;    // rows in flight per warp
+constexpr int kSumAll = 148 * kSumWarps;           // shares times slabs; a constant, so that results do not depend on the device
+constexpr int kSlab = 1024;                        // columns of a warp, 32 per lane
+constexpr int kRingBytes = 24576;                  // per warp
+constexpr int kLeastShare = 8;
+
+struct SumSmem {
+    alignas(128) uint8_t ring[kSumWarps][kRingBytes];
+    uint64_t full[kSumWarps][kRingBytes / (kSlab * 2)];
+    int abort_flag;
+};
+
+// 8 columns each of four groups of 256 per lane
+struct RowSum {
+    float2 v[4][4];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[g][j] = make_float2(0.0f, 0.0f);
+    }
+    __device__ __forceinline__ void add(int g, const float2 (&w)[4])
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[g][j] = make_float2(v[g][j].x + w[j].x, v[g][j].y + w[j].y);
+    }
+};
 
 template <class Out>
-__device__ __forceinline__ void write_row(const SumParams& p, uint32_t id, int col, float2 (&acc)[4])
+__device__ __forceinline__ void write_row(const SumParams& p, uint32_t id, int col, RowSum& s)
 {
     Out* to = static_cast<Out*>(p.table) + id * p.ld_table + col;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = make_float2(acc[j].x * p.scale, acc[j].y * p.scale);
-    if (p.accumulate) {
-        float2 old[4];
-        load8_stream(to, old);
+    for (int g = 0; g < 4; ++g) {
+        if (col + g * 256 >= p.width) break;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = make_float2(acc[j].x + old[j].x, acc[j].y + old[j].y);
+        for (int j = 0; j < 4; ++j) s.v[g][j] = make_float2(s.v[g][j].x * p.scale, s.v[g][j].y * p.scale);
+        if (p.accumulate) {
+            float2 old[4];
+            load8_stream(to + g * 256, old);
+            s.add(g, old);
+        }
+        store8(to + g * 256, s.v[g]);
     }
-    store8(to, acc);
 }
 
-// A chunk's first row, where earlier chunks have positions of it too, is a partial sum in slot 0; its last row, where it
-// begins here and goes on in later chunks, in slot 1.
+// A warp per share of the sorted positions and 1024 columns.  The rows come through a ring of bulk copies in shared memory,
+// 24 KB per warp, whatever runs they belong to: most runs are one position long, and what a warp could keep on its way
+// in registers is one or two rows.  The part of a run that began in an earlier share is partial sum 0 of this share, the
+// part of one that goes on behind it partial sum 1.
 template <class In, class Out>
-__global__ void __launch_bounds__(kSumWarps * 32) sum_kernel(const SumParams p)
+__global__ void __launch_bounds__(kSumWarps * 32, 1) sum_kernel(const __grid_constant__ SumParams p)
 {
+    extern __shared__ uint8_t smem_raw[];
+    SumSmem& sm = *reinterpret_cast<SumSmem*>(smem_align_1024(smem_raw));
+    constexpr int kRowBytes = kSlab * sizeof(In), kSlots = kRingBytes / kRowBytes;
+    const int warp = threadIdx.x >> 5, lane = lane_id();
+    if (threadIdx.x == 0) {
+        sm.abort_flag = 0;
+        for (int w = 0; w < kSumWarps; ++w)
+            for (int i = 0; i < kSlots; ++i) mbar_init(&sm.full[w][i], 1);
+        fence_barrier_init();
+    }
+    __syncthreads();
     griddep_launch_dependents();
     griddep_wait();
-    const int64_t work = static_cast<int64_t>(blockIdx.x) * kSumWarps + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    const int chunk = static_cast<int>(work / p.slabs);
-    if (chunk >= p.chunks) return;
-    const int col = (static_cast<int>(work - static_cast<int64_t>(chunk) * p.slabs) * 32 + lane) * 8;
-    const bool col_ok = col < p.width;
-    const int begin = chunk * p.chunk, end = min(p.tokens, begin + p.chunk);
-    const uint32_t before = begin > 0 ? p.sorted[begin - 1].x : 0xFFFFFFFFu;
-    const uint32_t after = end < p.tokens ? p.sorted[end].x : 0xFFFFFFFFu;
-    float2 acc[4];
-    uint32_t id = p.sorted[begin].x;
-    bool fresh = true;           // nothing of `id` added yet
-    bool first = true;           // `id` is the chunk's first
-    auto finish = [&](bool last) {
-        if (!col_ok || id >= p.vocab) return;
-        if (first && id == before) store8(p.parts + (static_cast<int64_t>(chunk) * 2) * p.width + col, acc);
-        else if (last && id == after) store8(p.parts + (static_cast<int64_t>(chunk) * 2 + 1) * p.width + col, acc);
-        else write_row<Out>(p, id, col, acc);
-    };
-    for (int i0 = begin; i0 < end; i0 += kSumUnroll) {
-        uint2 e[kSumUnroll];
-        float2 v[kSumUnroll][4];
+    uint8_t* ring = sm.ring[warp];
+    uint64_t* full = sm.full[warp];
+    int slot = 0;                                  // of the row to be added next
+    uint32_t parity = 0;
+    // neighbouring units go to different SMs
+    for (int u = blockIdx.x + gridDim.x * warp; u < p.shares * p.slabs; u += gridDim.x * kSumWarps) {
+        const int share = u / p.slabs, col0 = (u - share * p.slabs) * kSlab, col = col0 + lane * 8;
+        const int begin = share * p.share, end = min(p.tokens, begin + p.share);
+        const uint32_t bytes = static_cast<uint32_t>(min(kSlab, p.width - col0)) * sizeof(In);
+        const In* grads = static_cast<const In*>(p.grads) + col0;
+        const uint32_t before = begin > 0 ? p.sorted[begin - 1].x : 0xFFFFFFFFu;
+        const uint32_t after = end < p.tokens ? p.sorted[end].x : 0xFFFFFFFFu;
+        // 64 positions' entries from `base` on
+        auto entries = [&](int i) { return i < end ? p.sorted[i] : make_uint2(0xFFFFFFFFu, 0u); };
+        int base = begin;
+        uint2 near = entries(begin + lane), far = entries(begin + 32 + lane);
+        auto id_of = [&](int i) { return __shfl_sync(0xffffffffu, i - base < 32 ? near.x : far.x, (i - base) & 31); };
+        auto issue = [&](int i, int to) {
+            const uint32_t pos = __shfl_sync(0xffffffffu, i - base < 32 ? near.y : far.y, (i - base) & 31);
+            if (id_of(i) < p.vocab && lane == 0) {
+                mbar_arrive_expect_tx(&full[to], bytes);
+                bulk_load_1d(ring + to * kRowBytes, grads + pos * p.ld_grads, bytes, &full[to]);
+            }
+        };
+        for (int i = 0; i < kSlots; ++i) issue(begin + i, slot + i < kSlots ? slot + i : slot + i - kSlots);
+        RowSum s;
+        s.clear();
+        uint32_t id = id_of(begin);
+        bool first = true, alive = true;           // `id` is the share's first
+        auto finish = [&](bool last) {
+            const int part = first && id == before ? 0 : last && id == after ? 1 : -1;
+            if (part < 0) {
+                write_row<Out>(p, id, col, s);
+                return;
+            }
+            float* to = p.parts + (static_cast<int64_t>(share) * 2 + part) * p.width + col;
 #pragma unroll
-        for (int u = 0; u < kSumUnroll; ++u) e[u] = i0 + u < end ? p.sorted[i0 + u] : make_uint2(p.vocab, 0u);
-#pragma unroll
-        for (int u = 0; u < kSumUnroll; ++u) {
-            if (col_ok && e[u].x < p.vocab)
-                load8_stream(static_cast<const In*>(p.grads) + e[u].y * p.ld_grads + col, v[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < kSumUnroll; ++u) {
-            if (i0 + u >= end) break;
-            if (e[u].x != id) {
+            for (int g = 0; g < 4; ++g)
+                if (col + g * 256 < p.width) store8(to + g * 256, s.v[g]);
+        };
+        int i = begin;
+        for (; i < end; ++i) {
+            const uint32_t next = id_of(i);
+            if (next >= p.vocab) break;            // these come last
+            if (next != id) {
                 finish(false);
-                id = e[u].x;
-                fresh = true;
+                s.clear();
+                id = next;
                 first = false;
             }
+            if (!mbar_wait(&full[slot], parity, &sm.abort_flag)) {
+                alive = false;
+                break;
+            }
+            const uint8_t* row = ring + slot * kRowBytes;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[j] = fresh ? v[u][j] : make_float2(acc[j].x + v[u][j].x, acc[j].y + v[u][j].y);
-            fresh = false;
+            for (int g = 0; g < 4; ++g) {
+                float2 v[4];
+                if constexpr (sizeof(In) == 2) {
+                    unpack8(smem_load<uint4>(row + g * 512 + lane * 16, ring, kRingBytes), v);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float4 f = smem_load<float4>(row + g * 1024 + lane * 32 + k * 16, ring, kRingBytes);
+                        v[2 * k] = make_float2(f.x, f.y);
+                        v[2 * k + 1] = make_float2(f.z, f.w);
+                    }
+                }
+                s.add(g, v);
+            }
+            __syncwarp();
+            if (i + 1 - base == 32) {
+                base += 32;
+                near = far;
+                far = entries(base + 32 + lane);
+            }
+            issue(i + kSlots, slot);
+            if (++slot == kSlots) {
+                slot = 0;
+                parity ^= 1;
+            }
         }
+        if (!alive) {                              // given up: what is in flight lands before the CTA leaves
+            linger();
+            break;
+        }
+        if (i > begin) finish(i == end);
     }
-    finish(true);
 }
 
-// Rows that span chunks, from the chunk they begin in.
+// Rows whose runs span shares, a warp per share that one begins in and 1024 columns.
 template <class Out>
-__global__ void __launch_bounds__(kSumWarps * 32) sum_join_kernel(const SumParams p)
+__global__ void __launch_bounds__(kSumWarps * 32) sum_join_kernel(const __grid_constant__ SumParams p)
 {
     griddep_launch_dependents();
     griddep_wait();
-    const int64_t work = static_cast<int64_t>(blockIdx.x) * kSumWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    const int chunk = static_cast<int>(work / p.slabs);
-    if (chunk + 1 >= p.chunks) return;
-    const int col = (static_cast<int>(work - static_cast<int64_t>(chunk) * p.slabs) * 32 + lane) * 8;
-    const int begin = chunk * p.chunk;
-    const uint32_t id = p.sorted[begin + p.chunk].x;
-    // it goes on in the next chunk, and begins in this one
-    if (id >= p.vocab || p.sorted[begin + p.chunk - 1].x != id || (begin > 0 && p.sorted[begin - 1].x == id)) return;
-    if (col >= p.width) return;
-    float2 acc[4];
-    load8_stream(p.parts + (static_cast<int64_t>(chunk) * 2 + 1) * p.width + col, acc);
-    for (int c = chunk + 1; c < p.chunks && p.sorted[c * p.chunk].x == id; ++c) {
-        float2 v[4];
-        load8_stream(p.parts + (static_cast<int64_t>(c) * 2) * p.width + col, v);
+    const int u = blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+    const int share = u / p.slabs, col = (u - share * p.slabs) * kSlab + lane * 8;
+    if (share + 1 >= p.shares) return;
+    const int begin = share * p.share;
+    const uint32_t id = p.sorted[begin + p.share].x;
+    // it goes on in the next share, and begins in this one
+    if (id >= p.vocab || p.sorted[begin + p.share - 1].x != id || (begin > 0 && p.sorted[begin - 1].x == id)) return;
+    RowSum s;
+    s.clear();
+    auto add = [&](const float* row) {
+        float2 v[4][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = make_float2(acc[j].x + v[j].x, acc[j].y + v[j].y);
+        for (int g = 0; g < 4; ++g)
+            if (col + g * 256 < p.width) load8_stream(row + g * 256, v[g]);
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            if (col + g * 256 < p.width) s.add(g, v[g]);
+    };
+    add(p.parts + (static_cast<int64_t>(share) * 2 + 1) * p.width + col);
+    for (int c = share + 1;; c += 32) {
+        const bool in = c + lane < p.shares && p.sorted[(c + lane) * p.share].x == id;
+        const uint32_t out = ~__ballot_sync(0xffffffffu, in);
+        const int n = out == 0 ? 32 : __ffs(out) - 1;
+#pragma unroll 2
+        for (int k = 0; k < n; ++k) add(p.parts + static_cast<int64_t>(c + k) * 2 * p.width + col);
+        if (n < 32) break;
     }
-    write_row<Out>(p, id, col, acc);
+    if (col < p.width) write_row<Out>(p, id, col, s);
 }
 
-// Positions per chunk: few enough that the device is full at some thousand tokens, and not more than 4096 chunks, so that
-// a token that is most of a long text has not too many partial sums to join.
-static int64_t sum_chunk(int64_t tokens)
+// Rows without tokens of a dense gradient: eight rows per CTA.
+struct FillParams {
+    const uint2* sorted;
+    const uint32_t* first;
+    uint8_t* table;
+    int64_t pitch;               // bytes
+    int32_t vectors;             // 16-byte pieces per row
+    uint32_t tokens, vocab;
+};
+
+constexpr int kFillRows = 8;
+
+__global__ void __launch_bounds__(kFillRows * 32) fill_kernel(const __grid_constant__ FillParams p)
 {
-    const int64_t c = (tokens + 4095) / 4096;
-    return c < 32 ? 32 : (c + 31) / 32 * 32;
+    griddep_launch_dependents();
+    griddep_wait();
+    const uint32_t row = blockIdx.x * kFillRows + (threadIdx.x >> 5);
+    if (row >= p.vocab) return;
+    const uint32_t at = p.first[row];
+    if (at < p.tokens && p.sorted[at].x == row && (at == 0 || p.sorted[at - 1].x != row)) return;
+    uint8_t* to = p.table + row * p.pitch;
+    for (int i = threadIdx.x & 31; i < p.vectors; i += 32) st_stream(to + i * 16, make_uint4(0u, 0u, 0u, 0u));
+}
+
+template <class In, class Out>
+static int launch_sums(const SumParams& s, int64_t units, int sm_count, cudaStream_t st)
+{
+    static PerDeviceOnce once;
+    const size_t smem = sizeof(SumSmem) + 1024;
+    const int rc = ensure_smem_attribute(once, sum_kernel<In, Out>, smem);
+    if (rc != MXFP4_OK) return rc;
+    const int grid = static_cast<int>(std::min<int64_t>(units, sm_count));
+    return launch_kernel_pdl(sum_kernel<In, Out>, grid, kSumWarps * 32, smem, st, s) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
+}
+
+static int64_t sum_slabs(int64_t width) { return (width + kSlab - 1) / kSlab; }
+
+// Sorted positions per warp: all warps of the device have one share of one slab, none less than a few positions.
+static int64_t sum_share(int64_t tokens, int64_t width)
+{
+    const int64_t slabs = sum_slabs(width), shares = slabs < kSumAll ? kSumAll / slabs : 1;
+    return std::max<int64_t>(kLeastShare, (tokens + shares - 1) / shares);
+}
+
+static int64_t sum_shares(int64_t tokens, int64_t width)
+{
+    const int64_t share = sum_share(tokens, width);
+    return (tokens + share - 1) / share;
 }
 
 static size_t sorted_bytes(int64_t tokens) { return round_up(static_cast<size_t>(tokens) * sizeof(uint2), 256); }
@@ -412,11 +588,13 @@ int mxfp4_embedding_forward(const int64_t* ids, int64_t tokens, const void* tabl
                ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
-size_t mxfp4_embedding_workspace_bytes(int64_t tokens, int64_t width)
+size_t mxfp4_embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width)
 {
-    if (tokens <= 0 || width <= 0 || width % 8 != 0 || tokens > 0x3FFFFFFF || width > 0x3FFFFFFF) return 0;
-    const int64_t chunk = sum_chunk(tokens), chunks = (tokens + chunk - 1) / chunk;
-    return 2 * sorted_bytes(tokens) + static_cast<size_t>(chunks) * 2 * width * sizeof(float);
+    if (tokens <= 0 || width <= 0 || vocab <= 0 || width % 8 != 0 || tokens > 0x3FFFFFFF || width > 0x3FFFFFFF ||
+        vocab > 0x3FFFFFFF)
+        return 0;
+    return 2 * sorted_bytes(tokens) + round_up(static_cast<size_t>(vocab) * sizeof(uint32_t), 256) +
+           static_cast<size_t>(sum_shares(tokens, width)) * 2 * width * sizeof(float);
 }
 
 int mxfp4_embedding_backward(const int64_t* ids, int64_t tokens, const void* d_out, int d_out_dtype, int64_t ld_d_out,
@@ -427,57 +605,70 @@ int mxfp4_embedding_backward(const int64_t* ids, int64_t tokens, const void* d_o
     if (!type_ok(d_out_dtype) || !type_ok(d_table_dtype) || !isfinite(scale)) return MXFP4_ERR_ENUM;
     int rc = rows_check(d_out, ld_d_out, d_table, ld_d_table, tokens, width, vocab);
     if (rc != MXFP4_OK) return rc;
-    const size_t need = mxfp4_embedding_workspace_bytes(tokens, width);
+    const size_t need = mxfp4_embedding_workspace_bytes(tokens, vocab, width);
     if (!workspace || workspace_bytes < need) return MXFP4_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MXFP4_ERR_ALIGN;
-    SumParams s;
-    s.slabs = static_cast<int32_t>((width + 255) / 256);
-    s.chunk = static_cast<int32_t>(sum_chunk(tokens));
-    s.chunks = static_cast<int32_t>((tokens + s.chunk - 1) / s.chunk);
-    const int64_t blocks = (static_cast<int64_t>(s.chunks) * s.slabs + kSumWarps - 1) / kSumWarps;
-    if (blocks > 0x7FFFFFFF) return MXFP4_ERR_SHAPE;
     const DeviceInfo& dev = device_info();
     if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool out32 = d_table_dtype == MXFP4_OUT_FP32, in32 = d_out_dtype == MXFP4_OUT_FP32;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
 
     SortParams q;
     q.ids = ids;
-    q.a = static_cast<uint2*>(workspace);
-    q.b = reinterpret_cast<uint2*>(static_cast<uint8_t*>(workspace) + sorted_bytes(tokens));
+    q.a = reinterpret_cast<uint2*>(ws);
+    q.b = reinterpret_cast<uint2*>(ws + sorted_bytes(tokens));
+    q.first = reinterpret_cast<uint32_t*>(ws + 2 * sorted_bytes(tokens));
     q.tokens = static_cast<int32_t>(tokens);
     q.vocab = vocab;
     q.passes = 1;
     while ((vocab >> (kSortBits * q.passes)) != 0) ++q.passes;
-    q.table = static_cast<uint8_t*>(d_table);
-    q.pitch = ld_d_table * (out32 ? 4 : 2);
-    q.row_vectors = static_cast<int32_t>(width * (out32 ? 4 : 2) / 16);
-    static PerDeviceOnce once;
-    const size_t smem = sizeof(SortFillSmem) + 1024;
-    if ((rc = ensure_smem_attribute(once, sort_fill_kernel, smem)) != MXFP4_OK) return rc;
-    // two CTAs of 1024 threads per SM
-    const int fill = accumulate ? 0 : 2 * (dev.sm_count / kSortCtas) - 1;
-    if (launch_kernel_pdl(sort_fill_kernel, kSortCtas * (1 + fill), kSortThreads, smem, st, q) != cudaSuccess)
-        return MXFP4_ERR_CUDA;
+    if (tokens <= kRankMost) {
+        if (launch_kernel_pdl(rank_kernel, (q.tokens + 31) / 32, kRankWarps * 32, 0, st, q) != cudaSuccess) return MXFP4_ERR_CUDA;
+    } else {
+        static PerDeviceOnce once;
+        const size_t smem = sizeof(SortSmem) + 1024;
+        if ((rc = ensure_smem_attribute(once, sort_kernel, smem)) != MXFP4_OK) return rc;
+        if (launch_kernel_pdl(sort_kernel, kSortCtas, kSortThreads, smem, st, q) != cudaSuccess) return MXFP4_ERR_CUDA;
+    }
 
+    SumParams s;
     s.sorted = q.a;
     s.grads = d_out;
     s.table = d_table;
-    s.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 2 * sorted_bytes(tokens));
+    s.parts = reinterpret_cast<float*>(ws + 2 * sorted_bytes(tokens) + round_up(static_cast<size_t>(vocab) * sizeof(uint32_t), 256));
     s.ld_grads = ld_d_out;
     s.ld_table = ld_d_table;
     s.tokens = q.tokens;
     s.width = static_cast<int32_t>(width);
+    s.share = static_cast<int32_t>(sum_share(tokens, width));
+    s.shares = static_cast<int32_t>(sum_shares(tokens, width));
     s.vocab = static_cast<uint32_t>(vocab);
+    s.slabs = static_cast<int32_t>(sum_slabs(width));
     s.accumulate = accumulate != 0;
     s.scale = scale;
-    auto sum = in32 ? (out32 ? sum_kernel<float, float> : sum_kernel<float, __nv_bfloat16>)
-                    : (out32 ? sum_kernel<__nv_bfloat16, float> : sum_kernel<__nv_bfloat16, __nv_bfloat16>);
-    if (launch_kernel_pdl(sum, static_cast<int>(blocks), kSumWarps * 32, 0, st, s) != cudaSuccess) return MXFP4_ERR_CUDA;
-    if (s.chunks == 1) return MXFP4_OK;
-    auto join = out32 ? sum_join_kernel<float> : sum_join_kernel<__nv_bfloat16>;
-    return launch_kernel_pdl(join, static_cast<int>(blocks), kSumWarps * 32, 0, st, s) == cudaSuccess ? MXFP4_OK
-                                                                                                      : MXFP4_ERR_CUDA;
+    const int64_t units = static_cast<int64_t>(s.shares) * s.slabs;
+    rc = in32 ? (out32 ? launch_sums<float, float>(s, units, dev.sm_count, st) : launch_sums<float, __nv_bfloat16>(s, units, dev.sm_count, st))
+              : (out32 ? launch_sums<__nv_bfloat16, float>(s, units, dev.sm_count, st)
+                       : launch_sums<__nv_bfloat16, __nv_bfloat16>(s, units, dev.sm_count, st));
+    if (rc != MXFP4_OK) return rc;
+    if (s.shares > 1) {
+        auto join = out32 ? sum_join_kernel<float> : sum_join_kernel<__nv_bfloat16>;
+        if (launch_kernel_pdl(join, static_cast<int>((units + kSumWarps - 1) / kSumWarps), kSumWarps * 32, 0, st, s) != cudaSuccess)
+            return MXFP4_ERR_CUDA;
+    }
+    if (accumulate) return MXFP4_OK;
+    FillParams f;
+    f.sorted = q.a;
+    f.first = q.first;
+    f.table = static_cast<uint8_t*>(d_table);
+    f.pitch = ld_d_table * (out32 ? 4 : 2);
+    f.vectors = static_cast<int32_t>(width * (out32 ? 4 : 2) / 16);
+    f.tokens = static_cast<uint32_t>(tokens);
+    f.vocab = static_cast<uint32_t>(vocab);
+    return launch_kernel_pdl(fill_kernel, static_cast<int>((vocab + kFillRows - 1) / kFillRows), kFillRows * 32, 0, st, f) ==
+                   cudaSuccess
+               ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -25,13 +25,14 @@
 namespace mxfp4 {
 
 constexpr int kNormBlock = 16384;                  // elements
-constexpr int kNormThreads = 512;
+constexpr int kNormThreads = 256;
 constexpr int kNormWarps = kNormThreads / 32;
-constexpr int kNormUnroll = 4;                     // 16-byte pieces in flight per thread
-constexpr int kNormCtas = 296;                     // two per SM; a constant, so that results do not depend on the device
+constexpr int kNormUnroll = 8;                     // 16-byte pieces in flight per thread
+constexpr int kClipUnroll = 4;
+constexpr int kNormCtas = 592;                     // four per SM; a constant, so that results do not depend on the device
 constexpr int kNormMostTensors = 640;              // per launch: 30 KB of arguments
 
-struct NormTensor {
+struct GradTensor {
     const void* in;
     void* out;
     int64_t numel;
@@ -40,7 +41,7 @@ struct NormTensor {
 };
 
 template <int N>
-struct NormParams {
+struct GradNormParams {
     double* parts;               // of this launch: [kNormCtas]
     const double* all;           // of all launches
     int32_t launches;            // whose partial sums are in `all`
@@ -48,12 +49,12 @@ struct NormParams {
     float* norm;
     float max_norm, eps;
     int32_t write_norm;
-    NormTensor t[N];
+    GradTensor t[N];
 };
 
 // The tensor a block belongs to.
 template <int N>
-__device__ __forceinline__ int norm_tensor_of(const NormParams<N>& p, int block)
+__device__ __forceinline__ int norm_tensor_of(const GradNormParams<N>& p, int block)
 {
     int lo = 0, hi = p.count - 1;
     while (lo < hi) {
@@ -136,14 +137,14 @@ __device__ __forceinline__ double warp_sum(double v)
 }
 
 template <int N>
-__global__ void __launch_bounds__(kNormThreads, 2) norm_kernel(const __grid_constant__ NormParams<N> p)
+__global__ void __launch_bounds__(kNormThreads, 4) grad_norm_kernel(const __grid_constant__ GradNormParams<N> p)
 {
     __shared__ double part[kNormWarps];
     griddep_launch_dependents();
     griddep_wait();
     double sum = 0.0;
     for (int b = blockIdx.x; b < p.blocks; b += kNormCtas) {
-        const NormTensor& t = p.t[norm_tensor_of(p, b)];
+        const GradTensor& t = p.t[norm_tensor_of(p, b)];
         const int64_t at = static_cast<int64_t>(b - t.first_block) * kNormBlock;
         const int n = static_cast<int>(min(t.numel - at, static_cast<int64_t>(kNormBlock)));
         sum += t.in32 ? block_squares(static_cast<const float*>(t.in) + at, n)
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_kernel(const __grid_cons
 
 // The norm from the partial sums, the same in every CTA.
 template <int N>
-__device__ __forceinline__ float norm_of(const NormParams<N>& p, double (&part)[kNormWarps])
+__device__ __forceinline__ float norm_of(const GradNormParams<N>& p, double (&part)[kNormWarps])
 {
     double sum = 0.0;
     for (int i = threadIdx.x; i < p.launches * kNormCtas; i += kNormThreads) sum += p.all[i];
@@ -188,17 +189,17 @@ __device__ __forceinline__ void block_scale(const In* x, Out* y, int n, float fa
         return;
     }
     const int pieces = (n - head) / kPer, tail = head + pieces * kPer;
-    for (int i = threadIdx.x; i < pieces; i += kNormThreads * kNormUnroll) {
-        uint4 w[kNormUnroll][sizeof(In) * kPer / 16];
+    for (int i = threadIdx.x; i < pieces; i += kNormThreads * kClipUnroll) {
+        uint4 w[kClipUnroll][sizeof(In) * kPer / 16];
 #pragma unroll
-        for (int u = 0; u < kNormUnroll; ++u) {
+        for (int u = 0; u < kClipUnroll; ++u) {
             if (i + u * kNormThreads >= pieces) break;
 #pragma unroll
             for (int h = 0; h < static_cast<int>(sizeof(In)) * kPer / 16; ++h)
                 w[u][h] = ld_stream(reinterpret_cast<const uint4*>(x + head + (i + u * kNormThreads) * kPer) + h);
         }
 #pragma unroll
-        for (int u = 0; u < kNormUnroll; ++u) {
+        for (int u = 0; u < kClipUnroll; ++u) {
             if (i + u * kNormThreads >= pieces) break;
             float v[kPer];
             if constexpr (sizeof(In) == 2) {
@@ -239,7 +240,7 @@ __device__ __forceinline__ void block_scale(const In* x, Out* y, int n, float fa
 }
 
 template <int N>
-__global__ void __launch_bounds__(kNormThreads, 2) clip_kernel(const __grid_constant__ NormParams<N> p)
+__global__ void __launch_bounds__(kNormThreads, 4) clip_grads_kernel(const __grid_constant__ GradNormParams<N> p)
 {
     __shared__ double part[kNormWarps];
     griddep_launch_dependents();
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) clip_kernel(const __grid_cons
     const float share = p.max_norm / (norm + p.eps);
     const float factor = norm <= 3.402823466e38f && share < 1.0f ? share : 1.0f;       // not finite: as they are
     for (int b = p.blocks - 1 - static_cast<int>(blockIdx.x); b >= 0; b -= gridDim.x) {
-        const NormTensor& t = p.t[norm_tensor_of(p, b)];
+        const GradTensor& t = p.t[norm_tensor_of(p, b)];
         if (factor == 1.0f && t.in == t.out && t.in32 == t.out32) continue;
         const int64_t at = static_cast<int64_t>(b - t.first_block) * kNormBlock;
         const int n = static_cast<int>(min(t.numel - at, static_cast<int64_t>(kNormBlock)));
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) clip_kernel(const __grid_cons
 }
 
 // The norm alone.
-__global__ void __launch_bounds__(kNormThreads) norm_join_kernel(const __grid_constant__ NormParams<1> p)
+__global__ void __launch_bounds__(kNormThreads) grad_norm_join_kernel(const __grid_constant__ GradNormParams<1> p)
 {
     __shared__ double part[kNormWarps];
     griddep_launch_dependents();
@@ -277,7 +278,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_join_kernel(const __grid_co
     if (threadIdx.x == 0) *p.norm = norm;
 }
 
-struct NormCall {
+struct GradNormCall {
     const void* const* in;
     void* const* out;            // NULL: the norm alone
     const int64_t* numel;
@@ -288,7 +289,7 @@ struct NormCall {
 
 // Fills a launch's descriptors from tensor `first` on; returns how many tensors it took.  Empty ones are passed by.
 template <int N>
-static int64_t norm_fill(NormParams<N>& p, const NormCall& c, int64_t first)
+static int64_t norm_fill(GradNormParams<N>& p, const GradNormCall& c, int64_t first)
 {
     p.count = p.blocks = 0;
     int64_t i = first;
@@ -296,7 +297,7 @@ static int64_t norm_fill(NormParams<N>& p, const NormCall& c, int64_t first)
         if (c.numel[i] == 0) continue;
         const int64_t blocks = (c.numel[i] + kNormBlock - 1) / kNormBlock;
         if (blocks > 0x7FFFFFFF - p.blocks) break;
-        NormTensor& t = p.t[p.count++];
+        GradTensor& t = p.t[p.count++];
         t.in = c.in[i];
         t.out = c.out ? c.out[i] : nullptr;
         t.numel = c.numel[i];
@@ -311,10 +312,10 @@ static int64_t norm_fill(NormParams<N>& p, const NormCall& c, int64_t first)
 static int64_t norm_launches(int64_t count) { return (count + kNormMostTensors - 1) / kNormMostTensors; }
 
 template <int N>
-static int norm_run(const NormCall& c, float max_norm, float eps, float* norm, double* parts, cudaStream_t st)
+static int norm_run(const GradNormCall& c, float max_norm, float eps, float* norm, double* parts, cudaStream_t st)
 {
-    NormParams<N> p;
-    memset(&p, 0, offsetof(NormParams<N>, t));
+    GradNormParams<N> p;
+    memset(&p, 0, offsetof(GradNormParams<N>, t));
     p.all = parts;
     p.norm = norm;
     p.max_norm = max_norm;
@@ -323,35 +324,35 @@ static int norm_run(const NormCall& c, float max_norm, float eps, float* norm, d
     for (int64_t i = 0; i < c.count;) {
         i += norm_fill(p, c, i);
         p.parts = parts + launches++ * kNormCtas;
-        if (launch_kernel_pdl(norm_kernel<N>, kNormCtas, kNormThreads, 0, st, p) != cudaSuccess) return MXFP4_ERR_CUDA;
+        if (launch_kernel_pdl(grad_norm_kernel<N>, kNormCtas, kNormThreads, 0, st, p) != cudaSuccess) return MXFP4_ERR_CUDA;
     }
     if (!c.out) {
-        NormParams<1> q;
+        GradNormParams<1> q;
         memset(&q, 0, sizeof(q));
         q.all = parts;
         q.norm = norm;
         q.launches = static_cast<int32_t>(launches);
-        return launch_kernel_pdl(norm_join_kernel, 1, kNormThreads, 0, st, q) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
+        return launch_kernel_pdl(grad_norm_join_kernel, 1, kNormThreads, 0, st, q) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
     }
     p.launches = static_cast<int32_t>(launches);
     p.write_norm = 1;
     for (int64_t i = 0; i < c.count; p.write_norm = 0) {
         i += norm_fill(p, c, i);
         const int ctas = p.blocks < kNormCtas ? (p.blocks > 0 ? p.blocks : 1) : kNormCtas;
-        if (launch_kernel_pdl(clip_kernel<N>, ctas, kNormThreads, 0, st, p) != cudaSuccess) return MXFP4_ERR_CUDA;
+        if (launch_kernel_pdl(clip_grads_kernel<N>, ctas, kNormThreads, 0, st, p) != cudaSuccess) return MXFP4_ERR_CUDA;
     }
     return MXFP4_OK;
 }
 
 // Whether an output overlaps another tensor of the call.
-struct NormSpan {
+struct GradSpan {
     uintptr_t begin, end;
     bool written;
 };
 
-static int norm_overlap(const NormCall& c)
+static int norm_overlap(const GradNormCall& c)
 {
-    NormSpan* s = static_cast<NormSpan*>(malloc(sizeof(NormSpan) * 2 * static_cast<size_t>(c.count)));
+    GradSpan* s = static_cast<GradSpan*>(malloc(sizeof(GradSpan) * 2 * static_cast<size_t>(c.count)));
     if (!s) return MXFP4_ERR_WORKSPACE;
     size_t n = 0;
     for (int64_t i = 0; i < c.count; ++i) {
@@ -361,7 +362,7 @@ static int norm_overlap(const NormCall& c)
         if (a != b || c.in_dtype[i] != c.out_dtype[i])
             s[n++] = {a, a + c.numel[i] * (c.in_dtype[i] == MXFP4_OUT_FP32 ? 4u : 2u), false};
     }
-    std::sort(s, s + n, [](const NormSpan& x, const NormSpan& y) { return x.begin < y.begin; });
+    std::sort(s, s + n, [](const GradSpan& x, const GradSpan& y) { return x.begin < y.begin; });
     uintptr_t all = 0, written = 0;    // ends of what began so far, and of what of it is written
     int rc = MXFP4_OK;
     for (size_t i = 0; i < n && rc == MXFP4_OK; ++i) {
@@ -387,7 +388,7 @@ size_t mxfp4_grad_norm_workspace_bytes(int64_t count)
     return static_cast<size_t>(norm_launches(count)) * kNormCtas * sizeof(double);
 }
 
-static int norm_call(const NormCall& c, float max_norm, float eps, float* norm, void* workspace, size_t workspace_bytes,
+static int norm_call(const GradNormCall& c, float max_norm, float eps, float* norm, void* workspace, size_t workspace_bytes,
                      void* stream)
 {
     if (c.count <= 0 || c.count > 0x3FFFFFFF) return MXFP4_ERR_SHAPE;
@@ -418,7 +419,7 @@ int mxfp4_grad_norm(const void* const* tensors, const int64_t* numel, const int3
                     void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!tensors || !numel || !dtypes || !norm) return MXFP4_ERR_NULL;
-    const NormCall c = {tensors, nullptr, numel, dtypes, nullptr, count};
+    const GradNormCall c = {tensors, nullptr, numel, dtypes, nullptr, count};
     return norm_call(c, 0.0f, 0.0f, norm, workspace, workspace_bytes, stream);
 }
 
@@ -428,7 +429,7 @@ int mxfp4_clip_grads(const void* const* tensors, const int64_t* numel, const int
 {
     if (!tensors || !numel || !dtypes || !out || !out_dtypes || !norm) return MXFP4_ERR_NULL;
     if (!(max_norm >= 0.0f) || !(eps >= 0.0f) || isinf(eps)) return MXFP4_ERR_ENUM;
-    const NormCall c = {tensors, out, numel, dtypes, out_dtypes, count};
+    const GradNormCall c = {tensors, out, numel, dtypes, out_dtypes, count};
     return norm_call(c, max_norm, eps, norm, workspace, workspace_bytes, stream);
 }
 

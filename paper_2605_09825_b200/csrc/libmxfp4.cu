@@ -964,12 +964,12 @@ int mxfp4_check(void* stream)
     // each translation unit has a word of its own; the first one set is reported
     int status = 0, more[7] = {};
     if (take_device_status(&status) != 0 || block128_take_status(&more[0]) != 0 ||
-        residual_norm_take_status(&more[1]) != 0 || dense_take_status(&more[2]) != 0)
+        residual_norm_take_status(&more[1]) != 0 || dense_take_status(&more[2]) != 0 || embedding_take_status(&more[5]) != 0)
         return MXFP4_ERR_CUDA;
     // the kernels of these have no wait that could run out: only the bounds-checking build sets their words
     if (mxfp4_bounds_checked() &&
         (logprobs_take_status(&more[3]) != 0 || linear_logprobs_take_status(&more[4]) != 0 ||
-         embedding_take_status(&more[5]) != 0 || grad_norm_take_status(&more[6]) != 0))
+         grad_norm_take_status(&more[6]) != 0))
         return MXFP4_ERR_CUDA;
     for (int m : more)
         if (status == 0) status = m;

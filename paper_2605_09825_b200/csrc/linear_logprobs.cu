@@ -35,9 +35,10 @@ struct LossJoinParams {
     int32_t rows, pieces;
 };
 
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 32;
+constexpr int kJoinUnroll = 4;   // partial results in flight per lane
 
-// 32 rows per CTA, one per lane; the warps take every eighth partial result and are joined in their order.
+// 32 rows per CTA, one per lane; the warps take the partial results in turn and are joined in their order.
 __global__ void __launch_bounds__(kJoinWarps * 32) loss_join_kernel(const LossJoinParams p)
 {
     __shared__ float2 part[kJoinWarps][32];
@@ -52,8 +53,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32) loss_join_kernel(const LossJo
     };
     float2 v = make_float2(-INFINITY, 0.0f);
     if (row < p.rows) {
-#pragma unroll 4
-        for (int i = warp; i < p.pieces; i += kJoinWarps) join(v, p.parts[i * p.ld_parts + row]);
+        for (int i = warp; i < p.pieces; i += kJoinWarps * kJoinUnroll) {
+            float2 w[kJoinUnroll];
+#pragma unroll
+            for (int u = 0; u < kJoinUnroll; ++u)
+                w[u] = i + u * kJoinWarps < p.pieces ? p.parts[(i + u * kJoinWarps) * p.ld_parts + row] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int u = 0; u < kJoinUnroll; ++u) join(v, w[u]);
+        }
     }
     smem_store(&part[warp][lane], v, part, sizeof(part));
     __syncthreads();

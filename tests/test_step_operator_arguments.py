@@ -35,7 +35,8 @@ def test_sizes(lib):
     assert l(8192, 64, 128256, 1) == 8192 * 16384 * 2 + 8192 * 64 * 4
     assert l(0, 8, 8, 0) == l(8, 12, 8, 0) == l(8, 8, 0, 1) == l(HUGE, 8, 8, 1) == 0
     e = lib.mxfp4_embedding_workspace_bytes
-    assert e(1, 8) == 2 * 256 + 2 * 8 * 4 and e(0, 8) == e(8, 12) == e(1 << 31, 8) == 0
+    assert e(1, 10, 8) == 3 * 256 + 64 and e(100, 10, 8) == 2 * 1024 + 256 + 13 * 64
+    assert e(0, 8, 8) == e(8, 8, 12) == e(1 << 31, 8, 8) == e(8, 0, 8) == 0
     n = lib.mxfp4_grad_norm_workspace_bytes
     assert n(1) == n(640) == n(641) // 2 and n(0) == n(-1) == 0
 
