@@ -541,7 +541,7 @@ int mxfp4_logprobs_backward(const void* logits, int dtype, int64_t tokens, int64
  *     dx = dg Wg + du Wu,      dWg = dg^T x,   dWu = du^T x
  *   dx bf16 [tokens x in_features]; dw_gate, dw_up (dw_dtype, MXFP4_OUT_*) [features x in_features], ld_dw; dx, or
  *   both weight gradients, may be NULL: not wanted.  act' of _RELU at 0 is 0.
- *   workspace: mxfp4_gated_linear_workspace_bytes bytes (dg and du), 16-byte aligned.
+ *   workspace: mxfp4_gated_linear_workspace_bytes bytes (dg and du, and partial sums of dx for few tokens), 16-byte aligned.
  * Calls repeat bit for bit.
  */
 typedef struct mxfp4_gated_desc {
@@ -556,7 +556,7 @@ typedef struct mxfp4_gated_desc {
 } mxfp4_gated_desc;
 int mxfp4_gated_linear_forward(const mxfp4_gated_desc* gated, void* h, int64_t ld_h, void* gate, void* up,
                                int64_t ld_kept, void* stream);
-size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t features);
+size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t in_features, int64_t features);
 int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, int64_t ld_dh, const void* gate,
                                 const void* up, int64_t ld_kept, void* dx, int64_t ld_dx, void* dw_gate, void* dw_up,
                                 int64_t ld_dw, int dw_dtype, void* workspace, size_t workspace_bytes, void* stream);

@@ -157,7 +157,7 @@ def load_library() -> ctypes.CDLL:
             ("mxfp4_logprobs_forward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, ci, vp, vp, vp, sz, vp], ci),
             ("mxfp4_logprobs_backward", [vp, ci, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp], ci),
             ("mxfp4_gated_linear_forward", [gated, vp, i64, vp, vp, i64, vp], ci),
-            ("mxfp4_gated_linear_workspace_bytes", [i64, i64], sz),
+            ("mxfp4_gated_linear_workspace_bytes", [i64, i64, i64], sz),
             ("mxfp4_gated_linear_backward", [gated, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, ci, vp, sz, vp], ci),
             ("mxfp4_linear_logprobs_workspace_bytes", [i64, i64, i64, ci], sz),
             ("mxfp4_linear_logprobs_forward", [vp, i64, vp, i64, i64, i64, i64, vp, f32, vp, vp, vp, sz, vp], ci),
@@ -939,7 +939,7 @@ def gated_linear_backward(dh, x, w_gate, w_up, kept, act: int = GATE_SILU, dw_dt
         if ld_dw != ld_du:
             raise ValueError("dw_gate and dw_up must have the same row stride")
     if workspace is None:
-        workspace = torch.empty(max(lib.mxfp4_gated_linear_workspace_bytes(T, F), 1), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(lib.mxfp4_gated_linear_workspace_bytes(T, D, F), 1), dtype=torch.uint8, device=dev)
     _on_current_device(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, workspace)
     rc = lib.mxfp4_gated_linear_backward(ctypes.byref(d), dh_ptr, ld_dh, g_ptr, u_ptr, ld_kept, dx_ptr, ld_dx, dg_ptr, du_ptr,
                                          ld_dw, dw_dtype, _dev_ptr(workspace), workspace.numel(), _raw_stream())

@@ -6,32 +6,47 @@
 
 namespace mxfp4 {
 
-enum DenseEpilogue { kDenseBf16, kDenseF32, kDenseAddF32, kDenseGated, kDensePartials, kDenseLogitGrad };
+enum DenseEpilogue { kDenseStore, kDenseGated, kDensePartials, kDenseLogitGrad };
+enum DenseOut { kDenseBf16, kDenseF32, kDenseAddF32 };
 
 constexpr int64_t kDenseMaxDim = 0x7FFFFF00;
+constexpr int kDensePairs = 74;  // work is shared out for the pairs of CTAs of this many SMs, whatever the device has
 
-// What the kernel reads besides its tensor maps.
-struct DenseParams {
+// Sizes of one product as the kernel needs them.
+struct DenseShape {
     int32_t M, N, K;             // of one segment; gated: N features of each projection
     int32_t tiles_m, tiles_n;    // of all segments
     int32_t seg_tiles_m;
     int32_t k_steps;             // of all segments
     int32_t seg_k_steps;
     int32_t band;                // tile columns per band of the tile order
-    // gated
-    int32_t act;
+    int32_t splits;              // pieces along K, each with an output of its own
+    int32_t split_rows;          // output rows from one piece's to the next one's
+    int32_t items;               // tiles * splits
+    int32_t a_mn;                // A is stored along its own rows
+    int32_t out;                 // DenseOut
+};
+
+// What the epilogues read.
+struct DenseExtra {
+    int32_t act;                 // gated
     int32_t keep;                // g and u are stored too
     // log probabilities: columns col_base .. col_base + N of `vocab`
+    float scale;
+    int32_t ld_grad;             // columns of the gradient's buffer, those past N set to 0
     int64_t vocab, col_base;
     const int64_t* targets;
-    float scale;
     const float* lse;
     const float* d_logp;
     const float* d_lse;
     float2* parts;               // [ceil(N / 128)][ld_parts]: maximum, sum of exponentials
     int64_t ld_parts;
     float* picked;               // the target's value
-    int32_t ld_grad;             // columns of the gradient's buffer, those past N set to 0
+};
+
+struct DenseParams {
+    DenseShape q[2];             // a launch's products
+    DenseExtra x;
 };
 
 struct DenseMatrix {
@@ -39,18 +54,44 @@ struct DenseMatrix {
     int64_t ld;                  // elements
 };
 
-// One launch.  a and b are stored along K, or (a_mn, b_mn) along their own rows: [K x M], [K x N].  `stack_m`: two
-// matrices a, each with its own output; `stack_k`: two pairs (a, b) whose products are added.
-struct DenseCall {
-    DenseEpilogue epilogue;
+// a and b are stored along K, or (a_mn, b_mn) along their own rows: [K x M], [K x N].  `stack_m`: two matrices a, each with
+// its own output; `stack_k`: two pairs (a, b) whose products are added.  splits > 1 (not with stack_m): out[0] has
+// dense_split_rows(M) rows per piece.
+struct DenseProduct {
+    int64_t M = 0, N = 0, K = 0;
     bool a_mn = false, b_mn = false;
     bool stack_m = false, stack_k = false;
+    int splits = 1;
+    DenseOut kind = kDenseBf16;
     DenseMatrix a[2] = {}, b[2] = {}, out[3] = {};
-    DenseParams p = {};
 };
 
-int dense_launch(DenseCall& call, int sm_count, cudaStream_t st);
+// One launch of one or two products with plain outputs (b stored along its rows), or of one with another epilogue.
+int dense_store(const DenseProduct* products, int n, int sm_count, cudaStream_t st);
+int dense_fused(DenseEpilogue epilogue, const DenseProduct& product, const DenseExtra& extra, int sm_count, cudaStream_t st);
+
+// The sum of `pieces` products of splits as dense_store leaves them, to bf16; cols a multiple of 8.
+int dense_round(const float* from, int pieces, int64_t rows, int64_t cols, void* to, int64_t ld, int sm_count, cudaStream_t st);
 
 inline int64_t dense_tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+inline int64_t dense_split_rows(int64_t M) { return dense_tiles(M, 256) * 256; }
+
+// Pieces along K for a product of few tiles: as many as keep the pairs busiest, none shorter than eight steps of 64; a piece
+// costs about eight steps besides its own.  With
+// more tiles than pairs a tile stays whole; what a last, partial wave leaves idle is filled by a launch's other product.
+inline int dense_splits(int64_t M, int64_t N, int64_t K_all)
+{
+    const int64_t tiles = dense_tiles(M, 256) * dense_tiles(N, 256), steps = dense_tiles(K_all, 64);
+    int best = 1;
+    int64_t least = (steps + 8) * 3 / 4;             // the pieces have to be written, read and added up
+    for (int s = 2; s <= 32 && tiles < kDensePairs && steps / s >= 8; ++s) {
+        const int64_t t = dense_tiles(tiles * s, kDensePairs) * (dense_tiles(steps, s) + 8);
+        if (t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
+}
 
 }  // namespace mxfp4

@@ -9,12 +9,13 @@
 // descriptor names the transposed layout.  No transposed copy exists anywhere.
 //
 // Two matrices of the same shape may stand in for one along M (both weight gradients of a pair of projections in
-// one launch) or along K (the input's gradient, a sum of two products).
+// one launch) or along K (the input's gradient, a sum of two products).  A launch may take two products, the one with the
+// longer tiles first: the shorter tiles of the other fill the pairs that a last round of long ones leaves idle.  A
+// product of few tiles is split along K, each piece with an output of its own, which the caller adds up.
 //
 // Epilogues:
-//   kDenseBf16, kDenseF32   the sums, rounded or not
-//   kDenseAddF32            added to the fp32 output by the copy engine; one addition per element and launch,
-//                           so results do not depend on scheduling
+//   kDenseStore             the sums, rounded or not, or added to the fp32 output by the copy engine: one addition per element
+//                           and launch, so results do not depend on scheduling
 //   kDenseGated             columns 0..127 of a tile are a gate's, 128..255 the other projection's of the same features
 //                           (the pair's first CTA loads the rows of one weight, the second those of the other): act(g) * u,
 //                           and g and u on request
@@ -42,19 +43,23 @@ namespace mxfp4 {
 constexpr int kDTile = 256;                        // both ways
 constexpr int kDHalf = 128;                        // rows of A, and of B, per CTA
 constexpr int kDBlockK = 64;                       // elements: 128 bytes
-constexpr int kDStages = 6;
 constexpr int kDOperandBytes = kDHalf * kDBlockK * 2;
 constexpr int kDBoxBytes = kDOperandBytes / 2;     // 64 columns x 64 rows of a transposed operand
 constexpr int kDEpiWarps = 8;
 constexpr int kDProducerWarp = 8;
 constexpr int kDMmaWarp = 9;
 constexpr int kDThreads = 320;
-constexpr int kDStageBytes = 32 * 128;             // output staging per epilogue warp
+constexpr int kDStageBytes = 32 * 128;             // output staging per epilogue warp and box
 
+// Two output boxes per warp, so that one is filled while the other leaves, are worth a stage of operands where tiles are
+// short (weight gradients of few tokens) or have several outputs.
+template <int EPI>
 struct DenseSmem {
+    static constexpr int kBoxes = EPI == kDenseStore || EPI == kDenseGated ? 2 : 1;
+    static constexpr int kDStages = 7 - kBoxes;
     alignas(1024) uint8_t a[kDStages][kDOperandBytes];
     alignas(1024) uint8_t b[kDStages][kDOperandBytes];
-    alignas(1024) uint8_t out_stage[kDEpiWarps][kDStageBytes];
+    alignas(1024) uint8_t out_stage[kDEpiWarps][kBoxes][kDStageBytes];
     alignas(16) uint64_t full[kDStages];           // leader's copy is the live one
     uint64_t empty[kDStages];                      // both, via multicast commit
     uint64_t tmem_full[2];                         // both, via multicast commit
@@ -66,24 +71,74 @@ struct DenseSmem {
 struct DenseMaps {
     CUtensorMap a[2], b[2], out[3];
 };
+struct DenseMaps2 {
+    DenseMaps q[2];              // of a launch's products
+};
 
-// Row and column of a tile.  Tiles are numbered band by band: a band is `band` tile columns, and inside it the tile
-// column varies fastest, so that the tiles in flight share rows of A and of B.
-__device__ __forceinline__ void dense_place(const DenseParams& p, int tile, int& tm, int& tn)
+// A piece of work: a tile of one of the products, a range of K-steps of it.
+struct DenseWork {
+    int q;                       // product; -1: no more work
+    int tm, tn;
+    int seg;                     // segment along M
+    int row;                     // first row of the tile, in its segment
+    int out_row;                 // in the output
+    int k0, k1;
+};
+
+// The j-th piece of work of a pair.  The first product's pieces go round the pairs; those that a last round leaves out take
+// as many of the second product's as one of the first's is long, and the rest of these goes round all pairs,
+// beginning with them.
+template <bool TWO>
+__device__ __forceinline__ DenseWork dense_work(const DenseParams& p, int pair, int pairs, int j)
 {
-    const int per_band = p.band * p.tiles_m;
+    DenseWork w;
+    int item = pair + j * pairs;
+    w.q = 0;
+    if (item >= p.q[0].items) {
+        w.q = -1;
+        if (!TWO || p.q[1].items == 0) return w;
+        const int n0 = p.q[0].items, n1 = p.q[1].items;
+        const int left = n0 % pairs;               // pairs that the first product's last round keeps busy
+        const int idle = pairs - left;
+        int extra = 0;                             // pieces of the second product for each of the others
+        if (left > 0) {
+            // a tile costs about eight steps besides its own
+            extra = (p.q[0].k_steps / p.q[0].splits + 8) / (p.q[1].k_steps + 8);
+            extra = min(extra, n1 / idle);
+        }
+        int i = j - n0 / pairs - (pair < left);
+        if (pair >= left && i < extra) {
+            item = pair - left + i * idle;
+        } else {
+            if (pair >= left) i -= extra;
+            item = idle * extra + (pair >= left ? pair - left : pair + idle) + i * pairs;
+        }
+        if (item >= n1) return w;
+        w.q = 1;
+    }
+    const DenseShape& q = p.q[w.q];
+    // tiles band by band: a band is `band` tile columns, and inside it the tile column varies fastest, so that the tiles
+    // in flight share rows of A and of B
+    const int tiles = q.tiles_m * q.tiles_n;
+    const int split = item / tiles, tile = item - split * tiles;
+    const int per_band = q.band * q.tiles_m;
     const int b = tile / per_band;
     const int r = tile - b * per_band;
-    const int cols = min(p.band, p.tiles_n - b * p.band);
-    tm = r / cols;
-    tn = b * p.band + (r - tm * cols);
+    const int cols = min(q.band, q.tiles_n - b * q.band);
+    w.tm = r / cols;
+    w.tn = b * q.band + (r - w.tm * cols);
+    w.seg = w.tm >= q.seg_tiles_m;
+    w.row = (w.tm - w.seg * q.seg_tiles_m) * kDTile;
+    w.out_row = w.row + split * q.split_rows;
+    w.k0 = static_cast<int>(static_cast<int64_t>(q.k_steps) * split / q.splits);
+    w.k1 = static_cast<int>(static_cast<int64_t>(q.k_steps) * (split + 1) / q.splits);
+    return w;
 }
 
 // One operand of a K-step: 128 rows x 64 elements of K, or the transposed 64 x 128 in two boxes.
-template <bool MN>
-__device__ __forceinline__ void dense_load(uint8_t* to, const CUtensorMap* map, uint32_t bar, int row, int k)
+__device__ __forceinline__ void dense_load(bool mn, uint8_t* to, const CUtensorMap* map, uint32_t bar, int row, int k)
 {
-    if (MN) {
+    if (mn) {
         tma_load_2d_pair(to, map, bar, row, k);
         tma_load_2d_pair(to + kDBoxBytes, map, bar, row + 64, k);
     } else {
@@ -106,18 +161,20 @@ __device__ __forceinline__ float dense_exp(float x)
     return r;
 }
 
-template <int EPI, bool A_MN, bool B_MN>
+// kDenseStore takes B along its own rows and two products; the other epilogues take both operands along K and one product.
+template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDThreads, 1)
-dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseParams p)
+dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant__ DenseParams p)
 {
     extern __shared__ uint8_t smem_raw[];
-    DenseSmem& sm = *reinterpret_cast<DenseSmem*>(smem_align_1024(smem_raw));
+    DenseSmem<EPI>& sm = *reinterpret_cast<DenseSmem<EPI>*>(smem_align_1024(smem_raw));
+    constexpr int kDStages = DenseSmem<EPI>::kDStages, kBoxes = DenseSmem<EPI>::kBoxes;
     const int warp = threadIdx.x >> 5;
     const int lane = lane_id();
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1;
     const int n_clusters = gridDim.x >> 1;
-    const int tiles = p.tiles_m * p.tiles_n;
+    constexpr bool kStore = EPI == kDenseStore;
     constexpr bool kGated = EPI == kDenseGated;
 
     if (threadIdx.x == 0) {
@@ -150,23 +207,25 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
             int s = 0;
             uint32_t parity = 1;                       // of the phase before: a fresh barrier passes
             bool alive = true;
-            for (int tile = cluster_id; alive && tile < tiles; tile += n_clusters) {
-                int tm, tn;
-                dense_place(p, tile, tm, tn);
-                const int seg_m = tm >= p.seg_tiles_m;
-                const int ya = (tm - seg_m * p.seg_tiles_m) * kDTile + static_cast<int>(rank) * kDHalf;
-                const int yb = kGated ? tn * kDHalf : tn * kDTile + static_cast<int>(rank) * kDHalf;
-                for (int k = 0; k < p.k_steps; ++k) {
+            for (int j = 0; alive; ++j) {
+                const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, j);
+                if (w.q < 0) break;
+                const DenseShape& q = p.q[w.q];
+                const DenseMaps& m = maps.q[w.q];
+                const bool a_mn = kStore && q.a_mn;
+                const int ya = w.row + static_cast<int>(rank) * kDHalf;
+                const int yb = kGated ? w.tn * kDHalf : w.tn * kDTile + static_cast<int>(rank) * kDHalf;
+                for (int k = w.k0; k < w.k1; ++k) {
                     if (!mbar_wait(&sm.empty[s], parity, &sm.abort_flag)) {
                         alive = false;
                         break;
                     }
-                    const int seg_k = k >= p.seg_k_steps;
-                    const int kk = (k - seg_k * p.seg_k_steps) * kDBlockK;
+                    const int seg_k = k >= q.seg_k_steps;
+                    const int kk = (k - seg_k * q.seg_k_steps) * kDBlockK;
                     const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
                     mbar_arrive_expect_tx_cluster(full, 2 * kDOperandBytes);
-                    dense_load<A_MN>(sm.a[s], &maps.a[seg_m + seg_k], full, ya, kk);
-                    dense_load<B_MN>(sm.b[s], &maps.b[kGated ? rank : seg_k], full, yb, kk);
+                    dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk);
+                    dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk);
                     if (++s == kDStages) {
                         s = 0;
                         parity ^= 1;
@@ -189,33 +248,39 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         // ------------------------------------------------------------ MMA issuer
         if (rank == 0 && elect_one_sync()) {
             // fp32 accumulator, bf16 x bf16, 256 x 256 x 16
-            constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
-                                       (static_cast<uint32_t>(kDTile >> 3) << 17) | (static_cast<uint32_t>(kDTile >> 4) << 24);
+            constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | (kStore ? 1u << 16 : 0u) |
+                                        (static_cast<uint32_t>(kDTile >> 3) << 17) | (static_cast<uint32_t>(kDTile >> 4) << 24);
             // along K: 8-row groups 1024 bytes apart, an instruction's 16 elements are 32 bytes; transposed: 64-column boxes
             // 8 KB apart, 8-row groups of K 1024 bytes apart, 16 rows are 2 KB
-            const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), A_MN ? kDBoxBytes : 16, 1024, 2);
-            const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), B_MN ? kDBoxBytes : 16, 1024, 2);
-            constexpr int kStepA = A_MN ? 128 : 2, kStepB = B_MN ? 128 : 2;
+            const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), kStore ? kDBoxBytes : 16, 1024, 2);
+            constexpr int kStepB = kStore ? 128 : 2;
             int s = 0, b = 0;
             uint32_t parity = 0, buf_parity = 1;       // a fresh tmem_empty passes for the phase before
             bool alive = true;
-            for (int tile = cluster_id; alive && tile < tiles; tile += n_clusters) {
+            for (int i = 0; alive; ++i) {
+                const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, i);
+                if (w.q < 0) break;
+                const DenseShape& q = p.q[w.q];
+                const bool a_mn = kStore && q.a_mn;
+                const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), a_mn ? kDBoxBytes : 16, 1024, 2);
+                const int step_a = a_mn ? 128 : 2;
+                const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u);
                 if (!mbar_wait(&sm.tmem_empty[b], buf_parity, &sm.abort_flag)) break;
                 tcgen05_fence_after();
-                for (int k = 0; k < p.k_steps; ++k) {
+                for (int k = w.k0; k < w.k1; ++k) {
                     if (!mbar_wait(&sm.full[s], parity, &sm.abort_flag)) {
                         alive = false;
                         break;
                     }
                     tcgen05_fence_after();
-                    const int kk = (k >= p.seg_k_steps ? k - p.seg_k_steps : k) * kDBlockK;
-                    const int nmma = (min(kDBlockK, p.K - kk) + 15) / 16;      // what lies past K is filled with zeros
+                    const int kk = (k >= q.seg_k_steps ? k - q.seg_k_steps : k) * kDBlockK;
+                    const int nmma = (min(kDBlockK, q.K - kk) + 15) / 16;      // what lies past K is filled with zeros
                     const uint64_t a_desc = a_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
                     const uint64_t b_desc = b_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
 #pragma unroll
                     for (int j = 0; j < kDBlockK / 16; ++j)
                         if (j < nmma)
-                            tcgen05_mma_f16_pair(tmem + b * kDTile, a_desc + kStepA * j, b_desc + kStepB * j, idesc, (k | j) > 0);
+                            tcgen05_mma_f16_pair(tmem + b * kDTile, a_desc + step_a * j, b_desc + kStepB * j, idesc, k > w.k0 || j > 0);
                     tcgen05_commit_pair(&sm.empty[s], 3);
                     if (++s == kDStages) {
                         s = 0;
@@ -232,33 +297,40 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         // ------------------------------------------------------------ epilogue warps
         const int quad = warp & 3;                     // TMEM lane quadrant of this warp
         const int half = warp >> 2;                    // which 128 columns
-        uint8_t* stg = sm.out_stage[warp];
+        const uint64_t streaming = l2_policy_evict_first();      // outputs should not displace operands
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const uint32_t tmem_empty_leader = map_to_cta(smem_u32(&sm.tmem_empty[0]), 0);
-        // 32 rows x 128 bytes, staged in the 128-byte swizzle for a TMA store that clips at the matrix edges
+        // boxes of 32 rows x 128 bytes, staged in the 128-byte swizzle for a TMA store that clips at the matrix edges; the
+        // boxes' buffers take turns
+        int box = 0;
         auto stage_wait = [&]() {
-            if (lane == 0) bulk_wait_group_read<0>();
+            if (lane == 0) bulk_wait_group_read<kBoxes - 1>();
             __syncwarp();
         };
-        auto stage_put = [&](int q, const uint4& v) {
-            smem_store(stg + lane * 128 + ((q ^ (lane & 7)) * 16), v, stg, kDStageBytes);
+        auto stage_put_in = [&](int which, int i, const uint4& v) {
+            smem_store(&sm.out_stage[warp][which][0] + lane * 128 + ((i ^ (lane & 7)) * 16), v, sm.out_stage[warp], kBoxes * kDStageBytes);
         };
-        auto stage_store = [&](const CUtensorMap* map, int col, int row) {
+        auto stage_put = [&](int i, const uint4& v) { stage_put_in(box, i, v); };
+        auto stage_store = [&](const CUtensorMap* map, int col, int row, bool add = false) {
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-                if (EPI == kDenseAddF32) tma_add_2d(map, stg, col, row);
-                else tma_store_2d(map, stg, col, row);
+                if (add) tma_add_2d(map, sm.out_stage[warp][box], col, row);
+                else tma_store_2d_hint(map, sm.out_stage[warp][box], col, row, streaming);
                 bulk_commit_group();
             }
+            if (++box == kBoxes) box = 0;
         };
         int b = 0;
         uint32_t parity = 0;
-        for (int tile = cluster_id; tile < tiles; tile += n_clusters) {
-            int tm, tn;
-            dense_place(p, tile, tm, tn);
-            const int seg_m = tm >= p.seg_tiles_m;
-            const int row0 = (tm - seg_m * p.seg_tiles_m) * kDTile + static_cast<int>(rank) * kDHalf + quad * 32;
+        for (int j = 0;; ++j) {
+            const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, j);
+            if (w.q < 0) break;
+            const DenseShape& q = p.q[w.q];
+            const DenseMaps& m = maps.q[w.q];
+            const int tn = w.tn;
+            const int in_tile = static_cast<int>(rank) * kDHalf + quad * 32;
+            const int row0 = w.row + in_tile;
             const int row = row0 + lane;
             if (!mbar_wait(&sm.tmem_full[b], parity, &sm.abort_flag)) break;       // given up: nothing more is stored
             tcgen05_fence_after();
@@ -273,87 +345,92 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
                 tmem_ld_32x32b_x32(from + col, r);
                 tmem_ld_wait_for(r);
             };
-            if (row0 >= p.M) {                         // warp-uniform: no rows here
+            if (row0 >= q.M || w.k0 == w.k1) {         // warp-uniform: no rows here, or a piece without products
                 hand_back();
-            } else if constexpr (EPI == kDenseBf16 || EPI == kDenseF32 || EPI == kDenseAddF32) {
+            } else if constexpr (kStore) {
                 const int col0 = tn * kDTile + half * kDHalf;
-                constexpr bool k32 = EPI != kDenseBf16;
+                const CUtensorMap* out = &m.out[w.seg];
+                const int out_row = w.out_row + in_tile;
+                const bool k32 = q.out != kDenseBf16;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int col = col0 + c * 32;
-                    if (col < p.N) {
+                    if (col < q.N) {
                         read(half * kDHalf + c * 32);
                         if (k32 || (c & 1) == 0) stage_wait();
+                        if (k32) {
 #pragma unroll
-                        for (int q = 0; q < (k32 ? 8 : 4); ++q) {
-                            const uint32_t* v = r + q * (k32 ? 4 : 8);
-                            if constexpr (k32) stage_put(q, make_uint4(v[0], v[1], v[2], v[3]));
-                            else stage_put((c & 1) * 4 + q, dense_pack8(v));
+                            for (int i = 0; i < 8; ++i) stage_put(i, make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) stage_put((c & 1) * 4 + i, dense_pack8(r + 8 * i));
                         }
                     }
-                    if (k32 ? col < p.N : (c & 1) != 0 && col - 32 < p.N)
-                        stage_store(&maps.out[seg_m], k32 ? col : col - 32, row0);
+                    if (k32 ? col < q.N : (c & 1) != 0 && col - 32 < q.N)
+                        stage_store(out, k32 ? col : col - 32, out_row, q.out == kDenseAddF32);
                 }
                 hand_back();
             } else if constexpr (EPI == kDenseGated) {
                 const int col0 = tn * kDHalf + half * 64;
-                if (col0 < p.N) {
-                    uint4 gate[8], up[8];              // as stored, eight features each
-                    stage_wait();
+                if (col0 < q.N) {
+                    // kept projections leave through the two buffers first; h follows from registers
+                    const bool keep = p.x.keep != 0;
+                    uint4 h[8];
+                    if (lane == 0 && keep) bulk_wait_group_read<0>();
+                    __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t u[32];
                         tmem_ld_32x32b_x32(from + kDHalf + half * 64 + c * 32, u);
                         read(half * 64 + c * 32);
                         tmem_ld_wait_for(u);
+                        if (keep) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            gate[c * 4 + q] = dense_pack8(r + 8 * q);
-                            up[c * 4 + q] = dense_pack8(u + 8 * q);
+                            for (int i = 0; i < 4; ++i) {
+                                stage_put_in(box, c * 4 + i, dense_pack8(r + 8 * i));
+                                stage_put_in(box ^ 1, c * 4 + i, dense_pack8(u + 8 * i));
+                            }
                         }
-                        with_act(p.act, [&](auto act) {
+                        with_act(p.x.act, [&](auto act) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 r[i] = __float_as_uint(act_value<decltype(act)::value>(__uint_as_float(r[i])) *
                                                        __uint_as_float(u[i]));
                         });
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) stage_put(c * 4 + q, dense_pack8(r + 8 * q));
+                        for (int i = 0; i < 4; ++i) h[c * 4 + i] = dense_pack8(r + 8 * i);
                     }
                     hand_back();
-                    stage_store(&maps.out[0], col0, row0);
-                    if (p.keep) {
-                        stage_wait();
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) stage_put(q, gate[q]);
-                        stage_store(&maps.out[1], col0, row0);
-                        stage_wait();
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) stage_put(q, up[q]);
-                        stage_store(&maps.out[2], col0, row0);
+                    if (keep) {
+                        stage_store(&m.out[1], col0, row0);
+                        stage_store(&m.out[2], col0, row0);
                     }
+                    stage_wait();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) stage_put(i, h[i]);
+                    stage_store(&m.out[0], col0, row0);
                 } else {
                     hand_back();
                 }
             } else {
                 // rows of logits
                 const int col0 = tn * kDTile + half * kDHalf;
-                const bool row_ok = row < p.M;
-                const int64_t target = row_ok && p.targets ? p.targets[row] : -1;
-                const int at = target >= p.col_base + col0 && target < p.col_base + col0 + kDHalf
-                                   ? static_cast<int>(target - p.col_base - col0) : -1;
+                const bool row_ok = row < q.M;
+                const int64_t target = row_ok && p.x.targets ? p.x.targets[row] : -1;
+                const int at = target >= p.x.col_base + col0 && target < p.x.col_base + col0 + kDHalf
+                                   ? static_cast<int>(target - p.x.col_base - col0) : -1;
                 const bool any_here = __any_sync(0xffffffffu, at >= 0);
                 if constexpr (EPI == kDensePartials) {
-                    if (col0 < p.N) {
-                        float m = -INFINITY, sum = 0.0f, picked = 0.0f;
+                    if (col0 < q.N) {
+                        float top_so_far = -INFINITY, sum = 0.0f, picked = 0.0f;
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
                             read(half * kDHalf + c * 32);
-                            float z[32], top = m;
+                            float z[32], top = top_so_far;
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
-                                z[i] = __uint_as_float(r[i]) * p.scale;
-                                if (col0 + c * 32 + i >= p.N) z[i] = -INFINITY;
+                                z[i] = __uint_as_float(r[i]) * p.x.scale;
+                                if (col0 + c * 32 + i >= q.N) z[i] = -INFINITY;
                                 top = fmaxf(top, z[i]);
                             }
                             if (any_here) {
@@ -363,48 +440,48 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
                             }
                             // a row of nothing but -infinity so far has sum 0; a NaN passes the maximum by and enters the sum
                             const float ref = top == -INFINITY ? 0.0f : top;
-                            sum *= dense_exp(m - ref);
+                            sum *= dense_exp(top_so_far - ref);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) sum += dense_exp(z[i] - ref);
-                            m = top;
+                            top_so_far = top;
                         }
                         hand_back();
                         if (row_ok) {
-                            p.parts[static_cast<int64_t>(tn * 2 + half) * p.ld_parts + row] = make_float2(m, sum);
-                            if (at >= 0 && target < p.col_base + p.N) p.picked[row] = picked;
+                            p.x.parts[static_cast<int64_t>(tn * 2 + half) * p.x.ld_parts + row] = make_float2(top_so_far, sum);
+                            if (at >= 0 && target < p.x.col_base + q.N) p.x.picked[row] = picked;
                         }
                     } else {
                         hand_back();
                     }
                 } else {
-                    const float lse = row_ok ? p.lse[row] : 0.0f;
-                    float gl = row_ok && p.d_logp && target >= 0 ? p.d_logp[row] : 0.0f;
-                    const float gn = row_ok && p.d_lse ? p.d_lse[row] : 0.0f;
-                    if (target >= p.vocab) gl = NAN;
+                    const float lse = row_ok ? p.x.lse[row] : 0.0f;
+                    float gl = row_ok && p.x.d_logp && target >= 0 ? p.x.d_logp[row] : 0.0f;
+                    const float gn = row_ok && p.x.d_lse ? p.x.d_lse[row] : 0.0f;
+                    if (target >= p.x.vocab) gl = NAN;
                     const bool zero = (gl == 0.0f && gn == 0.0f);
-                    const float coef = p.scale * (gn - gl);
+                    const float coef = p.x.scale * (gn - gl);
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         const int col = col0 + c * 32;
-                        if (col < p.ld_grad) {
+                        if (col < p.x.ld_grad) {
                             read(half * kDHalf + c * 32);
                             if ((c & 1) == 0) stage_wait();
                             float z[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
-                                z[i] = coef * dense_exp(__uint_as_float(r[i]) * p.scale - lse);
-                                if (zero || col + i >= p.N) z[i] = 0.0f;
+                                z[i] = coef * dense_exp(__uint_as_float(r[i]) * p.x.scale - lse);
+                                if (zero || col + i >= q.N) z[i] = 0.0f;
                             }
                             if (any_here) {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    if (c * 32 + i == at) z[i] += p.scale * gl;
+                                    if (c * 32 + i == at) z[i] += p.x.scale * gl;
                             }
 #pragma unroll
-                            for (int q = 0; q < 4; ++q)
-                                stage_put((c & 1) * 4 + q, dense_pack8(reinterpret_cast<uint32_t*>(z) + 8 * q));
+                            for (int i = 0; i < 4; ++i)
+                                stage_put((c & 1) * 4 + i, dense_pack8(reinterpret_cast<uint32_t*>(z) + 8 * i));
                         }
-                        if ((c & 1) != 0 && col - 32 < p.ld_grad) stage_store(&maps.out[0], col - 32, row0);
+                        if ((c & 1) != 0 && col - 32 < p.x.ld_grad) stage_store(&m.out[0], col - 32, row0);
                     }
                     hand_back();
                 }

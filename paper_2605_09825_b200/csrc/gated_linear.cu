@@ -60,6 +60,11 @@ __global__ void __launch_bounds__(kGradThreads) gated_grad_kernel(const GatedGra
     });
 }
 
+static size_t gated_grad_bytes(int64_t tokens, int64_t features)
+{
+    return round_up(static_cast<size_t>(tokens) * features * 2, 256);
+}
+
 // Sizes, leading dimensions and alignment of what both directions read.
 static int gated_check(const mxfp4_gated_desc* d)
 {
@@ -114,26 +119,30 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
                                  static_cast<cudaStream_t>(stream), p) == cudaSuccess
                    ? MXFP4_OK : MXFP4_ERR_CUDA;
     }
-    DenseCall c;
-    c.epilogue = kDenseGated;
+    DenseProduct c;
+    c.M = d->tokens;
+    c.N = d->features;
+    c.K = d->in_features;
     c.a[0] = {d->x, d->ld_x};
     c.b[0] = {d->w_gate, d->ld_gate};
     c.b[1] = {d->w_up, d->ld_up};
     c.out[0] = {h, ld_h};
     c.out[1] = {gate, ld_kept};
     c.out[2] = {up, ld_kept};
-    c.p.M = static_cast<int32_t>(d->tokens);
-    c.p.N = static_cast<int32_t>(d->features);
-    c.p.K = static_cast<int32_t>(d->in_features);
-    c.p.act = d->act;
-    c.p.keep = gate != nullptr;
-    return dense_launch(c, dev.sm_count, static_cast<cudaStream_t>(stream));
+    DenseExtra extra = {};
+    extra.act = d->act;
+    extra.keep = gate != nullptr;
+    return dense_fused(kDenseGated, c, extra, dev.sm_count, static_cast<cudaStream_t>(stream));
 }
 
-size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t features)
+size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t in_features, int64_t features)
 {
-    if (tokens <= 0 || features <= 0 || features % 8 != 0 || tokens > kDenseMaxDim || features > kDenseMaxDim) return 0;
-    return 2 * round_up(static_cast<size_t>(tokens) * features * 2, 256);
+    if (tokens <= 0 || in_features <= 0 || features <= 0 || in_features % 8 != 0 || features % 8 != 0 ||
+        tokens > kDenseMaxDim || in_features > kDenseMaxDim || features > kDenseMaxDim)
+        return 0;
+    const int splits = dense_splits(tokens, in_features, 2 * features);
+    return 2 * gated_grad_bytes(tokens, features) +
+           (splits > 1 ? static_cast<size_t>(splits) * dense_split_rows(tokens) * in_features * 4 : 0);
 }
 
 int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64_t ld_dh, const void* gate, const void* up,
@@ -149,7 +158,7 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64
     if (!aligned16(dh) || !aligned16(gate) || !aligned16(up) || ld_dh % 8 != 0 || ld_kept % 8 != 0 ||
         (dx && (!aligned16(dx) || ld_dx % 8 != 0)) || (dw_gate && (!aligned16(dw_gate) || !aligned16(dw_up) || ld_dw % 8 != 0)))
         return MXFP4_ERR_ALIGN;
-    const size_t need = mxfp4_gated_linear_workspace_bytes(d->tokens, d->features);
+    const size_t need = mxfp4_gated_linear_workspace_bytes(d->tokens, d->in_features, d->features);
     if (!workspace || workspace_bytes < need) return MXFP4_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MXFP4_ERR_ALIGN;
     const DeviceInfo& dev = device_info();
@@ -161,7 +170,7 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64
     g.gate = static_cast<const __nv_bfloat16*>(gate);
     g.up = static_cast<const __nv_bfloat16*>(up);
     g.dg = static_cast<__nv_bfloat16*>(workspace);
-    g.du = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(workspace) + need / 2);
+    g.du = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(workspace) + gated_grad_bytes(d->tokens, d->features));
     g.ld_dh = ld_dh;
     g.ld_kept = ld_kept;
     g.items = d->tokens * (d->features / 8);
@@ -173,35 +182,39 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64
         cudaSuccess)
         return MXFP4_ERR_CUDA;
     const DenseMatrix mg = {g.dg, d->features}, mu = {g.du, d->features};
+    DenseProduct c[2];
+    int n = 0;
+    const int splits = dense_splits(d->tokens, d->in_features, 2 * d->features);
+    float* sums = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 2 * gated_grad_bytes(d->tokens, d->features));
     if (dx) {
-        DenseCall c;                       // dx = dg Wg + du Wu
-        c.epilogue = kDenseBf16;
-        c.b_mn = c.stack_k = true;
-        c.a[0] = mg;
-        c.a[1] = mu;
-        c.b[0] = {d->w_gate, d->ld_gate};
-        c.b[1] = {d->w_up, d->ld_up};
-        c.out[0] = {dx, ld_dx};
-        c.p.M = static_cast<int32_t>(d->tokens);
-        c.p.N = static_cast<int32_t>(d->in_features);
-        c.p.K = static_cast<int32_t>(d->features);
-        if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        DenseProduct& x = c[n++];          // dx = dg Wg + du Wu
+        x.M = d->tokens;
+        x.N = d->in_features;
+        x.K = d->features;
+        x.b_mn = x.stack_k = true;
+        x.splits = splits;
+        x.kind = splits > 1 ? kDenseF32 : kDenseBf16;
+        x.a[0] = mg;
+        x.a[1] = mu;
+        x.b[0] = {d->w_gate, d->ld_gate};
+        x.b[1] = {d->w_up, d->ld_up};
+        x.out[0] = splits > 1 ? DenseMatrix{sums, d->in_features} : DenseMatrix{dx, ld_dx};
     }
     if (dw_gate) {
-        DenseCall c;                       // dWg = dg^T x, dWu = du^T x
-        c.epilogue = dw_dtype == MXFP4_OUT_FP32 ? kDenseF32 : kDenseBf16;
-        c.a_mn = c.b_mn = c.stack_m = true;
-        c.a[0] = mg;
-        c.a[1] = mu;
-        c.b[0] = {d->x, d->ld_x};
-        c.out[0] = {dw_gate, ld_dw};
-        c.out[1] = {dw_up, ld_dw};
-        c.p.M = static_cast<int32_t>(d->features);
-        c.p.N = static_cast<int32_t>(d->in_features);
-        c.p.K = static_cast<int32_t>(d->tokens);
-        if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        DenseProduct& w = c[n++];          // dWg = dg^T x, dWu = du^T x
+        w.M = d->features;
+        w.N = d->in_features;
+        w.K = d->tokens;
+        w.a_mn = w.b_mn = w.stack_m = true;
+        w.kind = dw_dtype == MXFP4_OUT_FP32 ? kDenseF32 : kDenseBf16;
+        w.a[0] = mg;
+        w.a[1] = mu;
+        w.b[0] = {d->x, d->ld_x};
+        w.out[0] = {dw_gate, ld_dw};
+        w.out[1] = {dw_up, ld_dw};
     }
-    return MXFP4_OK;
+    if ((rc = dense_store(c, n, dev.sm_count, st)) != MXFP4_OK || !dx || splits == 1) return rc;
+    return dense_round(sums, splits, d->tokens, d->in_features, dx, ld_dx, dev.sm_count, st);
 }
 
 }  // extern "C"

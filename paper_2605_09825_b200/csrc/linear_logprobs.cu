@@ -76,25 +76,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) loss_join_kernel(const LossJo
     p.logp[row] = logp;
 }
 
-struct RoundRowsParams {
-    const float* from;           // [rows x cols]
-    __nv_bfloat16* to;
-    int64_t ld, items;           // items: rows * cols / 8
-    int32_t per_row;
-};
-
-__global__ void __launch_bounds__(256) round_rows_kernel(const RoundRowsParams p)
-{
-    griddep_launch_dependents();
-    griddep_wait();
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < p.items; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = i / p.per_row, col = (i - row * p.per_row) * 8;
-        const float4 a = *reinterpret_cast<const float4*>(p.from + i * 8), b = *reinterpret_cast<const float4*>(p.from + i * 8 + 4);
-        const float2 v[4] = {make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)};
-        *reinterpret_cast<uint4*>(p.to + row * p.ld + col) = pack8(v);
-    }
-}
-
 // Columns of the vocabulary per piece of the backward pass: 256 MB of gradients, at least 8192 columns, so that the fp32
 // sums of dx, which every piece reads and writes once, stay a small part of the traffic.
 static int64_t loss_piece(int64_t tokens, int64_t vocab)
@@ -136,8 +117,10 @@ size_t mxfp4_linear_logprobs_workspace_bytes(int64_t tokens, int64_t in_features
         in_features > kDenseMaxDim || vocab > kDenseMaxDim)
         return 0;
     if (backward) {
-        const bool one = loss_piece(tokens, vocab) == vocab;
-        return loss_grad_bytes(tokens, vocab) + (one ? 0 : static_cast<size_t>(tokens) * in_features * 4);
+        const int64_t piece = loss_piece(tokens, vocab);
+        const int splits = dense_splits(tokens, in_features, piece);
+        return loss_grad_bytes(tokens, vocab) +
+               (piece == vocab && splits == 1 ? 0 : static_cast<size_t>(splits) * dense_split_rows(tokens) * in_features * 4);
     }
     const size_t rows = round_up(static_cast<size_t>(tokens < kLossRows ? tokens : kLossRows), 32);
     return rows * static_cast<size_t>(dense_tiles(vocab, 128)) * sizeof(float2) + rows * sizeof(float);
@@ -160,29 +143,29 @@ int mxfp4_linear_logprobs_forward(const void* x, int64_t ld_x, const void* w, in
     const int64_t pieces = dense_tiles(vocab, 128);
     for (int64_t r = 0; r < tokens; r += kLossRows) {
         const int64_t rows = tokens - r < kLossRows ? tokens - r : kLossRows;
-        DenseCall c;
-        c.epilogue = kDensePartials;
+        DenseProduct c;
+        c.M = rows;
+        c.N = vocab;
+        c.K = in_features;
         c.a[0] = {static_cast<const __nv_bfloat16*>(x) + r * ld_x, ld_x};
         c.b[0] = {w, ld_w};
-        c.p.M = static_cast<int32_t>(rows);
-        c.p.N = static_cast<int32_t>(vocab);
-        c.p.K = static_cast<int32_t>(in_features);
-        c.p.vocab = vocab;
-        c.p.targets = targets ? targets + r : nullptr;
-        c.p.scale = scale;
-        c.p.parts = static_cast<float2*>(workspace);
-        c.p.ld_parts = pitch;
-        c.p.picked = reinterpret_cast<float*>(c.p.parts + pitch * pieces);
-        if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+        DenseExtra e = {};
+        e.vocab = vocab;
+        e.targets = targets ? targets + r : nullptr;
+        e.scale = scale;
+        e.parts = static_cast<float2*>(workspace);
+        e.ld_parts = pitch;
+        e.picked = reinterpret_cast<float*>(e.parts + pitch * pieces);
+        if ((rc = dense_fused(kDensePartials, c, e, dev.sm_count, st)) != MXFP4_OK) return rc;
         LossJoinParams j;
-        j.parts = c.p.parts;
-        j.picked = c.p.picked;
-        j.targets = c.p.targets;
+        j.parts = e.parts;
+        j.picked = e.picked;
+        j.targets = e.targets;
         j.logp = logp ? logp + r : nullptr;
         j.lse = lse + r;
         j.ld_parts = pitch;
         j.vocab = vocab;
-        j.rows = c.p.M;
+        j.rows = static_cast<int32_t>(rows);
         j.pieces = static_cast<int32_t>(pieces);
         if (launch_kernel_pdl(loss_join_kernel, (j.rows + 31) / 32, kJoinWarps * 32, 0, st, j) != cudaSuccess)
             return MXFP4_ERR_CUDA;
@@ -211,68 +194,59 @@ int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, i
 
     const int64_t piece = loss_piece(tokens, vocab);
     const int64_t ld_grad = round_up(piece, 8);
+    // the pieces' shares of dx are added up in fp32, those of a split piece side by side
+    const int splits = dense_splits(tokens, in_features, piece);
+    const bool direct = piece == vocab && splits == 1;
     __nv_bfloat16* grad = static_cast<__nv_bfloat16*>(workspace);
     float* sums = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + loss_grad_bytes(tokens, vocab));
     for (int64_t v = 0; v < vocab; v += piece) {
         const int64_t cols = vocab - v < piece ? vocab - v : piece;
         const DenseMatrix wp = {static_cast<const __nv_bfloat16*>(w) + v * ld_w, ld_w};
         const DenseMatrix gp = {grad, ld_grad};
-        {
-            DenseCall c;
-            c.epilogue = kDenseLogitGrad;
-            c.a[0] = {x, ld_x};
-            c.b[0] = wp;
-            c.out[0] = gp;
-            c.p.M = static_cast<int32_t>(tokens);
-            c.p.N = static_cast<int32_t>(cols);
-            c.p.K = static_cast<int32_t>(in_features);
-            c.p.vocab = vocab;
-            c.p.col_base = v;
-            c.p.targets = targets;
-            c.p.scale = scale;
-            c.p.lse = lse;
-            c.p.d_logp = d_logp;
-            c.p.d_lse = d_lse;
-            c.p.ld_grad = static_cast<int32_t>(round_up(cols, 8));
-            if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
-        }
+        DenseProduct c[2];
+        c[0].M = tokens;
+        c[0].N = cols;
+        c[0].K = in_features;
+        c[0].a[0] = {x, ld_x};
+        c[0].b[0] = wp;
+        c[0].out[0] = gp;
+        DenseExtra e = {};
+        e.vocab = vocab;
+        e.col_base = v;
+        e.targets = targets;
+        e.scale = scale;
+        e.lse = lse;
+        e.d_logp = d_logp;
+        e.d_lse = d_lse;
+        e.ld_grad = static_cast<int32_t>(round_up(cols, 8));
+        if ((rc = dense_fused(kDenseLogitGrad, c[0], e, dev.sm_count, st)) != MXFP4_OK) return rc;
+        int n = 0;
         if (dx) {
-            DenseCall c;                   // dx (+)= dz W
-            c.epilogue = piece == vocab ? kDenseBf16 : v == 0 ? kDenseF32 : kDenseAddF32;
-            c.b_mn = true;
-            c.a[0] = gp;
-            c.b[0] = wp;
-            c.out[0] = piece == vocab ? DenseMatrix{dx, ld_dx} : DenseMatrix{sums, in_features};
-            c.p.M = static_cast<int32_t>(tokens);
-            c.p.N = static_cast<int32_t>(in_features);
-            c.p.K = static_cast<int32_t>(cols);
-            if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+            DenseProduct& q = c[n++] = {};     // dx (+)= dz W
+            q.M = tokens;
+            q.N = in_features;
+            q.K = cols;
+            q.b_mn = true;
+            q.splits = splits;
+            q.kind = direct ? kDenseBf16 : v == 0 ? kDenseF32 : kDenseAddF32;
+            q.a[0] = gp;
+            q.b[0] = wp;
+            q.out[0] = direct ? DenseMatrix{dx, ld_dx} : DenseMatrix{sums, in_features};
         }
         if (dw) {
-            DenseCall c;                   // dW = dz^T x
-            c.epilogue = dw_dtype == MXFP4_OUT_FP32 ? kDenseF32 : kDenseBf16;
-            c.a_mn = c.b_mn = true;
-            c.a[0] = gp;
-            c.b[0] = {x, ld_x};
-            c.out[0] = {static_cast<uint8_t*>(dw) + v * ld_dw * (dw_dtype == MXFP4_OUT_FP32 ? 4 : 2), ld_dw};
-            c.p.M = static_cast<int32_t>(cols);
-            c.p.N = static_cast<int32_t>(in_features);
-            c.p.K = static_cast<int32_t>(tokens);
-            if ((rc = dense_launch(c, dev.sm_count, st)) != MXFP4_OK) return rc;
+            DenseProduct& q = c[n++] = {};     // dW = dz^T x
+            q.M = cols;
+            q.N = in_features;
+            q.K = tokens;
+            q.a_mn = q.b_mn = true;
+            q.kind = dw_dtype == MXFP4_OUT_FP32 ? kDenseF32 : kDenseBf16;
+            q.a[0] = gp;
+            q.b[0] = {x, ld_x};
+            q.out[0] = {static_cast<uint8_t*>(dw) + v * ld_dw * (dw_dtype == MXFP4_OUT_FP32 ? 4 : 2), ld_dw};
         }
+        if ((rc = dense_store(c, n, dev.sm_count, st)) != MXFP4_OK) return rc;
     }
-    if (dx && piece != vocab) {
-        RoundRowsParams p;
-        p.from = sums;
-        p.to = static_cast<__nv_bfloat16*>(dx);
-        p.ld = ld_dx;
-        p.items = tokens * (in_features / 8);
-        p.per_row = static_cast<int32_t>(in_features / 8);
-        const int64_t blocks = (p.items + 255) / 256, most = 8 * static_cast<int64_t>(dev.sm_count);
-        if (launch_kernel_pdl(round_rows_kernel, static_cast<int>(blocks < most ? blocks : most), 256, 0, st, p) != cudaSuccess)
-            return MXFP4_ERR_CUDA;
-    }
-    return MXFP4_OK;
+    return dx && !direct ? dense_round(sums, splits, tokens, in_features, dx, ld_dx, dev.sm_count, st) : MXFP4_OK;
 }
 
 }  // extern "C"

@@ -27,12 +27,14 @@ INF, NAN = float("inf"), float("nan")
 
 def test_sizes(lib):
     g = lib.mxfp4_gated_linear_workspace_bytes
-    assert g(100, 64) == 2 * 12800 and g(0, 8) == g(8, 0) == g(8, 12) == g(HUGE, 8) == 0
+    assert g(1024, 4096, 14336) == 2 * 1024 * 14336 * 2 and g(100, 64, 64) == 2 * 12800     # tiles enough; too short to split
+    assert g(64, 4096, 14336) == 2 * 64 * 14336 * 2 + 9 * 256 * 4096 * 4
+    assert g(0, 8, 8) == g(8, 8, 0) == g(8, 8, 12) == g(8, 12, 8) == g(HUGE, 8, 8) == 0
     l = lib.mxfp4_linear_logprobs_workspace_bytes
     assert l(1, 64, 1000, 0) == 32 * 8 * 8 + 32 * 4
     assert l(16384, 64, 128256, 0) == l(1 << 20, 64, 128256, 0) < 1 << 28         # does not grow with the text
-    assert l(100, 64, 1000, 1) == 100 * 1000 * 2 + 192                            # one piece
-    assert l(8192, 64, 128256, 1) == 8192 * 16384 * 2 + 8192 * 64 * 4
+    assert l(100, 64, 500, 1) == 100864                                           # one piece, too short to split: 100 * 504 * 2, rounded up
+    assert l(8192, 8192, 128256, 1) == 8192 * 16384 * 2 + 8192 * 8192 * 4         # several pieces
     assert l(0, 8, 8, 0) == l(8, 12, 8, 0) == l(8, 8, 0, 1) == l(HUGE, 8, 8, 1) == 0
     e = lib.mxfp4_embedding_workspace_bytes
     assert e(1, 10, 8) == 3 * 256 + 64 and e(100, 10, 8) == 2 * 1024 + 256 + 13 * 64
