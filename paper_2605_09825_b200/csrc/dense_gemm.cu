@@ -43,18 +43,18 @@ static int launch(const DenseMaps2& maps, const DenseParams& p, int sm_count, cu
     return launch_kernel_pdl(kernel, 2 * clusters, kDThreads, smem, st, maps, p) == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
-static bool operand_map(CUtensorMap* map, const DenseMatrix& m, bool mn, int64_t rows, int64_t K)
+static bool operand_map(CUtensorMap* map, const DenseMatrix& m, bool mn, int64_t rows, int64_t K, int box_rows = kDHalf)
 {
     return mn ? make_tmap_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.p, K, rows, m.ld * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B)
-              : make_tmap_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.p, rows, K, m.ld * 2, kDHalf, kDBlockK,
+              : make_tmap_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.p, rows, K, m.ld * 2, box_rows, kDBlockK,
                              CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // Sizes and tensor maps of one product; `outs` outputs of `out_cols` columns.
-static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool gated, int outs, int64_t out_cols)
+static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool gated, int outs, int64_t out_cols, int width = kDHalf)
 {
     const int64_t seg_m = dense_tiles(c.M, kDTile), seg_k = dense_tiles(c.K, kDBlockK);
-    const int64_t tiles_n = dense_tiles(c.N, gated ? kDHalf : kDTile);
+    const int64_t tiles_n = dense_tiles(c.N, gated ? width : 2 * width);
     const int64_t tiles_m = seg_m * (c.stack_m ? 2 : 1), k_steps = seg_k * (c.stack_k ? 2 : 1);
     if (tiles_m * tiles_n * c.splits > 0x1FFFFFFF || k_steps > 0x3FFFFFFF / kDBlockK) return MXFP4_ERR_SHAPE;
     if (c.splits > 1 && dense_split_rows(c.M) * c.splits > 0x7FFFFFFF) return MXFP4_ERR_SHAPE;
@@ -66,6 +66,7 @@ static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool g
     q.tiles_n = static_cast<int32_t>(tiles_n);
     q.seg_k_steps = static_cast<int32_t>(seg_k);
     q.k_steps = static_cast<int32_t>(k_steps);
+    q.width = width;
     q.band = static_cast<int32_t>(tiles_n < 16 ? tiles_n : 16);
     q.splits = c.splits;
     q.split_rows = static_cast<int32_t>(dense_split_rows(c.M));
@@ -76,7 +77,7 @@ static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool g
     const int n_a = c.stack_m || c.stack_k ? 2 : 1, n_b = gated || c.stack_k ? 2 : 1;
     bool ok = true;
     for (int i = 0; i < n_a && ok; ++i) ok = operand_map(&maps.a[i], c.a[i], c.a_mn, c.M, c.K);
-    for (int i = 0; i < n_b && ok; ++i) ok = operand_map(&maps.b[i], c.b[i], c.b_mn, c.N, c.K);
+    for (int i = 0; i < n_b && ok; ++i) ok = operand_map(&maps.b[i], c.b[i], c.b_mn, c.N, c.K, width);
     for (int i = 0; i < outs && ok; ++i)
         ok = make_tmap_2d(&maps.out[i], out32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, out32 ? 4 : 2,
                           c.out[i].p, c.splits > 1 ? dense_split_rows(c.M) * c.splits : c.M, out_cols,
@@ -106,7 +107,8 @@ int dense_fused(DenseEpilogue epilogue, const DenseProduct& product, const Dense
     p.x = extra;
     const bool gated = epilogue == kDenseGated;
     const int outs = epilogue == kDensePartials ? 0 : gated && extra.keep ? 3 : 1;
-    const int rc = prepare(p.q[0], maps.q[0], product, gated, outs, epilogue == kDenseLogitGrad ? extra.ld_grad : product.N);
+    const int rc = prepare(p.q[0], maps.q[0], product, gated, outs, epilogue == kDenseLogitGrad ? extra.ld_grad : product.N,
+                           epilogue == kDenseLogitGrad ? kDHalf : dense_width(product.M, product.N, gated ? 1 : 2));
     if (rc != MXFP4_OK) return rc;
     if (gated) return launch<kDenseGated>(maps, p, sm_count, st);
     return epilogue == kDensePartials ? launch<kDensePartials>(maps, p, sm_count, st)

@@ -1,6 +1,7 @@
 // The 16-bit product with its fused epilogues as the other translation units call it (see dense_gemm_kernel.cuh).
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -19,6 +20,7 @@ struct DenseShape {
     int32_t seg_tiles_m;
     int32_t k_steps;             // of all segments
     int32_t seg_k_steps;
+    int32_t width;               // rows of B per CTA and tile: a tile has 2 * width columns
     int32_t band;                // tile columns per band of the tile order
     int32_t splits;              // pieces along K, each with an output of its own
     int32_t split_rows;          // output rows from one piece's to the next one's
@@ -31,6 +33,8 @@ struct DenseShape {
 struct DenseExtra {
     int32_t act;                 // gated
     int32_t keep;                // g and u are stored too
+    __nv_bfloat16* out[3];       // h, g, u, for the parts of tiles that are not whole boxes
+    int64_t ld_out[3];
     // log probabilities: columns col_base .. col_base + N of `vocab`
     float scale;
     int32_t ld_grad;             // columns of the gradient's buffer, those past N set to 0
@@ -39,7 +43,7 @@ struct DenseExtra {
     const float* lse;
     const float* d_logp;
     const float* d_lse;
-    float2* parts;               // [ceil(N / 128)][ld_parts]: maximum, sum of exponentials
+    float2* parts;               // [ceil(N / width)][ld_parts]: maximum, sum of exponentials
     int64_t ld_parts;
     float* picked;               // the target's value
 };
@@ -75,6 +79,24 @@ int dense_round(const float* from, int pieces, int64_t rows, int64_t cols, void*
 
 inline int64_t dense_tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 inline int64_t dense_split_rows(int64_t M) { return dense_tiles(M, 256) * 256; }
+
+// Columns per CTA and tile of a product with few rows (64 to 128, a multiple of 8; `per_tile`: 1 or 2 of these widths side by side
+// make a tile's columns): 224 tiles are three rounds of the pairs and two tiles more, where narrower ones make
+// four even rounds.  A step costs a tile its columns and about 32 more.
+inline int dense_width(int64_t M, int64_t N, int per_tile)
+{
+    int best = 128;
+    int64_t least = 0;
+    for (int w = 128; w >= 64; w -= 8) {
+        const int64_t cost = dense_tiles(dense_tiles(M, 256) * dense_tiles(N, w * per_tile), kDensePairs) * (w + 32);
+        if (w == 128) least = cost * 19 / 20;       // full width unless it costs a twentieth more
+        else if (cost < least) {
+            least = cost;
+            best = w;
+        }
+    }
+    return best;
+}
 
 // Pieces along K for a product of few tiles: as many as keep the pairs busiest, none shorter than eight steps of 64; a piece
 // costs about eight steps besides its own.  With

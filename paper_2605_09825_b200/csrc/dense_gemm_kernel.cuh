@@ -214,7 +214,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                 const DenseMaps& m = maps.q[w.q];
                 const bool a_mn = kStore && q.a_mn;
                 const int ya = w.row + static_cast<int>(rank) * kDHalf;
-                const int yb = kGated ? w.tn * kDHalf : w.tn * kDTile + static_cast<int>(rank) * kDHalf;
+                const int yb = kGated ? w.tn * q.width : w.tn * 2 * q.width + static_cast<int>(rank) * q.width;
                 for (int k = w.k0; k < w.k1; ++k) {
                     if (!mbar_wait(&sm.empty[s], parity, &sm.abort_flag)) {
                         alive = false;
@@ -223,7 +223,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                     const int seg_k = k >= q.seg_k_steps;
                     const int kk = (k - seg_k * q.seg_k_steps) * kDBlockK;
                     const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
-                    mbar_arrive_expect_tx_cluster(full, 2 * kDOperandBytes);
+                    mbar_arrive_expect_tx_cluster(full, kDOperandBytes + q.width * (kDBlockK * 2));
                     dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk);
                     dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk);
                     if (++s == kDStages) {
@@ -247,9 +247,9 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
     } else if (warp == kDMmaWarp) {
         // ------------------------------------------------------------ MMA issuer
         if (rank == 0 && elect_one_sync()) {
-            // fp32 accumulator, bf16 x bf16, 256 x 256 x 16
+            // fp32 accumulator, bf16 x bf16, 256 x 2 * width x 16
             constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | (kStore ? 1u << 16 : 0u) |
-                                        (static_cast<uint32_t>(kDTile >> 3) << 17) | (static_cast<uint32_t>(kDTile >> 4) << 24);
+                                        (static_cast<uint32_t>(kDTile >> 4) << 24);
             // along K: 8-row groups 1024 bytes apart, an instruction's 16 elements are 32 bytes; transposed: 64-column boxes
             // 8 KB apart, 8-row groups of K 1024 bytes apart, 16 rows are 2 KB
             const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), kStore ? kDBoxBytes : 16, 1024, 2);
@@ -264,7 +264,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                 const bool a_mn = kStore && q.a_mn;
                 const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), a_mn ? kDBoxBytes : 16, 1024, 2);
                 const int step_a = a_mn ? 128 : 2;
-                const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u);
+                const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u) | (static_cast<uint32_t>(2 * q.width) >> 3 << 17);
                 if (!mbar_wait(&sm.tmem_empty[b], buf_parity, &sm.abort_flag)) break;
                 tcgen05_fence_after();
                 for (int k = w.k0; k < w.k1; ++k) {
@@ -371,24 +371,35 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                 }
                 hand_back();
             } else if constexpr (EPI == kDenseGated) {
-                const int col0 = tn * kDHalf + half * 64;
-                if (col0 < q.N) {
-                    // kept projections leave through the two buffers first; h follows from registers
-                    const bool keep = p.x.keep != 0;
+                const int col0 = tn * q.width + half * 64, col1 = min(q.N, (tn + 1) * q.width);
+                if (col0 < col1) {
+                    // kept projections leave through the two buffers first; h follows from registers.  A box that the tile's end
+                    // cuts is written by the threads themselves, eight features at a time
+                    const bool keep = p.x.keep != 0, cut = col0 + 64 > col1;
                     uint4 h[8];
                     if (lane == 0 && keep) bulk_wait_group_read<0>();
                     __syncwarp();
+                    auto write = [&](int which, int i, const uint4& v) {
+                        if (row < q.M && col0 + i * 8 < col1)
+                            *reinterpret_cast<uint4*>(p.x.out[which] + row * p.x.ld_out[which] + col0 + i * 8) = v;
+                    };
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t u[32];
-                        tmem_ld_32x32b_x32(from + kDHalf + half * 64 + c * 32, u);
+                        tmem_ld_32x32b_x32(from + q.width + half * 64 + c * 32, u);
                         read(half * 64 + c * 32);
                         tmem_ld_wait_for(u);
                         if (keep) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                stage_put_in(box, c * 4 + i, dense_pack8(r + 8 * i));
-                                stage_put_in(box ^ 1, c * 4 + i, dense_pack8(u + 8 * i));
+                                const uint4 g8 = dense_pack8(r + 8 * i), u8 = dense_pack8(u + 8 * i);
+                                if (cut) {
+                                    write(1, c * 4 + i, g8);
+                                    write(2, c * 4 + i, u8);
+                                } else {
+                                    stage_put_in(box, c * 4 + i, g8);
+                                    stage_put_in(box ^ 1, c * 4 + i, u8);
+                                }
                             }
                         }
                         with_act(p.x.act, [&](auto act) {
@@ -401,36 +412,41 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                         for (int i = 0; i < 4; ++i) h[c * 4 + i] = dense_pack8(r + 8 * i);
                     }
                     hand_back();
-                    if (keep) {
-                        stage_store(&m.out[1], col0, row0);
-                        stage_store(&m.out[2], col0, row0);
-                    }
-                    stage_wait();
+                    if (cut) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) stage_put(i, h[i]);
-                    stage_store(&m.out[0], col0, row0);
+                        for (int i = 0; i < 8; ++i) write(0, i, h[i]);
+                    } else {
+                        if (keep) {
+                            stage_store(&m.out[1], col0, row0);
+                            stage_store(&m.out[2], col0, row0);
+                        }
+                        stage_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) stage_put(i, h[i]);
+                        stage_store(&m.out[0], col0, row0);
+                    }
                 } else {
                     hand_back();
                 }
             } else {
                 // rows of logits
-                const int col0 = tn * kDTile + half * kDHalf;
+                const int col0 = (tn * 2 + half) * q.width, col1 = min(q.N, col0 + q.width);
                 const bool row_ok = row < q.M;
                 const int64_t target = row_ok && p.x.targets ? p.x.targets[row] : -1;
-                const int at = target >= p.x.col_base + col0 && target < p.x.col_base + col0 + kDHalf
+                const int at = target >= p.x.col_base + col0 && target < p.x.col_base + col1
                                    ? static_cast<int>(target - p.x.col_base - col0) : -1;
                 const bool any_here = __any_sync(0xffffffffu, at >= 0);
                 if constexpr (EPI == kDensePartials) {
-                    if (col0 < q.N) {
+                    if (col0 < col1) {
                         float top_so_far = -INFINITY, sum = 0.0f, picked = 0.0f;
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            read(half * kDHalf + c * 32);
+                        for (int c = 0; col0 + c * 32 < col1; ++c) {
+                            read(half * q.width + c * 32);
                             float z[32], top = top_so_far;
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
                                 z[i] = __uint_as_float(r[i]) * p.x.scale;
-                                if (col0 + c * 32 + i >= q.N) z[i] = -INFINITY;
+                                if (col0 + c * 32 + i >= col1) z[i] = -INFINITY;
                                 top = fmaxf(top, z[i]);
                             }
                             if (any_here) {
@@ -448,7 +464,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                         hand_back();
                         if (row_ok) {
                             p.x.parts[static_cast<int64_t>(tn * 2 + half) * p.x.ld_parts + row] = make_float2(top_so_far, sum);
-                            if (at >= 0 && target < p.x.col_base + q.N) p.x.picked[row] = picked;
+                            if (at >= 0) p.x.picked[row] = picked;
                         }
                     } else {
                         hand_back();

@@ -1,13 +1,18 @@
 // Gated projections of a feed-forward block kept in 16 bits (see include/mxfp4.h): argument checks, the products
 // (dense_gemm_kernel.cuh) and the elementwise step of the backward pass.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
 
 #include "../../include/mxfp4.h"
 #include "activations.cuh"
 #include "dense_gemm.cuh"
 #include "gated_rows_kernel.cuh"
+#include "gated_tokens_kernel.cuh"
 #include "host_common.cuh"
 #include "row_io.cuh"
 #include "ptx_sm100.cuh"
@@ -60,6 +65,68 @@ __global__ void __launch_bounds__(kGradThreads) gated_grad_kernel(const GatedGra
     });
 }
 
+// Up to this many tokens the kernel with the weights as rows is taken (4096 x 14336, weights from memory: 9 to 64 tokens
+// 44 us against 54, 128 tokens 49 against 56, 160 51 against 56, 200 57 against 56).
+constexpr int64_t kMostTokensAsColumns = 160;
+
+static int gated_tokens(const mxfp4_gated_desc& d, void* h, int64_t ld_h, void* gate, void* up, int64_t ld_kept, int sm_count,
+                        cudaStream_t st)
+{
+    const size_t smem = sizeof(GatedTokensSmem) + 1024;
+    static PerDeviceOnce once;
+    static int resident[kMaxDevices] = {};
+    const int dev = current_device();
+    if (dev < 0) return MXFP4_ERR_CUDA;
+    const int rc = once.run(dev, [&] {
+        if (cudaFuncSetAttribute(gated_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
+            cudaSuccess)
+            return MXFP4_ERR_CUDA;
+        // the persistent grid must not exceed what the device holds at once
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(sm_count & ~1), 1, 1);
+        cfg.blockDim = dim3(kTThreads, 1, 1);
+        cfg.dynamicSmemBytes = smem;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, gated_tokens_kernel, &cfg) != cudaSuccess || n <= 0) {
+            (void)cudaGetLastError();
+            n = sm_count / 2;
+        }
+        resident[dev] = n < sm_count / 2 ? n : sm_count / 2;
+        return resident[dev] > 0 ? MXFP4_OK : MXFP4_ERR_CUDA;
+    });
+    if (rc != MXFP4_OK) return rc;
+    const int64_t tiles_n = dense_tiles(d.tokens, 256), tile_tokens = dense_tiles(dense_tiles(d.tokens, tiles_n), 16) * 16;
+    GatedTokensMaps maps;
+    memset(&maps, 0, sizeof(maps));
+    const auto bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const auto swizzle = CU_TENSOR_MAP_SWIZZLE_128B;
+    void* outs[3] = {h, gate, up};
+    bool ok = make_tmap_2d(&maps.w[0], bf16, 2, d.w_gate, d.features, d.in_features, d.ld_gate * 2, 64, kTBlockK, swizzle) &&
+              make_tmap_2d(&maps.w[1], bf16, 2, d.w_up, d.features, d.in_features, d.ld_up * 2, 64, kTBlockK, swizzle) &&
+              make_tmap_2d(&maps.x, bf16, 2, d.x, d.tokens, d.in_features, d.ld_x * 2, static_cast<uint32_t>(tile_tokens / 2),
+                           kTBlockK, swizzle);
+    for (int i = 0; i < (gate ? 3 : 1) && ok; ++i)
+        ok = make_tmap_2d(&maps.out[i], bf16, 2, outs[i], d.tokens, d.features, (i ? ld_kept : ld_h) * 2, kTBox, 64, swizzle);
+    if (!ok) return MXFP4_ERR_CUDA;
+    GatedTokensParams p;
+    p.tokens = static_cast<int32_t>(d.tokens);
+    p.features = static_cast<int32_t>(d.features);
+    p.K = static_cast<int32_t>(d.in_features);
+    p.tile_tokens = static_cast<int32_t>(tile_tokens);
+    p.tiles_n = static_cast<int32_t>(tiles_n);
+    p.tiles = static_cast<int32_t>(tiles_n * dense_tiles(d.features, kTFeatures));
+    p.k_steps = static_cast<int32_t>(dense_tiles(d.in_features, kTBlockK));
+    p.stage_bytes = kTWeightBytes + p.tile_tokens / 2 * 128;
+    p.stages = std::min(kTMostStages, kTRing / p.stage_bytes);
+    p.act = d.act;
+    p.keep = gate != nullptr;
+    const int clusters = p.tiles < resident[dev] ? p.tiles : resident[dev];
+    return launch_kernel_pdl(gated_tokens_kernel, 2 * clusters, kTThreads, smem, st, maps, p) == cudaSuccess ? MXFP4_OK
+                                                                                                           : MXFP4_ERR_CUDA;
+}
+
+int gated_linear_take_status(int* status) { return take_unit_status(status); }
+
 static size_t gated_grad_bytes(int64_t tokens, int64_t features)
 {
     return round_up(static_cast<size_t>(tokens) * features * 2, 256);
@@ -97,7 +164,7 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
         return MXFP4_ERR_ALIGN;
     const DeviceInfo& dev = device_info();
     if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
-    if (d->tokens <= 8 * kGRowsMaxTiles) {
+    if (d->tokens <= kGRowsTokens) {
         GatedRowsParams p;
         p.x = static_cast<const __nv_bfloat16*>(d->x);
         p.w_gate = static_cast<const __nv_bfloat16*>(d->w_gate);
@@ -114,11 +181,12 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
         p.features = static_cast<int32_t>(d->features);
         p.K = static_cast<int32_t>(d->in_features);
         p.act = d->act;
-        auto kernel = d->tokens <= 8 ? gated_rows_kernel<1> : gated_rows_kernel<2>;
-        return launch_kernel_pdl(kernel, static_cast<int>(d->features / kGRowsFeatures), kGRowsWarps * 32, 0,
+        return launch_kernel_pdl(gated_rows_kernel, static_cast<int>(d->features / kGRowsFeatures), kGRowsWarps * 32, 0,
                                  static_cast<cudaStream_t>(stream), p) == cudaSuccess
                    ? MXFP4_OK : MXFP4_ERR_CUDA;
     }
+    if (d->tokens <= kMostTokensAsColumns)
+        return gated_tokens(*d, h, ld_h, gate, up, ld_kept, dev.sm_count, static_cast<cudaStream_t>(stream));
     DenseProduct c;
     c.M = d->tokens;
     c.N = d->features;
@@ -132,6 +200,10 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
     DenseExtra extra = {};
     extra.act = d->act;
     extra.keep = gate != nullptr;
+    for (int i = 0; i < 3; ++i) {
+        extra.out[i] = static_cast<__nv_bfloat16*>(const_cast<void*>(c.out[i].p));
+        extra.ld_out[i] = c.out[i].ld;
+    }
     return dense_fused(kDenseGated, c, extra, dev.sm_count, static_cast<cudaStream_t>(stream));
 }
 

@@ -1,4 +1,4 @@
-// The gated projections for few tokens (decoding steps): h[t][f] for t < 8 * TILES, bound by reading both weights once.
+// The gated projections for few tokens (decoding steps): h[t][f] for up to eight tokens, bound by reading both weights once.
 //
 // A CTA takes eight features, its eight warps take pieces of 64 elements of the reduction in turn and add their sums
 // through shared memory in a fixed order.  The products run on mma.sync m16n8k16: the instruction's first eight rows are
@@ -19,7 +19,7 @@ namespace mxfp4 {
 
 constexpr int kGRowsWarps = 8;
 constexpr int kGRowsFeatures = 8;                // per CTA
-constexpr int kGRowsMaxTiles = 2;                // of eight tokens each
+constexpr int kGRowsTokens = 8;
 
 struct GatedRowsParams {
     const __nv_bfloat16* x;
@@ -51,10 +51,9 @@ __device__ __forceinline__ void mma_bf16_16x8x16(float (&c)[4], uint32_t a0, uin
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int TILES>
 __global__ void __launch_bounds__(kGRowsWarps * 32, 2) gated_rows_kernel(const __grid_constant__ GatedRowsParams p)
 {
-    __shared__ float part[kGRowsWarps][TILES][4][32];
+    __shared__ float part[kGRowsWarps][4][32];
     griddep_launch_dependents();
     griddep_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -62,16 +61,12 @@ __global__ void __launch_bounds__(kGRowsWarps * 32, 2) gated_rows_kernel(const _
     const int f0 = blockIdx.x * kGRowsFeatures;      // features are a multiple of eight: none is missing
     const __nv_bfloat16* wg = p.w_gate + (f0 + g) * p.ld_gate;
     const __nv_bfloat16* wu = p.w_up + (f0 + g) * p.ld_up;
-    float acc[TILES][4];
-#pragma unroll
-    for (int m = 0; m < TILES; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[m][i] = 0.0f;
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 
     constexpr int kPiece = 64;                       // elements
-    constexpr int kUnroll = TILES == 1 ? 4 : 2;      // pieces in flight per warp
+    constexpr int kUnroll = 4;                       // pieces in flight per warp
     for (int k0 = warp * kPiece; k0 < p.K; k0 += kUnroll * kGRowsWarps * kPiece) {
-        uint4 a[kUnroll][2], b[kUnroll][2], x[kUnroll][TILES][2];
+        uint4 a[kUnroll][2], b[kUnroll][2], x[kUnroll][2];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
@@ -83,42 +78,36 @@ __global__ void __launch_bounds__(kGRowsWarps * 32, 2) gated_rows_kernel(const _
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int m = 0; m < TILES; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int k = k0 + u * kGRowsWarps * kPiece + h * 32 + q * 8, t = m * 8 + g;
-                    x[u][m][h] = t < p.tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(p.x + t * p.ld_x + k))
-                                                         : make_uint4(0u, 0u, 0u, 0u);
-                }
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + u * kGRowsWarps * kPiece + h * 32 + q * 8;
+                x[u][h] = g < p.tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(p.x + g * p.ld_x + k))
+                                                  : make_uint4(0u, 0u, 0u, 0u);
+            }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int m = 0; m < TILES; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 v = x[u][m][h];
-                    mma_bf16_16x8x16(acc[m], a[u][h].x, b[u][h].x, a[u][h].y, b[u][h].y, v.x, v.y);
-                    mma_bf16_16x8x16(acc[m], a[u][h].z, b[u][h].z, a[u][h].w, b[u][h].w, v.z, v.w);
-                }
+            for (int h = 0; h < 2; ++h) {
+                const uint4 v = x[u][h];
+                mma_bf16_16x8x16(acc, a[u][h].x, b[u][h].x, a[u][h].y, b[u][h].y, v.x, v.y);
+                mma_bf16_16x8x16(acc, a[u][h].z, b[u][h].z, a[u][h].w, b[u][h].w, v.z, v.w);
+            }
     }
     // this lane's sums: gate (0, 1) and other projection (2, 3) of feature g and tokens 2 q and 2 q + 1
 #pragma unroll
-    for (int m = 0; m < TILES; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) smem_store(&part[warp][m][i][lane], acc[m][i], part, sizeof(part));
+    for (int i = 0; i < 4; ++i) smem_store(&part[warp][i][lane], acc[i], part, sizeof(part));
     __syncthreads();
-    for (int e = threadIdx.x; e < TILES * 64; e += kGRowsWarps * 32) {
+    if (threadIdx.x < 64) {
         // eight threads in turn write a token's eight features
-        const int m = e >> 6, t = e >> 3 & 7, f = e & 7;
+        const int t = threadIdx.x >> 3, f = threadIdx.x & 7;
         const int l = f * 4 + (t >> 1), i = t & 1;
         float gate = 0.0f, up = 0.0f;
 #pragma unroll
         for (int w = 0; w < kGRowsWarps; ++w) {
-            gate += smem_load<float>(&part[w][m][i][l], part, sizeof(part));
-            up += smem_load<float>(&part[w][m][i + 2][l], part, sizeof(part));
+            gate += smem_load<float>(&part[w][i][l], part, sizeof(part));
+            up += smem_load<float>(&part[w][i + 2][l], part, sizeof(part));
         }
-        const int64_t row = m * 8 + t;
-        if (row >= p.tokens) continue;
+        const int64_t row = t;
+        if (row >= p.tokens) return;
         with_act(p.act, [&](auto act) {
             p.h[row * p.ld_h + f0 + f] = __float2bfloat16_rn(act_value<decltype(act)::value>(gate) * up);
         });

@@ -111,6 +111,7 @@ int block128_take_status(int* status);
 int residual_norm_take_status(int* status);
 int logprobs_take_status(int* status);
 int dense_take_status(int* status);
+int gated_linear_take_status(int* status);
 int linear_logprobs_take_status(int* status);
 int embedding_take_status(int* status);
 int grad_norm_take_status(int* status);

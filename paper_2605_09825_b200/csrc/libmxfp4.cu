@@ -962,9 +962,10 @@ int mxfp4_check(void* stream)
 {
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return MXFP4_ERR_CUDA;
     // each translation unit has a word of its own; the first one set is reported
-    int status = 0, more[7] = {};
+    int status = 0, more[8] = {};
     if (take_device_status(&status) != 0 || block128_take_status(&more[0]) != 0 ||
-        residual_norm_take_status(&more[1]) != 0 || dense_take_status(&more[2]) != 0 || embedding_take_status(&more[5]) != 0)
+        residual_norm_take_status(&more[1]) != 0 || dense_take_status(&more[2]) != 0 || embedding_take_status(&more[5]) != 0 ||
+        gated_linear_take_status(&more[7]) != 0)
         return MXFP4_ERR_CUDA;
     // the kernels of these have no wait that could run out: only the bounds-checking build sets their words
     if (mxfp4_bounds_checked() &&

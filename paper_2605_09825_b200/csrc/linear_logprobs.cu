@@ -12,6 +12,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/mxfp4.h"
 #include "dense_gemm.cuh"
 #include "host_common.cuh"
@@ -85,6 +87,9 @@ static int64_t loss_piece(int64_t tokens, int64_t vocab)
     return cols < vocab ? cols : vocab;
 }
 
+// Partial results per row of a forward product.
+static int64_t loss_pieces(int64_t rows, int64_t vocab) { return rows > 0 ? dense_tiles(vocab, dense_width(rows, vocab, 2)) : 0; }
+
 static size_t loss_grad_bytes(int64_t tokens, int64_t vocab)
 {
     return round_up(static_cast<size_t>(tokens) * round_up(loss_piece(tokens, vocab), 8) * 2, 256);
@@ -123,7 +128,9 @@ size_t mxfp4_linear_logprobs_workspace_bytes(int64_t tokens, int64_t in_features
                (piece == vocab && splits == 1 ? 0 : static_cast<size_t>(splits) * dense_split_rows(tokens) * in_features * 4);
     }
     const size_t rows = round_up(static_cast<size_t>(tokens < kLossRows ? tokens : kLossRows), 32);
-    return rows * static_cast<size_t>(dense_tiles(vocab, 128)) * sizeof(float2) + rows * sizeof(float);
+    // narrower tiles are for few rows only
+    const int64_t pieces = std::max(loss_pieces(std::min(tokens, kLossRows), vocab), loss_pieces(tokens % kLossRows, vocab));
+    return rows * static_cast<size_t>(pieces) * sizeof(float2) + rows * sizeof(float);
 }
 
 int mxfp4_linear_logprobs_forward(const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t tokens,
@@ -140,9 +147,8 @@ int mxfp4_linear_logprobs_forward(const void* x, int64_t ld_x, const void* w, in
     if ((rc = device_status_code(dev)) != MXFP4_OK) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t pitch = round_up(static_cast<size_t>(tokens < kLossRows ? tokens : kLossRows), 32);
-    const int64_t pieces = dense_tiles(vocab, 128);
     for (int64_t r = 0; r < tokens; r += kLossRows) {
-        const int64_t rows = tokens - r < kLossRows ? tokens - r : kLossRows;
+        const int64_t rows = tokens - r < kLossRows ? tokens - r : kLossRows, pieces = loss_pieces(rows, vocab);
         DenseProduct c;
         c.M = rows;
         c.N = vocab;

@@ -44,7 +44,7 @@ def check_forward(x, w, targets, logp, lse, scale=1.0):
     assert (logp[targets < 0] == 0).all()
 
 
-SIZES = [(1, 8, 1), (1, 64, 1000), (2, 72, 129), (31, 128, 8), (33, 264, 4097), (130, 64, 127), (257, 136, 2011), (300, 520, 32001)]
+SIZES = [(1, 8, 1), (1, 64, 1000), (2, 72, 129), (31, 128, 8), (33, 264, 4097), (130, 64, 127), (257, 136, 2011), (300, 520, 32001), (400, 64, 14900)]
 
 
 @pytest.mark.parametrize("T,D,V", SIZES)

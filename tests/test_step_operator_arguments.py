@@ -31,7 +31,7 @@ def test_sizes(lib):
     assert g(64, 4096, 14336) == 2 * 64 * 14336 * 2 + 9 * 256 * 4096 * 4
     assert g(0, 8, 8) == g(8, 8, 0) == g(8, 8, 12) == g(8, 12, 8) == g(HUGE, 8, 8) == 0
     l = lib.mxfp4_linear_logprobs_workspace_bytes
-    assert l(1, 64, 1000, 0) == 32 * 8 * 8 + 32 * 4
+    assert l(1, 64, 1000, 0) == 32 * 16 * 8 + 32 * 4 and l(8192, 64, 1000, 0) == 8192 * 8 * 8 + 8192 * 4
     assert l(16384, 64, 128256, 0) == l(1 << 20, 64, 128256, 0) < 1 << 28         # does not grow with the text
     assert l(100, 64, 500, 1) == 100864                                           # one piece, too short to split: 100 * 504 * 2, rounded up
     assert l(8192, 8192, 128256, 1) == 8192 * 16384 * 2 + 8192 * 8192 * 4         # several pieces
