@@ -56,7 +56,8 @@ def test_norm_and_clip(sizes, kinds, offset):
     copies = [t.clone() for t in tensors]
     got = api.clip_grads(copies, 0.5)
     api.check()
-    assert torch.equal(got, norm)
+    # a copy starts at another alignment, so other elements share a fp32 sum: both norms are within NORM of the exact one
+    assert abs(got.double() - norm.double()) <= 2 * NORM * norm.double()
     check_clip(tensors, 0.5, copies, got)
 
 
