@@ -19,10 +19,12 @@
 //   kDenseGated             columns 0..127 of a tile are a gate's, 128..255 the other projection's of the same features
 //                           (the pair's first CTA loads the rows of one weight, the second those of the other): act(g) * u,
 //                           and g and u on request
-//   kDensePartials          maximum and sum of exponentials of each row's 128 columns, and the target's value
+//   kDensePartials          maximum and sum of exponentials of each row's 128 columns, and the target's value.  The normaliser
+//                           goes by a row's largest logits, and truncating additions make these too small, all alike: sums of
+//                           4096 products left lse 1.9e-6 of itself off, sums of 1024, added in registers, 0.4e-6, at no cost
 //   kDenseLogitGrad         gradient of the log probabilities with respect to the logits, rounded to bf16
 //
-// Roles per CTA (320 threads): warps 0..7 epilogue (32 rows x 128 columns each), warp 8 TMA producer, warp 9 MMA
+// Roles per CTA (384 threads): warps 0..7 epilogue (32 rows x 128 columns each), warp 8 TMA producer, warp 9 MMA
 // issuer (leader CTA only).  Barrier ownership: full and tmem_empty live in the leader, empty and tmem_full are signalled
 // in both CTAs by a multicast commit.  All waits are bounded.
 #pragma once
@@ -48,7 +50,8 @@ constexpr int kDBoxBytes = kDOperandBytes / 2;     // 64 columns x 64 rows of a 
 constexpr int kDEpiWarps = 8;
 constexpr int kDProducerWarp = 8;
 constexpr int kDMmaWarp = 9;
-constexpr int kDThreads = 320;
+constexpr int kDThreads = 384;                      // two warps more than there are roles: registers go by four warps
+constexpr int kDChain = 16;
 constexpr int kDStageBytes = 32 * 128;             // output staging per epilogue warp and box
 
 // Two output boxes per warp, so that one is filled while the other leaves, are worth a stage of operands where tiles are
@@ -176,6 +179,8 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
     const int n_clusters = gridDim.x >> 1;
     constexpr bool kStore = EPI == kDenseStore;
     constexpr bool kGated = EPI == kDenseGated;
+    // K-steps that are added up in tensor memory, whose additions truncate; longer sums go on in registers (0: any length)
+    constexpr int kChain = EPI == kDensePartials ? kDChain : 0;
 
     if (threadIdx.x == 0) {
         sm.abort_flag = 0;
@@ -201,100 +206,117 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
     griddep_launch_dependents();
     griddep_wait();
 
-    if (warp == kDProducerWarp) {
-        // ------------------------------------------------------------ TMA producer
-        if (elect_one_sync()) {
-            int s = 0;
-            uint32_t parity = 1;                       // of the phase before: a fresh barrier passes
-            bool alive = true;
-            for (int j = 0; alive; ++j) {
-                const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, j);
-                if (w.q < 0) break;
-                const DenseShape& q = p.q[w.q];
-                const DenseMaps& m = maps.q[w.q];
-                const bool a_mn = kStore && q.a_mn;
-                const int ya = w.row + static_cast<int>(rank) * kDHalf;
-                const int yb = kGated ? w.tn * q.width : w.tn * 2 * q.width + static_cast<int>(rank) * q.width;
-                for (int k = w.k0; k < w.k1; ++k) {
-                    if (!mbar_wait(&sm.empty[s], parity, &sm.abort_flag)) {
-                        alive = false;
-                        break;
+    // registers: 384 x 168 at launch = 256 x 216 (epilogue) + 128 x 72 (the others)
+    if (warp >= kDEpiWarps) {
+        setmaxnreg_dec<72>();
+        if (warp == kDProducerWarp) {
+            // ------------------------------------------------------------ TMA producer
+            if (elect_one_sync()) {
+                int s = 0;
+                uint32_t parity = 1;                       // of the phase before: a fresh barrier passes
+                bool alive = true;
+                for (int j = 0; alive; ++j) {
+                    const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, j);
+                    if (w.q < 0) break;
+                    const DenseShape& q = p.q[w.q];
+                    const DenseMaps& m = maps.q[w.q];
+                    const bool a_mn = kStore && q.a_mn;
+                    const int ya = w.row + static_cast<int>(rank) * kDHalf;
+                    const int yb = kGated ? w.tn * q.width : w.tn * 2 * q.width + static_cast<int>(rank) * q.width;
+                    for (int k = w.k0; k < w.k1; ++k) {
+                        if (!mbar_wait(&sm.empty[s], parity, &sm.abort_flag)) {
+                            alive = false;
+                            break;
+                        }
+                        const int seg_k = k >= q.seg_k_steps;
+                        const int kk = (k - seg_k * q.seg_k_steps) * kDBlockK;
+                        const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
+                        mbar_arrive_expect_tx_cluster(full, kDOperandBytes + q.width * (kDBlockK * 2));
+                        dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk);
+                        dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk);
+                        if (++s == kDStages) {
+                            s = 0;
+                            parity ^= 1;
+                        }
                     }
-                    const int seg_k = k >= q.seg_k_steps;
-                    const int kk = (k - seg_k * q.seg_k_steps) * kDBlockK;
-                    const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
-                    mbar_arrive_expect_tx_cluster(full, kDOperandBytes + q.width * (kDBlockK * 2));
-                    dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk);
-                    dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk);
+                }
+                // the last stages' release signals: one that arrived after the CTA is gone would be counted on a barrier
+                // of the next launch
+                for (int i = 0; alive && i < kDStages; ++i) {
+                    alive = mbar_wait(&sm.empty[s], parity, &sm.abort_flag);
                     if (++s == kDStages) {
                         s = 0;
                         parity ^= 1;
                     }
                 }
+                if (!alive) linger();      // given up: what is in flight lands before the CTA leaves
             }
-            // the last stages' release signals: one that arrived after the CTA is gone would be counted on a barrier
-            // of the next launch
-            for (int i = 0; alive && i < kDStages; ++i) {
-                alive = mbar_wait(&sm.empty[s], parity, &sm.abort_flag);
-                if (++s == kDStages) {
-                    s = 0;
-                    parity ^= 1;
-                }
-            }
-            if (!alive) linger();      // given up: what is in flight lands before the CTA leaves
-        }
-        __syncwarp();
-    } else if (warp == kDMmaWarp) {
-        // ------------------------------------------------------------ MMA issuer
-        if (rank == 0 && elect_one_sync()) {
-            // fp32 accumulator, bf16 x bf16, 256 x 2 * width x 16
-            constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | (kStore ? 1u << 16 : 0u) |
-                                        (static_cast<uint32_t>(kDTile >> 4) << 24);
-            // along K: 8-row groups 1024 bytes apart, an instruction's 16 elements are 32 bytes; transposed: 64-column boxes
-            // 8 KB apart, 8-row groups of K 1024 bytes apart, 16 rows are 2 KB
-            const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), kStore ? kDBoxBytes : 16, 1024, 2);
-            constexpr int kStepB = kStore ? 128 : 2;
-            int s = 0, b = 0;
-            uint32_t parity = 0, buf_parity = 1;       // a fresh tmem_empty passes for the phase before
-            bool alive = true;
-            for (int i = 0; alive; ++i) {
-                const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, i);
-                if (w.q < 0) break;
-                const DenseShape& q = p.q[w.q];
-                const bool a_mn = kStore && q.a_mn;
-                const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), a_mn ? kDBoxBytes : 16, 1024, 2);
-                const int step_a = a_mn ? 128 : 2;
-                const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u) | (static_cast<uint32_t>(2 * q.width) >> 3 << 17);
-                if (!mbar_wait(&sm.tmem_empty[b], buf_parity, &sm.abort_flag)) break;
-                tcgen05_fence_after();
-                for (int k = w.k0; k < w.k1; ++k) {
-                    if (!mbar_wait(&sm.full[s], parity, &sm.abort_flag)) {
-                        alive = false;
-                        break;
-                    }
+            __syncwarp();
+        } else if (warp == kDMmaWarp) {
+            // ------------------------------------------------------------ MMA issuer
+            if (rank == 0 && elect_one_sync()) {
+                // fp32 accumulator, bf16 x bf16, 256 x 2 * width x 16
+                constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | (kStore ? 1u << 16 : 0u) |
+                                            (static_cast<uint32_t>(kDTile >> 4) << 24);
+                // along K: 8-row groups 1024 bytes apart, an instruction's 16 elements are 32 bytes; transposed: 64-column boxes
+                // 8 KB apart, 8-row groups of K 1024 bytes apart, 16 rows are 2 KB
+                const uint64_t b_desc0 = make_smem_desc(smem_u32(sm.b[0]), kStore ? kDBoxBytes : 16, 1024, 2);
+                constexpr int kStepB = kStore ? 128 : 2;
+                int s = 0, b = 0;
+                uint32_t parity = 0, buf_parity = 1;       // a fresh tmem_empty passes for the phase before
+                bool alive = true;
+                for (int i = 0; alive; ++i) {
+                    const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, i);
+                    if (w.q < 0) break;
+                    const DenseShape& q = p.q[w.q];
+                    const bool a_mn = kStore && q.a_mn;
+                    const uint64_t a_desc0 = make_smem_desc(smem_u32(sm.a[0]), a_mn ? kDBoxBytes : 16, 1024, 2);
+                    const int step_a = a_mn ? 128 : 2;
+                    const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u) | (static_cast<uint32_t>(2 * q.width) >> 3 << 17);
+                    if (!mbar_wait(&sm.tmem_empty[b], buf_parity, &sm.abort_flag)) break;
                     tcgen05_fence_after();
-                    const int kk = (k >= q.seg_k_steps ? k - q.seg_k_steps : k) * kDBlockK;
-                    const int nmma = (min(kDBlockK, q.K - kk) + 15) / 16;      // what lies past K is filled with zeros
-                    const uint64_t a_desc = a_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
-                    const uint64_t b_desc = b_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
+                    int first = w.k0;                      // of the chain of additions
+                    for (int k = w.k0; k < w.k1; ++k) {
+                        if (kChain > 0 && k - first == kChain) {
+                            tcgen05_commit_pair(&sm.tmem_full[b], 3);
+                            buf_parity ^= b;
+                            b ^= 1;
+                            first = k;
+                            if (!mbar_wait(&sm.tmem_empty[b], buf_parity, &sm.abort_flag)) {
+                                alive = false;
+                                break;
+                            }
+                            tcgen05_fence_after();
+                        }
+                        if (!mbar_wait(&sm.full[s], parity, &sm.abort_flag)) {
+                            alive = false;
+                            break;
+                        }
+                        tcgen05_fence_after();
+                        const int kk = (k >= q.seg_k_steps ? k - q.seg_k_steps : k) * kDBlockK;
+                        const int nmma = (min(kDBlockK, q.K - kk) + 15) / 16;      // what lies past K is filled with zeros
+                        const uint64_t a_desc = a_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
+                        const uint64_t b_desc = b_desc0 + static_cast<uint64_t>(s * (kDOperandBytes >> 4));
 #pragma unroll
-                    for (int j = 0; j < kDBlockK / 16; ++j)
-                        if (j < nmma)
-                            tcgen05_mma_f16_pair(tmem + b * kDTile, a_desc + step_a * j, b_desc + kStepB * j, idesc, k > w.k0 || j > 0);
-                    tcgen05_commit_pair(&sm.empty[s], 3);
-                    if (++s == kDStages) {
-                        s = 0;
-                        parity ^= 1;
+                        for (int j = 0; j < kDBlockK / 16; ++j)
+                            if (j < nmma)
+                                tcgen05_mma_f16_pair(tmem + b * kDTile, a_desc + step_a * j, b_desc + kStepB * j, idesc, k > first || j > 0);
+                        tcgen05_commit_pair(&sm.empty[s], 3);
+                        if (++s == kDStages) {
+                            s = 0;
+                            parity ^= 1;
+                        }
                     }
+                    if (alive) tcgen05_commit_pair(&sm.tmem_full[b], 3);
+                    buf_parity ^= b;
+                    b ^= 1;
                 }
-                if (alive) tcgen05_commit_pair(&sm.tmem_full[b], 3);
-                buf_parity ^= b;
-                b ^= 1;
             }
+            __syncwarp();
         }
-        __syncwarp();
     } else {
         // ------------------------------------------------------------ epilogue warps
+        setmaxnreg_inc<216>();
         const int quad = warp & 3;                     // TMEM lane quadrant of this warp
         const int half = warp >> 2;                    // which 128 columns
         const uint64_t streaming = l2_policy_evict_first();      // outputs should not displace operands
@@ -334,7 +356,6 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
             const int row = row0 + lane;
             if (!mbar_wait(&sm.tmem_full[b], parity, &sm.abort_flag)) break;       // given up: nothing more is stored
             tcgen05_fence_after();
-            const uint32_t from = lanes + b * kDTile;
             auto hand_back = [&]() {
                 tcgen05_fence_before();
                 __syncwarp();
@@ -342,10 +363,70 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
             };
             uint32_t r[32];
             auto read = [&](int col) {
-                tmem_ld_32x32b_x32(from + col, r);
+                tmem_ld_32x32b_x32(lanes + b * kDTile + col, r);
                 tmem_ld_wait_for(r);
             };
-            if (row0 >= q.M || w.k0 == w.k1) {         // warp-uniform: no rows here, or a piece without products
+            if constexpr (EPI == kDensePartials) {
+                const int col0 = (tn * 2 + half) * q.width, col1 = min(q.N, col0 + q.width);
+                const bool any = row0 < q.M && col0 < col1;                    // warp-uniform
+                bool alive = true;
+                float z[4][32];
+                for (int k = w.k0;;) {
+                    if (any) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (col0 + c * 32 >= col1) break;
+                            read(half * q.width + c * 32);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                z[c][i] = k == w.k0 ? __uint_as_float(r[i]) : z[c][i] + __uint_as_float(r[i]);
+                        }
+                    }
+                    hand_back();
+                    k += kDChain;
+                    if (k >= w.k1) break;
+                    parity ^= b;
+                    b ^= 1;
+                    alive = mbar_wait(&sm.tmem_full[b], parity, &sm.abort_flag);
+                    if (!alive) break;
+                    tcgen05_fence_after();
+                }
+                if (!alive) break;                     // given up: nothing more is stored
+                if (any) {
+                    const bool row_ok = row < q.M;
+                    const int64_t target = row_ok && p.x.targets ? p.x.targets[row] : -1;
+                    const int at = target >= p.x.col_base + col0 && target < p.x.col_base + col1
+                                       ? static_cast<int>(target - p.x.col_base - col0) : -1;
+                    const bool any_here = __any_sync(0xffffffffu, at >= 0);
+                    float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            z[c][i] = col0 + c * 32 + i < col1 ? z[c][i] * p.x.scale : -INFINITY;
+                            top = fmaxf(top, z[c][i]);
+                        }
+                        if (any_here) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (c * 32 + i == at) picked = z[c][i];
+                        }
+                    }
+                    // a row of nothing but -infinity has sum 0; a NaN passes the maximum by and enters the sum
+                    const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float part = 0.0f;             // four sums of 32
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) part += dense_exp(z[c][i] - ref);
+                        sum += part;
+                    }
+                    if (row_ok) {
+                        p.x.parts[static_cast<int64_t>(tn * 2 + half) * p.x.ld_parts + row] = make_float2(top, sum);
+                        if (at >= 0) p.x.picked[row] = picked;
+                    }
+                }
+            } else if (row0 >= q.M || w.k0 == w.k1) {         // warp-uniform: no rows here, or a piece without products
                 hand_back();
             } else if constexpr (kStore) {
                 const int col0 = tn * kDTile + half * kDHalf;
@@ -386,7 +467,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t u[32];
-                        tmem_ld_32x32b_x32(from + q.width + half * 64 + c * 32, u);
+                        tmem_ld_32x32b_x32(lanes + b * kDTile + q.width + half * 64 + c * 32, u);
                         read(half * 64 + c * 32);
                         tmem_ld_wait_for(u);
                         if (keep) {
@@ -429,78 +510,43 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                     hand_back();
                 }
             } else {
-                // rows of logits
+                // gradients of rows of logits
                 const int col0 = (tn * 2 + half) * q.width, col1 = min(q.N, col0 + q.width);
                 const bool row_ok = row < q.M;
                 const int64_t target = row_ok && p.x.targets ? p.x.targets[row] : -1;
                 const int at = target >= p.x.col_base + col0 && target < p.x.col_base + col1
                                    ? static_cast<int>(target - p.x.col_base - col0) : -1;
                 const bool any_here = __any_sync(0xffffffffu, at >= 0);
-                if constexpr (EPI == kDensePartials) {
-                    if (col0 < col1) {
-                        float top_so_far = -INFINITY, sum = 0.0f, picked = 0.0f;
+                const float lse = row_ok ? p.x.lse[row] : 0.0f;
+                float gl = row_ok && p.x.d_logp && target >= 0 ? p.x.d_logp[row] : 0.0f;
+                const float gn = row_ok && p.x.d_lse ? p.x.d_lse[row] : 0.0f;
+                if (target >= p.x.vocab) gl = NAN;
+                const bool zero = (gl == 0.0f && gn == 0.0f);
+                const float coef = p.x.scale * (gn - gl);
 #pragma unroll 1
-                        for (int c = 0; col0 + c * 32 < col1; ++c) {
-                            read(half * q.width + c * 32);
-                            float z[32], top = top_so_far;
+                for (int c = 0; c < 4; ++c) {
+                    const int col = col0 + c * 32;
+                    if (col < p.x.ld_grad) {
+                        read(half * kDHalf + c * 32);
+                        if ((c & 1) == 0) stage_wait();
+                        float z[32];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                z[i] = __uint_as_float(r[i]) * p.x.scale;
-                                if (col0 + c * 32 + i >= col1) z[i] = -INFINITY;
-                                top = fmaxf(top, z[i]);
-                            }
-                            if (any_here) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (c * 32 + i == at) picked = z[i];
-                            }
-                            // a row of nothing but -infinity so far has sum 0; a NaN passes the maximum by and enters the sum
-                            const float ref = top == -INFINITY ? 0.0f : top;
-                            sum *= dense_exp(top_so_far - ref);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) sum += dense_exp(z[i] - ref);
-                            top_so_far = top;
+                        for (int i = 0; i < 32; ++i) {
+                            z[i] = coef * dense_exp(__uint_as_float(r[i]) * p.x.scale - lse);
+                            if (zero || col + i >= q.N) z[i] = 0.0f;
                         }
-                        hand_back();
-                        if (row_ok) {
-                            p.x.parts[static_cast<int64_t>(tn * 2 + half) * p.x.ld_parts + row] = make_float2(top_so_far, sum);
-                            if (at >= 0) p.x.picked[row] = picked;
+                        if (any_here) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (c * 32 + i == at) z[i] += p.x.scale * gl;
                         }
-                    } else {
-                        hand_back();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            stage_put((c & 1) * 4 + i, dense_pack8(reinterpret_cast<uint32_t*>(z) + 8 * i));
                     }
-                } else {
-                    const float lse = row_ok ? p.x.lse[row] : 0.0f;
-                    float gl = row_ok && p.x.d_logp && target >= 0 ? p.x.d_logp[row] : 0.0f;
-                    const float gn = row_ok && p.x.d_lse ? p.x.d_lse[row] : 0.0f;
-                    if (target >= p.x.vocab) gl = NAN;
-                    const bool zero = (gl == 0.0f && gn == 0.0f);
-                    const float coef = p.x.scale * (gn - gl);
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        const int col = col0 + c * 32;
-                        if (col < p.x.ld_grad) {
-                            read(half * kDHalf + c * 32);
-                            if ((c & 1) == 0) stage_wait();
-                            float z[32];
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                z[i] = coef * dense_exp(__uint_as_float(r[i]) * p.x.scale - lse);
-                                if (zero || col + i >= q.N) z[i] = 0.0f;
-                            }
-                            if (any_here) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (c * 32 + i == at) z[i] += p.x.scale * gl;
-                            }
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                stage_put((c & 1) * 4 + i, dense_pack8(reinterpret_cast<uint32_t*>(z) + 8 * i));
-                        }
-                        if ((c & 1) != 0 && col - 32 < p.x.ld_grad) stage_store(&m.out[0], col - 32, row0);
-                    }
-                    hand_back();
+                    if ((c & 1) != 0 && col - 32 < p.x.ld_grad) stage_store(&m.out[0], col - 32, row0);
                 }
+                hand_back();
             }
             parity ^= b;
             b ^= 1;
