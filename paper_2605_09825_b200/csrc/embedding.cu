@@ -4,10 +4,12 @@
 // run is noted (a note counts only where the sorted ids confirm it, so the notes need no clearing).  Then
 //   - the sorted positions are shared out evenly, and gradients of equal ids are added in fp32 in the order of their
 //     positions; where a run spans shares, its partial sums are joined in the order of the shares;
-//   - the rows without tokens of a dense gradient are set to zero.  Small CTAs in the device's own order keep the rows being
-//     written close together: 128256 rows of 16 KB take 273 us that way (7.3 TB/s), 338 from CTAs that stay and take rows
-//     in turn.  Zeros first and sums after them cost 16 us more at 16384 tokens: what the zeros leave in L2 has to be written
-//     back before anything else finds room there.
+//   - beside that the rows without tokens of a dense gradient are set to zero.  Small CTAs in the device's own order keep
+//     the rows being written close together: 128256 rows of 16 KB take 273 us that way (7.3 TB/s), 338 from CTAs that stay
+//     and take rows in turn.
+// 16384 tokens of 4096 columns, fp32 gradient of 128256 rows: 344 us for 2.24 GB, as fast as a copy (19 us of it the sort;
+// 360 with the sums before the zeros, 378 with sums from registers, 464 with zeros first); 777 tokens of 2048, bf16, 32001
+// rows: 30 us for 134 MB.
 // No floating-point atomics: results depend on the inputs alone.
 //
 // Up to 4096 positions are sorted by counting, for each, the smaller ones: 2 T^2 comparisons over the whole device, one
@@ -323,22 +325,24 @@ struct RowSum {
     }
 };
 
+// Eight columns of a row from their sums.
+template <class Out>
+__device__ __forceinline__ void write8(const SumParams& p, uint32_t id, int col, float2 (&sum)[4])
+{
+    Out* to = static_cast<Out*>(p.table) + id * p.ld_table + col;
+    float2 old[4] = {};
+    if (p.accumulate) load8_stream(to, old);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = make_float2(fmaf(sum[j].x, p.scale, old[j].x), fmaf(sum[j].y, p.scale, old[j].y));
+    store8(to, sum);
+}
+
 template <class Out>
 __device__ __forceinline__ void write_row(const SumParams& p, uint32_t id, int col, RowSum& s)
 {
-    Out* to = static_cast<Out*>(p.table) + id * p.ld_table + col;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        if (col + g * 256 >= p.width) break;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s.v[g][j] = make_float2(s.v[g][j].x * p.scale, s.v[g][j].y * p.scale);
-        if (p.accumulate) {
-            float2 old[4];
-            load8_stream(to + g * 256, old);
-            s.add(g, old);
-        }
-        store8(to + g * 256, s.v[g]);
-    }
+    for (int g = 0; g < 4; ++g)
+        if (col + g * 256 < p.width) write8<Out>(p, id, col + g * 256, s.v[g]);
 }
 
 // A warp per share of the sorted positions and 1024 columns.  The rows come through a ring of bulk copies in shared memory,
@@ -359,8 +363,8 @@ __global__ void __launch_bounds__(kSumWarps * 32, 1) sum_kernel(const __grid_con
         fence_barrier_init();
     }
     __syncthreads();
-    griddep_launch_dependents();
     griddep_wait();
+    griddep_launch_dependents();                   // not before the wait: see fill_join_kernel
     uint8_t* ring = sm.ring[warp];
     uint64_t* full = sm.full[warp];
     int slot = 0;                                  // of the row to be added next
@@ -451,65 +455,65 @@ __global__ void __launch_bounds__(kSumWarps * 32, 1) sum_kernel(const __grid_con
     }
 }
 
-// Rows whose runs span shares, a warp per share that one begins in and 1024 columns.
-template <class Out>
-__global__ void __launch_bounds__(kSumWarps * 32) sum_join_kernel(const __grid_constant__ SumParams p)
-{
-    griddep_launch_dependents();
-    griddep_wait();
-    const int lane = threadIdx.x & 31;
-    const int u = blockIdx.x * kSumWarps + (threadIdx.x >> 5);
-    const int share = u / p.slabs, col = (u - share * p.slabs) * kSlab + lane * 8;
-    if (share + 1 >= p.shares) return;
-    const int begin = share * p.share;
-    const uint32_t id = p.sorted[begin + p.share].x;
-    // it goes on in the next share, and begins in this one
-    if (id >= p.vocab || p.sorted[begin + p.share - 1].x != id || (begin > 0 && p.sorted[begin - 1].x == id)) return;
-    RowSum s;
-    s.clear();
-    auto add = [&](const float* row) {
-        float2 v[4][4];
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-            if (col + g * 256 < p.width) load8_stream(row + g * 256, v[g]);
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-            if (col + g * 256 < p.width) s.add(g, v[g]);
-    };
-    add(p.parts + (static_cast<int64_t>(share) * 2 + 1) * p.width + col);
-    for (int c = share + 1;; c += 32) {
-        const bool in = c + lane < p.shares && p.sorted[(c + lane) * p.share].x == id;
-        const uint32_t out = ~__ballot_sync(0xffffffffu, in);
-        const int n = out == 0 ? 32 : __ffs(out) - 1;
-#pragma unroll 2
-        for (int k = 0; k < n; ++k) add(p.parts + static_cast<int64_t>(c + k) * 2 * p.width + col);
-        if (n < 32) break;
-    }
-    if (col < p.width) write_row<Out>(p, id, col, s);
-}
-
-// Rows without tokens of a dense gradient: eight rows per CTA.
+// The rows without tokens of a dense gradient, eight per CTA, and after them the rows whose runs span shares: a warp per share
+// that one begins in and 256 columns.
+//
+// The zeros are written beside the sums before them in the stream: other rows, and a CTA of this kernel starts only after
+// every CTA of that one has seen all work before it complete.  What this kernel reads of it comes past L1.  Every CTA waits
+// for the sums before it ends, so that what follows in the stream comes after both.
 struct FillParams {
-    const uint2* sorted;
     const uint32_t* first;
-    uint8_t* table;
     int64_t pitch;               // bytes
     int32_t vectors;             // 16-byte pieces per row
-    uint32_t tokens, vocab;
+    int32_t blocks;              // of zeros
+    int32_t slabs;               // pieces of 256 columns
 };
 
 constexpr int kFillRows = 8;
 
-__global__ void __launch_bounds__(kFillRows * 32) fill_kernel(const __grid_constant__ FillParams p)
+template <class Out>
+__global__ void __launch_bounds__(kFillRows * 32) fill_join_kernel(const __grid_constant__ SumParams p, const __grid_constant__ FillParams f)
 {
     griddep_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    if (static_cast<int>(blockIdx.x) < f.blocks) {
+        const uint32_t row = blockIdx.x * kFillRows + (threadIdx.x >> 5);
+        if (row < p.vocab) {
+            const uint32_t at = __ldcg(f.first + row);
+            const bool any = at < static_cast<uint32_t>(p.tokens) && __ldcg(&p.sorted[at].x) == row &&
+                             (at == 0 || __ldcg(&p.sorted[at - 1].x) != row);
+            uint8_t* to = static_cast<uint8_t*>(p.table) + row * f.pitch;
+            for (int i = lane; i < f.vectors && !any; i += 32) st_stream(to + i * 16, make_uint4(0u, 0u, 0u, 0u));
+        }
+        griddep_wait();
+        return;
+    }
     griddep_wait();
-    const uint32_t row = blockIdx.x * kFillRows + (threadIdx.x >> 5);
-    if (row >= p.vocab) return;
-    const uint32_t at = p.first[row];
-    if (at < p.tokens && p.sorted[at].x == row && (at == 0 || p.sorted[at - 1].x != row)) return;
-    uint8_t* to = p.table + row * p.pitch;
-    for (int i = threadIdx.x & 31; i < p.vectors; i += 32) st_stream(to + i * 16, make_uint4(0u, 0u, 0u, 0u));
+    const int64_t u = static_cast<int64_t>(blockIdx.x - f.blocks) * kFillRows + (threadIdx.x >> 5);
+    const int share = static_cast<int>(u / f.slabs), col = (static_cast<int>(u - static_cast<int64_t>(share) * f.slabs) * 32 + lane) * 8;
+    if (share + 1 >= p.shares) return;
+    const int begin = share * p.share;
+    const uint32_t id = __ldcg(&p.sorted[begin + p.share].x);
+    // it goes on in the next share, and begins in this one
+    if (id >= p.vocab || __ldcg(&p.sorted[begin + p.share - 1].x) != id || (begin > 0 && __ldcg(&p.sorted[begin - 1].x) == id)) return;
+    const float* parts = p.parts + static_cast<int64_t>(share) * 2 * p.width + min(col, p.width - 8);
+    float2 sum[4];
+    load8_stream(parts + p.width, sum);
+    for (int c = share + 1;; c += 32) {
+        const bool in = c + lane < p.shares && __ldcg(&p.sorted[(c + lane) * p.share].x) == id;
+        const uint32_t out = ~__ballot_sync(0xffffffffu, in);
+        const int n = out == 0 ? 32 : __ffs(out) - 1;
+        parts = p.parts + static_cast<int64_t>(c) * 2 * p.width + min(col, p.width - 8);
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            float2 v[4];
+            load8_stream(parts + static_cast<int64_t>(k) * 2 * p.width, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] = make_float2(sum[j].x + v[j].x, sum[j].y + v[j].y);
+        }
+        if (n < 32) break;
+    }
+    if (col < p.width) write8<Out>(p, id, col, sum);
 }
 
 template <class In, class Out>
@@ -652,23 +656,18 @@ int mxfp4_embedding_backward(const int64_t* ids, int64_t tokens, const void* d_o
               : (out32 ? launch_sums<__nv_bfloat16, float>(s, units, dev.sm_count, st)
                        : launch_sums<__nv_bfloat16, __nv_bfloat16>(s, units, dev.sm_count, st));
     if (rc != MXFP4_OK) return rc;
-    if (s.shares > 1) {
-        auto join = out32 ? sum_join_kernel<float> : sum_join_kernel<__nv_bfloat16>;
-        if (launch_kernel_pdl(join, static_cast<int>((units + kSumWarps - 1) / kSumWarps), kSumWarps * 32, 0, st, s) != cudaSuccess)
-            return MXFP4_ERR_CUDA;
-    }
-    if (accumulate) return MXFP4_OK;
+    // zeros for a dense gradient, and rows that span shares
     FillParams f;
-    f.sorted = q.a;
     f.first = q.first;
-    f.table = static_cast<uint8_t*>(d_table);
     f.pitch = ld_d_table * (out32 ? 4 : 2);
     f.vectors = static_cast<int32_t>(width * (out32 ? 4 : 2) / 16);
-    f.tokens = static_cast<uint32_t>(tokens);
-    f.vocab = static_cast<uint32_t>(vocab);
-    return launch_kernel_pdl(fill_kernel, static_cast<int>((vocab + kFillRows - 1) / kFillRows), kFillRows * 32, 0, st, f) ==
-                   cudaSuccess
-               ? MXFP4_OK : MXFP4_ERR_CUDA;
+    f.blocks = accumulate ? 0 : static_cast<int32_t>((vocab + kFillRows - 1) / kFillRows);
+    f.slabs = static_cast<int32_t>((width + 255) / 256);
+    const int64_t joins = s.shares > 1 ? (static_cast<int64_t>(s.shares) * f.slabs + kFillRows - 1) / kFillRows : 0;
+    if (f.blocks + joins == 0) return MXFP4_OK;
+    auto fill = out32 ? fill_join_kernel<float> : fill_join_kernel<__nv_bfloat16>;
+    return launch_kernel_pdl(fill, static_cast<int>(f.blocks + joins), kFillRows * 32, 0, st, s, f) == cudaSuccess ? MXFP4_OK
+                                                                                                                : MXFP4_ERR_CUDA;
 }
 
 }  // extern "C"
