@@ -51,8 +51,9 @@ __device__ __forceinline__ float2 act_both(float g)
     }
     if constexpr (ACT == MXFP4_GATE_GELU_TANH) {
         const float s = logistic(2.0f * kGeluC * (g + kGeluCubic * g * g * g));
+        const float bend = s * (1.0f - s);            // 0 far from the origin, where the slope's square may overflow
         const float slope = kGeluC * (1.0f + 3.0f * kGeluCubic * g * g);
-        return make_float2(g * s, s + 2.0f * g * s * (1.0f - s) * slope);
+        return make_float2(g * s, bend > 0.0f ? s + 2.0f * g * bend * slope : s);
     }
     if constexpr (ACT == MXFP4_GATE_RELU) return make_float2(g < 0.0f ? 0.0f : g, g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g);
     return make_float2(g, 1.0f);

@@ -167,6 +167,39 @@ def test_strides_halves_of_one_weight_and_untouched_surroundings(T):
         assert (room[0] == 7).all() and (room[-1] == 7).all() and (room[:, :8] == 7).all() and (room[:, -8:] == 7).all()
 
 
+def test_more_than_2_to_the_31_elements():
+    T, D, F = 150100, 16, 14400                      # 2.16e9 in h, and in each of its companions
+    x, wg, wu, gen = inputs(T, D, F)
+    h, kept = api.gated_linear_forward(x, wg, wu)
+    api.check()
+    for rows in (slice(0, 40), slice(149120, 149160), slice(T - 40, T)):
+        check_forward(x[rows], wg, wu, api.GATE_SILU, h[rows], [t[rows] for t in kept])
+    dh = torch.zeros_like(h)
+    del h
+    dh[-3:] = rand(gen, 3, F)
+    dx, dwg, dwu = api.gated_linear_backward(dh, x, wg, wu, kept)
+    api.check()
+    assert (dx[:-3] == 0).all()
+    check_backward(dh[-3:], x[-3:], wg, wu, [t[-3:] for t in kept], api.GATE_SILU, dx[-3:], dwg, dwu, whole=False)
+
+
+def test_activations_far_from_the_origin():
+    """Where exponentials and squares leave fp32's range: values and slopes are the limits."""
+    x = torch.tensor([[1.0], [-1.0], [100.0], [-100.0]], device="cuda").bfloat16().expand(4, 8).contiguous()
+    x[:, 1:] = 0
+    wg = torch.zeros(8, 8, device="cuda").bfloat16()
+    wg[:, 0] = torch.tensor([1.0, 30.0, 100.0, 1e4, 1e10, 1e18, 1e25, 0.0], device="cuda")
+    one = torch.zeros(8, 8, device="cuda").bfloat16()
+    one[:, 0] = 1.0
+    for which in ACTS:
+        h, kept = api.gated_linear_forward(x, wg, one, which)
+        check_forward(x, wg, one, which, h, kept)
+        dh = torch.ones_like(h)
+        got = api.gated_linear_backward(dh, x, wg, one, kept, which)
+        api.check()
+        assert all(g.isfinite().all() for g in got), which
+
+
 def test_unwanted_gradients():
     x, wg, wu, gen = inputs(70, 128, 136)
     _, kept = api.gated_linear_forward(x, wg, wu)

@@ -104,6 +104,18 @@ def test_pieces_of_the_vocabulary():
     check_backward(x, w, targets, lse, gl, gn, dx, dw)
 
 
+def test_a_last_piece_shorter_than_its_splits():
+    """2048 tokens of 64 features: pieces of 65536 columns, split along K; the last one has a single step for them."""
+    T, D, V = 2048, 64, 65536 + 40
+    x, w, targets, gen = inputs(T, D, V)
+    targets[5] = V - 20
+    gl = torch.randn(T, generator=gen, device="cuda") / T
+    _, lse = api.linear_logprobs_forward(x, w, targets)
+    dx, dw = api.linear_logprobs_backward(x, w, targets, lse, gl)
+    api.check()
+    check_backward(x, w, targets, lse, gl, None, dx, dw)
+
+
 def test_more_rows_than_one_product_takes():
     x, w, targets, _ = inputs(16384 + 300, 16, 520)
     logp, lse = api.linear_logprobs_forward(x, w, targets)
