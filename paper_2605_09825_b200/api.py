@@ -861,10 +861,10 @@ def logprobs_backward(logits, targets, lse, entropy=None, d_logp=None, d_entropy
 
 # ---------------------------------------------------------------- gated projections, loss from the output layer's input
 def _on_current_device(*tensors) -> None:
-    """All CUDA tensors of a call live on the current device, whose current stream the call runs on."""
-    index = torch._C._cuda_getDevice() if torch.cuda.is_available() else -1
+    """All (CUDA) tensors of a call live on the current device, whose current stream the call runs on."""
+    index = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != index:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"tensors must be on the current device (cuda:{index})")
 
 
@@ -1062,9 +1062,10 @@ _DTYPE = operator.attrgetter("dtype")
 
 def _tensor_list(tensors, name: str) -> tuple:
     """Arrays of the pointers, element counts and types of contiguous CUDA tensors on the current device."""
-    index = torch._C._cuda_getDevice() if torch.cuda.is_available() else -2
     kinds = list(map(_STREAM_TYPES.get, map(_DTYPE, tensors)))
-    if None in kinds or not all(map(torch.Tensor.is_contiguous, tensors)) or not set(map(torch.Tensor.get_device, tensors)) <= {index}:
+    devices = set(map(torch.Tensor.get_device, tensors))
+    if None in kinds or not all(map(torch.Tensor.is_contiguous, tensors)) or -1 in devices or \
+            (devices and devices != {torch._C._cuda_getDevice()}):
         raise ValueError(f"{name} must be contiguous bf16 or fp32 tensors on the current device")
     return (array.array("q", map(torch.Tensor.data_ptr, tensors)), array.array("q", map(torch.Tensor.numel, tensors)),
             array.array("i", kinds))

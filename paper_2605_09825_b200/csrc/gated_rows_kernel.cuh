@@ -7,6 +7,9 @@
 // does not matter here, and it needs neither staging nor tensor memory.  The order of the 16 elements inside an
 // instruction is free as long as both operands agree, so a lane's 16-byte pieces of a row go in as they come: a quad
 // covers 64 contiguous bytes of each row.
+//
+// 4096 x 14336, one token: 36 us for 235 MB, the copy rate; eight tokens 38 us.  Sixteen took 49 us with two tiles of tokens (the
+// tokens' rows come from L2 once per CTA, and their registers halve the pieces in flight): the other kernel takes 43.
 #pragma once
 
 #include <cuda_bf16.h>

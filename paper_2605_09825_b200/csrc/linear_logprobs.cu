@@ -5,6 +5,9 @@
 // epilogue forms their gradient (bf16, in the workspace), then its product with the piece of the weight, added to the
 // input's gradient in fp32, and with the input, which is the piece of the weight's gradient.
 //
+// Bound by the products: 8192 tokens of 4096 features, vocabulary 128256, forward 5430 us by itself (1.6 PFLOP/s), 6440 pass after
+// pass, where the power cap sustains 1.34 to 1.40; 19 us are the join.  Backward, 4096 tokens: 8540 and 9670 to 10040.
+//
 // The gradient of the logits is rounded to bf16 because it is an operand of the tensor cores' products: sums over
 // hundreds of them are off by about 2^-9 / sqrt(3) of their value, less than the rounding of a bf16 result.
 #include <cuda_bf16.h>
