@@ -4,6 +4,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "../../include/mxfp4.h"
 #include "dense_gemm.cuh"
 #include "dense_gemm_kernel.cuh"
@@ -67,7 +69,14 @@ static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool g
     q.seg_k_steps = static_cast<int32_t>(seg_k);
     q.k_steps = static_cast<int32_t>(k_steps);
     q.width = width;
-    q.band = static_cast<int32_t>(tiles_n < 16 ? tiles_n : 16);
+    // A panel of one operand stays in L2 while the other passes, whichever order leaves less to be read from memory; where K
+    // is so long that no panel fits, the bands are about as wide as the tiles in flight are high.
+    const int64_t fits = kDensePanelBytes / (k_steps * kDBlockK * kDTile * 2);
+    const int64_t panel = std::max<int64_t>(8, fits);
+    const int64_t band_n = std::min(tiles_n, panel), band_m = std::min(tiles_m, panel);
+    q.band_m = tiles_m + dense_tiles(tiles_m, band_m) * tiles_n < tiles_n + dense_tiles(tiles_n, band_n) * tiles_m;
+    q.band = static_cast<int32_t>(q.band_m ? band_m : band_n);
+    q.hints = fits >= 8;
     q.splits = c.splits;
     q.split_rows = static_cast<int32_t>(dense_split_rows(c.M));
     q.items = static_cast<int32_t>(tiles_m * tiles_n * c.splits);

@@ -10,6 +10,11 @@ namespace mxfp4 {
 enum DenseEpilogue { kDenseStore, kDenseGated, kDensePartials, kDenseLogitGrad };
 enum DenseOut { kDenseBf16, kDenseF32, kDenseAddF32 };
 
+// What one operand's panel may take of L2.  The order decides how much is read from memory, which costs energy, and the power
+// cap makes that time: loss of 8192 tokens, pass after pass, 6250 us with bands of columns only and no hints, 6130 with
+// bands of rows where that reads less, 6060 with cache hints; gated forward pass 1470, 1450 and 1425.  Panels of 16, 24, 48
+// and 68 MB: 6400, 6330, 6340 and 6520 where 32 took 6220.
+constexpr int64_t kDensePanelBytes = int64_t{32} << 20;
 constexpr int64_t kDenseMaxDim = 0x7FFFFF00;
 constexpr int kDensePairs = 74;  // work is shared out for the pairs of CTAs of this many SMs, whatever the device has
 
@@ -21,7 +26,9 @@ struct DenseShape {
     int32_t k_steps;             // of all segments
     int32_t seg_k_steps;
     int32_t width;               // rows of B per CTA and tile: a tile has 2 * width columns
-    int32_t band;                // tile columns per band of the tile order
+    int32_t band;                // tile columns (band_m: rows) per band of the tile order
+    int32_t band_m;
+    int32_t hints;               // the panel is kept in L2, what passes it is not
     int32_t splits;              // pieces along K, each with an output of its own
     int32_t split_rows;          // output rows from one piece's to the next one's
     int32_t items;               // tiles * splits

@@ -125,16 +125,18 @@ __device__ __forceinline__ DenseWork dense_work(const DenseParams& p, int pair, 
         w.q = 1;
     }
     const DenseShape& q = p.q[w.q];
-    // tiles band by band: a band is `band` tile columns, and inside it the tile column varies fastest, so that the tiles
-    // in flight share rows of A and of B
+    // tiles band by band: a band is so many tile columns (or rows), and inside it they vary fastest, so that the tiles in
+    // flight share rows of A and columns of B, and the band's panel stays in L2 while the other operand passes
     const int tiles = q.tiles_m * q.tiles_n;
     const int split = item / tiles, tile = item - split * tiles;
-    const int per_band = q.band * q.tiles_m;
+    const int across = q.band_m ? q.tiles_m : q.tiles_n, along = q.band_m ? q.tiles_n : q.tiles_m;
+    const int per_band = q.band * along;
     const int b = tile / per_band;
     const int r = tile - b * per_band;
-    const int cols = min(q.band, q.tiles_n - b * q.band);
-    w.tm = r / cols;
-    w.tn = b * q.band + (r - w.tm * cols);
+    const int wide = min(q.band, across - b * q.band);
+    const int slow = r / wide, fast = b * q.band + (r - slow * wide);
+    w.tm = q.band_m ? fast : slow;
+    w.tn = q.band_m ? slow : fast;
     w.seg = w.tm >= q.seg_tiles_m;
     w.row = (w.tm - w.seg * q.seg_tiles_m) * kDTile;
     w.out_row = w.row + split * q.split_rows;
@@ -144,13 +146,15 @@ __device__ __forceinline__ DenseWork dense_work(const DenseParams& p, int pair, 
 }
 
 // One operand of a K-step: 128 rows x 64 elements of K, or the transposed 64 x 128 in two boxes.
-__device__ __forceinline__ void dense_load(bool mn, uint8_t* to, const CUtensorMap* map, uint32_t bar, int row, int k)
+__device__ __forceinline__ void dense_load(bool mn, uint8_t* to, const CUtensorMap* map, uint32_t bar, int row, int k, bool hint,
+                                           uint64_t policy)
 {
+    const int x = mn ? row : k, y = mn ? k : row;
+    if (hint) tma_load_2d_pair_hint(to, map, bar, x, y, policy);
+    else tma_load_2d_pair(to, map, bar, x, y);
     if (mn) {
-        tma_load_2d_pair(to, map, bar, row, k);
-        tma_load_2d_pair(to + kDBoxBytes, map, bar, row + 64, k);
-    } else {
-        tma_load_2d_pair(to, map, bar, k, row);
+        if (hint) tma_load_2d_pair_hint(to + kDBoxBytes, map, bar, x + 64, y, policy);
+        else tma_load_2d_pair(to + kDBoxBytes, map, bar, x + 64, y);
     }
 }
 
@@ -220,12 +224,14 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                 int s = 0;
                 uint32_t parity = 1;                       // of the phase before: a fresh barrier passes
                 bool alive = true;
+                const uint64_t kept = l2_policy_evict_last(), passing = l2_policy_evict_first();
                 for (int j = 0; alive; ++j) {
                     const DenseWork w = dense_work<kStore>(p, cluster_id, n_clusters, j);
                     if (w.q < 0) break;
                     const DenseShape& q = p.q[w.q];
                     const DenseMaps& m = maps.q[w.q];
                     const bool a_mn = kStore && q.a_mn;
+                    const uint64_t pol_a = q.band_m ? kept : passing, pol_b = q.band_m ? passing : kept;
                     const int ya = w.row + static_cast<int>(rank) * kDHalf;
                     const int yb = kGated ? w.tn * q.width : w.tn * 2 * q.width + static_cast<int>(rank) * q.width;
                     for (int k = w.k0; k < w.k1; ++k) {
@@ -237,8 +243,8 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                         const int kk = (k - seg_k * q.seg_k_steps) * kDBlockK;
                         const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
                         mbar_arrive_expect_tx_cluster(full, kDOperandBytes + q.width * (kDBlockK * 2));
-                        dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk);
-                        dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk);
+                        dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk, q.hints, pol_a);
+                        dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk, q.hints, pol_b);
                         if (++s == kDStages) {
                             s = 0;
                             parity ^= 1;

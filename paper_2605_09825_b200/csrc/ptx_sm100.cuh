@@ -338,6 +338,13 @@ __device__ __forceinline__ uint64_t l2_policy_evict_first()
     return pol;
 }
 
+__device__ __forceinline__ uint64_t l2_policy_evict_last()
+{
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
+    return pol;
+}
+
 // 2-D tiled store with an L2 cache hint (streaming outputs should not displace operands).
 __device__ __forceinline__ void tma_store_2d_hint(const void* tmap, const void* smem_src, int32_t x,
                                                   int32_t y, uint64_t policy)
@@ -608,6 +615,18 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const void* tma
         "[%0], [%1, {%3, %4}], [%2];"
         ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar_cluster_addr),
         "r"(x), "r"(y)
+        : "memory");
+}
+
+// The same with an L2 cache hint.
+__device__ __forceinline__ void tma_load_2d_pair_hint(void* smem_dst, const void* tmap, uint32_t bar_cluster_addr,
+                                                      int32_t x, int32_t y, uint64_t policy)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+        "[%0], [%1, {%3, %4}], [%2], %5;"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar_cluster_addr),
+        "r"(x), "r"(y), "l"(policy)
         : "memory");
 }
 
