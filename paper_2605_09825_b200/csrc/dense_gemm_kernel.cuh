@@ -6,7 +6,7 @@
 // tensor cores and as many of the way from L2 into shared memory (64 bytes per cycle and SM): a larger tile would need more
 // tensor memory.  The tensor pipe is busy 93 % of the cycles in the loss's forward product, 87 % in the gated one with both
 // projections kept, 90 % in a backward pass; what it does per second is set by the power cap: 1.63 PFLOP/s for the
-// loss of 8192 tokens by itself, 1.37 to 1.40 pass after pass (a library product: 1.69 and 1.39).
+// loss of 8192 tokens by itself, 1.38 to 1.42 pass after pass (a library product: 1.69 and 1.39).
 //
 // Either operand may be stored along K (rows of A, of B) or along its own rows (the transposed matrix, as the
 // gradients need it): a K-step is then fetched as two boxes of 64 columns x 64 rows, and the shared-memory
@@ -60,7 +60,7 @@ constexpr int kDStageBytes = 32 * 128;             // output staging per epilogu
 
 // Two output boxes per warp, so that one is filled while the other leaves, are worth a stage of operands where tiles are
 // short: the backward pass of 64 tokens (4096 x 14336) takes 147 us with them and 162 without.  The gated forward pass has
-// long ones: 104 us for 333 tokens with six stages, 107 with five and two boxes.
+// long ones: 104 us for 333 tokens with six stages, 107 with five and two boxes (before that size went to another kernel).
 template <int EPI>
 struct DenseSmem {
     static constexpr int kBoxes = EPI == kDenseStore ? 2 : 1;

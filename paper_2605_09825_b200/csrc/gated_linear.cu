@@ -65,9 +65,16 @@ __global__ void __launch_bounds__(kGradThreads) gated_grad_kernel(const GatedGra
     });
 }
 
-// Up to this many tokens the kernel with the weights as rows is taken (4096 x 14336, weights from memory: 9 to 64 tokens
-// 44 us against 54, 128 tokens 49 against 56, 160 51 against 56, 200 57 against 56).
-constexpr int64_t kMostTokensAsColumns = 160;
+// Whether the kernel with the weights as rows takes a forward pass: up to 160 tokens, where it computes for fewer rows than the
+// tile of 256 that the other one computes for in any case, and beyond that where its tiles, which need only be a multiple of 16
+// tokens, hold at most 7/8 of the other's rows and K is long enough for its epilogue.  4096 x 14336, pass after pass: 16 to
+// 64 tokens 42 to 45 us against 54 to 56, 160 tokens 55 and 61, 240 66 and 63, 333 91 and 102, 400 100 and 104, 512 115 and
+// 108, 600 129 and 144, 1100 207 and 225; 1024 x 4096: 600 tokens 21 and 15.5, 2048 x 8192: 43 and 45.
+static bool gated_as_columns(int64_t tokens, int64_t in_features)
+{
+    const int64_t tiles = dense_tiles(tokens, 256), rows = tiles * dense_tiles(dense_tiles(tokens, tiles), 16) * 16;
+    return tokens <= 160 || (in_features >= 2048 && tokens > 256 && rows * 8 <= tiles * 256 * 7);
+}
 
 static int gated_tokens(const mxfp4_gated_desc& d, void* h, int64_t ld_h, void* gate, void* up, int64_t ld_kept, int sm_count,
                         cudaStream_t st)
@@ -185,7 +192,7 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
                                  static_cast<cudaStream_t>(stream), p) == cudaSuccess
                    ? MXFP4_OK : MXFP4_ERR_CUDA;
     }
-    if (d->tokens <= kMostTokensAsColumns)
+    if (gated_as_columns(d->tokens, d->in_features))
         return gated_tokens(*d, h, ld_h, gate, up, ld_kept, dev.sm_count, static_cast<cudaStream_t>(stream));
     DenseProduct c;
     c.M = d->tokens;

@@ -1,4 +1,4 @@
-// The gated projections for some tens to hundreds of tokens, with the weights as the tensor cores' 256 rows and the tokens as
+// The gated projections for tens to some hundreds of tokens, and for numbers that fill tiles of 256 badly, with the weights as the tensor cores' 256 rows and the tokens as
 // their columns: a product of 17 tokens costs a sixteenth of the instructions of one of 256, where the other way round
 // (dense_gemm_kernel.cuh) it costs the same, and both weights are read as fast as memory gives them.
 //
@@ -11,8 +11,9 @@
 // projection hand it over through shared memory; the two that hold the gate form h.  Results are staged as rows of 64
 // features and leave by TMA stores of 16 tokens, which clip at the last token.
 //
-// 4096 x 14336: 9 to 64 tokens 43 to 44 us (235 MB, 5.4 TB/s; 112 tiles are one round and a half of 74 pairs), 128 tokens 49.  With
-// the K-steps of all tiles shared out evenly and a joining kernel it was 42 + 4.5.
+// 4096 x 14336, pass after pass: 9 to 64 tokens 42 to 45 us (235 MB, 5.5 TB/s; 112 tiles are one round and a half of 74 pairs),
+// 128 tokens 51, 333 tokens 91.  With the K-steps of all tiles shared out evenly and a joining kernel a call of 17 tokens
+// took 42 + 4.5 us by itself, one of 333 tokens 92 + 20.
 //
 // Roles per CTA as in the other kernel: warps 0..7 epilogue, 8 TMA producer, 9 MMA issuer (leader CTA only).
 #pragma once
@@ -110,6 +111,8 @@ gated_tokens_kernel(const __grid_constant__ GatedTokensMaps maps, const __grid_c
             uint32_t parity = 1;                       // of the phase before: a fresh barrier passes
             bool alive = true;
             const uint32_t bytes = kTWeightBytes + p.tile_tokens / 2 * 128;
+            // the weights go past the tokens, which every tile reads
+            const uint64_t kept = l2_policy_evict_last(), passing = l2_policy_evict_first();
             for (int tile = cluster_id; alive && tile < p.tiles; tile += n_clusters) {
                 const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n;
                 const int f = tm * kTFeatures + static_cast<int>(rank) * 64;
@@ -122,9 +125,9 @@ gated_tokens_kernel(const __grid_constant__ GatedTokensMaps maps, const __grid_c
                     uint8_t* to = sm.ring + s * p.stage_bytes;
                     const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
                     mbar_arrive_expect_tx_cluster(full, bytes);
-                    tma_load_2d_pair(to, &maps.w[0], full, k * kTBlockK, f);
-                    tma_load_2d_pair(to + kTWeightBytes / 2, &maps.w[1], full, k * kTBlockK, f);
-                    tma_load_2d_pair(to + kTWeightBytes, &maps.x, full, k * kTBlockK, t);
+                    tma_load_2d_pair_hint(to, &maps.w[0], full, k * kTBlockK, f, passing);
+                    tma_load_2d_pair_hint(to + kTWeightBytes / 2, &maps.w[1], full, k * kTBlockK, f, passing);
+                    tma_load_2d_pair_hint(to + kTWeightBytes, &maps.x, full, k * kTBlockK, t, kept);
                     if (++s == p.stages) {
                         s = 0;
                         parity ^= 1;

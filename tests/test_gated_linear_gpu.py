@@ -71,7 +71,7 @@ def check_forward(x, wg, wu, which, h, kept):
         within(kept[1], u, HALF * u.abs() + eu, "up")
 
 
-SIZES = [(1, 8, 8), (1, 4096, 264), (20, 2056, 1000), (300, 2048, 1304), (290, 64, 14336), (170, 1024, 1304), (400, 1536, 9608), (1100, 1024, 2056), (200, 72, 9608), (9, 136, 328), (2, 64, 72), (17, 72, 128), (31, 200, 136), (129, 128, 520), (255, 1032, 264),
+SIZES = [(1, 8, 8), (1, 4096, 264), (20, 2056, 1000), (300, 2048, 1304), (290, 64, 14336), (170, 1024, 1304), (400, 1536, 9608), (1100, 1024, 2056), (1100, 2048, 136), (333, 2056, 72), (200, 72, 9608), (9, 136, 328), (2, 64, 72), (17, 72, 128), (31, 200, 136), (129, 128, 520), (255, 1032, 264),
          (257, 96, 1000), (600, 520, 392), (1030, 64, 16), (5, 16, 20000)]
 
 
