@@ -231,6 +231,9 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                     const DenseShape& q = p.q[w.q];
                     const DenseMaps& m = maps.q[w.q];
                     const bool a_mn = kStore && q.a_mn;
+                    // without the hints where a launch holds two products: they bring nothing there (backward of 4096 tokens
+                    // 1570 us either way), and issuing them costs where K is short (512 tokens: 188 us, 195 with them)
+                    const bool hints = !kStore && q.hints;
                     const uint64_t pol_a = q.band_m ? kept : passing, pol_b = q.band_m ? passing : kept;
                     const int ya = w.row + static_cast<int>(rank) * kDHalf;
                     const int yb = kGated ? w.tn * q.width : w.tn * 2 * q.width + static_cast<int>(rank) * q.width;
@@ -243,8 +246,8 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                         const int kk = (k - seg_k * q.seg_k_steps) * kDBlockK;
                         const uint32_t full = map_to_cta(smem_u32(&sm.full[s]), 0);
                         mbar_arrive_expect_tx_cluster(full, kDOperandBytes + q.width * (kDBlockK * 2));
-                        dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk, q.hints, pol_a);
-                        dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk, q.hints, pol_b);
+                        dense_load(a_mn, sm.a[s], &m.a[w.seg + seg_k], full, ya, kk, hints, pol_a);
+                        dense_load(kStore, sm.b[s], &m.b[kGated ? rank : seg_k], full, yb, kk, hints, pol_b);
                         if (++s == kDStages) {
                             s = 0;
                             parity ^= 1;
