@@ -21,7 +21,7 @@
 namespace mxfp4 {
 
 // dg = dh * u * act'(g), du = dh * act(g), rounded to bf16: they are operands of the tensor cores' products, whose sums
-// over hundreds of them are off by about 2^-9 / sqrt(3) of their value, less than the rounding of a bf16 result.
+// over hundreds of them are off by about 0.0017 of their value (norm), as much as the rounding of a bf16 result.
 // Eight elements per thread and step, bound by memory: 10 bytes per element (4096 x 14336: 97 us, 6.0 TB/s).
 struct GatedGradParams {
     const __nv_bfloat16* dh;

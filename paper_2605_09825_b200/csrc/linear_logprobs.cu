@@ -5,11 +5,12 @@
 // epilogue forms their gradient (bf16, in the workspace), then its product with the piece of the weight, added to the
 // input's gradient in fp32, and with the input, which is the piece of the weight's gradient.
 //
-// Bound by the products: 8192 tokens of 4096 features, vocabulary 128256, forward 5430 us by itself (1.6 PFLOP/s), 6440 pass after
-// pass, where the power cap sustains 1.34 to 1.40; 19 us are the join.  Backward, 4096 tokens: 8540 and 9670 to 10040.
+// Bound by the products: 8192 tokens of 4096 features, vocabulary 128256, forward 5430 to 5700 us by itself (1.5 to 1.6 PFLOP/s),
+// 6060 to 6600 pass after pass, on one device and another: the power cap sustains 1.3 to 1.42; 19 us are the join.  Backward,
+// 4096 tokens: 8320, and 9470 to 9970.
 //
 // The gradient of the logits is rounded to bf16 because it is an operand of the tensor cores' products: sums over
-// hundreds of them are off by about 2^-9 / sqrt(3) of their value, less than the rounding of a bf16 result.
+// hundreds of them are off by about 0.0017 of their value (norm), as much as the rounding of a bf16 result.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
