@@ -655,6 +655,15 @@ int mxfp4_check(void* stream);
 int mxfp4_selftest_wait_timeout(void* stream);
 
 /*
+ * The same in one part of the library, each of which has a status word of its own: 0 the MXFP4 and MXFP8 path (as above),
+ * 1 the 128-block products, 2 the residual norm, 3 the 16-bit product, 4 the gated projections, 5 the embeddings, 6 the log
+ * probabilities, 7 those from an output layer's input, 8 the gradient norm.  mxfp4_check looks at the words of the parts
+ * whose kernels have been launched on the current device by an operator; the kernels of 6 to 8 have no waits, and
+ * only the bounds-checking build looks at theirs.  Any other number: MXFP4_ERR_ENUM.
+ */
+int mxfp4_selftest_unit_timeout(int unit, void* stream);
+
+/*
  * The library can be built with -DMXFP4_BOUNDS (no counterpart in the paper): a debug build that
  * stands in for a memory sanitizer.  Every shared-memory access whose address a kernel computes is
  * then checked against the buffer it belongs to (range and natural alignment); a miss is skipped

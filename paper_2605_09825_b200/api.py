@@ -34,7 +34,7 @@ EXPORTS = (
     "mxfp4_linear_dgrad", "mxfp4_linear_wgrad", "mxfp4_linear_layer_bytes", "mxfp4_linear_forward",
     "mxfp4_linear_backward", "mxfp4_linear_layer_host", "mxfp4_linear_layer_host_drain", "mxfp4_quantize_fp8", "mxfp4_gemm_fp8",
     "mxfp4_linear_pass_workspace_bytes", "mxfp4_linear_pass", "mxfp4_linear_host", "mxfp4_linear_static",
-    "mxfp4_check", "mxfp4_selftest_wait_timeout", "mxfp4_bounds_checked", "mxfp4_selftest_bounds",
+    "mxfp4_check", "mxfp4_selftest_wait_timeout", "mxfp4_selftest_unit_timeout", "mxfp4_bounds_checked", "mxfp4_selftest_bounds",
     "mxfp4_probe_mma_rate",
     "mxfp4_block128_scales_bytes", "mxfp4_quantize_block128", "mxfp4_gemm_block128_workspace_bytes",
     "mxfp4_gemm_block128", "mxfp4_linear_pass_block128_workspace_bytes", "mxfp4_linear_pass_block128",
@@ -172,6 +172,7 @@ def load_library() -> ctypes.CDLL:
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, res
     lib.mxfp4_selftest_wait_timeout.argtypes, lib.mxfp4_selftest_wait_timeout.restype = [vp], ci
+    lib.mxfp4_selftest_unit_timeout.argtypes, lib.mxfp4_selftest_unit_timeout.restype = [ci, vp], ci
     lib.mxfp4_selftest_bounds.argtypes, lib.mxfp4_selftest_bounds.restype = [vp], ci
     lib.mxfp4_bounds_checked.argtypes, lib.mxfp4_bounds_checked.restype = [], ci
     lib.mxfp4_probe_mma_rate.argtypes = [ci, ci, vp, ctypes.POINTER(ctypes.c_double)]
@@ -1141,6 +1142,11 @@ def selftest_bounds() -> None:
 def selftest_wait_timeout() -> None:
     """Enqueue the bounded-wait self-test; the next :func:`check` raises with status -7."""
     _raise(load_library().mxfp4_selftest_wait_timeout(_stream()), "mxfp4_selftest_wait_timeout")
+
+
+def selftest_unit_timeout(unit: int) -> None:
+    """The same in one part of the library (``mxfp4_selftest_unit_timeout``)."""
+    _raise(load_library().mxfp4_selftest_unit_timeout(unit, _stream()), "mxfp4_selftest_unit_timeout")
 
 
 def check() -> None:

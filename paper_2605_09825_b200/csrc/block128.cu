@@ -227,6 +227,7 @@ static Pass128 pass128(int pass, int64_t T, int64_t in_f, int64_t out_f)
 
 // Status word of this translation unit's kernels, cleared when it is set.
 int block128_take_status(int* status) { return take_unit_status(status); }
+int block128_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 }  // namespace mxfp4
 

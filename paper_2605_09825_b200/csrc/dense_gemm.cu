@@ -171,5 +171,6 @@ int dense_round(const float* from, int pieces, int64_t rows, int64_t cols, void*
 
 // Status word of this translation unit's kernels, cleared when it is set.
 int dense_take_status(int* status) { return take_unit_status(status); }
+int dense_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 }  // namespace mxfp4

@@ -556,6 +556,7 @@ static int rows_check(const void* a, int64_t ld_a, const void* b, int64_t ld_b, 
 }
 
 int embedding_take_status(int* status) { return take_unit_status(status); }
+int embedding_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 }  // namespace mxfp4
 

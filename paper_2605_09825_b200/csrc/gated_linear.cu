@@ -133,6 +133,7 @@ static int gated_tokens(const mxfp4_gated_desc& d, void* h, int64_t ld_h, void* 
 }
 
 int gated_linear_take_status(int* status) { return take_unit_status(status); }
+int gated_linear_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 static size_t gated_grad_bytes(int64_t tokens, int64_t features)
 {

@@ -388,6 +388,7 @@ static int norm_overlap(const GradNormCall& c)
 }
 
 int grad_norm_take_status(int* status) { return take_unit_status(status); }
+int grad_norm_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 }  // namespace mxfp4
 

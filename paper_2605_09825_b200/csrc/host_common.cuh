@@ -47,8 +47,9 @@ static inline int current_device()
     return dev;
 }
 
-// Whether this translation unit has been called on a device.  Every entry point asks for device_info() before it
-// launches anything, which sets it; until then the unit's status word cannot be set either.
+// Whether this translation unit has launched a kernel on a device.  launch_kernel_pdl_cluster (tma_host.cuh) notes it, and no
+// other unit than the one whose word is read in any case launches by another route; until then the unit's status word
+// cannot be set either.
 static inline std::atomic<bool>& unit_used(int dev)
 {
     static std::atomic<bool> used[kMaxDevices];
@@ -63,7 +64,6 @@ static inline const DeviceInfo& device_info()
     const int dev = current_device();
     if (dev < 0) return none;
     once.run(dev, [&] {
-        unit_used(dev) = true;
         cudaDeviceProp prop;
         if (cudaGetDeviceProperties(&prop, dev) == cudaSuccess) {
             info[dev].sm_count = prop.multiProcessorCount;
@@ -98,12 +98,34 @@ static inline int device_status_code(const DeviceInfo& dev)
 }
 
 // The status of this translation unit's kernels, cleared if it was set; 0 without a look at the device where the
-// unit has not been called (a look costs a copy of its own, 11 us).
+// unit has launched none (a look costs a copy of its own, 11 us).
 static inline int take_unit_status(int* status)
 {
     const int dev = current_device();
     *status = 0;
     return dev >= 0 && !unit_used(dev) ? 0 : take_device_status(status);
+}
+
+// Self-test of the bounded-wait discipline in this translation unit: one warp waits on a barrier that nothing will ever
+// complete, with a spin limit of a few hundred attempts.  The wait gives up, records the timeout status in the unit's word
+// and the kernel returns normally.
+static __global__ void unit_timeout_kernel()
+{
+    __shared__ uint64_t bar;
+    __shared__ int abort_flag;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        mbar_init(&bar, 1);
+        fence_barrier_init();
+    }
+    __syncthreads();
+    mbar_wait(&bar, 0, &abort_flag, 256u);
+}
+
+static inline int unit_selftest(cudaStream_t st)
+{
+    unit_timeout_kernel<<<1, 32, 0, st>>>();
+    return cudaGetLastError() == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
 // The same of the other translation units (each has its own status word).
@@ -115,5 +137,13 @@ int gated_linear_take_status(int* status);
 int linear_logprobs_take_status(int* status);
 int embedding_take_status(int* status);
 int grad_norm_take_status(int* status);
+int block128_selftest(cudaStream_t st);
+int residual_norm_selftest(cudaStream_t st);
+int logprobs_selftest(cudaStream_t st);
+int dense_selftest(cudaStream_t st);
+int gated_linear_selftest(cudaStream_t st);
+int linear_logprobs_selftest(cudaStream_t st);
+int embedding_selftest(cudaStream_t st);
+int grad_norm_selftest(cudaStream_t st);
 
 }  // namespace mxfp4

@@ -226,22 +226,6 @@ static int launch_quantize_dual(const QuantDualJob& job, int grid, cudaStream_t 
     return launch_quantize_dual_as<HMODE, SR, false>(job, grid, stream);
 }
 
-// Self-test of the bounded-wait discipline: one warp waits on a barrier that nothing will ever
-// complete, with a spin limit of a few hundred attempts.  The wait gives up, records the
-// timeout status and the kernel returns normally.
-__global__ void selftest_wait_timeout_kernel()
-{
-    __shared__ uint64_t bar;
-    __shared__ int abort_flag;
-    if (threadIdx.x == 0) {
-        abort_flag = 0;
-        mbar_init(&bar, 1);
-        fence_barrier_init();
-    }
-    __syncthreads();
-    mbar_wait(&bar, 0, &abort_flag, 256u);
-}
-
 // Self-test of the bounds discipline: the checker is handed an address one element past a
 // shared array.  It refuses (the store never happens) and records the status.
 __global__ void selftest_bounds_kernel()
@@ -915,11 +899,17 @@ int mxfp4_linear_static(int pass, const void* a, const void* b, void* out, int64
 
 int mxfp4_selftest_wait_timeout(void* stream)
 {
-    const DeviceInfo& dev = device_info();
-    if (!dev.ok) return MXFP4_ERR_CUDA;
-    if (dev.cc_major != 10) return MXFP4_ERR_DEVICE;
-    selftest_wait_timeout_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>();
-    return cudaGetLastError() == cudaSuccess ? MXFP4_OK : MXFP4_ERR_CUDA;
+    return mxfp4_selftest_unit_timeout(0, stream);
+}
+
+int mxfp4_selftest_unit_timeout(int unit, void* stream)
+{
+    static int (*const tests[])(cudaStream_t) = {unit_selftest, block128_selftest, residual_norm_selftest, dense_selftest,
+                                                 gated_linear_selftest, embedding_selftest, logprobs_selftest,
+                                                 linear_logprobs_selftest, grad_norm_selftest};
+    if (unit < 0 || unit >= static_cast<int>(sizeof(tests) / sizeof(tests[0]))) return MXFP4_ERR_ENUM;
+    const int rc = device_status_code(device_info());
+    return rc != MXFP4_OK ? rc : tests[unit](static_cast<cudaStream_t>(stream));
 }
 
 int mxfp4_probe_mma_rate(int iterations, int random_operands, void* stream, double* flops)

@@ -113,6 +113,7 @@ static int loss_check(const void* x, int64_t ld_x, const void* w, int64_t ld_w, 
 }
 
 int linear_logprobs_take_status(int* status) { return take_unit_status(status); }
+int linear_logprobs_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 }  // namespace mxfp4
 

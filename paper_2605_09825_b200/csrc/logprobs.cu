@@ -833,6 +833,7 @@ static int logprobs_splits(int64_t tokens, int64_t vocab)
 
 // Status word of this translation unit's kernels, cleared when it is set.
 int logprobs_take_status(int* status) { return take_unit_status(status); }
+int logprobs_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 static int logprobs_shape_ok(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld, float scale)
 {

@@ -772,6 +772,7 @@ static int norm_params(const mxfp4_norm_desc* n, NormParams* p)
 
 // Status word of this translation unit's kernels, cleared when it is set.
 int residual_norm_take_status(int* status) { return take_unit_status(status); }
+int residual_norm_selftest(cudaStream_t st) { return unit_selftest(st); }
 
 // A [tokens x width] output or gradient: leading dimension and alignment.
 static int norm_matrix_ok(const void* t, int64_t ld, int64_t width)

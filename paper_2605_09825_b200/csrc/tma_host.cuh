@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "host_common.cuh"
+
 namespace mxfp4 {
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
@@ -77,10 +79,13 @@ inline bool pdl_enabled()
 }
 
 // `cluster` > 1: CTAs come in clusters of that many (for kernels without a compile-time cluster size).
+// Static, as unit_used is: an instantiation that two units shared would note one unit's launches for the other.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_kernel_pdl_cluster(void (*kernel)(KArgs...), int grid, int block, size_t smem, int cluster,
+static inline cudaError_t launch_kernel_pdl_cluster(void (*kernel)(KArgs...), int grid, int block, size_t smem, int cluster,
                                              cudaStream_t stream, Args&&... args)
 {
+    const int dev = current_device();
+    if (dev >= 0 && !unit_used(dev)) unit_used(dev) = true;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(static_cast<unsigned>(block), 1, 1);
@@ -104,7 +109,7 @@ inline cudaError_t launch_kernel_pdl_cluster(void (*kernel)(KArgs...), int grid,
 }
 
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_kernel_pdl(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t stream,
+static inline cudaError_t launch_kernel_pdl(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t stream,
                                      Args&&... args)
 {
     return launch_kernel_pdl_cluster(kernel, grid, block, smem, 1, stream, static_cast<Args&&>(args)...);
