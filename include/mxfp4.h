@@ -579,7 +579,8 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, i
  *   d_logp, d_lse fp32 [tokens], one of them may be NULL (zero; targets may then be NULL with d_logp);
  *   dx bf16 [tokens x in_features]; dw (dw_dtype, MXFP4_OUT_*) [vocab x in_features]; either may be NULL: not wanted.
  *   A position whose two gradients are 0 adds nothing, whatever its z; its x must be finite all the same, since dW
- *   sums 0 * x.
+ *   sums 0 * x.  With d_logp a target >= vocab makes its position's dx NaN, whatever d_logp is there, and with it dW;
+ *   without d_logp targets are not looked at.
  * workspace: mxfp4_linear_logprobs_workspace_bytes(..., backward 0 / 1) bytes, 16-byte aligned: forward 131 MB at most at a
  *   vocabulary of 128256; backward the gradients of 2^27 / tokens logits per token (at least 8192), and dx in fp32 where
  *   the vocabulary takes more than one piece.

@@ -525,7 +525,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                 const float lse = row_ok ? p.x.lse[row] : 0.0f;
                 float gl = row_ok && p.x.d_logp && target >= 0 ? p.x.d_logp[row] : 0.0f;
                 const float gn = row_ok && p.x.d_lse ? p.x.d_lse[row] : 0.0f;
-                if (target >= p.x.vocab) gl = NAN;
+                if (p.x.d_logp && target >= p.x.vocab) gl = NAN;
                 const bool zero = (gl == 0.0f && gn == 0.0f);
                 const float coef = p.x.scale * (gn - gl);
 #pragma unroll 1
