@@ -573,14 +573,19 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, i
  *   logp (with targets; both may be NULL), lse   fp32 [tokens]
  * A NaN or +infinity among a row's z makes its lse NaN.
  *
- * Backward: dz = scale * (d_logp * (delta(target) - p) + d_lse * p),  p = exp(z - lse), from the forward's lse (or that of
- *   a vocabulary split over devices), rounded to bf16 (the products' operand);
+ * Backward: dz = scale * (d_logp * (delta(target) - p) + d_lse * p),  p = exp(z - lse), from the forward's lse, rounded to
+ *   bf16 (the products' operand);
  *     dx = dz W,   dW = dz^T x
  *   d_logp, d_lse fp32 [tokens], one of them may be NULL (zero; targets may then be NULL with d_logp);
  *   dx bf16 [tokens x in_features]; dw (dw_dtype, MXFP4_OUT_*) [vocab x in_features]; either may be NULL: not wanted.
  *   A position whose two gradients are 0 adds nothing, whatever its z; its x must be finite all the same, since dW
  *   sums 0 * x.  With d_logp a target >= vocab makes its position's dx NaN, whatever d_logp is there, and with it dW;
  *   without d_logp targets are not looked at.
+ * A vocabulary split over devices: a share is called with its rows of w and the targets that lie in it, counted from its first
+ *   row, -1 for the others.  lse = log sum exp of the shares' lse; a target's logp is its share's logp + that share's lse - lse.
+ *   Backward takes the lse of the whole, and for d_lse the value d_lse - d_logp at positions whose target lies in
+ *   another share (such a target's -d_logp * p is still due in this one), d_lse elsewhere; dW is the share's own, dx
+ *   the sum over the shares.
  * workspace: mxfp4_linear_logprobs_workspace_bytes(..., backward 0 / 1) bytes, 16-byte aligned: forward 131 MB at most at a
  *   vocabulary of 128256; backward the gradients of 2^27 / tokens logits per token (at least 8192), and dx in fp32 where
  *   the vocabulary takes more than one piece.

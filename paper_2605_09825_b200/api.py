@@ -982,7 +982,8 @@ def linear_logprobs_forward(x, w, targets=None, scale: float = 1.0, workspace=No
 def linear_logprobs_backward(x, w, targets, lse, d_logp=None, d_lse=None, scale: float = 1.0, dw_dtype: int = OUT_BF16,
                              want_dx: bool = True, want_dw: bool = True, dx=None, dw=None, workspace=None):
     """``mxfp4_linear_logprobs_backward``: ``(dx, dw)`` from the forward's ``lse`` and the gradients of logp and lse (fp32
-    [tokens], None: zero); dx bf16, dw of type ``dw_dtype``.  What is not wanted is None."""
+    [tokens], None: zero); dx bf16, dw of type ``dw_dtype``.  What is not wanted is None.  The header says what a share of a
+    vocabulary that is split over devices is given."""
     args = _loss_operands(x, w, targets)
     (T, D, V), dev = args[4:7], x.device
     row = lambda t, name: _expect(t, name, torch.float32, T) if t is not None else None
