@@ -574,7 +574,8 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, i
  * A NaN or +infinity among a row's z makes its lse NaN.
  *
  * Backward: dz = scale * (d_logp * (delta(target) - p) + d_lse * p),  p = exp(z - lse), from the forward's lse, rounded to
- *   bf16 (the products' operand);
+ *   bf16 (the products' operand) but for scale and a factor that all positions have in common, by which the sums are
+ *   multiplied in fp32 (a mean's gradient is not rounded);
  *     dx = dz W,   dW = dz^T x
  *   d_logp, d_lse fp32 [tokens], one of them may be NULL (zero; targets may then be NULL with d_logp);
  *   dx bf16 [tokens x in_features]; dw (dw_dtype, MXFP4_OUT_*) [vocab x in_features]; either may be NULL: not wanted.

@@ -94,17 +94,18 @@ static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool g
     return ok ? MXFP4_OK : MXFP4_ERR_CUDA;
 }
 
-int dense_store(const DenseProduct* products, int n, int sm_count, cudaStream_t st)
+int dense_store(const DenseProduct* products, int n, const DenseExtra* extra, int sm_count, cudaStream_t st)
 {
     DenseMaps2 maps;
     DenseParams p;
     memset(&maps, 0, sizeof(maps));
     memset(&p, 0, sizeof(p));
+    if (extra) p.x = *extra;
     for (int i = 0; i < n; ++i) {
         const int rc = prepare(p.q[i], maps.q[i], products[i], false, products[i].stack_m ? 2 : 1, products[i].N);
         if (rc != MXFP4_OK) return rc;
     }
-    return launch<kDenseStore>(maps, p, sm_count, st);
+    return extra ? launch<kDenseScaled>(maps, p, sm_count, st) : launch<kDenseStore>(maps, p, sm_count, st);
 }
 
 int dense_fused(DenseEpilogue epilogue, const DenseProduct& product, const DenseExtra& extra, int sm_count, cudaStream_t st)

@@ -7,7 +7,7 @@
 
 namespace mxfp4 {
 
-enum DenseEpilogue { kDenseStore, kDenseGated, kDensePartials, kDenseLogitGrad };
+enum DenseEpilogue { kDenseStore, kDenseScaled, kDenseGated, kDensePartials, kDenseLogitGrad };
 enum DenseOut { kDenseBf16, kDenseF32, kDenseAddF32 };
 
 // What one operand's panel may take of L2.  The order decides how much is read from memory, which costs energy, and the power
@@ -45,6 +45,7 @@ struct DenseExtra {
     // log probabilities: columns col_base .. col_base + N of `vocab`
     float scale;
     int32_t ld_grad;             // columns of the gradient's buffer, those past N set to 0
+    int32_t rows;                // gradient of the logits, and products of it: positions (see dense_common)
     int64_t vocab, col_base;
     const int64_t* targets;
     const float* lse;
@@ -78,7 +79,8 @@ struct DenseProduct {
 };
 
 // One launch of one or two products with plain outputs (b stored along its rows), or of one with another epilogue.
-int dense_store(const DenseProduct* products, int n, int sm_count, cudaStream_t st);
+// `extra`: of the gradient of the logits that the products are of; NULL for others.
+int dense_store(const DenseProduct* products, int n, const DenseExtra* extra, int sm_count, cudaStream_t st);
 int dense_fused(DenseEpilogue epilogue, const DenseProduct& product, const DenseExtra& extra, int sm_count, cudaStream_t st);
 
 // The sum of `pieces` products of splits as dense_store leaves them, to bf16; cols a multiple of 8.

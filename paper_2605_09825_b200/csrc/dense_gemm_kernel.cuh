@@ -20,13 +20,15 @@
 // Epilogues:
 //   kDenseStore             the sums, rounded or not, or added to the fp32 output by the copy engine: one addition per element
 //                           and launch, so results do not depend on scheduling
+//   kDenseScaled            the same of sums multiplied by a common factor (dense_common)
 //   kDenseGated             columns 0..127 of a tile are a gate's, 128..255 the other projection's of the same features
 //                           (the pair's first CTA loads the rows of one weight, the second those of the other): act(g) * u,
 //                           and g and u on request
 //   kDensePartials          maximum and sum of exponentials of each row's 128 columns, and the target's value.  The normaliser
 //                           goes by a row's largest logits, and truncating additions make these too small, all alike: sums of
 //                           4096 products left lse 1.9e-6 of itself off, sums of 1024, added in registers, 0.4e-6, at no cost
-//   kDenseLogitGrad         gradient of the log probabilities with respect to the logits, rounded to bf16
+//   kDenseLogitGrad         gradient of the log probabilities with respect to the logits, without the factor that the
+//                           positions have in common, rounded to bf16
 //
 // Roles per CTA (384 threads): warps 0..7 epilogue (32 rows x 128 columns each), warp 8 TMA producer, warp 9 MMA
 // issuer (leader CTA only).  Barrier ownership: full and tmem_empty live in the leader, empty and tmem_full are signalled
@@ -63,7 +65,7 @@ constexpr int kDStageBytes = 32 * 128;             // output staging per epilogu
 // long ones: 104 us for 333 tokens with six stages, 107 with five and two boxes (before that size went to another kernel).
 template <int EPI>
 struct DenseSmem {
-    static constexpr int kBoxes = EPI == kDenseStore ? 2 : 1;
+    static constexpr int kBoxes = EPI == kDenseStore || EPI == kDenseScaled ? 2 : 1;
     static constexpr int kDStages = 7 - kBoxes;
     alignas(1024) uint8_t a[kDStages][kDOperandBytes];
     alignas(1024) uint8_t b[kDStages][kDOperandBytes];
@@ -72,6 +74,7 @@ struct DenseSmem {
     uint64_t empty[kDStages];                      // both, via multicast commit
     uint64_t tmem_full[2];                         // both, via multicast commit
     uint64_t tmem_empty[2];                        // leader's copy is the live one
+    float2 common[kDEpiWarps];                     // of dense_common
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -173,7 +176,43 @@ __device__ __forceinline__ float dense_exp(float x)
     return r;
 }
 
-// kDenseStore takes B along its own rows and two products; the other epilogues take both operands along K and one product.
+// The factor that the gradients of all positions have in common, by which those of the logits are divided before they are
+// rounded, and sums of them multiplied: the largest magnitude of d_logp at a target, so that the gradient of a mean is 1 or -1
+// everywhere, unless d_lse is 2^60 times as large.  What is not finite is passed by.  The epilogue's warps find it while the
+// first tile's products run; rounding the common factor with the rest would leave every result off by as much, up to
+// 2^-8, all to the same side.  The multiplications show where tiles are one step long (loss backward of 64 tokens 617 -> 637 us,
+// 512 tokens and more the same), so other products have an epilogue without them.
+__device__ __forceinline__ float dense_common(const DenseExtra& x, float2 (&part)[kDEpiWarps], int warp, int lane)
+{
+    float2 most = make_float2(0.0f, 0.0f);
+    auto take = [](float& m, float v) {
+        v = fabsf(v);
+        if (v <= 3.402823466e38f) m = fmaxf(m, v);
+    };
+#pragma unroll 8
+    for (int64_t i = warp * 32 + lane; i < x.rows; i += kDEpiWarps * 32) {
+        const int64_t target = x.d_logp ? x.targets[i] : -1;
+        const float gl = x.d_logp ? x.d_logp[i] : 0.0f, gn = x.d_lse ? x.d_lse[i] : 0.0f;
+        if (target >= 0) take(most.x, gl);
+        take(most.y, gn);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        most.x = fmaxf(most.x, __shfl_xor_sync(0xffffffffu, most.x, d));
+        most.y = fmaxf(most.y, __shfl_xor_sync(0xffffffffu, most.y, d));
+    }
+    if (lane == 0) smem_put(part, warp, most);
+    bar_sync(1, kDEpiWarps * 32);
+    for (int w = 0; w < kDEpiWarps; ++w) {
+        const float2 v = smem_get(part, w);
+        most = make_float2(fmaxf(most.x, v.x), fmaxf(most.y, v.y));
+    }
+    const float common = fmaxf(most.x, most.y * 0x1p-60f);
+    return common > 0.0f ? common : 1.0f;
+}
+
+// kDenseStore and kDenseScaled take B along its own rows and two products; the other epilogues take both operands along K
+// and one product.
 template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDThreads, 1)
 dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant__ DenseParams p)
@@ -186,7 +225,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1;
     const int n_clusters = gridDim.x >> 1;
-    constexpr bool kStore = EPI == kDenseStore;
+    constexpr bool kStore = EPI == kDenseStore || EPI == kDenseScaled;
     constexpr bool kGated = EPI == kDenseGated;
     // K-steps that are added up in tensor memory, whose additions truncate; longer sums go on in registers (0: any length)
     constexpr int kChain = EPI == kDensePartials ? kDChain : 0;
@@ -356,6 +395,9 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
             }
             if (++box == kBoxes) box = 0;
         };
+        float common = 1.0f;
+        if constexpr (EPI == kDenseScaled || EPI == kDenseLogitGrad) common = dense_common(p.x, sm.common, warp, lane);
+        const float2 alpha = pair(p.x.scale * common);           // kDenseScaled: of all sums
         int b = 0;
         uint32_t parity = 0;
         for (int j = 0;; ++j) {
@@ -451,6 +493,14 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                     const int col = col0 + c * 32;
                     if (col < q.N) {
                         read(half * kDHalf + c * 32);
+                        if constexpr (EPI == kDenseScaled) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const float2 v = __fmul2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), alpha);
+                                r[i] = __float_as_uint(v.x);
+                                r[i + 1] = __float_as_uint(v.y);
+                            }
+                        }
                         if (k32 || (c & 1) == 0) stage_wait();
                         if (k32) {
 #pragma unroll
@@ -524,10 +574,12 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                 const bool any_here = __any_sync(0xffffffffu, at >= 0);
                 const float lse = row_ok ? p.x.lse[row] : 0.0f;
                 float gl = row_ok && p.x.d_logp && target >= 0 ? p.x.d_logp[row] : 0.0f;
-                const float gn = row_ok && p.x.d_lse ? p.x.d_lse[row] : 0.0f;
+                float gn = row_ok && p.x.d_lse ? p.x.d_lse[row] : 0.0f;
                 if (p.x.d_logp && target >= p.x.vocab) gl = NAN;
                 const bool zero = (gl == 0.0f && gn == 0.0f);
-                const float coef = p.x.scale * (gn - gl);
+                gl = __fdiv_rn(gl, common);
+                gn = __fdiv_rn(gn, common);
+                const float coef = gn - gl;
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
                     const int col = col0 + c * 32;
@@ -543,7 +595,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps2 maps, const __grid_constant
                         if (any_here) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (c * 32 + i == at) z[i] += p.x.scale * gl;
+                                if (c * 32 + i == at) z[i] += gl;
                         }
 #pragma unroll
                         for (int i = 0; i < 4; ++i)

@@ -293,7 +293,7 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64
         w.out[0] = {dw_gate, ld_dw};
         w.out[1] = {dw_up, ld_dw};
     }
-    if ((rc = dense_store(c, n, dev.sm_count, st)) != MXFP4_OK || !dx || splits == 1) return rc;
+    if ((rc = dense_store(c, n, nullptr, dev.sm_count, st)) != MXFP4_OK || !dx || splits == 1) return rc;
     return dense_round(sums, splits, d->tokens, d->in_features, dx, ld_dx, dev.sm_count, st);
 }
 

@@ -10,7 +10,9 @@
 // 4096 tokens: 8320, and 9470 to 9970.
 //
 // The gradient of the logits is rounded to bf16 because it is an operand of the tensor cores' products: sums over
-// hundreds of them are off by about 0.0017 of their value (norm), as much as the rounding of a bf16 result.
+// hundreds of them are off by about 0.0017 of their value (norm), as much as the rounding of a bf16 result.  What the
+// positions' gradients have in common is not rounded but multiplied into the sums (dense_common): that of a mean over 255
+// positions, 1/255, would be 0.0039 off, and all of dx and dW with it.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -230,6 +232,7 @@ int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, i
         e.d_logp = d_logp;
         e.d_lse = d_lse;
         e.ld_grad = static_cast<int32_t>(round_up(cols, 8));
+        e.rows = static_cast<int32_t>(tokens);
         if ((rc = dense_fused(kDenseLogitGrad, c[0], e, dev.sm_count, st)) != MXFP4_OK) return rc;
         int n = 0;
         if (dx) {
@@ -255,7 +258,7 @@ int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, i
             q.b[0] = {x, ld_x};
             q.out[0] = {static_cast<uint8_t*>(dw) + v * ld_dw * (dw_dtype == MXFP4_OUT_FP32 ? 4 : 2), ld_dw};
         }
-        if ((rc = dense_store(c, n, dev.sm_count, st)) != MXFP4_OK) return rc;
+        if ((rc = dense_store(c, n, &e, dev.sm_count, st)) != MXFP4_OK) return rc;
     }
     return dx && !direct ? dense_round(sums, splits, tokens, in_features, dx, ld_dx, dev.sm_count, st) : MXFP4_OK;
 }
