@@ -1,5 +1,6 @@
 // Activations of a gate and their derivatives, in fp32.  Sigmoid and tanh come from the exponential of the
-// hardware (2 units in the last place and one division): far below the 2^-9 of a bf16 result.
+// hardware (2 + 1.17 |x| units in the last place, and |x| is at most 103 where a result is not 0) and one division: below
+// 2^-16 of a value, far below the 2^-9 of a bf16 result.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -11,10 +12,13 @@
 
 namespace mxfp4 {
 
-__device__ __forceinline__ float exp_neg(float x) { return __expf(-x); }
-
-// 1 / (1 + exp(-x)).  The fast quotient is 0 for a divisor above 2^126: the result is below 2^-126 there.
-__device__ __forceinline__ float logistic(float x) { return __fdividef(1.0f, 1.0f + exp_neg(x)); }
+// 1 / (1 + exp(-x)), from e = exp(-|x|): e / (1 + e) for a negative x, so that the exponential never overflows and results
+// below 2^-126 are not lost (times x, or the other projection, they are normal numbers).
+__device__ __forceinline__ float logistic(float x)
+{
+    const float e = __expf(-fabsf(x)), r = __fdividef(1.0f, 1.0f + e);
+    return x < 0.0f ? e * r : r;
+}
 
 constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
