@@ -42,8 +42,9 @@ template <int ACT>
 __device__ __forceinline__ float2 act_both(float g)
 {
     if constexpr (ACT == MXFP4_GATE_SIGMOID) {
-        const float s = logistic(g);
-        return make_float2(s, s * (1.0f - s));
+        // s (1 - s) = e / (1 + e)^2: 1 - s itself would have lost its bits from g = 10 on
+        const float e = __expf(-fabsf(g)), r = __fdividef(1.0f, 1.0f + e);
+        return make_float2(g < 0.0f ? e * r : r, e * r * r);
     }
     if constexpr (ACT == MXFP4_GATE_SILU) {
         const float s = logistic(g);
