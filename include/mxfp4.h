@@ -531,7 +531,8 @@ int mxfp4_logprobs_backward(const void* logits, int dtype, int64_t tokens, int64
  *   w_gate, w_up    bf16 [features x in_features], ld_gate, ld_up (two halves of one matrix are two such pointers)
  *   act             MXFP4_GATE_LINEAR, _SIGMOID, _SILU, _GELU (x * normal distribution function), _GELU_TANH (its usual
  *                   approximation by tanh), _RELU
- * in_features and features multiples of 8; matrices 16-byte aligned with leading dimensions that are multiples of 8;
+ * in_features and features multiples of 8, in_features at most 2^30 - 64 (backward: tokens too, features 2^29 - 64);
+ * matrices 16-byte aligned with leading dimensions that are multiples of 8;
  * nothing an output overlaps may be read.  The struct is a HOST struct of DEVICE pointers.
  *
  * Forward: h bf16 [tokens x features], ld_h; gate and up (both or neither NULL): g and u rounded to bf16, [tokens x
@@ -566,8 +567,8 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, i
  * Log probabilities of given tokens straight from an output layer's input and weight (softmax cross entropy), in
  * pieces of the vocabulary: the logits are never stored.
  *     z = scale * x W^T,   lse = log sum exp z,   logp = z[target] - lse
- *   x        bf16 [tokens x in_features], ld_x;  w bf16 [vocab x in_features], ld_w; in_features a multiple of 8,
- *            any vocab; 16-byte aligned, leading dimensions multiples of 8
+ *   x        bf16 [tokens x in_features], ld_x;  w bf16 [vocab x in_features], ld_w; in_features a multiple of 8, at most
+ *            2^30 - 64 (backward: tokens too), any vocab; 16-byte aligned, leading dimensions multiples of 8
  *   targets  int64 [tokens], as in mxfp4_logprobs_forward: negative: none (logp 0, no gradient through it); >= vocab: NaN
  *   scale    finite, > 0
  *   logp (with targets; both may be NULL), lse   fp32 [tokens]

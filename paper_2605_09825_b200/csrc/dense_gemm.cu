@@ -58,7 +58,7 @@ static int prepare(DenseShape& q, DenseMaps& maps, const DenseProduct& c, bool g
     const int64_t seg_m = dense_tiles(c.M, kDTile), seg_k = dense_tiles(c.K, kDBlockK);
     const int64_t tiles_n = dense_tiles(c.N, gated ? width : 2 * width);
     const int64_t tiles_m = seg_m * (c.stack_m ? 2 : 1), k_steps = seg_k * (c.stack_k ? 2 : 1);
-    if (tiles_m * tiles_n * c.splits > 0x1FFFFFFF || k_steps > 0x3FFFFFFF / kDBlockK) return MXFP4_ERR_SHAPE;
+    if (tiles_m * tiles_n * c.splits > 0x1FFFFFFF || k_steps > kDenseMaxK / kDBlockK) return MXFP4_ERR_SHAPE;
     if (c.splits > 1 && dense_split_rows(c.M) * c.splits > 0x7FFFFFFF) return MXFP4_ERR_SHAPE;
     q.M = static_cast<int32_t>(c.M);
     q.N = static_cast<int32_t>(c.N);

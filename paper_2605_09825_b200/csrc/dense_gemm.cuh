@@ -16,6 +16,7 @@ enum DenseOut { kDenseBf16, kDenseF32, kDenseAddF32 };
 // and 68 MB: 6400, 6330, 6340 and 6520 where 32 took 6220.
 constexpr int64_t kDensePanelBytes = int64_t{32} << 20;
 constexpr int64_t kDenseMaxDim = 0x7FFFFF00;
+constexpr int64_t kDenseMaxK = (int64_t{1} << 30) - 64;      // of all segments: positions along K, and steps past them, fit 32 bits
 constexpr int kDensePairs = 74;  // work is shared out for the pairs of CTAs of this many SMs, whatever the device has
 
 // Sizes of one product as the kernel needs them.

@@ -140,6 +140,12 @@ static size_t gated_grad_bytes(int64_t tokens, int64_t features)
     return round_up(static_cast<size_t>(tokens) * features * 2, 256);
 }
 
+// Whether the backward pass takes these sizes: sums go over the features of both projections (dx) and over the tokens (dW).
+static bool gated_backward_takes(int64_t tokens, int64_t in_features, int64_t features)
+{
+    return tokens <= kDenseMaxK && in_features <= kDenseMaxK && features <= kDenseMaxK / 2 / 64 * 64;
+}
+
 // Sizes, leading dimensions and alignment of what both directions read.
 static int gated_check(const mxfp4_gated_desc* d)
 {
@@ -147,7 +153,7 @@ static int gated_check(const mxfp4_gated_desc* d)
     if (d->act < MXFP4_GATE_LINEAR || d->act > MXFP4_GATE_RELU) return MXFP4_ERR_ENUM;
     if (d->tokens <= 0 || d->in_features <= 0 || d->features <= 0 || d->in_features % 8 != 0 || d->features % 8 != 0)
         return MXFP4_ERR_SHAPE;
-    if (d->tokens > kDenseMaxDim || d->in_features > kDenseMaxDim || d->features > kDenseMaxDim) return MXFP4_ERR_SHAPE;
+    if (d->tokens > kDenseMaxDim || d->in_features > kDenseMaxK || d->features > kDenseMaxDim) return MXFP4_ERR_SHAPE;
     if (d->ld_x < d->in_features || d->ld_gate < d->in_features || d->ld_up < d->in_features) return MXFP4_ERR_SHAPE;
     if (!aligned16(d->x) || !aligned16(d->w_gate) || !aligned16(d->w_up) || d->ld_x % 8 != 0 || d->ld_gate % 8 != 0 ||
         d->ld_up % 8 != 0)
@@ -218,7 +224,7 @@ int mxfp4_gated_linear_forward(const mxfp4_gated_desc* d, void* h, int64_t ld_h,
 size_t mxfp4_gated_linear_workspace_bytes(int64_t tokens, int64_t in_features, int64_t features)
 {
     if (tokens <= 0 || in_features <= 0 || features <= 0 || in_features % 8 != 0 || features % 8 != 0 ||
-        tokens > kDenseMaxDim || in_features > kDenseMaxDim || features > kDenseMaxDim)
+        !gated_backward_takes(tokens, in_features, features))
         return 0;
     const int splits = dense_splits(tokens, in_features, 2 * features);
     return 2 * gated_grad_bytes(tokens, features) +
@@ -233,6 +239,7 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* d, const void* dh, int64
     if (rc != MXFP4_OK) return rc;
     if (!dh || !gate || !up || (dw_gate == nullptr) != (dw_up == nullptr) || (!dx && !dw_gate)) return MXFP4_ERR_NULL;
     if (dw_dtype != MXFP4_OUT_BF16 && dw_dtype != MXFP4_OUT_FP32) return MXFP4_ERR_ENUM;
+    if (!gated_backward_takes(d->tokens, d->in_features, d->features)) return MXFP4_ERR_SHAPE;
     if (ld_dh < d->features || ld_kept < d->features || (dx && ld_dx < d->in_features) || (dw_gate && ld_dw < d->in_features))
         return MXFP4_ERR_SHAPE;
     if (!aligned16(dh) || !aligned16(gate) || !aligned16(up) || ld_dh % 8 != 0 || ld_kept % 8 != 0 ||

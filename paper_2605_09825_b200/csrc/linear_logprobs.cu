@@ -107,7 +107,7 @@ static int loss_check(const void* x, int64_t ld_x, const void* w, int64_t ld_w, 
     if (!x || !w) return MXFP4_ERR_NULL;
     if (!(scale > 0.0f) || isinf(scale)) return MXFP4_ERR_ENUM;
     if (tokens <= 0 || in_features <= 0 || vocab <= 0 || in_features % 8 != 0 || tokens > kDenseMaxDim ||
-        in_features > kDenseMaxDim || vocab > kDenseMaxDim)
+        in_features > kDenseMaxK || vocab > kDenseMaxDim)
         return MXFP4_ERR_SHAPE;
     if (ld_x < in_features || ld_w < in_features) return MXFP4_ERR_SHAPE;
     if (!aligned16(x) || !aligned16(w) || ld_x % 8 != 0 || ld_w % 8 != 0) return MXFP4_ERR_ALIGN;
@@ -125,8 +125,8 @@ extern "C" {
 
 size_t mxfp4_linear_logprobs_workspace_bytes(int64_t tokens, int64_t in_features, int64_t vocab, int backward)
 {
-    if (tokens <= 0 || in_features <= 0 || vocab <= 0 || in_features % 8 != 0 || tokens > kDenseMaxDim ||
-        in_features > kDenseMaxDim || vocab > kDenseMaxDim)
+    if (tokens <= 0 || in_features <= 0 || vocab <= 0 || in_features % 8 != 0 || in_features > kDenseMaxK ||
+        tokens > (backward ? kDenseMaxK : kDenseMaxDim) || vocab > kDenseMaxDim)      // dW sums over the tokens
         return 0;
     if (backward) {
         const int64_t piece = loss_piece(tokens, vocab);
@@ -196,6 +196,7 @@ int mxfp4_linear_logprobs_backward(const void* x, int64_t ld_x, const void* w, i
     if (rc != MXFP4_OK) return rc;
     if (!lse || (!d_logp && !d_lse) || (d_logp && !targets) || (!dx && !dw)) return MXFP4_ERR_NULL;
     if (dw_dtype != MXFP4_OUT_BF16 && dw_dtype != MXFP4_OUT_FP32) return MXFP4_ERR_ENUM;
+    if (tokens > kDenseMaxK) return MXFP4_ERR_SHAPE;
     if ((dx && ld_dx < in_features) || (dw && ld_dw < in_features)) return MXFP4_ERR_SHAPE;
     if ((dx && (!aligned16(dx) || ld_dx % 8 != 0)) || (dw && (!aligned16(dw) || ld_dw % 8 != 0))) return MXFP4_ERR_ALIGN;
     const size_t need = mxfp4_linear_logprobs_workspace_bytes(tokens, in_features, vocab, 1);
