@@ -1079,6 +1079,7 @@ def _norm_buffers(count: int, lib, device, workspace) -> tuple:
     if workspace is None:
         both = torch.empty(need // 4 + 4, dtype=torch.float32, device=device)
         return both[need // 4], both.data_ptr(), need, both
+    _on_current_device(workspace)
     return torch.empty((), dtype=torch.float32, device=device), _dev_ptr(workspace), workspace.numel(), workspace
 
 
