@@ -48,13 +48,14 @@ def make_weights(hidden: int, vocab: int, seed: int = 0, device="cuda", inner: i
 
 
 def train_step(w: dict, ids: torch.Tensor, targets: torch.Tensor, entropy_weight: float = 0.0):
-    """``(loss, gradients)`` for int64 ``ids`` and ``targets`` [tokens] (negative targets count for nothing);
+    """``(loss, gradients)`` for ``ids`` and int64 ``targets`` [tokens] (negative targets count for nothing);
     tokens a multiple of 16, hidden and vocab of 16.  Matrix gradients are fp32 [out, in], the
     embedding's a bf16 [tokens, hidden] row per token, as a sparse update takes it."""
     linear = lambda x, m: api.linear_pass_block128(api.PASS_FPROP, x, m)
     grad_x = lambda dy, m: api.linear_pass_block128(api.PASS_DGRAD, dy, m)
     grad_w = lambda dy, x: api.linear_pass_block128(api.PASS_WGRAD, dy, x, api.OUT_FP32)
     act = api.GATE_SIGMOID
+    ids = ids.long().contiguous()                           # of either integer type and any stride, as PyTorch's lookup
     # forward
     s0, h0 = api.residual_norm_forward(api.embedding_forward(ids, w["embedding"]), w_pre=w["w_in"])
     u, g = linear(h0, w["w_up"]), linear(h0, w["w_gate"])
@@ -77,7 +78,7 @@ def train_step(w: dict, ids: torch.Tensor, targets: torch.Tensor, entropy_weight
 
 
 def train_step_gated(w: dict, ids: torch.Tensor, targets: torch.Tensor, lse_weight: float = 0.0, max_norm: float = float("inf")):
-    """``(loss, gradients, norm)`` of a model with a feed-forward block, for int64 ``ids`` and ``targets`` [tokens] (negative
+    """``(loss, gradients, norm)`` of a model with a feed-forward block, for ``ids`` and int64 ``targets`` [tokens] (negative
     ids: no token there; negative targets count for nothing); tokens a multiple of 16, the other sizes of 16.  The
     gradients of the table and of the 16-bit linears are bf16, the others fp32; all are scaled so that their norm, which
     is returned as it was, is at most ``max_norm``."""
@@ -85,6 +86,7 @@ def train_step_gated(w: dict, ids: torch.Tensor, targets: torch.Tensor, lse_weig
     grad_x = lambda dy, m: api.linear_pass_block128(api.PASS_DGRAD, dy, m)
     grad_w = lambda dy, x: api.linear_pass_block128(api.PASS_WGRAD, dy, x, api.OUT_FP32)
     act = api.GATE_SIGMOID
+    ids = ids.long().contiguous()                           # of either integer type and any stride, as PyTorch's lookup
     # forward
     s0, h0 = api.residual_norm_forward(api.embedding_forward(ids, w["embedding"]), w_pre=w["w_in"])
     u, g = linear(h0, w["w_up"]), linear(h0, w["w_gate"])
