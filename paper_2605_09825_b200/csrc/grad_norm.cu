@@ -205,16 +205,42 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_join_kernel(const doub
     *norm = static_cast<float>(sqrt(sum));
 }
 
+// What gradients are multiplied by: `factor`, then `step`.  A factor far below the normal numbers (the limit of a norm that
+// exploded) would have lost its bits: it is held 2^64 times as large then, and step is 2^-64.
+struct ClipFactor {
+    float factor, step;
+};
+
+__device__ __forceinline__ ClipFactor clip_factor(float norm, float max_norm, float eps)
+{
+    constexpr float kLargest = 3.402823466e38f;
+    ClipFactor f = {1.0f, 1.0f};
+    if (!(norm <= kLargest)) return f;                 // not finite: as they are
+    const float total = norm + eps, share = max_norm / total;
+    if (total <= kLargest && !(share < 0x1p-100f)) {
+        if (share < 1.0f) f.factor = share;
+        return f;
+    }
+    const double exact = static_cast<double>(max_norm) / (static_cast<double>(norm) + static_cast<double>(eps));
+    if (exact < 0x1p-100) {
+        f.factor = static_cast<float>(exact * 0x1p64);
+        f.step = 0x1p-64f;
+    } else if (exact < 1.0) {
+        f.factor = static_cast<float>(exact);
+    }
+    return f;
+}
+
 template <class In, class Out>
-__device__ __forceinline__ void block_scale(const In* x, Out* y, int n, float factor)
+__device__ __forceinline__ void block_scale(const In* x, Out* y, int n, const ClipFactor& f)
 {
     constexpr int kPer = 16 / (sizeof(In) < sizeof(Out) ? sizeof(In) : sizeof(Out));       // elements per step: 16 or 32 bytes
     const int head = head_of(x, n);
     const bool vectors = kPer == 8 ? (reinterpret_cast<uintptr_t>(y + head) & 15u) == 0 && (reinterpret_cast<uintptr_t>(x + head) & 15u) == 0
                                    : (reinterpret_cast<uintptr_t>(y + head) & 15u) == 0;
-    if (!vectors) {
+    if (!vectors || f.step != 1.0f) {
         for (int i = threadIdx.x; i < n; i += kNormThreads) {
-            const float v = as_float(x[i]) * factor;
+            const float v = as_float(x[i]) * f.factor * f.step;
             if constexpr (sizeof(Out) == 2) y[i] = __float2bfloat16_rn(v);
             else y[i] = v;
         }
@@ -239,16 +265,16 @@ __device__ __forceinline__ void block_scale(const In* x, Out* y, int n, float fa
                 unpack8(w[u][0], q);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    v[2 * j] = q[j].x * factor;
-                    v[2 * j + 1] = q[j].y * factor;
+                    v[2 * j] = q[j].x * f.factor;
+                    v[2 * j + 1] = q[j].y * f.factor;
                 }
             } else {
 #pragma unroll
                 for (int h = 0; h < kPer / 4; ++h) {
-                    v[4 * h] = __uint_as_float(w[u][h].x) * factor;
-                    v[4 * h + 1] = __uint_as_float(w[u][h].y) * factor;
-                    v[4 * h + 2] = __uint_as_float(w[u][h].z) * factor;
-                    v[4 * h + 3] = __uint_as_float(w[u][h].w) * factor;
+                    v[4 * h] = __uint_as_float(w[u][h].x) * f.factor;
+                    v[4 * h + 1] = __uint_as_float(w[u][h].y) * f.factor;
+                    v[4 * h + 2] = __uint_as_float(w[u][h].z) * f.factor;
+                    v[4 * h + 3] = __uint_as_float(w[u][h].w) * f.factor;
                 }
             }
             uint4* to = reinterpret_cast<uint4*>(y + head + (i + u * kNormThreads) * kPer);
@@ -263,7 +289,7 @@ __device__ __forceinline__ void block_scale(const In* x, Out* y, int n, float fa
         }
     }
     auto one = [&](int i) {
-        const float v = as_float(x[i]) * factor;
+        const float v = as_float(x[i]) * f.factor;
         if constexpr (sizeof(Out) == 2) y[i] = __float2bfloat16_rn(v);
         else y[i] = v;
     };
@@ -279,9 +305,8 @@ __global__ void __launch_bounds__(kNormThreads, 4) clip_grads_kernel(const __gri
     const GradTensor& t = p.t[norm_tensor_of(p, b)];
     griddep_wait();
     const float norm = __ldcg(p.norm);
-    const float share = p.max_norm / (norm + p.eps);
-    const float factor = norm <= 3.402823466e38f && share < 1.0f ? share : 1.0f;       // not finite: as they are
-    if (factor == 1.0f && t.in == t.out && t.in32 == t.out32) return;
+    const ClipFactor factor = clip_factor(norm, p.max_norm, p.eps);
+    if (factor.factor == 1.0f && t.in == t.out && t.in32 == t.out32) return;
     {
         const int64_t at = static_cast<int64_t>(b - t.first_block) * kNormBlock;
         const int n = static_cast<int>(min(t.numel - at, static_cast<int64_t>(kNormBlock)));
