@@ -541,7 +541,8 @@ int mxfp4_logprobs_backward(const void* logits, int dtype, int64_t tokens, int64
  *     dg = dh * u * act'(g),   du = dh * act(g)            rounded to bf16 (the products' operands)
  *     dx = dg Wg + du Wu,      dWg = dg^T x,   dWu = du^T x
  *   dx bf16 [tokens x in_features]; dw_gate, dw_up (dw_dtype, MXFP4_OUT_*) [features x in_features], ld_dw; dx, or
- *   both weight gradients, may be NULL: not wanted.  act' of _RELU at 0 is 0.
+ *   both weight gradients, may be NULL: not wanted.  act' of _RELU at 0 is 0.  The rounding of dg and du leaves the gradients
+ *   0.0017 of their norm off, those in fp32 too; with the rounding of a bf16 result it is 0.0024.
  *   workspace: mxfp4_gated_linear_workspace_bytes bytes (dg and du, and partial sums of dx for few tokens), 16-byte aligned.
  * Calls repeat bit for bit.
  */
@@ -576,7 +577,8 @@ int mxfp4_gated_linear_backward(const mxfp4_gated_desc* gated, const void* dh, i
  *
  * Backward: dz = scale * (d_logp * (delta(target) - p) + d_lse * p),  p = exp(z - lse), from the forward's lse, rounded to
  *   bf16 (the products' operand) but for scale and a factor that all positions have in common, by which the sums are
- *   multiplied in fp32 (a mean's gradient is not rounded);
+ *   multiplied in fp32 (a mean's gradient is not rounded).  The rounding leaves sums of many terms of like size
+ *   0.0017 of their norm off, those in fp32 too;
  *     dx = dz W,   dW = dz^T x
  *   d_logp, d_lse fp32 [tokens], one of them may be NULL (zero; targets may then be NULL with d_logp);
  *   dx bf16 [tokens x in_features]; dw (dw_dtype, MXFP4_OUT_*) [vocab x in_features]; either may be NULL: not wanted.

@@ -919,7 +919,8 @@ def gated_linear_forward(x, w_gate, w_up, act: int = GATE_SILU, keep: bool = Tru
 def gated_linear_backward(dh, x, w_gate, w_up, kept, act: int = GATE_SILU, dw_dtype: int = OUT_BF16, want_dx: bool = True,
                           want_dw: bool = True, dx=None, dw_gate=None, dw_up=None, workspace=None):
     """``mxfp4_gated_linear_backward``: ``(dx, dw_gate, dw_up)`` from the gradient of h and the ``(gate, up)`` that the
-    forward call kept; dx bf16, the weights' of type ``dw_dtype``.  What is not wanted is None."""
+    forward call kept; dx bf16, the weights' of type ``dw_dtype`` (in fp32 too they carry the rounding of the products'
+    operands to bf16).  What is not wanted is None."""
     d = _gated_desc(x, w_gate, w_up, act)
     (T, D), F, dev = x.shape, w_gate.shape[0], x.device
     gate, up = kept
@@ -982,7 +983,8 @@ def linear_logprobs_forward(x, w, targets=None, scale: float = 1.0, workspace=No
 def linear_logprobs_backward(x, w, targets, lse, d_logp=None, d_lse=None, scale: float = 1.0, dw_dtype: int = OUT_BF16,
                              want_dx: bool = True, want_dw: bool = True, dx=None, dw=None, workspace=None):
     """``mxfp4_linear_logprobs_backward``: ``(dx, dw)`` from the forward's ``lse`` and the gradients of logp and lse (fp32
-    [tokens], None: zero); dx bf16, dw of type ``dw_dtype``.  What is not wanted is None.  The header says what a share of a
+    [tokens], None: zero); dx bf16, dw of type ``dw_dtype`` (in fp32 too it carries the rounding of the logits' gradient to
+    bf16).  What is not wanted is None.  The header says what a share of a
     vocabulary that is split over devices is given."""
     args = _loss_operands(x, w, targets)
     (T, D, V), dev = args[4:7], x.device

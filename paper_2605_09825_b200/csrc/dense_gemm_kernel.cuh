@@ -1,20 +1,20 @@
 // Product of 16-bit matrices with a fused epilogue: D[m][n] = sum_k A[m][k] * B[n][k], fp32 sums in tensor memory.
 //
 // CTA-pair kernel (tcgen05 cta_group::2, kind::f16) on 256 x 256 output tiles: each CTA holds 128 rows of A and 128
-// rows of B per K-step of 64 elements (32 KB), six steps in flight, two accumulators of 256 columns (all of
+// rows of B per K-step of 64 elements (32 KB), five or six steps in flight, two accumulators of 256 columns (all of
 // tensor memory), so that the epilogue of one tile runs under the products of the next.  A step takes 512 cycles of the
 // tensor cores and as many of the way from L2 into shared memory (64 bytes per cycle and SM): a larger tile would need more
-// tensor memory.  The tensor pipe is busy 93 % of the cycles in the loss's forward product, 87 % in the gated one with both
-// projections kept, 90 % in a backward pass; what it does per second is set by the power cap: 1.63 PFLOP/s for the
-// loss of 8192 tokens by itself, 1.38 to 1.42 pass after pass (a library product: 1.69 and 1.39).
+// tensor memory.  The tensor pipe is busy 91 % of the cycles in the loss's forward product, 87 % in the gated one with both
+// projections kept, 88 % in a backward pass; what it does per second is set by the power cap: 1.5 to 1.6 PFLOP/s for the
+// loss of 8192 tokens by itself, 1.3 to 1.42 pass after pass (a library product: 1.69 and 1.39).
 //
 // Either operand may be stored along K (rows of A, of B) or along its own rows (the transposed matrix, as the
 // gradients need it): a K-step is then fetched as two boxes of 64 columns x 64 rows, and the shared-memory
 // descriptor names the transposed layout.  No transposed copy exists anywhere.
 //
 // Two matrices of the same shape may stand in for one along M (both weight gradients of a pair of projections in
-// one launch) or along K (the input's gradient, a sum of two products).  A launch may take two products, the one with the
-// longer tiles first: the shorter tiles of the other fill the pairs that a last round of long ones leaves idle.  A
+// one launch) or along K (the input's gradient, a sum of two products).  A launch may take two products: tiles of the
+// second fill the pairs that a last round of the first leaves idle, as many as one of the first's is long.  A
 // product of few tiles is split along K, each piece with an output of its own, which the caller adds up.
 //
 // Epilogues:
@@ -61,7 +61,7 @@ constexpr int kDChain = 16;
 constexpr int kDStageBytes = 32 * 128;             // output staging per epilogue warp and box
 
 // Two output boxes per warp, so that one is filled while the other leaves, are worth a stage of operands where tiles are
-// short: the backward pass of 64 tokens (4096 x 14336) takes 147 us with them and 162 without.  The gated forward pass has
+// short: the backward pass of 64 tokens (4096 x 14336) took 147 us with them and 162 without.  The gated forward pass has
 // long ones: 104 us for 333 tokens with six stages, 107 with five and two boxes (before that size went to another kernel).
 template <int EPI>
 struct DenseSmem {

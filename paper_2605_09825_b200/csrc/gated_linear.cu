@@ -67,9 +67,10 @@ __global__ void __launch_bounds__(kGradThreads) gated_grad_kernel(const GatedGra
 
 // Whether the kernel with the weights as rows takes a forward pass: up to 160 tokens, where it computes for fewer rows than the
 // tile of 256 that the other one computes for in any case, and beyond that where its tiles, which need only be a multiple of 16
-// tokens, hold at most 7/8 of the other's rows and K is long enough for its epilogue.  4096 x 14336, pass after pass: 16 to
-// 64 tokens 42 to 45 us against 54 to 56, 160 tokens 55 and 61, 240 66 and 63, 333 91 and 102, 400 100 and 104, 512 115 and
-// 108, 600 129 and 144, 1100 207 and 225; 1024 x 4096: 600 tokens 21 and 15.5, 2048 x 8192: 43 and 45.
+// tokens, hold at most 7/8 of the other's rows and K is long enough for its epilogue.  4096 x 14336, pass after pass on one
+// device, this kernel and the other: 16 tokens 41 and 48 us, 64 42 and 49, 128 47 and 51, 160 49 and 52, 200 55 and 53, 240 58
+// and 54, 333 78 and 87, 400 86 and 89, 512 97 and 93, 600 111 and 123, 1100 180 and 196; of 600 tokens with other
+// weights: 4096 x 2048 34 and 30, 4096 x 8192 70 and 76, 4096 x 28672 216 and 253, 2048 x 8192 43 and 45, 1024 x 4096 24 and 19.
 static bool gated_as_columns(int64_t tokens, int64_t in_features)
 {
     const int64_t tiles = dense_tiles(tokens, 256), rows = tiles * dense_tiles(dense_tiles(tokens, tiles), 16) * 16;

@@ -1,19 +1,20 @@
-// The gated projections for tens to some hundreds of tokens, and for numbers that fill tiles of 256 badly, with the weights as the tensor cores' 256 rows and the tokens as
-// their columns: a product of 17 tokens costs a sixteenth of the instructions of one of 256, where the other way round
-// (dense_gemm_kernel.cuh) it costs the same, and both weights are read as fast as memory gives them.
+// The gated projections for tens to some hundreds of tokens, and for numbers that fill tiles of 256 badly, with the
+// weights as the tensor cores' 256 rows and the tokens as their columns: an instruction for 17 tokens has an eighth of the
+// columns of one for 256 (a tile is a multiple of 16 tokens), where the other way round (dense_gemm_kernel.cuh) both cost
+// the same, and both weights are read as fast as memory gives them.
 //
 // CTA-pair kernel (tcgen05 cta_group::2, kind::f16).  A tile is 128 features and up to 256 tokens (a multiple of 16, the same
 // for all tiles).  Each CTA holds 64 rows of the gate's weight and the same 64 of the other one -- lanes 0..63 and 64..127
-// of its tensor memory -- and half of the tokens, per K-step of 64 elements; as many steps are in flight as fit 160 KB: ten
+// of its tensor memory -- and half of the tokens, per K-step of 64 elements; as many steps are in flight as fit 160 KB: nine
 // for up to 16 tokens, five for 256.  Two accumulators take turns.
 //
 // Epilogue: chunks of 32 tokens, the even ones for warps 0..3, the odd ones for warps 4..7.  The two warps that hold the other
 // projection hand it over through shared memory; the two that hold the gate form h.  Results are staged as rows of 64
 // features and leave by TMA stores of 16 tokens, which clip at the last token.
 //
-// 4096 x 14336, pass after pass: 9 to 64 tokens 42 to 45 us (235 MB, 5.5 TB/s; 112 tiles are one round and a half of 74 pairs),
-// 128 tokens 51, 333 tokens 91.  With the K-steps of all tiles shared out evenly and a joining kernel a call of 17 tokens
-// took 42 + 4.5 us by itself, one of 333 tokens 92 + 20.
+// 4096 x 14336, pass after pass, on one device and another: 9 to 64 tokens 41 to 44 us (235 MB, 5.5 TB/s; 112 tiles are one
+// round and a half of 74 pairs), 128 tokens 47 to 49, 333 tokens 78 to 91.  With the K-steps of all tiles shared out
+// evenly and a joining kernel a call of 17 tokens took 42 + 4.5 us by itself, one of 333 tokens 92 + 20.
 //
 // Roles per CTA as in the other kernel: warps 0..7 epilogue, 8 TMA producer, 9 MMA issuer (leader CTA only).
 #pragma once
@@ -32,7 +33,7 @@ constexpr int kTFeatures = 128;                    // per tile and pair
 constexpr int kTBlockK = 64;                       // elements: 128 bytes
 constexpr int kTWeightBytes = 2 * 64 * 128;        // per CTA and step: 64 rows of both weights
 constexpr int kTRing = 160 * 1024;
-constexpr int kTMostStages = 10;
+constexpr int kTMostStages = 9;                     // of 17 KB, the least
 constexpr int kTProducerWarp = 8;
 constexpr int kTMmaWarp = 9;
 constexpr int kTThreads = 320;

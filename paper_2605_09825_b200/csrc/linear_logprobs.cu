@@ -7,7 +7,8 @@
 //
 // Bound by the products: 8192 tokens of 4096 features, vocabulary 128256, forward 5430 to 5700 us by itself (1.5 to 1.6 PFLOP/s),
 // 6060 to 6600 pass after pass, on one device and another: the power cap sustains 1.3 to 1.42; 19 us are the join.  Backward,
-// 4096 tokens: 8320, and 9470 to 9970.
+// 4096 tokens: 8320 to 8470, and 9100 to 9970; of 16 and 64 tokens 630 and 660, where a weight read once and its gradient
+// take 325: the logits' product and dx each read it.
 //
 // The gradient of the logits is rounded to bf16 because it is an operand of the tensor cores' products: sums over
 // hundreds of them are off by about 0.0017 of their value (norm), as much as the rounding of a bf16 result.  What the
